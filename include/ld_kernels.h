@@ -173,6 +173,89 @@ ld_status ldk_argmax(const float *logits, int32_t R, int32_t V, int32_t *out, vo
 ld_status ldk_sample(const float *logits, int32_t R, int32_t V, const float *temperature, const uint64_t *seed,
                      const int32_t *pos, int32_t *out, void *stream);
 
+/* ---- A decode step that reads few bytes: 4-bit weights, attention over selected cache blocks, choice under rules. ---- */
+
+/* 4-bit weights with group scales: W[n, k] = (c[n, k] - z[n, k / group]) * s[n, k / group], codes c in 0..15, group 32,
+ * 64 or 128 input columns, scales s of scale_dtype (LD_F32 | LD_BF16), zero points z in 0..15 or, without them
+ * (zeros NULL / 0), z = 8 everywhere.  Any N >= 1 and K >= 1; a last group may be short.
+ * ldk_linear_w4 reads a matrix from an image that is laid out once: `parts` matrices of N rows each (1; 2 for
+ * LDK_SWIGLU: the gate rows, then the up rows), ldk_w4_image_bytes(...) bytes of DEVICE memory, 16-byte aligned.
+ * ldk_w4_image_bytes returns 0 for arguments that no image has.
+ * ldk_w4_pack lays out given codes: codes [parts * N][(K + 1) / 2] bytes, the even column in the low four bits, scales
+ * and zeros [parts * N][ceil(K / group)].
+ * ldk_w4_quantize rounds a matrix [parts * N, K] (dtype LD_F32 | LD_BF16, finite) to nearest: without zero points
+ * s = max |w| / 7 over the group, with them s = (max - min) / 15 over the group and 0, z = round(-min / s); s is
+ * rounded to scale_dtype before the codes are formed. */
+size_t ldk_w4_image_bytes(int32_t N, int32_t K, int32_t group, int32_t parts, int32_t scale_dtype, int32_t zeros);
+ld_status ldk_w4_pack(const uint8_t *codes, const void *scales, int32_t scale_dtype, const uint8_t *zeros, int32_t N, int32_t K,
+                      int32_t group, int32_t parts, void *image, size_t image_bytes, void *stream);
+ld_status ldk_w4_quantize(const void *W, int32_t dtype, int32_t N, int32_t K, int32_t group, int32_t parts, int32_t scale_dtype,
+                          int32_t zeros, void *image, size_t image_bytes, void *stream);
+
+/* ldk_linear on such an image (same epilogues, same optional RMS normalisation of the input; the image's parts follow
+ * from the epilogue).  x [T, K], y [T, N] dense row-major float32.  The codes are exact in the products; the
+ * activations enter as two fp16 terms of a row scaled by a power of two (22 significant bits), sums are float32.
+ * A row of x that holds a NaN or an infinity (after the normalisation) gives NaN in all of its outputs; no other row is touched by it.
+ * scratch: ldk_linear_w4_scratch_bytes(T, N, K, epilogue) bytes, 16-byte aligned, needed at every T; a buffer for more rows serves fewer. */
+size_t ldk_linear_w4_scratch_bytes(int32_t T, int32_t N, int32_t K, int32_t epilogue);
+ld_status ldk_linear_w4(const void *image, int32_t scale_dtype, int32_t zeros, int32_t group, const float *x, const float *g, float eps,
+                        int32_t T, int32_t N, int32_t K, int32_t epilogue, float *y, void *scratch, size_t scratch_bytes, void *stream);
+
+/* 8-bit bounds of the keys of cache blocks, which ldk_sparse_attention scores with.  For physical block b and KV head j, over
+ * the block's cached positions: unit[b][j] = 2^e, e = floor(log2 max |k|) - 6 (at least -126; 1 for keys that are all zero),
+ *   bounds[b][j][0][i] = min(127, ceil(max_p k[p][i] / unit)),  bounds[b][j][1][i] = max(-127, floor(min_p k[p][i] / unit)).
+ * A block with a key that is not finite gets unit = infinity and is always preferred by the selection.
+ * bounds: int8 [n_blocks][Hkv][2][hd] (16-byte aligned), unit: float [n_blocks][Hkv], DEVICE, one pair per layer.
+ * To be called after keys have been written (ldk_rope_kv_write, ldk_qkv_rope): ranges DEVICE int32 [n_ranges][3] =
+ * (block-table row, first new position, end of the sequence's positions); every block that first .. end - 1 touch is described anew, over its
+ * positions below end.  max_len (HOST) >= end - first of every range.  Ranges of one call name distinct blocks.  Blocks the
+ * table does not map (< 0) are skipped. */
+ld_status ldk_kv_summary(const void *pool_layer, int32_t dtype, const int32_t *table, int32_t table_stride, const int32_t *ranges,
+                         int32_t n_ranges, int32_t max_len, int32_t Hkv, int32_t hd, int8_t *bounds, float *unit, void *stream);
+
+/* ldk_paged_attention over `budget` of the visible blocks for each row and KV head (all of them where there are no more):
+ * the first keep_first and the last keep_last (>= 1) visible blocks, and the others by descending score, the lower
+ * index first among equal scores.  With q'_h the query head rounded to integers of v_h = 2^(floor(log2 max |q_h|) - 6),
+ * clamped to +-127,
+ *   score(b) = max over the KV head's query heads of v_h unit[b] sum_i (q'_i >= 0 ? q'_i bounds[b][0][i] : q'_i bounds[b][1][i]).
+ * Sums of integers and powers of two: the choice depends on nothing but the row and the bounds (which every visible block must have).  A query
+ * head with a NaN or an infinity scores 0 everywhere.
+ * out [T, H, hd]: softmax attention over the selected blocks' visible positions, arguments as in
+ * ldk_paged_attention; ctx_len[t] may be 0: the row's out is 0 and it selects nothing.  max_ctx (HOST) >= every ctx_len.
+ * sel (DEVICE, int32 [T, Hkv, budget]): the selected logical blocks, ascending, then -1.
+ * scratch: ldk_sparse_attention_scratch_bytes(...) bytes, 16-byte aligned; a buffer for more rows or longer contexts serves less. */
+size_t ldk_sparse_attention_scratch_bytes(int32_t T, int32_t H, int32_t Hkv, int32_t hd, int32_t max_ctx, int32_t window, int32_t budget);
+ld_status ldk_sparse_attention(const float *q, int32_t q_stride, const void *pool_layer, int32_t dtype, const int8_t *bounds, const float *unit,
+                               const int32_t *table, int32_t table_stride, const int32_t *seq_slot, const int32_t *ctx_len, int32_t max_ctx,
+                               int32_t T, int32_t H, int32_t Hkv, int32_t hd, int32_t window, int32_t budget, int32_t keep_first,
+                               int32_t keep_last, float *out, int32_t *sel, void *scratch, size_t scratch_bytes, void *stream);
+
+/* What ldk_choose applies to the logits of row r, in this order.  All pointers DEVICE; a NULL member leaves its rule out.
+ *   history [R][history_stride], history_len [R], penalties [R][3] = (repetition > 0, presence, frequency):
+ *     for a token i among history[r][0 .. history_len[r]), l = l > 0 ? l / repetition : l * repetition, and with c = its number among
+ *     history[r][n_prompt[r] .. history_len[r]) (n_prompt NULL: 0), l -= frequency * c + (c > 0 ? presence : 0).  Tokens outside 0 .. V-1
+ *     are ignored.
+ *   bias_start [R + 1], bias_token, bias: l += bias[j], j the last of bias_start[r] .. bias_start[r + 1] - 1 with bias_token[j] = i.
+ *   mask [mask_rows][ceil(V / 32)], mask_row [R] (NULL: row r's mask is row r): bit i % 32 of word i / 32 clear: l = -infinity.  mask_row[r] < 0:
+ *     no mask; mask_row[r] >= mask_rows: no token is allowed. */
+typedef struct {
+    const int32_t *history, *history_len, *n_prompt;
+    const float *penalties;
+    const int32_t *bias_start, *bias_token;
+    const float *bias;
+    const uint32_t *mask;
+    const int32_t *mask_row;
+    int32_t history_stride, mask_rows;
+} ld_token_rules;
+
+/* Token choice under rules (HOST struct, may be NULL): token[r] = lowest index of the largest adjusted logit or, where temperature[r] > 0, the
+ * draw that ldk_sample makes from the adjusted logits (temperature NULL: greedy; seed and pos as there); -1 where every
+ * adjusted logit is -infinity or NaN.  adjusted (may be NULL, may be logits itself): the adjusted logits [R, V].
+ * scratch: ldk_choose_scratch_bytes(R, V) bytes, 8-byte aligned. */
+size_t ldk_choose_scratch_bytes(int32_t R, int32_t V);
+ld_status ldk_choose(const float *logits, int32_t R, int32_t V, const ld_token_rules *rules, const float *temperature, const uint64_t *seed,
+                     const int32_t *pos, float *adjusted, int32_t *token, void *scratch, size_t scratch_bytes, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -28,6 +28,8 @@ __all__ = [
     "ldk_attention_scratch_bytes", "ldk_paged_attention", "ldk_static_scratch_bytes", "ldk_paged_attention_static",
     "ldk_prefill_attention_scratch_bytes",
     "ldk_prefill_attention", "ldk_argmax", "ldk_sample", "Model", "KV",
+    "ldk_w4_image_bytes", "ldk_w4_pack", "ldk_w4_quantize", "ldk_linear_w4_scratch_bytes", "ldk_linear_w4", "W4Matrix",
+    "ldk_kv_summary", "ldk_sparse_attention_scratch_bytes", "ldk_sparse_attention", "ld_token_rules", "ldk_choose_scratch_bytes", "ldk_choose",
 ]
 
 
@@ -56,6 +58,11 @@ LD_PROF_NAMES = ("qkv", "rope_kv", "attention", "wo", "gate_up", "down", "lm_hea
 
 class ld_profile(C.Structure):
     _fields_ = [("ms", C.c_double * 8), ("launches", C.c_int64 * 8)]
+
+
+class ld_token_rules(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("history", "history_len", "n_prompt", "penalties", "bias_start", "bias_token", "bias",
+                                          "mask", "mask_row")] + [("history_stride", C.c_int32), ("mask_rows", C.c_int32)]
 
 
 ld_token_cb = C.CFUNCTYPE(C.c_int, C.c_void_p, C.c_int32, C.c_int32, C.c_int32)
@@ -120,6 +127,18 @@ _SIGS = {
     "ldk_prefill_attention_f16": (C.c_int, [_vp, C.c_int32, _vp, C.c_int32, _vp, C.c_int32, _vp, C.c_int32, C.c_int32,
                                             C.c_int32, C.c_int32, C.c_int32, C.c_int32, _vp, _vp, C.c_size_t, _vp, _vp]),
     "ldk_argmax": (C.c_int, [_vp, C.c_int32, C.c_int32, _vp, _vp]),
+    "ldk_w4_image_bytes": (C.c_size_t, [C.c_int32] * 6),
+    "ldk_w4_pack": (C.c_int, [_vp, _vp, C.c_int32, _vp, C.c_int32, C.c_int32, C.c_int32, C.c_int32, _vp, C.c_size_t, _vp]),
+    "ldk_w4_quantize": (C.c_int, [_vp] + [C.c_int32] * 7 + [_vp, C.c_size_t, _vp]),
+    "ldk_linear_w4_scratch_bytes": (C.c_size_t, [C.c_int32] * 4),
+    "ldk_linear_w4": (C.c_int, [_vp, C.c_int32, C.c_int32, C.c_int32, _vp, _vp, C.c_float, C.c_int32, C.c_int32, C.c_int32, C.c_int32, _vp,
+                               _vp, C.c_size_t, _vp]),
+    "ldk_kv_summary": (C.c_int, [_vp, C.c_int32, _vp, C.c_int32, _vp, C.c_int32, C.c_int32, C.c_int32, C.c_int32, _vp, _vp, _vp]),
+    "ldk_sparse_attention_scratch_bytes": (C.c_size_t, [C.c_int32] * 7),
+    "ldk_sparse_attention": (C.c_int, [_vp, C.c_int32, _vp, C.c_int32, _vp, _vp, _vp, C.c_int32, _vp, _vp] + [C.c_int32] * 9 +
+                             [_vp, _vp, _vp, C.c_size_t, _vp]),
+    "ldk_choose_scratch_bytes": (C.c_size_t, [C.c_int32, C.c_int32]),
+    "ldk_choose": (C.c_int, [_vp, C.c_int32, C.c_int32, C.POINTER(ld_token_rules), _vp, _vp, _vp, _vp, _vp, _vp, C.c_size_t, _vp]),
 }
 EXPORTS = tuple(_SIGS)
 
@@ -492,7 +511,100 @@ def ldk_argmax(logits, out, stream=None):
     _check(lib().ldk_argmax(_ptr(logits), R, V, _ptr(out), _stream(stream)))
 
 
+def ldk_w4_image_bytes(N, K, group, parts, scale_dtype, zeros):
+    return lib().ldk_w4_image_bytes(N, K, group, parts, _dt(scale_dtype), int(bool(zeros)))
+
+
+def ldk_w4_pack(codes, scales, zeros, image, N, K, group, parts=1, stream=None):
+    _check(lib().ldk_w4_pack(_ptr(codes), _ptr(scales), _dt(scales.dtype), _ptr(zeros), N, K, group, parts, _ptr(image), _nbytes(image),
+                             _stream(stream)))
+
+
+def ldk_w4_quantize(W, image, N, K, group, parts=1, scale_dtype=torch.bfloat16, zeros=False, stream=None):
+    _check(lib().ldk_w4_quantize(_ptr(W), _dt(W.dtype), N, K, group, parts, _dt(scale_dtype), int(bool(zeros)), _ptr(image), _nbytes(image),
+                                 _stream(stream)))
+
+
+def ldk_linear_w4_scratch_bytes(T, N, K, epilogue=LDK_STORE):
+    return lib().ldk_linear_w4_scratch_bytes(T, N, K, epilogue)
+
+
+def ldk_linear_w4(w, x, y, epilogue=LDK_STORE, g=None, eps=0.0, scratch=None, stream=None):
+    """w: a W4Matrix whose parts fit the epilogue (two for LDK_SWIGLU)."""
+    T, K = x.shape
+    if K != w.K or y.shape != (T, w.N) or w.parts != (2 if epilogue == LDK_SWIGLU else 1):
+        raise LdError(LD_E_INVAL, f"ldk_linear_w4: x {tuple(x.shape)}, y {tuple(y.shape)} and epilogue {epilogue} do not fit {w.parts} x "
+                                  f"{w.N} x {w.K} weights")
+    _check(lib().ldk_linear_w4(_ptr(w.image), _dt(w.scale_dtype), int(w.zeros), w.group, _ptr(x), _ptr(g), eps, T, w.N, K, epilogue, _ptr(y),
+                               _ptr(scratch), _nbytes(scratch), _stream(stream)))
+
+
+def ldk_kv_summary(pool_layer, table, ranges, max_len, Hkv, hd, bounds, unit, stream=None):
+    """ranges int32 [n, 3]: (block-table row, first new position, end); bounds int8 [blocks, Hkv, 2, hd], unit float32 [blocks, Hkv]."""
+    _check(lib().ldk_kv_summary(_ptr(pool_layer), _dt(pool_layer.dtype), _ptr(table), table.shape[1], _ptr(ranges), ranges.shape[0], max_len,
+                                Hkv, hd, _ptr(bounds), _ptr(unit), _stream(stream)))
+
+
+def ldk_sparse_attention_scratch_bytes(T, H, Hkv, hd, max_ctx, window, budget):
+    return lib().ldk_sparse_attention_scratch_bytes(T, H, Hkv, hd, max_ctx, window, budget)
+
+
+def ldk_sparse_attention(q, q_stride, pool_layer, bounds, unit, table, seq_slot, ctx_len, max_ctx, H, Hkv, hd, budget, keep_first, keep_last,
+                         out, sel, scratch, window=0, stream=None):
+    _check(lib().ldk_sparse_attention(_ptr(q), q_stride, _ptr(pool_layer), _dt(pool_layer.dtype), _ptr(bounds), _ptr(unit), _ptr(table),
+                                      table.shape[1], _ptr(seq_slot), _ptr(ctx_len), max_ctx, out.shape[0], H, Hkv, hd, window, budget,
+                                      keep_first, keep_last, _ptr(out), _ptr(sel), _ptr(scratch), _nbytes(scratch), _stream(stream)))
+
+
+def ldk_choose_scratch_bytes(R, V):
+    return lib().ldk_choose_scratch_bytes(R, V)
+
+
+def ldk_choose(logits, token, history=None, history_len=None, n_prompt=None, penalties=None, bias_start=None, bias_token=None, bias=None,
+               mask=None, mask_row=None, temperature=None, seed=None, pos=None, adjusted=None, scratch=None, stream=None):
+    """Device tensors: history int32 [R, n], history_len, n_prompt, mask_row, pos, token int32 [R], penalties float32 [R, 3] (repetition,
+    presence, frequency), bias_start int32 [R + 1], mask int32 [rows, ceil(V / 32)] (bit patterns), seed int64 [R] (bit patterns)."""
+    R, V = logits.shape
+    rules = ld_token_rules(_ptr(history), _ptr(history_len), _ptr(n_prompt), _ptr(penalties), _ptr(bias_start), _ptr(bias_token), _ptr(bias),
+                           _ptr(mask), _ptr(mask_row), 0 if history is None else history.shape[1], 0 if mask is None else mask.shape[0])
+    _check(lib().ldk_choose(_ptr(logits), R, V, C.byref(rules), _ptr(temperature), _ptr(seed), _ptr(pos), _ptr(adjusted), _ptr(token),
+                            _ptr(scratch), _nbytes(scratch), _stream(stream)))
+
+
 # ------------------------------------------------------------------ owners of handles + device memory
+
+class W4Matrix:
+    """4-bit weights with group scales, laid out for ldk_linear_w4 (parts matrices of N rows: two for gate/up)."""
+
+    def __init__(self, N, K, group=128, parts=1, scale_dtype=torch.bfloat16, zeros=False, device="cuda"):
+        self.N, self.K, self.group, self.parts, self.scale_dtype, self.zeros = N, K, group, parts, scale_dtype, bool(zeros)
+        n = ldk_w4_image_bytes(N, K, group, parts, scale_dtype, zeros) if scale_dtype in (torch.bfloat16, torch.float32) else 0
+        if n == 0:
+            raise LdError(LD_E_INVAL, f"no 4-bit image has {parts} x {N} x {K} weights in groups of {group} with {scale_dtype} scales")
+        self.image = torch.empty(n, dtype=torch.uint8, device=device)
+
+    @classmethod
+    def pack(cls, codes, scales, zeros, N, K, group=128, parts=1, stream=None):
+        """codes uint8 [parts N, ceil(K / 2)] (even column in the low half), scales [parts N, ceil(K / group)], zeros uint8 likewise or None."""
+        groups = -(-K // group)
+        if tuple(codes.shape) != (parts * N, (K + 1) // 2) or tuple(scales.shape) != (parts * N, groups) or \
+                (zeros is not None and zeros.shape != scales.shape) or codes.dtype != torch.uint8 or \
+                (zeros is not None and zeros.dtype != torch.uint8):
+            raise LdError(LD_E_INVAL, "W4Matrix.pack: shapes or types of codes, scales and zeros do not fit")
+        w = cls(N, K, group, parts, scales.dtype, zeros is not None, codes.device)
+        ldk_w4_pack(codes, scales, zeros, w.image, N, K, group, parts, stream)
+        return w
+
+    @classmethod
+    def quantize(cls, W, group=128, parts=1, scale_dtype=torch.bfloat16, zeros=False, stream=None):
+        """W [parts N, K], bf16 or float32, rounded to nearest."""
+        N, K = W.shape[0] // parts, W.shape[1]
+        if W.shape[0] != parts * N:
+            raise LdError(LD_E_INVAL, "W4Matrix.quantize: rows are not a multiple of parts")
+        w = cls(N, K, group, parts, scale_dtype, zeros, W.device)
+        ldk_w4_quantize(W, w.image, N, K, group, parts, scale_dtype, zeros, stream)
+        return w
+
 
 class Model:
     """Keeps the weight tensors alive and owns the ld_model handle."""

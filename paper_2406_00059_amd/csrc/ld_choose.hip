@@ -1,0 +1,145 @@
+// Token choice under rules: penalties for repeated tokens, biases, a grammar's mask, then the arg-max or a draw.
+//
+// A workgroup takes a slice of one row's vocabulary.  It counts the history's tokens that lie in the slice in LDS (integer
+// atomics, whose order cannot matter) and notes the last bias entry of each token, walks the slice's logits once, and leaves
+// its best token; a second launch joins the slices.  No count table outlives a call: a sequence that is forked, swapped or
+// rolled back needs nothing but its token history.  Bound by launch latency at few rows, by the logits' bytes at many.
+#include "ld_device.h"
+
+using namespace ldd;
+
+namespace {
+
+inline ld_status launched(const char *what) {
+    hipError_t e = hipGetLastError();
+    if (e != hipSuccess) {
+        ld::set_error("launch of %s failed: %s", what, hipGetErrorString(e));
+        return LD_E_HIP;
+    }
+    return LD_OK;
+}
+
+constexpr int SLICE = 2048;
+constexpr uint32_t SEEN = 0x80000000u;
+
+struct Best { float v; int i; };
+// The larger score, the lower index among equal ones; i < 0: nothing yet.
+__device__ __forceinline__ void better(Best &a, float v, int i) {
+    if (i >= 0 && (a.i < 0 || v > a.v || (v == a.v && i < a.i))) { a.v = v; a.i = i; }
+}
+__device__ __forceinline__ void wave_best(Best &b) {
+#pragma unroll
+    for (int off = 32; off > 0; off >>= 1) {
+        const float v = __shfl_xor(b.v, off, WAVE);
+        const int i = __shfl_xor(b.i, off, WAVE);
+        better(b, v, i);
+    }
+}
+
+__global__ __launch_bounds__(256) void k_choose_slice(const float *logits, int V, ld_token_rules rules,
+                                                      const float *__restrict__ temperature, const uint64_t *__restrict__ seed,
+                                                      const int32_t *__restrict__ pos, float *adjusted, Best *__restrict__ part) {
+    __shared__ uint32_t seen[SLICE];       // bit 31: in the history; the rest: times in its answer part
+    __shared__ int32_t bias_at[SLICE];     // last entry naming the token, + 1
+    __shared__ Best sm[4];
+    const int r = blockIdx.y, base = blockIdx.x * SLICE, tid = threadIdx.x;
+    const int size = min(SLICE, V - base);
+    const bool counted = rules.history && rules.penalties;
+    const bool biased = rules.bias != nullptr;
+    for (int i = tid; i < SLICE; i += 256) { seen[i] = 0; bias_at[i] = 0; }
+    __syncthreads();
+    if (counted) {
+        const int32_t *h = rules.history + (int64_t)r * rules.history_stride;
+        const int n = min(rules.history_len[r], rules.history_stride), answer = rules.n_prompt ? rules.n_prompt[r] : 0;
+        for (int j = tid; j < n; j += 256) {
+            const uint32_t k = (uint32_t)h[j] - (uint32_t)base;      // a token outside the vocabulary lies in no slice
+            if (k < (uint32_t)size) {
+                atomicOr(&seen[k], SEEN);
+                if (j >= answer) atomicAdd(&seen[k], 1u);
+            }
+        }
+    }
+    const int b0 = biased ? rules.bias_start[r] : 0;
+    if (biased) {
+        const int b1 = rules.bias_start[r + 1];
+        for (int j = b0 + tid; j < b1; j += 256) {
+            const uint32_t k = (uint32_t)rules.bias_token[j] - (uint32_t)base;
+            if (k < (uint32_t)size) atomicMax(&bias_at[k], j - b0 + 1);
+        }
+    }
+    __syncthreads();
+    float rep = 1.f, pres = 0.f, freq = 0.f;
+    if (counted) { rep = rules.penalties[3 * r]; pres = rules.penalties[3 * r + 1]; freq = rules.penalties[3 * r + 2]; }
+    const int mrow = rules.mask ? (rules.mask_row ? rules.mask_row[r] : r) : -1;
+    const uint32_t *mask = mrow >= 0 && mrow < rules.mask_rows ? rules.mask + (int64_t)mrow * ((V + 31) / 32) : nullptr;
+    const bool nothing = mrow >= 0 && !mask;      // a row of the mask that does not exist allows no token
+    const float temp = temperature ? temperature[r] : 0.f;
+    const float inv_t = temp > 0.f ? 1.0f / temp : 1.0f;
+    const uint64_t sd = temp > 0.f ? seed[r] : 0, ctr = temp > 0.f ? (uint64_t)pos[r] * (uint64_t)V : 0;
+    const float *row = logits + (int64_t)r * V;
+    Best best{-INFINITY, -1};
+    for (int k = tid; k < size; k += 256) {
+        const int i = base + k;
+        float l = row[i];
+        const uint32_t c = seen[k];
+        if (c) {
+            const float n = (float)(c & ~SEEN);
+            l = l > 0.f ? l / rep : l * rep;
+            l = l - (freq * n + (n > 0.f ? pres : 0.f));
+        }
+        if (bias_at[k]) l += rules.bias[b0 + bias_at[k] - 1];
+        if (nothing || (mask && !((mask[i >> 5] >> (i & 31)) & 1u))) l = -INFINITY;
+        if (adjusted) adjusted[(int64_t)r * V + i] = l;
+        if (temp > 0.f && l > -INFINITY) l = l * inv_t + gumbel_noise(sd, ctr + i);
+        if (l > -INFINITY) better(best, l, i);      // neither -inf nor NaN
+    }
+    wave_best(best);
+    if ((tid & 63) == 0) sm[tid >> 6] = best;
+    __syncthreads();
+    if (tid == 0) {
+        for (int w = 1; w < 4; w++) better(best, sm[w].v, sm[w].i);
+        part[(int64_t)r * gridDim.x + blockIdx.x] = best;
+    }
+}
+
+__global__ __launch_bounds__(64) void k_choose_join(const Best *__restrict__ part, int slices, int32_t *__restrict__ token) {
+    const int r = blockIdx.x;
+    Best best{-INFINITY, -1};
+    for (int i = threadIdx.x; i < slices; i += 64) {
+        const Best b = part[(int64_t)r * slices + i];
+        better(best, b.v, b.i);
+    }
+    wave_best(best);
+    if (threadIdx.x == 0) token[r] = best.i;
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t ldk_choose_scratch_bytes(int32_t R, int32_t V) {
+    return R > 0 && V > 0 ? (size_t)R * ((V + SLICE - 1) / SLICE) * sizeof(Best) : 0;
+}
+
+ld_status ldk_choose(const float *logits, int32_t R, int32_t V, const ld_token_rules *rules, const float *temperature, const uint64_t *seed,
+                     const int32_t *pos, float *adjusted, int32_t *token, void *scratch, size_t scratch_bytes, void *stream) {
+    if (R == 0) return LD_OK;
+    if (!logits || !token || R < 0 || V <= 0 || (temperature && (!seed || !pos)))
+        return ld::fail(LD_E_INVAL, "ldk_choose: bad argument (a temperature needs seed and pos)");
+    const ld_token_rules none{};
+    const ld_token_rules &u = rules ? *rules : none;
+    if ((u.history && (!u.history_len || !u.penalties || u.history_stride < 0)) || (u.penalties && !u.history) ||
+        (u.bias && (!u.bias_start || !u.bias_token)) || (u.mask && u.mask_rows <= 0) || (u.mask && !u.mask_row && u.mask_rows < R))
+        return ld::fail(LD_E_INVAL, "ldk_choose: bad argument (history comes with history_len and penalties, bias with bias_start and "
+                                    "bias_token, mask with mask_rows and, unless it has a row for each of the logits', mask_row)");
+    if (!scratch || ((uintptr_t)scratch & 7) || scratch_bytes < ldk_choose_scratch_bytes(R, V))
+        return ld::fail(LD_E_INVAL, "ldk_choose: scratch missing, not 8-byte aligned or too small");
+    if (R > 65535) return ld::fail(LD_E_RANGE, "ldk_choose: more than 65535 rows");
+    const int slices = (V + SLICE - 1) / SLICE;
+    hipStream_t s = (hipStream_t)stream;
+    LD_LAUNCH(k_choose_slice, dim3(slices, R), dim3(256), 0, s, logits, V, u, temperature, seed, pos, adjusted, (Best *)scratch);
+    LD_LAUNCH(k_choose_join, dim3(R), dim3(64), 0, s, (const Best *)scratch, slices, token);
+    return launched("k_choose");
+}
+
+}  // extern "C"

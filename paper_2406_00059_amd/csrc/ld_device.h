@@ -183,6 +183,17 @@ __device__ __forceinline__ int64_t kv_v_offset(int Hkv, int hd, int kvh, int slo
 
 __device__ __forceinline__ float fast_exp2(float x) { return __builtin_amdgcn_exp2f(x); }
 
+// Standard Gumbel noise -log(-log(u)): u = (k + 1/2) / 2^23, k = top 23 bits of the SplitMix64 output function applied to
+// seed + (counter + 1) * 0x9E3779B97F4A7C15: a pure function of (seed, counter), u exact in float32.
+__device__ __forceinline__ float gumbel_noise(uint64_t seed, uint64_t counter) {
+    uint64_t z = seed + (counter + 1) * 0x9E3779B97F4A7C15ull;
+    z = (z ^ (z >> 30)) * 0xBF58476D1CE4E5B9ull;
+    z = (z ^ (z >> 27)) * 0x94D049BB133111EBull;
+    z ^= z >> 31;
+    const float u = ((float)(uint32_t)(z >> 41) + 0.5f) * (1.0f / 8388608.0f);
+    return -logf(-logf(u));
+}
+
 // acc + p[0] + p[stride] + ... + p[(ks - 1) stride], added in that order (split-K slabs: the order is part of
 // the result).  The loads of eight (then four) slabs are issued together; a plain loop would pay one memory
 // latency per slab.

@@ -501,19 +501,8 @@ __global__ __launch_bounds__(1024) void k_argmax(const float *__restrict__ logit
 
 // ---------------------------------------------------------------- token choice with temperature
 //
-// argmax_i (logit_i / T + g_i), g_i = -log(-log(u_i)) standard Gumbel noise: a draw from softmax(logits / T).
-// u_i = (k + 1/2) / 2^23, k = top 23 bits of the SplitMix64 output function applied to
-// seed + (counter + 1) * 0x9E3779B97F4A7C15, counter = pos * V + i: a pure function of (seed, pos, i), exact in
-// float32.  Rows with temperature 0 are the plain argmax.  Lowest index on ties.
-
-__device__ __forceinline__ float gumbel_noise(uint64_t seed, uint64_t counter) {
-    uint64_t z = seed + (counter + 1) * 0x9E3779B97F4A7C15ull;
-    z = (z ^ (z >> 30)) * 0xBF58476D1CE4E5B9ull;
-    z = (z ^ (z >> 27)) * 0x94D049BB133111EBull;
-    z ^= z >> 31;
-    const float u = ((float)(uint32_t)(z >> 41) + 0.5f) * (1.0f / 8388608.0f);
-    return -logf(-logf(u));
-}
+// argmax_i (logit_i / T + g_i), g_i standard Gumbel noise (gumbel_noise, counter pos * V + i): a draw from softmax(logits / T).
+// Rows with temperature 0 are the plain argmax.  Lowest index on ties.
 
 __global__ __launch_bounds__(1024) void k_sample(const float *__restrict__ logits, int V,
                                                  const float *__restrict__ temperature,

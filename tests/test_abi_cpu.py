@@ -472,3 +472,82 @@ def test_rows_too_long_for_32_bit_offsets_take_no_tile():
     assert _f16_rows(65, 100, K, ld.LDK_STORE) == 0
     for T in (65, 300):
         assert ld.ldk_linear_scratch_bytes(T, 8, K, ld.LDK_STORE) == 4 * T * K + -(-K // 1024) * 64 * 8 * 4
+
+
+# ---------------------------------------------------------------- the operators of a light decode step: sizes and refusals
+
+def _refused(status, call, *args):
+    assert getattr(ld.lib(), call)(*args) == status and call in ld.ld_last_error()
+
+
+def test_w4_image_and_scratch_sizes():
+    import torch
+    # tiles of 16 x 128 codes, scales, zero points; nothing else
+    assert ld.ldk_w4_image_bytes(4096, 4096, 128, 1, torch.bfloat16, False) == 4096 * 4096 // 2 + 4096 * 32 * 2
+    assert ld.ldk_w4_image_bytes(4096, 4096, 32, 2, torch.float32, True) == 2 * (4096 * 4096 // 2 + 4096 * 128 * 5)
+    assert ld.ldk_w4_image_bytes(1, 1, 64, 1, torch.float32, False) >= 1024 + 2 * 16 * 4
+    for bad in [(0, 8, 64, 1), (8, 0, 64, 1), (8, 8, 48, 1), (8, 8, 64, 3), (-1, 8, 64, 1)]:
+        assert ld.ldk_w4_image_bytes(*bad, torch.bfloat16, False) == 0
+    n = [ld.ldk_linear_w4_scratch_bytes(T, 4096, 4096) for T in (1, 2, 8, 9, 16, 17, 64, 65, 300, 2111)]
+    assert n == sorted(n) and n[0] > 0 and ld.ldk_linear_w4_scratch_bytes(0, 8, 8) == 0
+    with pytest.raises(ld.LdError):
+        ld.W4Matrix(16, 16, 64, scale_dtype=torch.float16, device="cpu")
+    with pytest.raises(ld.LdError):
+        ld.W4Matrix.pack(torch.zeros(4, 7, dtype=torch.uint8), torch.ones(4, 1), None, 4, 16, 64)
+    with pytest.raises(ld.LdError):
+        ld.W4Matrix.quantize(torch.zeros(5, 64), 64, parts=2)
+
+
+def test_w4_refusals():
+    big = 1 << 40
+    pack = lambda **k: [{**dict(c=FAKE, s=FAKE, d=0, z=None, N=16, K=128, g=64, p=1, i=FAKE, b=big, st=None), **k}[n] for n in "c s d z N K g p i b st".split()]
+    for k in [dict(c=None), dict(s=None), dict(i=None), dict(i=FAKE + 8), dict(d=7), dict(g=96), dict(p=0), dict(N=0), dict(K=-4), dict(b=1024)]:
+        _refused(ld.LD_E_INVAL, "ldk_w4_pack", *pack(**k))
+    quant = lambda **k: [{**dict(W=FAKE, d=1, N=16, K=128, g=64, p=1, sd=1, z=0, i=FAKE, b=big, st=None), **k}[n] for n in "W d N K g p sd z i b st".split()]
+    for k in [dict(W=None), dict(d=2), dict(sd=-1), dict(i=FAKE + 4), dict(g=16), dict(b=100)]:
+        _refused(ld.LD_E_INVAL, "ldk_w4_quantize", *quant(**k))
+    lin = lambda **k: [{**dict(i=FAKE, sd=1, z=0, g=64, x=FAKE, w=None, e=0.0, T=3, N=16, K=128, ep=0, y=FAKE, s=FAKE, b=big, st=None), **k}[n]
+                       for n in "i sd z g x w e T N K ep y s b st".split()]
+    for k in [dict(i=None), dict(i=FAKE + 2), dict(x=None), dict(y=None), dict(s=None), dict(s=FAKE + 8), dict(b=64), dict(T=-1), dict(N=0), dict(K=0),
+              dict(g=100), dict(sd=3), dict(ep=3), dict(ep=-1)]:
+        _refused(ld.LD_E_INVAL, "ldk_linear_w4", *lin(**k))
+    assert ld.lib().ldk_linear_w4(*lin(T=0, x=None, y=None, i=None)) == ld.LD_OK
+
+
+def test_key_bounds_and_sparse_attention_refusals():
+    big = 1 << 40
+    summ = lambda **k: [{**dict(p=FAKE, d=1, t=FAKE, ts=4, r=FAKE, n=2, m=16, h=2, hd=128, b=FAKE, u=FAKE, st=None), **k}[n] for n in "p d t ts r n m h hd b u st".split()]
+    for k in [dict(p=None), dict(t=None), dict(r=None), dict(b=None), dict(u=None), dict(d=2), dict(n=-1), dict(m=-1), dict(h=0), dict(hd=96),
+              dict(p=FAKE + 8), dict(b=FAKE + 4)]:
+        _refused(ld.LD_E_INVAL, "ldk_kv_summary", *summ(**k))
+    _refused(ld.LD_E_RANGE, "ldk_kv_summary", *summ(n=70000))
+    assert ld.lib().ldk_kv_summary(*summ(n=0, p=None)) == ld.LD_OK and ld.lib().ldk_kv_summary(*summ(m=0)) == ld.LD_OK
+    names = "q qs p d b u t ts sl c mc T H Hkv hd w bu kf kl o se s sb st".split()
+    base = dict(q=FAKE, qs=512, p=FAKE, d=1, b=FAKE, u=FAKE, t=FAKE, ts=8, sl=FAKE, c=FAKE, mc=100, T=2, H=4, Hkv=2, hd=128, w=0, bu=4, kf=1, kl=1, o=FAKE,
+                se=FAKE, s=FAKE, sb=big, st=None)
+    sparse = lambda **k: [{**base, **k}[n] for n in names]
+    for k in [dict(q=None), dict(p=None), dict(b=None), dict(u=None), dict(t=None), dict(sl=None), dict(c=None), dict(o=None), dict(se=None), dict(s=None),
+              dict(d=2), dict(mc=0), dict(T=-1), dict(H=5), dict(Hkv=0), dict(hd=80), dict(w=-1), dict(bu=0), dict(kl=0), dict(kf=-1), dict(kf=3, kl=2),
+              dict(sb=16), dict(p=FAKE + 8), dict(s=FAKE + 4)]:
+        _refused(ld.LD_E_INVAL, "ldk_sparse_attention", *sparse(**k))
+    _refused(ld.LD_E_RANGE, "ldk_sparse_attention", *sparse(T=70000))
+    assert ld.lib().ldk_sparse_attention(*sparse(T=0, q=None)) == ld.LD_OK
+    # a buffer for more rows, longer contexts or larger budgets serves less
+    n = lambda T, mc, bu: ld.ldk_sparse_attention_scratch_bytes(T, 32, 8, 128, mc, 0, bu)
+    for T in range(1, 40):
+        assert n(T, 5000, 64) <= n(T + 1, 5000, 64) and n(T, 100 * T, 64) <= n(T, 100 * T + 100, 64)
+    assert ld.ldk_sparse_attention_scratch_bytes(1, 5, 2, 128, 10, 0, 4) == 0
+
+
+def test_choose_refusals():
+    R, V = 4, 5000
+    call = lambda rules=None, **k: [{**dict(l=FAKE, R=R, V=V, r=C.byref(rules) if rules is not None else None, te=None, se=None, po=None, a=None, to=FAKE, s=FAKE,
+                                            b=1 << 20, st=None), **k}[n] for n in "l R V r te se po a to s b st".split()]
+    for k in [dict(l=None), dict(to=None), dict(R=-1), dict(V=0), dict(s=None), dict(s=FAKE + 4), dict(b=8), dict(te=FAKE), dict(te=FAKE, se=FAKE)]:
+        _refused(ld.LD_E_INVAL, "ldk_choose", *call(**k))
+    for k in [dict(history=FAKE), dict(history=FAKE, history_len=FAKE), dict(penalties=FAKE), dict(history=FAKE, history_len=FAKE, penalties=FAKE, history_stride=-1),
+              dict(bias=FAKE), dict(bias=FAKE, bias_start=FAKE), dict(mask=FAKE, mask_row=FAKE), dict(mask=FAKE, mask_rows=3)]:
+        _refused(ld.LD_E_INVAL, "ldk_choose", *call(ld.ld_token_rules(**k)))
+    _refused(ld.LD_E_RANGE, "ldk_choose", *call(R=70000, b=1 << 40))
+    assert ld.lib().ldk_choose(*call(R=0, l=None)) == ld.LD_OK
+    assert ld.ldk_choose_scratch_bytes(0, V) == 0 and ld.ldk_choose_scratch_bytes(R, V) > 0

@@ -1,0 +1,568 @@
+"""The operators of a light decode step (4-bit linear layers, key bounds, block-sparse attention, choice under rules) on the GPU,
+against plain implementations in 64 bits written here."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+import paper_2406_00059_amd as ld
+from workloads import gen
+from helpers import device_pool
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda"
+
+
+def _rel(got, ref):
+    """2-norm of the difference over the 2-norm of the reference."""
+    got, ref = got.double().cpu(), ref.double().cpu()
+    return ((got - ref).norm() / ref.norm()).item()
+
+
+# ---------------------------------------------------------------- 4-bit linear layers
+
+def _w4(seed, rows, K, group, zeros, scales):
+    """Row-major codes (one a byte), scales and zero points; the matrix they stand for in float64."""
+    groups = -(-K // group)
+    c = gen.randint(seed, 1, 0, 15, rows * K).view(rows, K)
+    s = (0.01 + 0.02 * gen.uniform01(seed, 2, 0, rows * groups).view(rows, groups)).to(scales)
+    z = gen.randint(seed, 3, 0, 15, rows * groups).view(rows, groups) if zeros else None
+    col = torch.arange(K) // group
+    W = (c - (z[:, col] if zeros else 8)).double() * s.double()[:, col]
+    return c, s, z, W
+
+
+def _packed(c, s, z, rows, K, group, parts=1):
+    even = torch.zeros(c.shape[0], (K + 1) // 2 * 2, dtype=torch.int64)
+    even[:, :K] = c
+    bytes_ = (even[:, 0::2] + 16 * even[:, 1::2]).to(torch.uint8)
+    return ld.W4Matrix.pack(bytes_.to(DEV), s.to(DEV), None if z is None else z.to(torch.uint8).to(DEV), rows, K, group, parts)
+
+
+def _linear(w, x, epilogue=ld.LDK_STORE, g=None, y=None, spare=0):
+    T, K = x.shape
+    y = torch.full((T, w.N), float("nan"), device=DEV) if y is None else y
+    n = ld.ldk_linear_w4_scratch_bytes(T, w.N, K, epilogue)
+    scratch = torch.full((n + spare,), 255, dtype=torch.uint8, device=DEV)      # NaN patterns: nothing in it has to be clear
+    ld.ldk_linear_w4(w, x.to(DEV), y, epilogue, g=None if g is None else g.to(DEV), eps=1e-5, scratch=scratch)
+    return y
+
+
+# Relative 2-norm error of a random product.  A term's two fp16 parts keep 22 bits (2^-23 off at most, 2^-24 in the mean); a group's sum
+# of c x runs to 8.7 sqrt(128) |x| where its result is 4.6 sqrt(128) |x|, and each of its some ten roundings is 2^-25 in the mean: 2e-7 in all.
+LINEAR = 1e-6
+
+
+@pytest.mark.parametrize("zeros,scales", [(False, torch.bfloat16), (True, torch.bfloat16), (True, torch.float32)],
+                         ids=["bf16", "bf16-zeros", "f32-zeros"])
+@pytest.mark.parametrize("group", [32, 64, 128])
+@pytest.mark.parametrize("T", [1, 2, 7, 8, 9, 16, 17, 33, 64, 65, 130, 257])
+def test_w4_linear_rows_groups_and_types(T, group, zeros, scales):
+    N, K = 301, 688
+    c, s, z, W = _w4(T, N, K, group, zeros, scales)
+    x = gen.normal(T, 5, (T, K))
+    y = _linear(_packed(c, s, z, N, K, group), x)
+    assert _rel(y, x.double() @ W.t()) <= LINEAR
+
+
+@pytest.mark.parametrize("N,K", [(1, 1), (1, 4096), (3, 31), (16, 32), (15, 33), (17, 127), (33, 129), (256, 256), (48, 1000), (1024, 11008), (4100, 520)])
+@pytest.mark.parametrize("T", [1, 5, 20, 100, 300])
+def test_w4_linear_odd_shapes(T, N, K):
+    c, s, z, W = _w4(N, N, K, 64, True, torch.bfloat16)
+    x = gen.normal(K, 5, (T, K))
+    y = _linear(_packed(c, s, z, N, K, 64), x)
+    ref = x.double() @ W.t()
+    mass = x.double().abs() @ (W.abs() + 8 * s.double()[:, torch.arange(K) // 64]).t()
+    assert ((y.cpu().double() - ref).abs() <= 2.0 ** -23 * (60 + K / 32) * mass + 1e-30).all()      # every rounding the same way
+    if N * T >= 100 and K >= 100:
+        assert _rel(y, ref) <= LINEAR
+
+
+@pytest.mark.parametrize("T", [1, 3, 12, 40, 150])
+def test_w4_linear_residual_norm_and_gated_activation(T):
+    N, K, group = 173, 512, 128
+    c, s, z, W = _w4(9, 2 * N, K, group, False, torch.bfloat16)
+    s, W = s * 0.125, W * 0.125
+    x, g = gen.normal(9, 5, (T, K)), gen.normal(9, 6, (K,), std=0.1, mean=1.0)
+    xn = x.double() / torch.sqrt((x.double() ** 2).mean(1, keepdim=True) + 1e-5) * g.double()
+    y = _linear(_packed(c, s, z, N, K, group, 2), x, ld.LDK_SWIGLU, g)
+    gu = xn @ W.t()
+    ref = gu[:, :N] * torch.sigmoid(gu[:, :N]) * gu[:, N:]
+    assert _rel(y, ref) <= 3 * LINEAR      # two products and the activation between
+    one = _packed(c[:N], s[:N], None, N, K, group)
+    y0 = gen.normal(9, 7, (T, N))
+    y = _linear(one, x, ld.LDK_ADD, g, y0.to(DEV))
+    assert _rel(y.cpu().double() - y0.double(), gu[:, :N]) <= 2 * LINEAR
+    y = _linear(one, x, ld.LDK_STORE, g)
+    assert _rel(y, gu[:, :N]) <= LINEAR
+
+
+@pytest.mark.parametrize("group", [32, 64, 128])
+@pytest.mark.parametrize("zeros", [False, True])
+def test_w4_columns_come_back_exactly(group, zeros):
+    """Unit rows pick the columns of the matrix: (c - z) s with one rounding, every column in its place."""
+    N, K = 37, 300
+    c, s, z, W = _w4(21, N, K, group, zeros, torch.float32)
+    y = _linear(_packed(c, s, z, N, K, group), torch.eye(K))
+    assert torch.equal(y.cpu(), W.float().t())
+
+
+@pytest.mark.parametrize("T", [1, 6, 30, 100])
+def test_w4_rows_of_any_magnitude(T):
+    """Each row has a power of two of its own: tiny, huge, subnormal and zero rows, and columns far larger than the others."""
+    N, K, group = 64, 384, 128
+    c, s, z, W = _w4(31, N, K, group, True, torch.float32)
+    x = gen.normal(31, 5, (T, K))
+    for t in range(T):
+        x[t] *= [1.0, 1e-30, 1e30, 3e-39, 0.0, 2.0 ** 100][t % 6]
+        if t % 3 == 0:
+            x[t, 5::50] *= 1000.0
+    y = _linear(_packed(c, s, z, N, K, group), x).cpu()
+    ref = x.double() @ W.t()
+    for t in range(T):
+        if ref[t].abs().max() == 0:
+            assert (y[t] == 0).all()
+        else:
+            # the subnormal row's own outputs are subnormal floats: half a unit of 2^-149 on top
+            assert ((y[t].double() - ref[t]).norm() <= LINEAR * ref[t].norm() + 2.0 ** -150 * 8).all()
+
+
+@pytest.mark.parametrize("T", [2, 8, 9, 70])
+@pytest.mark.parametrize("bad", [float("nan"), float("inf"), -float("inf")])
+def test_w4_rows_that_are_not_finite_stay_alone(T, bad):
+    N, K, group = 40, 256, 64
+    c, s, z, W = _w4(33, N, K, group, False, torch.bfloat16)
+    x = gen.normal(33, 5, (T, K))
+    w = _packed(c, s, z, N, K, group)
+    clean = _linear(w, x)
+    x[T // 2, 100] = bad
+    y = _linear(w, x)
+    rest = [t for t in range(T) if t != T // 2]
+    assert torch.isnan(y[T // 2]).all() and torch.equal(y[rest], clean[rest])
+
+
+def test_w4_linear_runs_on_the_callers_stream_and_repeats_bit_for_bit():
+    N, K, group, T = 512, 1024, 128, 5
+    c, s, z, W = _w4(35, N, K, group, True, torch.bfloat16)
+    w = _packed(c, s, z, N, K, group)
+    x = gen.normal(35, 5, (T, K)).to(DEV)
+    a = _linear(w, x)
+    torch.cuda.synchronize()
+    st = torch.cuda.Stream()
+    with torch.cuda.stream(st):
+        b = _linear(w, x)
+    st.synchronize()
+    assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("zeros", [False, True])
+@pytest.mark.parametrize("group,parts,N,K", [(32, 1, 19, 200), (64, 2, 24, 128), (128, 1, 16, 130)])
+def test_w4_quantize_rounds_to_nearest(dtype, zeros, group, parts, N, K):
+    W = gen.normal(41, 1, (parts * N, K), std=0.02).to(dtype)
+    W[3] = 0
+    w = ld.W4Matrix.quantize(W.to(DEV), group, parts, torch.bfloat16, zeros)
+    # an image of two parts is read back part by part through the gated product's operands: pack the same codes and compare images
+    f = W.float()
+    groups = -(-K // group)
+    codes, scales, zs = torch.zeros(parts * N, K, dtype=torch.int64), torch.zeros(parts * N, groups), torch.zeros(parts * N, groups)
+    for j in range(groups):
+        part = f[:, j * group:(j + 1) * group]
+        lo, hi = part.amin(1).clamp(max=0), part.amax(1).clamp(min=0)
+        s = ((hi - lo) / 15 if zeros else torch.maximum(hi, -lo) / 7).bfloat16().float()
+        z = torch.where(s > 0, torch.round(-lo / s).clamp(0, 15), 0.0) if zeros else torch.full_like(s, 8)
+        q = torch.where(s[:, None] > 0, torch.round(part / s[:, None]) + z[:, None], z[:, None]).clamp(0, 15)
+        codes[:, j * group:(j + 1) * group], scales[:, j], zs[:, j] = q.long(), s, z
+    ref = _packed(codes, scales.bfloat16(), zs.long() if zeros else None, N, K, group, parts)
+    # columns past K hold whatever code stands for zero: their activations are zero
+    eye = torch.eye(K)
+    if parts == 1:
+        assert torch.equal(_linear(w, eye), _linear(ref, eye))
+        err = (_linear(w, eye).cpu().t() - f).abs()
+        step = scales.repeat_interleave(group, 1)[:, :K]
+        assert (err <= step * (0.51 if not zeros else 1.02)).all()      # half a step; with zero points the ends may clip by another half
+    else:
+        assert torch.equal(_linear(w, 30 * eye, ld.LDK_SWIGLU), _linear(ref, 30 * eye, ld.LDK_SWIGLU))
+
+
+# ---------------------------------------------------------------- key bounds
+
+def _units(top):
+    return np.array([2.0 ** max(math.floor(math.log2(v)) - 6, -126) if v > 0 else 1.0 for v in top.reshape(-1)]).reshape(top.shape)
+
+
+def _bounds64(keys, n):
+    """keys float64 [Hkv, 16, hd], n of them cached -> (bounds [Hkv, 2, hd], unit [Hkv])."""
+    k = keys[:, :n]
+    u = _units(np.abs(k).max((1, 2)))
+    up = np.minimum(np.ceil(k.max(1) / u[:, None]), 127)
+    down = np.maximum(np.floor(k.min(1) / u[:, None]), -127)
+    return np.stack([up, down], 1).astype(np.int8), u
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("hd", [64, 128])
+@pytest.mark.parametrize("Hkv", [1, 3, 8])
+def test_kv_summary_of_appended_ranges(dtype, hd, Hkv):
+    nblk = 40
+    pool = gen.normal(51, 1, (nblk, 2, Hkv, 16, hd), dtype=torch.float32).to(dtype)
+    pool[7, 0, 0] = 0
+    pool[9, 0] *= 2.0 ** 60
+    pool[11, 0] *= 2.0 ** -60
+    table = torch.full((4, 20), -1, dtype=torch.int32)
+    table[0, :18] = gen.permutation(52, 1, nblk)[:18]
+    table[1, :5] = gen.permutation(52, 1, nblk)[18:23]
+    table[3, 0] = gen.permutation(52, 1, nblk)[23].item()
+    ranges = [(0, 3, 275), (1, 64, 65), (3, 0, 1), (2, 0, 16), (1, 5, 5)]      # sequence 2 has no blocks, the last range is empty
+    host = pool.double().numpy()
+    bounds = torch.full((nblk, Hkv, 2, hd), 99, dtype=torch.int8, device=DEV)
+    unit = torch.full((nblk, Hkv), -5.0, device=DEV)
+    dev = pool.clone()
+    for s, first, end in ranges:      # what lies past a sequence's end is nobody's key
+        if end % 16 and table[s, end // 16] >= 0:
+            dev[table[s, end // 16], 0, :, end % 16:] = float("nan")
+    ld.ldk_kv_summary(dev.to(DEV), table.to(DEV), torch.tensor(ranges, dtype=torch.int32, device=DEV), 272, Hkv, hd, bounds, unit)
+    want_b, want_u = np.full((nblk, Hkv, 2, hd), 99, np.int8), np.full((nblk, Hkv), -5.0)
+    for s, first, end in ranges:
+        for b in range(first // 16, -(-end // 16) if end > first else 0):
+            p = int(table[s, b])
+            if p >= 0:
+                want_b[p], want_u[p] = _bounds64(host[p, 0], min(16, end - 16 * b))
+    np.testing.assert_array_equal(bounds.cpu().numpy(), want_b)
+    np.testing.assert_array_equal(unit.cpu().numpy().astype(np.float64), want_u)
+
+
+def test_kv_summary_marks_keys_that_are_not_finite():
+    pool = gen.normal(53, 1, (3, 2, 2, 16, 64))
+    pool[0, 0, 0, 3, 5] = float("nan")
+    pool[1, 0, 1, 15, 63] = -float("inf")
+    table = torch.tensor([[0, 1, 2]], dtype=torch.int32, device=DEV)
+    bounds, unit = torch.zeros((3, 2, 2, 64), dtype=torch.int8, device=DEV), torch.zeros((3, 2), device=DEV)
+    ld.ldk_kv_summary(pool.to(DEV), table, torch.tensor([[0, 0, 48]], dtype=torch.int32, device=DEV), 48, 2, 64, bounds, unit)
+    assert torch.isinf(unit.cpu()).tolist() == [[True, False], [False, True], [False, False]]
+
+
+# ---------------------------------------------------------------- block-sparse attention
+
+def _sparse64(q, pool, bounds, unit, table, slot, ctx, H, Hkv, hd, window, budget, first, last):
+    """pool float64 logical [block][2][Hkv][16][hd]; -> (out [T, H, hd], sel [T, Hkv, budget])."""
+    G, T = H // Hkv, q.shape[0]
+    out, sel = np.zeros((T, H, hd)), np.full((T, Hkv, budget), -1, np.int32)
+    for t in range(T):
+        start = max(0, ctx[t] - window) if window else 0
+        lo, hi = start // 16, -(-ctx[t] // 16)
+        if ctx[t] <= 0:
+            continue
+        phys = table[slot[t], lo:hi]
+        n = hi - lo
+        for j in range(Hkv):
+            score = np.full(n, -np.inf)
+            for h in range(j * G, (j + 1) * G):
+                qh = q[t, h].astype(np.float64)
+                finite = np.isfinite(qh).all()
+                v = _units(np.array([np.abs(qh).max()]))[0] if finite else 1.0
+                qi = np.clip(np.rint(qh / v), -127, 127).astype(np.int64) if finite else np.zeros(hd, np.int64)
+                b = bounds[phys, j].astype(np.int64)
+                dot = (np.maximum(qi, 0) * b[:, 0] + np.minimum(qi, 0) * b[:, 1]).sum(1)
+                u = unit[phys, j]
+                score = np.maximum(score, np.where(np.isinf(u), np.inf, dot * v * np.where(np.isinf(u), 1, u)))
+            order = np.argsort(-score, kind="stable").tolist()
+            kept = sorted(set(range(min(first, n))) | set(range(max(0, n - last), n)))
+            took = sorted((kept + [i for i in order if i not in set(kept)])[:budget])
+            sel[t, j, :len(took)] = np.array(took) + lo
+            pos = np.concatenate([np.arange(16) + 16 * (lo + i) for i in took])
+            keys = np.concatenate([pool[phys[i], 0, j] for i in took])
+            vals = np.concatenate([pool[phys[i], 1, j] for i in took])
+            ok = (pos >= start) & (pos < ctx[t])
+            for h in range(j * G, (j + 1) * G):
+                s = keys[ok] @ q[t, h].astype(np.float64) / math.sqrt(hd)
+                p = np.exp(s - s.max())
+                out[t, h] = p / p.sum() @ vals[ok]
+    return out, sel
+
+
+def _sparse_case(seed, dtype, H, Hkv, hd, ctx, std=1.0):
+    T = len(ctx)
+    nb = [-(-max(c, 1) // 16) for c in ctx]
+    perm = gen.permutation(seed, 1, sum(nb) + 3).numpy()
+    table = np.full((T, max(nb) + 1), -1, np.int32)
+    at = 0
+    for s, n in enumerate(nb):
+        table[s, :n] = perm[at:at + n]
+        at += n
+    logical = gen.normal(seed, 2, (sum(nb) + 3, 2, Hkv, 16, hd)).to(dtype)
+    slot = np.arange(T)[::-1].copy()
+    table = table[::-1].copy()      # row t's table row is not row t
+    for t in range(T):      # unwritten slots of a last block
+        if ctx[t] % 16:
+            logical[table[slot[t], ctx[t] // 16], :, :, ctx[t] % 16:] = float("nan")
+    q = gen.normal(seed, 3, (T, H, hd), std=std)
+    return q, logical, table, slot
+
+
+def _run_sparse(q, logical, table, slot, ctx, H, Hkv, hd, window, budget, first, last, fill=255, extra=0):
+    """Bounds through ldk_kv_summary, then the attention; q rows are the first H hd floats of longer ones."""
+    T = len(ctx)
+    pool = device_pool(logical).to(DEV)
+    tab = torch.as_tensor(table, device=DEV)
+    bounds = torch.zeros((pool.shape[0], Hkv, 2, hd), dtype=torch.int8, device=DEV)
+    unit = torch.zeros((pool.shape[0], Hkv), device=DEV)
+    ranges = torch.tensor([[slot[t], 0, ctx[t]] for t in range(T)], dtype=torch.int32, device=DEV)
+    ld.ldk_kv_summary(pool, tab, ranges, max(max(ctx), 1), Hkv, hd, bounds, unit)
+    qd = torch.full((T, H * hd + 64), float("nan"), device=DEV)
+    qd[:, :H * hd] = q.reshape(T, -1).to(DEV)
+    out = torch.full((T, H, hd), float("nan"), device=DEV)
+    sel = torch.full((T, Hkv, budget), -7, dtype=torch.int32, device=DEV)
+    n = ld.ldk_sparse_attention_scratch_bytes(T, H, Hkv, hd, max(max(ctx), 1), window, budget)
+    scratch = torch.full((n,), fill, dtype=torch.uint8, device=DEV)
+    ld.ldk_sparse_attention(qd, H * hd + 64, pool, bounds, unit, tab, torch.as_tensor(slot.astype(np.int32), device=DEV),
+                            torch.tensor(ctx, dtype=torch.int32, device=DEV), max(max(ctx), 1), H, Hkv, hd, budget, first, last, out, sel, scratch,
+                            window=window)
+    return out, sel, bounds.cpu().numpy(), unit.cpu().numpy().astype(np.float64)
+
+
+# Relative 2-norm error of attention: scores of magnitude up to some 4 in float32 (2^-24 of their terms' sum, exponent base 2) and operands of
+# 16 significant bits or more in the products of probabilities and values.
+ATTENTION = 5e-6
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32], ids=["bf16", "f32"])
+@pytest.mark.parametrize("H,Hkv,hd", [(4, 4, 128), (8, 2, 128), (4, 1, 64), (6, 2, 64), (20, 1, 128), (3, 3, 64)])
+@pytest.mark.parametrize("window", [0, 100])
+def test_sparse_attention_choice_and_result(dtype, H, Hkv, hd, window):
+    ctx = [1, 16, 17, 0, 333, 700, 95, 1029]
+    budget, first, last = 9, 1, 2
+    q, logical, table, slot = _sparse_case(61, dtype, H, Hkv, hd, ctx)
+    out, sel, bounds, unit = _run_sparse(q, logical, table, slot, ctx, H, Hkv, hd, window, budget, first, last)
+    ref, want = _sparse64(q.numpy(), logical.double().numpy(), bounds, unit, table, slot, ctx, H, Hkv, hd, window, budget, first, last)
+    np.testing.assert_array_equal(sel.cpu().numpy(), want)
+    assert (out[3] == 0).all()
+    assert _rel(out, torch.from_numpy(ref)) <= ATTENTION
+
+
+@pytest.mark.parametrize("budget,first,last", [(1, 0, 1), (2, 0, 2), (5, 2, 3), (6, 0, 1), (33, 3, 1), (64, 1, 4), (100, 0, 1)])
+def test_sparse_attention_budgets(budget, first, last):
+    """Nothing but the kept blocks, one more, some, all of them; a buffer sized for more serves fewer."""
+    H, Hkv, hd, ctx = 4, 2, 128, [1024, 80, 1, 1500]
+    q, logical, table, slot = _sparse_case(62, torch.bfloat16, H, Hkv, hd, ctx)
+    out, sel, bounds, unit = _run_sparse(q, logical, table, slot, ctx, H, Hkv, hd, 0, budget, first, last, fill=0)
+    ref, want = _sparse64(q.numpy(), logical.double().numpy(), bounds, unit, table, slot, ctx, H, Hkv, hd, 0, budget, first, last)
+    np.testing.assert_array_equal(sel.cpu().numpy(), want)
+    assert _rel(out, torch.from_numpy(ref)) <= ATTENTION
+    for T, mc in [(1, 1500), (2, 17), (4, 700)]:
+        assert ld.ldk_sparse_attention_scratch_bytes(T, H, Hkv, hd, mc, 0, budget) <= ld.ldk_sparse_attention_scratch_bytes(4, H, Hkv, hd, 1500, 0, budget)
+
+
+def test_sparse_attention_equal_scores_take_the_lowest_index():
+    """Every block the same keys: the kept ones, then the first others."""
+    H, Hkv, hd, ctx = 2, 1, 64, [16 * 300]
+    q, logical, table, slot = _sparse_case(63, torch.float32, H, Hkv, hd, ctx)
+    logical[:] = logical[0]
+    out, sel, _, _ = _run_sparse(q, logical, table, slot, ctx, H, Hkv, hd, 0, 20, 0, 3)
+    assert sel[0, 0].tolist() == list(range(17)) + [297, 298, 299]
+
+
+def test_sparse_attention_with_the_whole_context_is_the_dense_one():
+    H, Hkv, hd, ctx = 8, 2, 128, [500, 31, 272]
+    q, logical, table, slot = _sparse_case(64, torch.bfloat16, H, Hkv, hd, ctx)
+    out, sel, _, _ = _run_sparse(q, logical, table, slot, ctx, H, Hkv, hd, 0, 32, 0, 1)
+    pool, dense = device_pool(logical).to(DEV), torch.empty(3, H, hd, device=DEV)
+    scratch = torch.empty(ld.ldk_attention_scratch_bytes(3, H, Hkv, hd, 500), dtype=torch.uint8, device=DEV)
+    ld.ldk_paged_attention(q.reshape(3, -1).to(DEV), H * hd, pool, torch.as_tensor(table, device=DEV),
+                           torch.as_tensor(slot.astype(np.int32), device=DEV), torch.tensor(ctx, dtype=torch.int32, device=DEV), 500, H, Hkv, hd,
+                           dense, scratch)
+    assert _rel(out, dense) <= 2e-5
+    assert (sel[1, 0].tolist()) == [0, 1] + [-1] * 30
+
+
+def test_sparse_attention_long_context_and_sharp_scores():
+    """8192 blocks a sequence, scores spread widely: the running maximum moves, chunks and waves differ by many orders of magnitude."""
+    H, Hkv, hd, ctx = 8, 2, 128, [131070, 40000]
+    q, logical, table, slot = _sparse_case(65, torch.bfloat16, H, Hkv, hd, ctx, std=4.0)
+    out, sel, bounds, unit = _run_sparse(q, logical, table, slot, ctx, H, Hkv, hd, 0, 200, 1, 4)
+    ref, want = _sparse64(q.numpy(), logical.double().numpy(), bounds, unit, table, slot, ctx, H, Hkv, hd, 0, 200, 1, 4)
+    np.testing.assert_array_equal(sel.cpu().numpy(), want)
+    assert _rel(out, torch.from_numpy(ref)) <= 4 * ATTENTION      # four times the scores, four times their errors
+
+
+def test_sparse_attention_queries_and_keys_that_are_not_finite():
+    """A block with a NaN key is always chosen (its sequence's result shows the NaN, as dense attention's would), a query head with a NaN scores
+    nothing; other rows are not touched."""
+    H, Hkv, hd, ctx = 2, 1, 64, [1600, 1600, 1600]
+    q, logical, table, slot = _sparse_case(66, torch.float32, H, Hkv, hd, ctx)
+    q[2, 1, 3] = float("nan")
+    logical[table[slot[1], 40], 0, 0, 5, 7] = float("nan")
+    out, sel, bounds, unit = _run_sparse(q, logical, table, slot, ctx, H, Hkv, hd, 0, 12, 1, 1)
+    with np.errstate(invalid="ignore"):
+        ref, want = _sparse64(q.numpy(), logical.double().numpy(), bounds, unit, table, slot, ctx, H, Hkv, hd, 0, 12, 1, 1)
+    np.testing.assert_array_equal(sel.cpu().numpy(), want)
+    assert 40 in sel[1, 0].tolist() and torch.isnan(out[1]).all()
+    assert torch.isnan(out[2, 1]).all()
+    assert _rel(out[0], torch.from_numpy(ref[0])) <= ATTENTION and _rel(out[2, 0], torch.from_numpy(ref[2, 0])) <= ATTENTION
+
+
+def test_sparse_attention_offsets_beyond_32_bits():
+    """A pool of more than 2^32 bytes (and 2^31 elements) whose sequence lies in its last blocks."""
+    H, Hkv, hd, ctx = 32, 32, 128, [400]
+    nblk = 17000      # 131072 elements a block
+    pool = torch.zeros((nblk, 2, Hkv, 16, hd), dtype=torch.bfloat16, device=DEV)
+    q, logical, _, slot = _sparse_case(67, torch.bfloat16, H, Hkv, hd, ctx)
+    n = 25
+    table = np.array([[nblk - 1 - 2 * i for i in range(n)]], np.int32)
+    blocks = logical[:n].clone()
+    blocks[blocks != blocks] = 0
+    pool[torch.as_tensor(table[0], device=DEV).long()] = device_pool(blocks).to(DEV)
+    bounds, unit = torch.zeros((nblk, Hkv, 2, hd), dtype=torch.int8, device=DEV), torch.zeros((nblk, Hkv), device=DEV)
+    tab = torch.as_tensor(table, device=DEV)
+    ld.ldk_kv_summary(pool, tab, torch.tensor([[0, 0, 400]], dtype=torch.int32, device=DEV), 400, Hkv, hd, bounds, unit)
+    out, sel = torch.empty(1, H, hd, device=DEV), torch.empty((1, Hkv, 8), dtype=torch.int32, device=DEV)
+    scratch = torch.empty(ld.ldk_sparse_attention_scratch_bytes(1, H, Hkv, hd, 400, 0, 8), dtype=torch.uint8, device=DEV)
+    ld.ldk_sparse_attention(q.reshape(1, -1).to(DEV), H * hd, pool, bounds, unit, tab, torch.zeros(1, dtype=torch.int32, device=DEV),
+                            torch.tensor(ctx, dtype=torch.int32, device=DEV), 400, H, Hkv, hd, 8, 1, 2, out, sel, scratch)
+    where = torch.as_tensor(table[0], device=DEV).long()
+    small = np.arange(n, dtype=np.int32)[None]
+    ref, want = _sparse64(q.numpy(), blocks.double().numpy(), bounds[where].cpu().numpy(), unit[where].cpu().numpy().astype(np.float64), small,
+                          np.zeros(1, int), ctx, H, Hkv, hd, 0, 8, 1, 2)
+    np.testing.assert_array_equal(sel.cpu().numpy(), want)
+    assert _rel(out, torch.from_numpy(ref)) <= ATTENTION
+
+
+# ---------------------------------------------------------------- choice under rules
+
+def _choose(logits, **kw):
+    R, V = logits.shape
+    want = kw.pop("want", False)
+    token = torch.full((R,), -9, dtype=torch.int32, device=DEV)
+    adjusted = torch.full((R, V), float("nan"), device=DEV) if want else None
+    scratch = torch.full((max(8, ld.ldk_choose_scratch_bytes(R, V)),), 255, dtype=torch.uint8, device=DEV)
+    kw = {k: v.to(DEV) if isinstance(v, torch.Tensor) else v for k, v in kw.items()}
+    ld.ldk_choose(logits.to(DEV), token, adjusted=adjusted, scratch=scratch, **kw)
+    return token.cpu(), None if adjusted is None else adjusted.cpu()
+
+
+def _rules(seed, R, V, n):
+    """History with frequent tokens and tokens outside the vocabulary, prompt lengths, penalties, biases with repeated entries, masks."""
+    h = (V * gen.uniform01(seed, 1, 0, R * n).view(R, n) ** 3).int()
+    h[:, ::17] = V + 5
+    h[:, 1::19] = -3
+    length = gen.randint(seed, 2, 0, n, R).int()
+    prompt = (length * gen.uniform01(seed, 3, 0, R)).int()
+    pen = torch.stack([0.7 + 0.8 * gen.uniform01(seed, 4, 0, R), gen.uniform01(seed, 5, 0, R), 0.3 * gen.uniform01(seed, 6, 0, R)], 1).float()
+    counts = gen.randint(seed, 7, 0, 12, R)
+    start = torch.cat([torch.zeros(1, dtype=torch.int64), counts.cumsum(0)]).int()
+    total = int(start[-1])
+    tok = gen.randint(seed, 8, 0, min(V, 9) - 1, total).int()
+    bias = gen.normal(seed, 9, (total,), std=3.0)
+    words = (V + 31) // 32
+    mask = gen.randint(seed, 10, -(1 << 31), (1 << 31) - 1, 3 * words).view(3, words).int()
+    mrow = gen.randint(seed, 11, -1, 2, R).int()
+    return dict(history=h, history_len=length, n_prompt=prompt, penalties=pen, bias_start=start, bias_token=tok, bias=bias, mask=mask, mask_row=mrow)
+
+
+def _adjust64(logits, k):
+    l = logits.double().numpy().copy()
+    R, V = l.shape
+    for r in range(R):
+        if k.get("history") is not None:
+            n, p = int(k["history_len"][r]), int(k["n_prompt"][r]) if k.get("n_prompt") is not None else 0
+            rep, pres, freq = k["penalties"][r].double().tolist()
+            seen, count = {}, {}
+            for j, t in enumerate(k["history"][r, :n].tolist()):
+                if 0 <= t < V:
+                    seen[t] = True
+                    if j >= p:
+                        count[t] = count.get(t, 0) + 1
+            for t in seen:
+                l[r, t] = l[r, t] / rep if l[r, t] > 0 else l[r, t] * rep
+                l[r, t] -= freq * count.get(t, 0) + (pres if count.get(t, 0) else 0)
+        if k.get("bias") is not None:
+            last = {}
+            for j in range(int(k["bias_start"][r]), int(k["bias_start"][r + 1])):
+                last[int(k["bias_token"][j])] = float(k["bias"][j])
+            for t, b in last.items():
+                l[r, t] += b
+        if k.get("mask") is not None:
+            m = int(k["mask_row"][r]) if k.get("mask_row") is not None else r
+            if m >= 0:
+                for i in range(V):
+                    if m >= k["mask"].shape[0] or not (int(k["mask"][m, i // 32]) >> (i % 32)) & 1:
+                        l[r, i] = -np.inf
+    return l
+
+
+@pytest.mark.parametrize("V", [1, 31, 33, 1009, 2048, 2049, 6145])
+@pytest.mark.parametrize("R", [1, 3, 17])
+def test_choose_adjusts_and_takes_the_largest(V, R):
+    logits = gen.normal(71 + V, 20, (R, V), std=3.0)
+    k = _rules(71 + V, R, V, 200)
+    for names in (("history", "history_len", "penalties"), ("history", "history_len", "n_prompt", "penalties"), ("bias_start", "bias_token", "bias"),
+                  ("mask", "mask_row"), tuple(k)):
+        sub = {n: k[n] for n in names}
+        tok, adj = _choose(logits, want=True, **sub)
+        ref = _adjust64(logits, sub)
+        gone = np.isinf(ref)
+        assert (np.isinf(adj.numpy()) == gone).all()
+        # a quotient or product, the penalty and the bias: four roundings of numbers up to their sizes
+        size = np.abs(logits.numpy()).max() * 2 + 60 + 12
+        assert np.abs(adj.numpy()[~gone] - ref[~gone]).max(initial=0) <= 4 * 2.0 ** -24 * size
+        best = adj.max(1).values
+        for r in range(R):
+            assert tok[r] == (-1 if best[r] == -math.inf else int((adj[r] == best[r]).nonzero()[0, 0]))
+        only, _ = _choose(logits, **sub)
+        assert torch.equal(only, tok)
+
+
+def test_choose_without_rules_is_argmax_and_sample():
+    R, V = 9, 5000
+    logits = gen.normal(73, 1, (R, V), std=2.0).to(DEV)
+    out = torch.empty(R, dtype=torch.int32, device=DEV)
+    ld.ldk_argmax(logits, out)
+    assert torch.equal(_choose(logits)[0], out.cpu())
+    temp = torch.tensor([0.0, 0.5, 1.0, 1.5, 0.7, 0.0, 2.0, 0.1, 1.0], device=DEV)
+    seed, pos = torch.arange(R, device=DEV) * 7919 - 3, torch.arange(R, dtype=torch.int32, device=DEV) * 100
+    ld.ldk_sample(logits, temp, seed, pos, out)
+    assert torch.equal(_choose(logits, temperature=temp, seed=seed, pos=pos)[0], out.cpu())
+
+
+def test_choose_draws_from_the_adjusted_distribution():
+    """Frequencies over 4000 draws of a five-token distribution with one token forbidden, one penalised and one biased: within five standard deviations."""
+    V, R = 40, 4000
+    logits = torch.full((R, V), -50.0)
+    logits[:, :5] = torch.tensor([1.0, 0.5, 2.0, 0.0, -1.0])
+    k = dict(history=torch.full((R, 2), 2, dtype=torch.int32), history_len=torch.full((R,), 2, dtype=torch.int32),
+             penalties=torch.tensor([[2.0, 0.25, 0.125]]).repeat(R, 1), bias_start=torch.arange(R + 1, dtype=torch.int32),
+             bias_token=torch.full((R,), 3, dtype=torch.int32), bias=torch.full((R,), 0.75), mask=torch.tensor([[~2, 255]], dtype=torch.int32),
+             mask_row=torch.zeros(R, dtype=torch.int32), temperature=torch.full((R,), 0.8), seed=torch.arange(R) * 6364136223846793005 + 11,
+             pos=torch.arange(R, dtype=torch.int32))
+    tok, _ = _choose(logits, **k)
+    l = np.array([1.0, -np.inf, 2.0 / 2 - 0.25 - 0.25, 0.75, -1.0]) / 0.8
+    p = np.exp(l - l.max()); p /= p.sum()
+    f = np.bincount(tok.numpy(), minlength=5)[:5] / R
+    assert f.sum() == 1 and (np.abs(f - p) <= 5 * np.sqrt(p * (1 - p) / R) + 1e-12).all()
+
+
+def test_choose_rows_with_nothing_allowed_infinities_and_nan():
+    V = 3000
+    logits = gen.normal(75, 1, (6, V))
+    logits[0] = -math.inf
+    logits[1] = math.nan
+    logits[2, 2500] = math.inf
+    logits[3, 5:] = math.nan
+    logits[4, 100] = logits[4, 2900] = 77.0
+    mask = torch.zeros((2, (V + 31) // 32), dtype=torch.int32)
+    mask[1, 93] = 1 << 20      # token 2996 alone
+    tok, _ = _choose(logits)
+    assert tok.tolist()[:5] == [-1, -1, 2500, int(logits[3, :5].argmax()), 100]
+    tok, _ = _choose(logits, mask=mask, mask_row=torch.tensor([1, 1, 0, 2, 1, -1], dtype=torch.int32))
+    assert tok.tolist() == [-1, -1, -1, -1, 2996, int(logits[5].argmax())]
+
+
+def test_choose_adjusts_in_place():
+    R, V = 4, 5000
+    k = {n: v.to(DEV) for n, v in _rules(77, R, V, 300).items()}
+    logits = gen.normal(77, 20, (R, V)).to(DEV)
+    tok, adj = _choose(logits, want=True, **k)
+    token, scratch = torch.empty(R, dtype=torch.int32, device=DEV), torch.empty(ld.ldk_choose_scratch_bytes(R, V), dtype=torch.uint8, device=DEV)
+    ld.ldk_choose(logits, token, adjusted=logits, scratch=scratch, **k)
+    assert torch.equal(logits.cpu(), adj) and torch.equal(token.cpu(), tok)
