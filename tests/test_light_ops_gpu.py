@@ -386,16 +386,18 @@ def test_sparse_attention_long_context_and_sharp_scores():
     assert _rel(out, torch.from_numpy(ref)) <= 4 * ATTENTION      # four times the scores, four times their errors
 
 
-@pytest.mark.parametrize("blocks,equal", [(700, False), (2500, False), (2500, True), (17001, False), (17001, True)])
-def test_sparse_attention_choice_over_many_blocks(blocks, equal):
-    """Contexts of 11,000 to 272,000 positions, also with scores that many blocks share (keys repeated every 50 blocks)."""
+@pytest.mark.parametrize("blocks,equal,budget", [(300, False, 100), (300, True, 100), (700, False, 100), (700, True, 100), (2500, False, 100),
+                                                  (2500, True, 100), (10000, True, 100), (17001, False, 100), (17001, True, 100), (5000, True, 4500),
+                                                  (300, False, 100000), (5000, False, 100000)])
+def test_sparse_attention_choice_over_many_blocks(blocks, equal, budget):
+    """Contexts of 4,800 to 272,000 positions, also with scores that many blocks share (keys repeated every 50 blocks), and budgets beyond them."""
     H, Hkv, hd, ctx = 2, 1, 64, [16 * blocks - 5, 40]
     q, logical, table, slot = _sparse_case(68, torch.bfloat16, H, Hkv, hd, ctx)
     if equal:
         t = torch.as_tensor(table[slot[0], :blocks - 1]).long()
         logical[t] = logical[t[torch.arange(blocks - 1) % 50]]
-    out, sel, bounds, unit = _run_sparse(q, logical, table, slot, ctx, H, Hkv, hd, 0, 100, 2, 3)
-    ref, want = _sparse64(q.numpy(), logical.double().numpy(), bounds, unit, table, slot, ctx, H, Hkv, hd, 0, 100, 2, 3)
+    out, sel, bounds, unit = _run_sparse(q, logical, table, slot, ctx, H, Hkv, hd, 0, budget, 2, 3)
+    ref, want = _sparse64(q.numpy(), logical.double().numpy(), bounds, unit, table, slot, ctx, H, Hkv, hd, 0, budget, 2, 3)
     np.testing.assert_array_equal(sel.cpu().numpy(), want)
     assert _rel(out, torch.from_numpy(ref)) <= ATTENTION
 
