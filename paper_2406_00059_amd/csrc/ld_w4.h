@@ -19,12 +19,28 @@ struct W4Rows {
     uint16_t *image;       // fp16 operands
     float *sums;
     int32_t *expo;
+    float *part;           // sums of slabs of K
     int k_tiles;
 };
+
+// A product of many rows: workgroups of 16 tt rows and 256 outputs (128 gated ones), K in slabs.
+struct W4Plan {
+    int tt, slabs, n_blocks, t_blocks;
+    size_t part_bytes;
+};
+W4Plan w4_plan(int T, int N, int K, int epilogue);
+size_t w4_part_bound(int T, int N, int epilogue);      // of any plan of up to T rows
+void launch_w4_tile(const W4Image &w, int scale_dtype, const W4Rows &r, int group, int T, int N, int epilogue, const W4Plan &p, float *y, hipStream_t s);
+
+#if defined(__HIPCC__)
+// A finished sum of a row in units of 1, and the gated activation.
+__device__ __forceinline__ float w4_finish(float v, int expo) { return expo == W4_NOT_FINITE ? NAN : ldexpf(v, expo); }
+__device__ __forceinline__ float w4_gated(float gate, float up) { return gate / (1.f + expf(-gate)) * up; }
+#endif
 
 // The regions of an image, and its size.
 W4Image w4_image(const void *image, int N, int K, int group, int parts, int scale_dtype, bool zeros, size_t *bytes);
 // The regions of the scratch for T rows of K columns, and their size.
-W4Rows w4_rows(void *scratch, int T, int K, size_t *bytes);
+W4Rows w4_rows(void *scratch, int T, int K, size_t part_bytes, size_t *bytes);
 
 }  // namespace ld

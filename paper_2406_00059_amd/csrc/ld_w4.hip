@@ -19,6 +19,8 @@
 #include "ld_w4.h"
 #include "ld_device.h"
 
+#include <algorithm>
+
 using namespace ldd;
 
 namespace {
@@ -119,8 +121,8 @@ __global__ __launch_bounds__(256) void k_w4_quantize(const WT *__restrict__ W, i
 
 // Image of the activations: for every 16 rows and 32 columns the hi and the lo operand of one matrix instruction, 1 KB
 // each in lane order ([row tile][k / 32][term][lane][8]).  Up to eight rows share one operand: columns 0 .. 7 of it are
-// the hi terms, 8 .. 15 the lo terms ([k / 32][lane][8]).  sums [row tile][group][16]: 2^-24 times the sum of a group's
-// columns (packed: columns 8 .. 15 unused).  expo[t]: the exponent that takes a finished sum back, or W4_NOT_FINITE.
+// the hi terms, 8 .. 15 the lo terms ([k / 32][lane][8]).  sums [row tile][group][term][16]: 2^-24 times the sums of a group's
+// columns (packed: [group][16] like the operand; those of hi are exact).  expo[t]: the exponent that takes a finished sum back, or W4_NOT_FINITE.
 // One workgroup a row; a thread takes four columns at a time.
 template <bool PACKED>
 __global__ __launch_bounds__(256) void k_w4_split(const float *__restrict__ x, const float *__restrict__ gain, float eps, int K, int G,
@@ -173,7 +175,7 @@ __global__ __launch_bounds__(256) void k_w4_split(const float *__restrict__ x, c
     const int rt = t >> 4, col = PACKED ? t : t & 15;
     const int groups = Kp / G;
     for (int c = threadIdx.x * 4; c < Kp; c += 1024) {
-        float v[4], sum = 0.f;
+        float v[4], sum_hi = 0.f, sum_lo = 0.f;
         fetch(c, v);
 #pragma unroll
         for (int e = 0; e < 4; e++) v[e] *= inv;      // in the order of the definition: x / rms, then the gain
@@ -183,7 +185,6 @@ __global__ __launch_bounds__(256) void k_w4_split(const float *__restrict__ x, c
 #pragma unroll
         for (int e = 0; e < 4; e++) {
             v[e] = ldexpf(finite ? v[e] : 0.f, k);
-            sum += v[e];
             most = fmaxf(most, fabsf(v[e]));
         }
 #pragma unroll
@@ -197,6 +198,8 @@ __global__ __launch_bounds__(256) void k_w4_split(const float *__restrict__ x, c
             const float f = e < 2 ? 1.f : 0.0625f;      // e >= 2: codes in bits 4 .. 7 (c is a multiple of 4)
             hi.h[e] = (_Float16)(h * f);
             lo.h[e] = (_Float16)((v[e] - h) * f);
+            sum_hi += h;
+            sum_lo += v[e] - h;
         }
         const int kb = c >> 5, lane = col + 16 * ((c & 31) >> 3), half = (c & 7) * 2;      // bytes into the lane's 16
         if (PACKED) {
@@ -208,8 +211,15 @@ __global__ __launch_bounds__(256) void k_w4_split(const float *__restrict__ x, c
             *reinterpret_cast<uint2 *>(p) = hi.u;
             *reinterpret_cast<uint2 *>(p + 1024) = lo.u;
         }
-        for (int off = 1; off < G / 4; off <<= 1) sum += __shfl_xor(sum, off, WAVE);
-        if (c % G == 0) r.sums[((int64_t)rt * groups + c / G) * 16 + col] = ldexpf(sum, -24);
+        for (int off = 1; off < G / 4; off <<= 1) {
+            sum_hi += __shfl_xor(sum_hi, off, WAVE);
+            sum_lo += __shfl_xor(sum_lo, off, WAVE);
+        }
+        if (c % G == 0) {
+            float *p = r.sums + (PACKED ? (int64_t)(c / G) * 16 : ((int64_t)rt * groups + c / G) * 32) + col;
+            p[0] = ldexpf(sum_hi, -24);
+            p[PACKED ? 8 : 16] = ldexpf(sum_lo, -24);
+        }
     }
 }
 
@@ -219,8 +229,6 @@ __device__ __forceinline__ f16x8 codes_as_f16(uint32_t w) {
     const uint32_t s = w >> 8;
     return __builtin_bit_cast(f16x8, (u32x4){w & 0x000f000fu, w & 0x00f000f0u, s & 0x000f000fu, s & 0x00f000f0u});
 }
-
-__device__ __forceinline__ float finish(float v, int expo) { return expo == ld::W4_NOT_FINITE ? NAN : ldexpf(v, expo); }
 
 // A workgroup of eight waves takes R tiles of 16 output rows (SwiGLU: the gate tile and its up tile) and 16 CT activation rows;
 // wave w multiplies the column tiles w, w + 8, ..; the eight sums meet in LDS.  PACKED: up to eight activation rows, both terms in
@@ -287,7 +295,12 @@ __global__ __launch_bounds__(512) void k_w4_rows(ld::W4Image w, int scale_dtype,
 #pragma unroll
             for (int c = 0; c < CT; c++) {
                 sum[c] = 0.f;
-                if (!PACKED || col < T) sum[c] = r.sums[((int64_t)min(ct0 + c, ct_all - 1) * w.groups + g) * 16 + col];
+                if (PACKED) {
+                    if ((col & 7) < T) sum[c] = r.sums[(int64_t)g * 16 + col];
+                } else {
+                    const float *p = r.sums + ((int64_t)min(ct0 + c, ct_all - 1) * w.groups + g) * 32 + col;
+                    sum[c] = p[0] + p[16];
+                }
             }
 #pragma unroll
             for (int i = 0; i < R; i++) {
@@ -345,8 +358,8 @@ __global__ __launch_bounds__(512) void k_w4_rows(ld::W4Image w, int scale_dtype,
         float out[4];
 #pragma unroll
         for (int e = 0; e < 4; e++) {
-            out[e] = finish(v[0][e], expo);
-            if (pair) out[e] = out[e] / (1.f + expf(-out[e])) * finish(v[1][e], expo);
+            out[e] = ld::w4_finish(v[0][e], expo);
+            if (pair) out[e] = ld::w4_gated(out[e], ld::w4_finish(v[1][e], expo));
         }
         const int m = min(4, N - n);
         for (int e = 0; e < m; e++) dst[e] = epilogue == LDK_ADD ? dst[e] + out[e] : out[e];
@@ -367,6 +380,8 @@ void launch_group(const ld::W4Image &w, int scale_dtype, const ld::W4Rows &r, in
     else if (T <= 32) launch_rows<2, false, G>(w, scale_dtype, r, T, N, epilogue, y, s);
     else launch_rows<4, false, G>(w, scale_dtype, r, T, N, epilogue, y, s);
 }
+
+constexpr int TILE_ROWS = 65;      // rows from which the tiled product takes over
 
 bool bad_shape(int N, int K, int group, int parts, int scale_dtype) {
     return N <= 0 || K <= 0 || N > (1 << 28) || K > (1 << 28) || (group != 32 && group != 64 && group != 128) || (parts != 1 && parts != 2) ||
@@ -392,15 +407,17 @@ W4Image w4_image(const void *image, int N, int K, int group, int parts, int scal
     return w;
 }
 
-W4Rows w4_rows(void *scratch, int T, int K, size_t *bytes) {
+W4Rows w4_rows(void *scratch, int T, int K, size_t part_bytes, size_t *bytes) {
     W4Rows r{};
     r.k_tiles = (K + 127) / 128;
     const size_t tiles = (size_t)(T + 15) / 16 * r.k_tiles * 4;      // blocks of 16 rows x 32 columns
     char *p = (char *)scratch;
     r.image = (uint16_t *)p;
     r.sums = (float *)(p + tiles * 2048);                            // at the finest group
-    r.expo = (int32_t *)(p + tiles * (2048 + 64));
-    if (bytes) *bytes = align_up(tiles * (2048 + 64) + (size_t)T * 4, 256);
+    r.expo = (int32_t *)(p + tiles * (2048 + 128));
+    const size_t at = align_up(tiles * (2048 + 128) + (size_t)T * 4, 256);
+    r.part = (float *)(p + at);
+    if (bytes) *bytes = at + part_bytes;
     return r;
 }
 
@@ -445,7 +462,7 @@ ld_status ldk_w4_quantize(const void *W, int32_t dtype, int32_t N, int32_t K, in
 size_t ldk_linear_w4_scratch_bytes(int32_t T, int32_t N, int32_t K, int32_t epilogue) {
     if (T <= 0 || N <= 0 || K <= 0) return 0;
     size_t bytes = 0;
-    ld::w4_rows(nullptr, T, K, &bytes);
+    ld::w4_rows(nullptr, T, K, T >= TILE_ROWS ? ld::w4_part_bound(T, N, epilogue) : 0, &bytes);
     return bytes;
 }
 
@@ -455,14 +472,21 @@ ld_status ldk_linear_w4(const void *image, int32_t scale_dtype, int32_t zeros, i
     if (!image || ((uintptr_t)image & 15) || !x || !y || T < 0 || epilogue < 0 || epilogue > 2 ||
         bad_shape(N, K, group, epilogue == LDK_SWIGLU ? 2 : 1, scale_dtype))
         return ld::fail(LD_E_INVAL, "ldk_linear_w4: bad argument (group 32, 64 or 128; image 16-byte aligned)");
-    if (!scratch || ((uintptr_t)scratch & 15) || scratch_bytes < ldk_linear_w4_scratch_bytes(T, N, K, epilogue))
+    const ld::W4Plan plan = T >= TILE_ROWS ? ld::w4_plan(T, N, K, epilogue) : ld::W4Plan{};
+    size_t need = 0;
+    ld::w4_rows(nullptr, T, K, plan.part_bytes, &need);
+    if (!scratch || ((uintptr_t)scratch & 15) || scratch_bytes < need)
         return ld::fail(LD_E_INVAL, "ldk_linear_w4: scratch missing, not 16-byte aligned or too small");
     if (T > 1 << 20) return ld::fail(LD_E_RANGE, "ldk_linear_w4: more than 1048576 rows");
     hipStream_t s = (hipStream_t)stream;
     const ld::W4Image w = ld::w4_image(image, N, K, group, epilogue == LDK_SWIGLU ? 2 : 1, scale_dtype, zeros != 0, nullptr);
-    const ld::W4Rows r = ld::w4_rows(scratch, T, K, nullptr);
+    const ld::W4Rows r = ld::w4_rows(scratch, T, K, 0, nullptr);
     if (T <= 8) LD_LAUNCH(k_w4_split<true>, dim3(T), dim3(256), 0, s, x, g, eps, K, group, r);
     else LD_LAUNCH(k_w4_split<false>, dim3(T), dim3(256), 0, s, x, g, eps, K, group, r);
+    if (T >= TILE_ROWS) {
+        ld::launch_w4_tile(w, scale_dtype, r, group, T, N, epilogue, plan, y, s);
+        return launched("k_w4_tile");
+    }
     if (group == 32) launch_group<32>(w, scale_dtype, r, T, N, epilogue, y, s);
     else if (group == 64) launch_group<64>(w, scale_dtype, r, T, N, epilogue, y, s);
     else launch_group<128>(w, scale_dtype, r, T, N, epilogue, y, s);

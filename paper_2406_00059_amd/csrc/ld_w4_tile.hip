@@ -1,0 +1,285 @@
+// Linear layers on 4-bit weights for many rows: the operands and the arithmetic are those of ld_w4.hip.
+//
+// A workgroup of four waves multiplies 16 tiles of 16 output rows (SwiGLU: 8 gate tiles and their up tiles) with 16 TT activation
+// rows, a wave 4 tiles with all of them.  The activations of 128 columns (8 KB per 16 rows, both terms) are copied straight into
+// LDS in operand order, two stages, and every wave reads them all; codes go from memory into registers, a column tile ahead, are
+// unpacked once per group and meet TT x 2 operands there: 80 vector instructions for TT x 32 matrix instructions.  What a group's sums
+// owe to the zero point 8 enters as the first matrix instruction's addend, so that a group costs 2 vector instructions a
+// value (add, multiply-add with the scale).
+#include "ld_w4.h"
+#include "ld_device.h"
+
+#include <algorithm>
+
+using namespace ldd;
+
+namespace {
+
+typedef __attribute__((ext_vector_type(8))) _Float16 f16x8;
+typedef __attribute__((ext_vector_type(4))) float f32x4;
+typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;
+
+constexpr int NT = 4;      // tiles of 16 output rows a wave
+
+// 1 KB from src + 16 lane into LDS, in lane order.
+__device__ __forceinline__ void copy_kb(const char *src, char *dst, int lane) {
+#if defined(__HIP_DEVICE_COMPILE__)
+    __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)(src + lane * 16),
+                                     (__attribute__((address_space(3))) void *)dst, 16, 0, 0);
+#endif
+}
+
+template <int TT, int G, bool ZEROS, typename ST>
+__global__ __launch_bounds__(256, 2) void k_w4_tile(ld::W4Image w, ld::W4Rows r, int T, int N, int epilogue, int n_blocks, int slabs,
+                                                    float *__restrict__ y, float *__restrict__ part) {
+    constexpr int PER = 128 / G, JG = G / 32;
+    __shared__ __attribute__((aligned(16))) char sm_x[2][TT * 8192];
+    __shared__ float sm_s[2][TT * PER * 32];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int col = lane & 15, h = lane >> 4;
+    const bool pair = epilogue == LDK_SWIGLU;
+    const int nb = blockIdx.x % n_blocks, tb = blockIdx.x / n_blocks, slab = blockIdx.y;
+    const int rt_all = (T + 15) >> 4;
+    const int k0 = (int)((int64_t)w.k_tiles * slab / slabs), k1 = (int)((int64_t)w.k_tiles * (slab + 1) / slabs);
+    // this wave's tiles: pairs: gate 8 nb + 2 wave + (0, 1), then their up tiles; otherwise 16 nb + 4 wave + i
+    int tile_of[NT];
+    int64_t tile[NT];
+#pragma unroll
+    for (int i = 0; i < NT; i++) {
+        tile_of[i] = pair ? nb * 8 + wave * 2 + (i & 1) : nb * 16 + wave * 4 + i;
+        tile[i] = (int64_t)(pair && i >= 2 ? w.row_tiles : 0) + min(tile_of[i], w.row_tiles - 1);
+    }
+    auto copy_x = [&](int kt, int stage) {
+#pragma unroll
+        for (int u = 0; u < 2 * TT; u++) {
+            const int piece = u * 4 + wave, tt = piece >> 3;      // 8 KB a row tile, 1 KB a copy
+            const int64_t rt = min(tb * TT + tt, rt_all - 1);
+            copy_kb((const char *)r.image + (rt * w.k_tiles + kt) * 8192 + (piece & 7) * 1024, sm_x[stage] + piece * 1024, lane);
+        }
+    };
+    constexpr int SUMS = (TT * PER * 32 + 255) / 256;
+    auto load_sums = [&](int kt, float (&v)[SUMS]) {
+#pragma unroll
+        for (int u = 0; u < SUMS; u++) {
+            const int i = min(u * 256 + (int)threadIdx.x, TT * PER * 32 - 1);
+            const int64_t rt = min(tb * TT + i / (PER * 32), rt_all - 1);
+            v[u] = r.sums[(rt * w.groups + (int64_t)kt * PER) * 32 + i % (PER * 32)];
+        }
+    };
+    auto put_sums = [&](int stage, const float (&v)[SUMS]) {
+#pragma unroll
+        for (int u = 0; u < SUMS; u++)
+            if (u * 256 + (int)threadIdx.x < TT * PER * 32) sm_s[stage][u * 256 + threadIdx.x] = v[u];
+    };
+    auto load_codes = [&](int kt, u32x4 (&c)[NT]) {
+#pragma unroll
+        for (int i = 0; i < NT; i++) c[i] = load_stream16(w.codes + ((tile[i] * w.k_tiles + kt) * 64 + lane) * 4);
+    };
+
+    f32x4 total[NT][TT];
+#pragma unroll
+    for (int i = 0; i < NT; i++)
+#pragma unroll
+        for (int t = 0; t < TT; t++) total[i][t] = (f32x4){0.f, 0.f, 0.f, 0.f};
+    u32x4 code[NT];
+    float sums[SUMS];
+    copy_x(k0, 0);
+    load_codes(k0, code);
+    load_sums(k0, sums);
+    for (int kt = k0; kt < k1; kt++) {
+        const int stage = (kt - k0) & 1;
+        put_sums(stage, sums);
+        __syncthreads();      // this tile's copies have arrived, everyone is done with the other stage
+        u32x4 next[NT];
+        const int ahead = min(kt + 1, k1 - 1);
+        if (kt + 1 < k1) copy_x(ahead, stage ^ 1);
+        load_codes(ahead, next);
+        load_sums(ahead, sums);
+#pragma unroll
+        for (int p = 0; p < PER; p++) {
+            f16x8 a[NT][JG];
+#pragma unroll
+            for (int i = 0; i < NT; i++)
+#pragma unroll
+                for (int j = 0; j < JG; j++) {
+                    const uint32_t v = code[i][p * JG + j], u = v >> 8;
+                    a[i][j] = __builtin_bit_cast(f16x8, (u32x4){v & 0x000f000fu, v & 0x00f000f0u, u & 0x000f000fu, u & 0x00f000f0u});
+                }
+            float sc[NT][4], sz[NT][4];
+#pragma unroll
+            for (int i = 0; i < NT; i++) {
+                const int64_t at = (tile[i] * w.groups + (int64_t)kt * PER + p) * 16 + 4 * h;
+                if constexpr (sizeof(ST) == 2) {
+                    const uint2 v = *reinterpret_cast<const uint2 *>((const bf16_t *)w.scales + at);
+                    sc[i][0] = __uint_as_float(v.x << 16); sc[i][1] = __uint_as_float(v.x & 0xffff0000u);
+                    sc[i][2] = __uint_as_float(v.y << 16); sc[i][3] = __uint_as_float(v.y & 0xffff0000u);
+                } else {
+                    const float4 v = *reinterpret_cast<const float4 *>((const float *)w.scales + at);
+                    sc[i][0] = v.x; sc[i][1] = v.y; sc[i][2] = v.z; sc[i][3] = v.w;
+                }
+                if constexpr (ZEROS) {
+                    const uint32_t z = *reinterpret_cast<const uint32_t *>(w.zeros + at);
+#pragma unroll
+                    for (int e = 0; e < 4; e++) sz[i][e] = 8.f - (float)((z >> (8 * e)) & 255u);
+                }
+            }
+#pragma unroll
+            for (int t = 0; t < TT; t++) {
+                const float s_hi = sm_s[stage][(t * PER + p) * 32 + col], s_lo = sm_s[stage][(t * PER + p) * 32 + 16 + col];
+                const float c_hi = -8.f * s_hi, c_lo = -8.f * s_lo;
+                f32x4 hi[NT], lo[NT];
+#pragma unroll
+                for (int i = 0; i < NT; i++) {
+                    hi[i] = (f32x4){c_hi, c_hi, c_hi, c_hi};
+                    lo[i] = (f32x4){c_lo, c_lo, c_lo, c_lo};
+                }
+#pragma unroll
+                for (int j = 0; j < JG; j++) {
+                    const char *q = sm_x[stage] + (t * 4 + p * JG + j) * 2048 + lane * 16;
+                    const f16x8 bh = *reinterpret_cast<const f16x8 *>(q), bl = *reinterpret_cast<const f16x8 *>(q + 1024);
+#pragma unroll
+                    for (int i = 0; i < NT; i++) hi[i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(a[i][j], bh, hi[i], 0, 0, 0);
+#pragma unroll
+                    for (int i = 0; i < NT; i++) lo[i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(a[i][j], bl, lo[i], 0, 0, 0);
+                }
+#pragma unroll
+                for (int i = 0; i < NT; i++)
+#pragma unroll
+                    for (int e = 0; e < 4; e++) {
+                        float d = hi[i][e] + lo[i][e];
+                        if constexpr (ZEROS) d += sz[i][e] * (s_hi + s_lo);
+                        total[i][t][e] += sc[i][e] * d;
+                    }
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < NT; i++) code[i] = next[i];
+    }
+
+    const int np = w.row_tiles * 16;      // rows of a part, padded
+#pragma unroll
+    for (int t = 0; t < TT; t++) {
+        const int row = (tb * TT + t) * 16 + col;
+        if (row >= T) continue;
+        if (slabs > 1) {
+#pragma unroll
+            for (int i = 0; i < NT; i++)
+                if (tile_of[i] < w.row_tiles)
+                    *reinterpret_cast<f32x4 *>(part + (((int64_t)slab * T + row) * (pair ? 2 : 1) + (pair && i >= 2 ? 1 : 0)) * np + tile_of[i] * 16 + 4 * h) =
+                        total[i][t];
+            continue;
+        }
+        const int expo = r.expo[row];
+#pragma unroll
+        for (int i = 0; i < NT; i++) {
+            if (pair && i >= 2) break;
+            const int n = tile_of[i] * 16 + 4 * h;
+            float *dst = y + (int64_t)row * N + n;
+            float out[4];
+#pragma unroll
+            for (int e = 0; e < 4; e++) {
+                out[e] = ld::w4_finish(total[i][t][e], expo);
+                if (pair) out[e] = ld::w4_gated(out[e], ld::w4_finish(total[(i + 2) % NT][t][e], expo));
+            }
+            if (n + 4 <= N && N % 4 == 0) {
+                float4 v = make_float4(out[0], out[1], out[2], out[3]);
+                if (epilogue == LDK_ADD) {
+                    const float4 o = *reinterpret_cast<const float4 *>(dst);
+                    v.x += o.x; v.y += o.y; v.z += o.z; v.w += o.w;
+                }
+                *reinterpret_cast<float4 *>(dst) = v;
+            } else {
+                for (int e = 0; e < 4; e++)
+                    if (n + e < N) dst[e] = epilogue == LDK_ADD ? dst[e] + out[e] : out[e];
+            }
+        }
+    }
+}
+
+// The slabs' sums added in their order, then the epilogue.  A thread four outputs of a row.
+__global__ __launch_bounds__(256) void k_w4_join(const float *__restrict__ part, const int32_t *__restrict__ expo, int T, int N, int np, int slabs,
+                                                 int epilogue, float *__restrict__ y) {
+    const int quads = np / 4;
+    const int64_t id = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    const int row = (int)(id / quads), n = (int)(id % quads) * 4;
+    if (row >= T || n >= N) return;
+    const bool pair = epilogue == LDK_SWIGLU;
+    const int64_t wide = (int64_t)np * (pair ? 2 : 1);
+    const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
+    const f32x4 a = slab_sum(reinterpret_cast<const f32x4 *>(part + row * wide + n), T * wide / 4, slabs, zero);
+    const f32x4 b = pair ? slab_sum(reinterpret_cast<const f32x4 *>(part + row * wide + np + n), T * wide / 4, slabs, zero) : zero;
+    const int e2 = expo[row];
+    float *dst = y + (int64_t)row * N + n;
+#pragma unroll
+    for (int e = 0; e < 4; e++) {
+        if (n + e >= N) break;
+        float v = ld::w4_finish(a[e], e2);
+        if (pair) v = ld::w4_gated(v, ld::w4_finish(b[e], e2));
+        dst[e] = epilogue == LDK_ADD ? dst[e] + v : v;
+    }
+}
+
+template <int TT, int G>
+void launch_tile(const ld::W4Image &w, int scale_dtype, const ld::W4Rows &r, int T, int N, int epilogue, const ld::W4Plan &p, float *y, hipStream_t s) {
+    const dim3 grid(p.n_blocks * p.t_blocks, p.slabs), block(256);
+#define LD_TILE(Z_, S_) LD_LAUNCH((k_w4_tile<TT, G, Z_, S_>), grid, block, 0, s, w, r, T, N, epilogue, p.n_blocks, p.slabs, y, r.part)
+    if (scale_dtype == LD_BF16) { if (w.zeros) LD_TILE(true, bf16_t); else LD_TILE(false, bf16_t); }
+    else { if (w.zeros) LD_TILE(true, float); else LD_TILE(false, float); }
+#undef LD_TILE
+}
+template <int G>
+void launch_group(const ld::W4Image &w, int scale_dtype, const ld::W4Rows &r, int T, int N, int epilogue, const ld::W4Plan &p, float *y, hipStream_t s) {
+    if (p.tt == 2) launch_tile<2, G>(w, scale_dtype, r, T, N, epilogue, p, y, s);
+    else if (p.tt == 3) launch_tile<3, G>(w, scale_dtype, r, T, N, epilogue, p, y, s);
+    else launch_tile<4, G>(w, scale_dtype, r, T, N, epilogue, p, y, s);
+}
+
+}  // namespace
+
+namespace ld {
+
+constexpr int MOST_SLABS = 16, MOST_GROUPS = 1024;      // slabs, and workgroups of a launch with slabs
+
+size_t w4_part_bound(int T, int N, int epilogue) {
+    // n_blocks t_blocks slabs <= MOST_GROUPS, and a workgroup leaves at most 64 rows of 256 sums
+    const size_t row = (size_t)((N + 15) / 16 * 16) * (epilogue == LDK_SWIGLU ? 2 : 1) * 4;
+    return std::min((size_t)MOST_SLABS * T * row, (size_t)MOST_GROUPS * 64 * 256 * 4);
+}
+
+// Tile and slabs: the rounds of 512 workgroups (two a CU) times the column tiles each has, 16 tt rows wide plus what a column tile costs
+// beside its products, and the slabs' sums written and read again.
+W4Plan w4_plan(int T, int N, int K, int epilogue) {
+    W4Plan best{};
+    const int row_tiles = (N + 15) / 16, k_tiles = (K + 127) / 128, per_block = epilogue == LDK_SWIGLU ? 8 : 16;
+    double cost = 0;
+    for (int tt = 2; tt <= 4; tt++)
+        for (int slabs = 1; slabs <= MOST_SLABS && slabs <= k_tiles; slabs++) {
+            W4Plan p;
+            p.tt = tt;
+            p.slabs = slabs;
+            p.n_blocks = (row_tiles + per_block - 1) / per_block;
+            p.t_blocks = (T + 16 * tt - 1) / (16 * tt);
+            const int64_t groups = (int64_t)p.n_blocks * p.t_blocks * slabs;
+            if (slabs > 1 && groups > MOST_GROUPS) break;
+            const int64_t per = (k_tiles + slabs - 1) / slabs;
+            const double rounds = (double)((groups + 511) / 512);
+            // us: a column tile of 16 rows takes some 0.5 us with two workgroups a CU; sums at 4 TB/s, and a launch
+            const double c = rounds * ((per + 2) * (0.5 * tt + 0.3)) +
+                             (slabs > 1 ? 3 + 2.0 * slabs * T * (double)row_tiles * 16 * (epilogue == LDK_SWIGLU ? 2 : 1) * 4 / 4e6 : 0);
+            if (cost == 0 || c < cost) { cost = c; best = p; }
+        }
+    best.part_bytes = best.slabs > 1 ? (size_t)best.slabs * T * row_tiles * 16 * (epilogue == LDK_SWIGLU ? 2 : 1) * 4 : 0;
+    return best;
+}
+
+void launch_w4_tile(const W4Image &w, int scale_dtype, const W4Rows &r, int group, int T, int N, int epilogue, const W4Plan &p, float *y, hipStream_t s) {
+    if (group == 32) launch_group<32>(w, scale_dtype, r, T, N, epilogue, p, y, s);
+    else if (group == 64) launch_group<64>(w, scale_dtype, r, T, N, epilogue, p, y, s);
+    else launch_group<128>(w, scale_dtype, r, T, N, epilogue, p, y, s);
+    if (p.slabs > 1) {
+        const int np = w.row_tiles * 16;
+        LD_LAUNCH(k_w4_join, dim3((unsigned)(((int64_t)T * (np / 4) + 255) / 256)), dim3(256), 0, s, r.part, r.expo, T, N, np, p.slabs, epilogue, y);
+    }
+}
+
+}  // namespace ld
