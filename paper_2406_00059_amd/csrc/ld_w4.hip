@@ -123,49 +123,66 @@ __global__ __launch_bounds__(256) void k_w4_quantize(const WT *__restrict__ W, i
 // each in lane order ([row tile][k / 32][term][lane][8]).  Up to eight rows share one operand: columns 0 .. 7 of it are
 // the hi terms, 8 .. 15 the lo terms ([k / 32][lane][8]).  sums [row tile][group][term][16]: 2^-24 times the sums of a group's
 // columns (packed: [group][16] like the operand; those of hi are exact).  expo[t]: the exponent that takes a finished sum back, or W4_NOT_FINITE.
-// One workgroup a row; a thread takes four columns at a time.
-template <bool PACKED>
-__global__ __launch_bounds__(256) void k_w4_split(const float *__restrict__ x, const float *__restrict__ gain, float eps, int K, int G,
-                                                  ld::W4Rows r) {
-    const int t = blockIdx.x;
+// One workgroup of 512 threads a row; a thread takes four columns at a time, NC times, and keeps them (NC = 0: longer rows, read twice).
+constexpr int SPLIT_THREADS = 512;
+template <bool PACKED, int NC>
+__global__ __launch_bounds__(SPLIT_THREADS) void k_w4_split(const float *__restrict__ x, const float *__restrict__ gain, float eps, int T, int K, int G,
+                                                            ld::W4Rows r) {
+    constexpr int STEP = SPLIT_THREADS * 4, WAVES = SPLIT_THREADS / 64;
+    // the 16 rows of a tile fill the same lines of the image: they go to one XCD (workgroups take turns over eight), whose L2 puts the lines together
+    const int t = PACKED ? blockIdx.x : (int)(blockIdx.x / 128 * 8 + blockIdx.x % 8) * 16 + blockIdx.x / 8 % 16;
+    if (t >= T) return;
     const float *row = x + (int64_t)t * K;
-    const int Kp = r.k_tiles * 128;
+    const int Kp = r.k_tiles * 128, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const bool quads = K % 4 == 0 && ((uintptr_t)x & 15) == 0 && ((uintptr_t)gain & 15) == 0;
-    auto fetch = [&](int c, float (&v)[4]) {
-        if (quads && c + 4 <= K) {
-            const float4 a = *reinterpret_cast<const float4 *>(row + c);
-            v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w;
+    auto fetch = [&](const float *p, int c, f32x4 &v) {
+        if (quads) {
+            if (c < K) v = *reinterpret_cast<const f32x4 *>(p + c);
         } else {
 #pragma unroll
-            for (int e = 0; e < 4; e++) v[e] = c + e < K ? row[c + e] : 0.f;
+            for (int e = 0; e < 4; e++)
+                if (c + e < K) v[e] = p[c + e];
         }
-    };
-    auto weigh = [&](int c, float (&v)[4]) {
-        if (!gain) return;
-#pragma unroll
-        for (int e = 0; e < 4; e++)
-            if (c + e < K) v[e] *= gain[c + e];
     };
     float ss = 0.f;
     uint32_t top = 0;      // largest |x gain|, compared as bits: a NaN stays
-    for (int c = threadIdx.x * 4; c < K; c += 1024) {
-        float v[4];
-        fetch(c, v);
+    auto look = [&](const f32x4 &v, const f32x4 &g) {
 #pragma unroll
-        for (int e = 0; e < 4; e++) ss += v[e] * v[e];
-        weigh(c, v);
+        for (int e = 0; e < 4; e++) {
+            ss += v[e] * v[e];
+            top = max(top, __float_as_uint(v[e] * g[e]) & 0x7fffffffu);
+        }
+    };
+    const f32x4 zero = {0.f, 0.f, 0.f, 0.f}, one = {1.f, 1.f, 1.f, 1.f};
+    f32x4 kept[NC ? NC : 1], weight[NC ? NC : 1];
+    if constexpr (NC > 0) {
 #pragma unroll
-        for (int e = 0; e < 4; e++) top = max(top, __float_as_uint(v[e]) & 0x7fffffffu);
+        for (int i = 0; i < NC; i++) {
+            kept[i] = zero;
+            weight[i] = one;
+            fetch(row, i * STEP + threadIdx.x * 4, kept[i]);
+            if (gain) fetch(gain, i * STEP + threadIdx.x * 4, weight[i]);
+        }
+#pragma unroll
+        for (int i = 0; i < NC; i++) look(kept[i], weight[i]);
+    } else {
+        for (int c = threadIdx.x * 4; c < K; c += STEP) {
+            f32x4 v = zero, g = one;
+            fetch(row, c, v);
+            if (gain) fetch(gain, c, g);
+            look(v, g);
+        }
     }
-    __shared__ float sm_ss[4];
-    __shared__ uint32_t sm_top[4];
+    __shared__ float sm_ss[WAVES];
+    __shared__ uint32_t sm_top[WAVES];
     ss = wave_sum(ss);
 #pragma unroll
     for (int off = 32; off > 0; off >>= 1) top = max(top, (uint32_t)__shfl_xor((int)top, off, WAVE));
-    if ((threadIdx.x & 63) == 0) { sm_ss[threadIdx.x >> 6] = ss; sm_top[threadIdx.x >> 6] = top; }
+    if (lane == 0) { sm_ss[wave] = ss; sm_top[wave] = top; }
     __syncthreads();
-    ss = (sm_ss[0] + sm_ss[1]) + (sm_ss[2] + sm_ss[3]);
-    top = max(max(sm_top[0], sm_top[1]), max(sm_top[2], sm_top[3]));
+    ss = 0.f;
+#pragma unroll
+    for (int i = 0; i < WAVES; i++) { ss += sm_ss[i]; top = max(top, sm_top[i]); }
     const float inv = gain ? 1.f / sqrtf(ss / K + eps) : 1.f;
     const float m = __uint_as_float(top) * inv;
     const bool finite = m < INFINITY;      // false for NaN
@@ -174,17 +191,12 @@ __global__ __launch_bounds__(256) void k_w4_split(const float *__restrict__ x, c
 
     const int rt = t >> 4, col = PACKED ? t : t & 15;
     const int groups = Kp / G;
-    for (int c = threadIdx.x * 4; c < Kp; c += 1024) {
-        float v[4], sum_hi = 0.f, sum_lo = 0.f;
-        fetch(c, v);
-#pragma unroll
-        for (int e = 0; e < 4; e++) v[e] *= inv;      // in the order of the definition: x / rms, then the gain
-        weigh(c, v);
+    auto split = [&](int c, const f32x4 &raw, const f32x4 &g) {
+        float v[4], sum_hi = 0.f, sum_lo = 0.f, most = 0.f;
         union { _Float16 h[4]; uint2 u; } hi, lo;
-        float most = 0.f;
 #pragma unroll
         for (int e = 0; e < 4; e++) {
-            v[e] = ldexpf(finite ? v[e] : 0.f, k);
+            v[e] = ldexpf(finite ? raw[e] * inv * g[e] : 0.f, k);      // in the order of the definition: x / rms, then the gain
             most = fmaxf(most, fabsf(v[e]));
         }
 #pragma unroll
@@ -201,13 +213,13 @@ __global__ __launch_bounds__(256) void k_w4_split(const float *__restrict__ x, c
             sum_hi += h;
             sum_lo += v[e] - h;
         }
-        const int kb = c >> 5, lane = col + 16 * ((c & 31) >> 3), half = (c & 7) * 2;      // bytes into the lane's 16
+        const int kb = c >> 5, slot = col + 16 * ((c & 31) >> 3), half = (c & 7) * 2;      // half: bytes into the lane's 16
         if (PACKED) {
-            char *p = (char *)r.image + ((int64_t)kb * 64 + lane) * 16 + half;
+            char *p = (char *)r.image + ((int64_t)kb * 64 + slot) * 16 + half;
             *reinterpret_cast<uint2 *>(p) = hi.u;
             *reinterpret_cast<uint2 *>(p + 8 * 16) = lo.u;
         } else {
-            char *p = (char *)r.image + (((int64_t)rt * r.k_tiles * 4 + kb) * 128 + lane) * 16 + half;
+            char *p = (char *)r.image + (((int64_t)rt * r.k_tiles * 4 + kb) * 128 + slot) * 16 + half;
             *reinterpret_cast<uint2 *>(p) = hi.u;
             *reinterpret_cast<uint2 *>(p + 1024) = lo.u;
         }
@@ -220,7 +232,27 @@ __global__ __launch_bounds__(256) void k_w4_split(const float *__restrict__ x, c
             p[0] = ldexpf(sum_hi, -24);
             p[PACKED ? 8 : 16] = ldexpf(sum_lo, -24);
         }
+    };
+    if constexpr (NC > 0) {
+#pragma unroll
+        for (int i = 0; i < NC; i++)
+            if (i * STEP + (int)threadIdx.x * 4 < Kp) split(i * STEP + threadIdx.x * 4, kept[i], weight[i]);
+    } else {
+        for (int c = threadIdx.x * 4; c < Kp; c += STEP) {
+            f32x4 v = zero, g = one;
+            fetch(row, c, v);
+            if (gain) fetch(gain, c, g);
+            split(c, v, g);
+        }
     }
+}
+
+template <bool PACKED>
+void launch_split(const float *x, const float *g, float eps, int T, int K, int G, const ld::W4Rows &r, hipStream_t s) {
+    const dim3 grid(PACKED ? T : (T + 127) / 128 * 128), block(SPLIT_THREADS);
+    if (K <= 2 * 2048) LD_LAUNCH((k_w4_split<PACKED, 2>), grid, block, 0, s, x, g, eps, T, K, G, r);
+    else if (K <= 7 * 2048) LD_LAUNCH((k_w4_split<PACKED, 7>), grid, block, 0, s, x, g, eps, T, K, G, r);
+    else LD_LAUNCH((k_w4_split<PACKED, 0>), grid, block, 0, s, x, g, eps, T, K, G, r);
 }
 
 // ---------------------------------------------------------------- the product, few rows
@@ -481,8 +513,8 @@ ld_status ldk_linear_w4(const void *image, int32_t scale_dtype, int32_t zeros, i
     hipStream_t s = (hipStream_t)stream;
     const ld::W4Image w = ld::w4_image(image, N, K, group, epilogue == LDK_SWIGLU ? 2 : 1, scale_dtype, zeros != 0, nullptr);
     const ld::W4Rows r = ld::w4_rows(scratch, T, K, 0, nullptr);
-    if (T <= 8) LD_LAUNCH(k_w4_split<true>, dim3(T), dim3(256), 0, s, x, g, eps, K, group, r);
-    else LD_LAUNCH(k_w4_split<false>, dim3(T), dim3(256), 0, s, x, g, eps, K, group, r);
+    if (T <= 8) launch_split<true>(x, g, eps, T, K, group, r, s);
+    else launch_split<false>(x, g, eps, T, K, group, r, s);
     if (T >= TILE_ROWS) {
         ld::launch_w4_tile(w, scale_dtype, r, group, T, N, epilogue, plan, y, s);
         return launched("k_w4_tile");
