@@ -120,22 +120,51 @@ __global__ __launch_bounds__(256) void k_w4_quantize(const WT *__restrict__ W, i
 // ---------------------------------------------------------------- activations
 
 // Image of the activations: for every 16 rows and 32 columns the hi and the lo operand of one matrix instruction, 1 KB
-// each in lane order ([row tile][k / 32][term][lane][8]).  Up to eight rows share one operand: columns 0 .. 7 of it are
-// the hi terms, 8 .. 15 the lo terms ([k / 32][lane][8]).  sums [row tile][group][term][16]: 2^-24 times the sums of a group's
-// columns (packed: [group][16] like the operand; those of hi are exact).  expo[t]: the exponent that takes a finished sum back, or W4_NOT_FINITE.
-// One workgroup of 512 threads a row; a thread takes four columns at a time, NC times, and keeps them (NC = 0: longer rows, read twice).
-constexpr int SPLIT_THREADS = 512;
-template <bool PACKED, int NC>
-__global__ __launch_bounds__(SPLIT_THREADS) void k_w4_split(const float *__restrict__ x, const float *__restrict__ gain, float eps, int T, int K, int G,
-                                                            ld::W4Rows r) {
-    constexpr int STEP = SPLIT_THREADS * 4, WAVES = SPLIT_THREADS / 64;
-    // the 16 rows of a tile fill the same lines of the image: they go to one XCD (workgroups take turns over eight), whose L2 puts the lines together
-    const int t = PACKED ? blockIdx.x : (int)(blockIdx.x / 128 * 8 + blockIdx.x % 8) * 16 + blockIdx.x / 8 % 16;
-    if (t >= T) return;
-    const float *row = x + (int64_t)t * K;
-    const int Kp = r.k_tiles * 128, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const bool quads = K % 4 == 0 && ((uintptr_t)x & 15) == 0 && ((uintptr_t)gain & 15) == 0;
-    auto fetch = [&](const float *p, int c, f32x4 &v) {
+// each in lane order ([row tile][k / 32][term][lane][8]).  sums [row tile][group][term][16]: 2^-24 times the sums of a group's
+// columns (those of hi are exact).  expo[t]: the exponent that takes a finished sum back, or W4_NOT_FINITE.
+
+// Sum over 8, 16 or 32 neighbouring lanes, maximum over 32, in all of them: exchanges within the row of 16 lanes, then of whole rows.
+template <int CTRL> __device__ __forceinline__ float dpp(float v) {
+    return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), CTRL, 0xf, 0xf, false));
+}
+template <typename F> __device__ __forceinline__ float other_row(float v, F f) {
+    const auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return f(__uint_as_float(a[0]), __uint_as_float(a[1]));
+}
+__device__ __forceinline__ float lanes_sum(float v, int lanes) {
+    v += dpp<0xb1>(v);       // quads: 1 0 3 2
+    v += dpp<0x4e>(v);       // quads: 2 3 0 1
+    v += dpp<0x141>(v);      // mirrored halves of a row
+    if (lanes > 8) v += dpp<0x140>(v);      // mirrored rows
+    if (lanes > 16) v = other_row(v, [](float a, float b) { return a + b; });
+    return v;
+}
+__device__ __forceinline__ float max_of_32(float v) {
+    v = fmaxf(v, dpp<0xb1>(v));
+    v = fmaxf(v, dpp<0x4e>(v));
+    v = fmaxf(v, dpp<0x141>(v));
+    v = fmaxf(v, dpp<0x140>(v));
+    return other_row(v, [](float a, float b) { return fmaxf(a, b); });
+}
+
+// The other half's value, for one that is the same in the 32 lanes of each.
+__device__ __forceinline__ float swapped_half(float v) {
+    const auto a = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return threadIdx.x & 32 ? __uint_as_float(a[0]) : __uint_as_float(a[1]);
+}
+
+// One row by a workgroup of THREADS threads: a thread takes four columns at a time, NC times, and keeps them (NC = 0: longer rows, read
+// twice).  put(c, hi, lo): columns c .. c + 3 as fp16; put_sums(group, hi, lo), by one thread each.  Returns the row's exponent.
+template <int THREADS, int NC>
+struct SplitRow {
+    static constexpr int STEP = THREADS * 4, WAVES = THREADS / 64;
+    f32x4 kept[NC ? NC : 1], weight[NC ? NC : 1];
+    const float *row, *gain;
+    int K;
+    bool quads;
+    struct Room { float ss[WAVES]; uint32_t top[WAVES]; };
+
+    __device__ __forceinline__ void fetch(const float *p, int c, f32x4 &v) const {
         if (quads) {
             if (c < K) v = *reinterpret_cast<const f32x4 *>(p + c);
         } else {
@@ -143,116 +172,128 @@ __global__ __launch_bounds__(SPLIT_THREADS) void k_w4_split(const float *__restr
             for (int e = 0; e < 4; e++)
                 if (c + e < K) v[e] = p[c + e];
         }
-    };
-    float ss = 0.f;
-    uint32_t top = 0;      // largest |x gain|, compared as bits: a NaN stays
-    auto look = [&](const f32x4 &v, const f32x4 &g) {
+    }
+    __device__ __forceinline__ f32x4 value(int c) const {
+        f32x4 v = {0.f, 0.f, 0.f, 0.f};
+        fetch(row, c, v);
+        return v;
+    }
+    __device__ __forceinline__ f32x4 gain_at(int c) const {
+        f32x4 g = {1.f, 1.f, 1.f, 1.f};
+        if (gain) fetch(gain, c, g);
+        return g;
+    }
+    // Asks for the row (aligned: all rows' starts and the gain are 16-byte aligned).
+    __device__ __forceinline__ void load(const float *x, const float *g, int columns, bool aligned) {
+        row = x; gain = g; K = columns; quads = aligned;
+        if constexpr (NC > 0) {
 #pragma unroll
-        for (int e = 0; e < 4; e++) {
-            ss += v[e] * v[e];
-            top = max(top, __float_as_uint(v[e] * g[e]) & 0x7fffffffu);
-        }
-    };
-    const f32x4 zero = {0.f, 0.f, 0.f, 0.f}, one = {1.f, 1.f, 1.f, 1.f};
-    f32x4 kept[NC ? NC : 1], weight[NC ? NC : 1];
-    if constexpr (NC > 0) {
-#pragma unroll
-        for (int i = 0; i < NC; i++) {
-            kept[i] = zero;
-            weight[i] = one;
-            fetch(row, i * STEP + threadIdx.x * 4, kept[i]);
-            if (gain) fetch(gain, i * STEP + threadIdx.x * 4, weight[i]);
-        }
-#pragma unroll
-        for (int i = 0; i < NC; i++) look(kept[i], weight[i]);
-    } else {
-        for (int c = threadIdx.x * 4; c < K; c += STEP) {
-            f32x4 v = zero, g = one;
-            fetch(row, c, v);
-            if (gain) fetch(gain, c, g);
-            look(v, g);
+            for (int i = 0; i < NC; i++) {
+                kept[i] = value(i * STEP + threadIdx.x * 4);
+                weight[i] = gain_at(i * STEP + threadIdx.x * 4);
+            }
         }
     }
-    __shared__ float sm_ss[WAVES];
-    __shared__ uint32_t sm_top[WAVES];
-    ss = wave_sum(ss);
+    template <typename Put, typename Sums>
+    __device__ __forceinline__ int split(float eps, int Kp, int G, Room &sm, Put put, Sums put_sums) {
+        float ss = 0.f;
+        uint32_t top = 0;      // largest |x gain|, compared as bits: a NaN stays
+        auto look = [&](const f32x4 &v, const f32x4 &g) {
 #pragma unroll
-    for (int off = 32; off > 0; off >>= 1) top = max(top, (uint32_t)__shfl_xor((int)top, off, WAVE));
-    if (lane == 0) { sm_ss[wave] = ss; sm_top[wave] = top; }
-    __syncthreads();
-    ss = 0.f;
+            for (int e = 0; e < 4; e++) {
+                ss += v[e] * v[e];
+                top = max(top, __float_as_uint(v[e] * g[e]) & 0x7fffffffu);
+            }
+        };
+        if constexpr (NC > 0) {
 #pragma unroll
-    for (int i = 0; i < WAVES; i++) { ss += sm_ss[i]; top = max(top, sm_top[i]); }
-    const float inv = gain ? 1.f / sqrtf(ss / K + eps) : 1.f;
-    const float m = __uint_as_float(top) * inv;
-    const bool finite = m < INFINITY;      // false for NaN
-    const int k = finite && m > 0.f ? 14 - ilogbf(m) : 0;
-    if (threadIdx.x == 0) r.expo[t] = finite ? 24 - k : ld::W4_NOT_FINITE;
-
-    const int rt = t >> 4, col = PACKED ? t : t & 15;
-    const int groups = Kp / G;
-    auto split = [&](int c, const f32x4 &raw, const f32x4 &g) {
-        float v[4], sum_hi = 0.f, sum_lo = 0.f, most = 0.f;
-        union { _Float16 h[4]; uint2 u; } hi, lo;
-#pragma unroll
-        for (int e = 0; e < 4; e++) {
-            v[e] = ldexpf(finite ? raw[e] * inv * g[e] : 0.f, k);      // in the order of the definition: x / rms, then the gain
-            most = fmaxf(most, fabsf(v[e]));
-        }
-#pragma unroll
-        for (int off = 1; off < 32; off <<= 1) most = fmaxf(most, __shfl_xor(most, off, WAVE));      // 128 columns: 32 lanes
-        // quantum: 2^-12 of the power of two at or below the largest magnitude, as its bits; at least fp16's least subnormal
-        const float quantum = __uint_as_float(max((int)(__float_as_uint(most) & 0x7f800000u) - (12 << 23), (127 - 24) << 23));
-        const float per_quantum = __uint_as_float((254u << 23) - __float_as_uint(quantum));      // its reciprocal
-#pragma unroll
-        for (int e = 0; e < 4; e++) {
-            const float h = (float)(_Float16)(rintf(v[e] * per_quantum) * quantum);
-            const float f = e < 2 ? 1.f : 0.0625f;      // e >= 2: codes in bits 4 .. 7 (c is a multiple of 4)
-            hi.h[e] = (_Float16)(h * f);
-            lo.h[e] = (_Float16)((v[e] - h) * f);
-            sum_hi += h;
-            sum_lo += v[e] - h;
-        }
-        const int kb = c >> 5, slot = col + 16 * ((c & 31) >> 3), half = (c & 7) * 2;      // half: bytes into the lane's 16
-        if (PACKED) {
-            char *p = (char *)r.image + ((int64_t)kb * 64 + slot) * 16 + half;
-            *reinterpret_cast<uint2 *>(p) = hi.u;
-            *reinterpret_cast<uint2 *>(p + 8 * 16) = lo.u;
+            for (int i = 0; i < NC; i++) look(kept[i], weight[i]);
         } else {
-            char *p = (char *)r.image + (((int64_t)rt * r.k_tiles * 4 + kb) * 128 + slot) * 16 + half;
-            *reinterpret_cast<uint2 *>(p) = hi.u;
-            *reinterpret_cast<uint2 *>(p + 1024) = lo.u;
+            for (int c = threadIdx.x * 4; c < K; c += STEP) look(value(c), gain_at(c));
         }
-        for (int off = 1; off < G / 4; off <<= 1) {
-            sum_hi += __shfl_xor(sum_hi, off, WAVE);
-            sum_lo += __shfl_xor(sum_lo, off, WAVE);
-        }
-        if (c % G == 0) {
-            float *p = r.sums + (PACKED ? (int64_t)(c / G) * 16 : ((int64_t)rt * groups + c / G) * 32) + col;
-            p[0] = ldexpf(sum_hi, -24);
-            p[PACKED ? 8 : 16] = ldexpf(sum_lo, -24);
-        }
-    };
-    if constexpr (NC > 0) {
+        ss = lanes_sum(ss, 32);
+        ss += swapped_half(ss);
+        const float most = max_of_32(__uint_as_float(top));      // as floats here: a NaN is put aside first
+        top = __any(top > 0x7f800000u) ? 0x7fc00000u : __float_as_uint(fmaxf(most, swapped_half(most)));
+        if ((threadIdx.x & 63) == 0) { sm.ss[threadIdx.x >> 6] = ss; sm.top[threadIdx.x >> 6] = top; }
+        lds_barrier();
+        ss = 0.f;
 #pragma unroll
-        for (int i = 0; i < NC; i++)
-            if (i * STEP + (int)threadIdx.x * 4 < Kp) split(i * STEP + threadIdx.x * 4, kept[i], weight[i]);
-    } else {
-        for (int c = threadIdx.x * 4; c < Kp; c += STEP) {
-            f32x4 v = zero, g = one;
-            fetch(row, c, v);
-            if (gain) fetch(gain, c, g);
-            split(c, v, g);
+        for (int i = 0; i < WAVES; i++) { ss += sm.ss[i]; top = max(top, sm.top[i]); }
+        const float inv = gain ? 1.f / sqrtf(ss / K + eps) : 1.f;
+        const float m = __uint_as_float(top) * inv;
+        const bool finite = m < INFINITY;      // false for NaN
+        const int k = finite && m > 0.f ? 14 - ilogbf(m) : 0;
+        auto part = [&](int c, const f32x4 &raw, const f32x4 &g) {
+            float v[4], sum_hi = 0.f, sum_lo = 0.f, most = 0.f;
+            union { _Float16 h[4]; uint2 u; } hi, lo;
+#pragma unroll
+            for (int e = 0; e < 4; e++) {
+                v[e] = ldexpf(finite ? raw[e] * inv * g[e] : 0.f, k);      // in the order of the definition: x / rms, then the gain
+                most = fmaxf(most, fabsf(v[e]));
+            }
+            most = max_of_32(most);      // 128 columns
+            // quantum: 2^-12 of the power of two at or below the largest magnitude, as its bits; at least fp16's least subnormal
+            const float quantum = __uint_as_float(max((int)(__float_as_uint(most) & 0x7f800000u) - (12 << 23), (127 - 24) << 23));
+            const float per_quantum = __uint_as_float((254u << 23) - __float_as_uint(quantum));      // its reciprocal
+#pragma unroll
+            for (int e = 0; e < 4; e++) {
+                const float h = (float)(_Float16)(rintf(v[e] * per_quantum) * quantum);
+                const float f = e < 2 ? 1.f : 0.0625f;      // e >= 2: codes in bits 4 .. 7 (c is a multiple of 4)
+                hi.h[e] = (_Float16)(h * f);
+                lo.h[e] = (_Float16)((v[e] - h) * f);
+                sum_hi += h;
+                sum_lo += v[e] - h;
+            }
+            put(c, hi.u, lo.u);
+            sum_hi = lanes_sum(sum_hi, G / 4);
+            sum_lo = lanes_sum(sum_lo, G / 4);
+            if (c % G == 0) put_sums(c / G, ldexpf(sum_hi, -24), ldexpf(sum_lo, -24));
+        };
+        if constexpr (NC > 0) {
+#pragma unroll
+            for (int i = 0; i < NC; i++)
+                if (i * STEP + (int)threadIdx.x * 4 < Kp) part(i * STEP + threadIdx.x * 4, kept[i], weight[i]);
+        } else {
+            for (int c = threadIdx.x * 4; c < Kp; c += STEP) part(c, value(c), gain_at(c));
         }
+        return finite ? 24 - k : ld::W4_NOT_FINITE;
     }
+};
+
+// The activations of a product of many rows, a workgroup a row.
+constexpr int SPLIT_THREADS = 512;
+template <int NC>
+__global__ __launch_bounds__(SPLIT_THREADS) void k_w4_split(const float *__restrict__ x, const float *__restrict__ gain, float eps, int T, int K, int G,
+                                                            ld::W4Rows r) {
+    // the 16 rows of a tile fill the same lines of the image: they go to one XCD (workgroups take turns over eight), whose L2 puts the lines together
+    const int t = (int)(blockIdx.x / 128 * 8 + blockIdx.x % 8) * 16 + blockIdx.x / 8 % 16;
+    if (t >= T) return;
+    __shared__ typename SplitRow<SPLIT_THREADS, NC>::Room sm;
+    SplitRow<SPLIT_THREADS, NC> row;
+    row.load(x + (int64_t)t * K, gain, K, K % 4 == 0 && (((uintptr_t)x | (uintptr_t)gain) & 15) == 0);
+    const int Kp = r.k_tiles * 128, rt = t >> 4, col = t & 15, groups = Kp / G;
+    const int expo = row.split(
+        eps, Kp, G, sm,
+        [&](int c, uint2 hi, uint2 lo) {
+            const int kb = c >> 5, slot = col + 16 * ((c & 31) >> 3), half = (c & 7) * 2;      // half: bytes into the lane's 16
+            char *p = (char *)r.image + (((int64_t)rt * r.k_tiles * 4 + kb) * 128 + slot) * 16 + half;
+            *reinterpret_cast<uint2 *>(p) = hi;
+            *reinterpret_cast<uint2 *>(p + 1024) = lo;
+        },
+        [&](int g, float hi, float lo) {
+            float *p = r.sums + ((int64_t)rt * groups + g) * 32 + col;
+            p[0] = hi;
+            p[16] = lo;
+        });
+    if (threadIdx.x == 0) r.expo[t] = expo;
 }
 
-template <bool PACKED>
 void launch_split(const float *x, const float *g, float eps, int T, int K, int G, const ld::W4Rows &r, hipStream_t s) {
-    const dim3 grid(PACKED ? T : (T + 127) / 128 * 128), block(SPLIT_THREADS);
-    if (K <= 2 * 2048) LD_LAUNCH((k_w4_split<PACKED, 2>), grid, block, 0, s, x, g, eps, T, K, G, r);
-    else if (K <= 7 * 2048) LD_LAUNCH((k_w4_split<PACKED, 7>), grid, block, 0, s, x, g, eps, T, K, G, r);
-    else LD_LAUNCH((k_w4_split<PACKED, 0>), grid, block, 0, s, x, g, eps, T, K, G, r);
+    const dim3 grid((T + 127) / 128 * 128), block(SPLIT_THREADS);
+    if (K <= 2 * 2048) LD_LAUNCH(k_w4_split<2>, grid, block, 0, s, x, g, eps, T, K, G, r);
+    else if (K <= 7 * 2048) LD_LAUNCH(k_w4_split<7>, grid, block, 0, s, x, g, eps, T, K, G, r);
+    else LD_LAUNCH(k_w4_split<0>, grid, block, 0, s, x, g, eps, T, K, G, r);
 }
 
 // ---------------------------------------------------------------- the product, few rows
@@ -262,158 +303,171 @@ __device__ __forceinline__ f16x8 codes_as_f16(uint32_t w) {
     return __builtin_bit_cast(f16x8, (u32x4){w & 0x000f000fu, w & 0x00f000f0u, s & 0x000f000fu, s & 0x00f000f0u});
 }
 
-// A workgroup of eight waves takes R tiles of 16 output rows (SwiGLU: the gate tile and its up tile) and 16 CT activation rows;
-// wave w multiplies the column tiles w, w + 8, ..; the eight sums meet in LDS.  PACKED: up to eight activation rows, both terms in
-// one operand.
-template <int CT, bool PACKED, int G, int R>
-__global__ __launch_bounds__(512) void k_w4_rows(ld::W4Image w, int scale_dtype, ld::W4Rows r, int T, int N, int epilogue, float *__restrict__ y) {
-    constexpr int WAVES = 8, PER = 128 / G, TERMS = PACKED ? 1 : 2;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int col = lane & 15, h = lane >> 4;
-    const bool pair = epilogue == LDK_SWIGLU;
-    const int rt0 = pair ? blockIdx.x : blockIdx.x * R;
-    const int ct0 = blockIdx.y * CT;
-    const int ct_all = (T + 15) >> 4;
-    int64_t tile0[R], group0[R];
-#pragma unroll
-    for (int i = 0; i < R; i++) {
-        const int64_t t = pair ? (int64_t)i * w.row_tiles + rt0 : min(rt0 + i, w.row_tiles - 1);
-        tile0[i] = t * w.k_tiles;
-        group0[i] = t * w.groups;
-    }
-    f32x4 total[R][CT];
-#pragma unroll
-    for (int i = 0; i < R; i++)
-#pragma unroll
-        for (int c = 0; c < CT; c++) total[i][c] = (f32x4){0.f, 0.f, 0.f, 0.f};
-
-    for (int kt = wave; kt < w.k_tiles; kt += WAVES) {
-        u32x4 code[R];
-#pragma unroll
-        for (int i = 0; i < R; i++) code[i] = load_stream16(w.codes + ((tile0[i] + kt) * 64 + lane) * 4);
+// What a wave reads of a tile of 16 rows x 128 columns: its codes, the scales of its lanes' four rows, the zero points.
+template <int PER, typename ST>
+struct CodeTile {
+    u32x4 code;
+    uint32_t scale[PER][sizeof(ST)], zero[PER];
+    __device__ __forceinline__ void load(const ld::W4Image &w, int64_t tile, int kt, int lane) {
+        code = load_stream16(w.codes + ((tile * w.k_tiles + kt) * 64 + lane) * 4);
 #pragma unroll
         for (int p = 0; p < PER; p++) {
-            f32x4 acc[R][CT][TERMS];
+            const int64_t at = (tile * w.groups + (int64_t)kt * PER + p) * 16 + 4 * (lane >> 4);
+            if constexpr (sizeof(ST) == 2) {
+                const uint2 v = *reinterpret_cast<const uint2 *>((const bf16_t *)w.scales + at);
+                scale[p][0] = v.x; scale[p][1] = v.y;
+            } else {
+                const uint4 v = *reinterpret_cast<const uint4 *>((const float *)w.scales + at);
+                scale[p][0] = v.x; scale[p][1] = v.y; scale[p][2] = v.z; scale[p][3] = v.w;
+            }
+            zero[p] = w.zeros ? *reinterpret_cast<const uint32_t *>(w.zeros + at) : 0x08080808u;
+        }
+    }
+    __device__ __forceinline__ float s(int p, int e) const {
+        if constexpr (sizeof(ST) == 4) return __uint_as_float(scale[p][e]);
+        else return __uint_as_float((e & 1) ? scale[p][e >> 1] & 0xffff0000u : scale[p][e >> 1] << 16);
+    }
+    __device__ __forceinline__ float z(int p, int e) const { return (float)((zero[p] >> (8 * e)) & 255u); }
+};
+
+// One row, or a few short ones.  A workgroup of eight waves splits the rows into LDS by itself, while its first codes are on their way; a launch
+// ahead would take longer than the product.  It takes units of R tiles of 16 output rows (SwiGLU: the gate tile and its up tile), every
+// gridDim.x-th of them; wave w multiplies the column tiles w, w + 8, .., and the eight sums meet in LDS.  Up to eight rows make one
+// operand: columns 0 .. 7 are their hi terms, 8 .. 15 the lo terms, so that both cost what one does.
+// AHEAD column tiles are asked for at any time, also over the end of a unit, and without a condition (past an end the last one again): a wait
+// for one then leaves the younger ones in flight.
+template <int G, int R, int T, int NC, typename ST>
+__global__ __launch_bounds__(512, 4) void k_w4_rows(ld::W4Image w, const float *__restrict__ x, const float *__restrict__ gain, float eps, int N, int K,
+                                                    int epilogue, float *__restrict__ y) {
+    constexpr int WAVES = 8, PER = 128 / G;
+    constexpr int AHEAD = R == 1 && PER < 4 ? 4 : R * PER * sizeof(ST) < 32 ? 2 : 1;      // by the registers that a column tile takes
+    extern __shared__ __attribute__((aligned(16))) char sm_rows[];      // [row][term] of `stride` bytes, then sums [row][group][term]
+    __shared__ f32x4 sm[2][WAVES][R][64];
+    __shared__ int expo[T];
+    __shared__ typename SplitRow<512, NC>::Room room;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int col = lane & 15, h = lane >> 4;
+    const bool pair = epilogue == LDK_SWIGLU;
+    const int units = pair ? w.row_tiles : (w.row_tiles + R - 1) / R;
+    const int steps = ((w.k_tiles + WAVES - 1) / WAVES + AHEAD - 1) / AHEAD * AHEAD;      // column tiles a wave, up to a multiple of AHEAD
+    const int Kp = w.k_tiles * 128, stride = Kp * 2 + 64;      // 64: neighbouring rows' pieces lie in different banks
+    float *sm_sums = reinterpret_cast<float *>(sm_rows + 2 * T * stride);
+
+    CodeTile<PER, ST> ring[AHEAD][R];
+    // asks for step `at` of a unit, or of the workgroup's next one where the unit ends before it
+    auto fill = [&](CodeTile<PER, ST> (&q)[R], int unit, int at) {
+        if (at >= steps) { at -= steps; unit += gridDim.x; }
+        unit = min(unit, units - 1);
+        const int kt = min(wave + at * WAVES, w.k_tiles - 1);
+#pragma unroll
+        for (int i = 0; i < R; i++) q[i].load(w, pair ? (int64_t)i * w.row_tiles + unit : min(unit * R + i, w.row_tiles - 1), kt, lane);
+    };
+#pragma unroll
+    for (int t = 0; t < T; t++) {
+        SplitRow<512, NC> row;
+        row.load(x + (int64_t)t * K, gain, K, K % 4 == 0 && (((uintptr_t)x | (uintptr_t)gain) & 15) == 0);
+        if (t == 0) {
+#pragma unroll
+            for (int u = 0; u < AHEAD; u++) fill(ring[u], blockIdx.x, u);
+        } else {
+            lds_barrier();      // everyone has read the room
+        }
+        const int e = row.split(
+            eps, Kp, G, room,
+            [&](int c, uint2 hi, uint2 lo) {
+                *reinterpret_cast<uint2 *>(sm_rows + 2 * t * stride + c * 2) = hi;
+                *reinterpret_cast<uint2 *>(sm_rows + (2 * t + 1) * stride + c * 2) = lo;
+            },
+            [&](int g, float hi, float lo) { *reinterpret_cast<float2 *>(sm_sums + 2 * (t * w.groups + g)) = make_float2(hi, lo); });
+        if (threadIdx.x == 0) expo[t] = e;
+    }
+    lds_barrier();
+
+    f32x4 total[R];
+    const int t_col = min(col & 7, T - 1);      // columns past the rows repeat the last one's
+    const char *operand = sm_rows + (2 * t_col + (col >> 3)) * stride + 16 * h;
+    const float *my_sums = sm_sums + 2 * t_col * w.groups + (col >> 3);
+    auto multiply = [&](const CodeTile<PER, ST> (&q)[R], int kt) {
+#pragma unroll
+        for (int p = 0; p < PER; p++) {
+            f32x4 acc[R];
+#pragma unroll
+            for (int i = 0; i < R; i++) acc[i] = (f32x4){0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int j = p * (G / 32); j < (p + 1) * (G / 32); j++) {
+                const f16x8 b = *reinterpret_cast<const f16x8 *>(operand + kt * 256 + 64 * j);
+#pragma unroll
+                for (int i = 0; i < R; i++) acc[i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(codes_as_f16(q[i].code[j]), b, acc[i], 0, 0, 0);
+            }
+            const float sum = my_sums[2 * (kt * PER + p)];
 #pragma unroll
             for (int i = 0; i < R; i++)
 #pragma unroll
-                for (int c = 0; c < CT; c++)
+                for (int e = 0; e < 4; e++) total[i][e] += q[i].s(p, e) * (acc[i][e] - q[i].z(p, e) * sum);
+        }
+    };
+    int turn = 0;
+    for (int unit = blockIdx.x; unit < units; unit += gridDim.x, turn ^= 1) {
 #pragma unroll
-                    for (int q = 0; q < TERMS; q++) acc[i][c][q] = (f32x4){0.f, 0.f, 0.f, 0.f};
+        for (int i = 0; i < R; i++) total[i] = (f32x4){0.f, 0.f, 0.f, 0.f};
+        for (int at = 0; at < steps; at += AHEAD)
 #pragma unroll
-            for (int j = p * (G / 32); j < (p + 1) * (G / 32); j++) {
-                f16x8 b[CT][TERMS];
+            for (int u = 0; u < AHEAD; u++) {
+                const int kt = wave + (at + u) * WAVES;
+                if (kt < w.k_tiles) multiply(ring[u], kt);
+                fill(ring[u], unit, at + u + AHEAD);
+            }
 #pragma unroll
-                for (int c = 0; c < CT; c++)
+        for (int i = 0; i < R; i++) sm[turn][wave][i][lane] = total[i];
+        lds_barrier();      // the other half of sm is free by the next one: whoever reads it does so ahead of that
+        // 16 sums (8 waves, 2 terms) of each of 16 R values a row: one a lane, joined across the 16 lanes of a row of the wave; a value's
+        // two halves (R = 2) lie in neighbouring rows
+        const int part = R == 2 ? (threadIdx.x >> 4) & 1 : 0, j = threadIdx.x >> (R == 2 ? 5 : 4);
+        const int n = (R == 2 && !pair ? unit * 2 + part : unit) * 16 + j;
+        if (R == 2 || j < 16)
 #pragma unroll
-                    for (int q = 0; q < TERMS; q++) {
-                        const int ct = min(ct0 + c, ct_all - 1);
-                        const int64_t at = PACKED ? ((int64_t)kt * 4 + j) * 64 : (((int64_t)ct * w.k_tiles + kt) * 4 + j) * 128 + q * 64;
-                        u32x4 v = {0, 0, 0, 0};
-                        if (!PACKED || (col & 7) < T) v = *reinterpret_cast<const u32x4 *>((const char *)r.image + (at + lane) * 16);
-                        b[c][q] = __builtin_bit_cast(f16x8, v);
-                    }
-#pragma unroll
-                for (int i = 0; i < R; i++) {
-                    const f16x8 a = codes_as_f16(code[i][j]);
-#pragma unroll
-                    for (int c = 0; c < CT; c++)
-#pragma unroll
-                        for (int q = 0; q < TERMS; q++) acc[i][c][q] = __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b[c][q], acc[i][c][q], 0, 0, 0);
+            for (int t = 0; t < T; t++) {
+                float v = sm[turn][col & 7][part][(t + (col & 8)) + 16 * (j >> 2)][j & 3];
+                v += dpp<0xb1>(v);
+                v += dpp<0x4e>(v);
+                v += dpp<0x141>(v);
+                v += dpp<0x140>(v);
+                float out = ld::w4_finish(v, expo[t]);
+                if (pair) out = ld::w4_gated(out, other_row(out, [](float, float b) { return b; }));
+                if (col == 0 && n < N && !(pair && part)) {
+                    float *dst = y + (int64_t)t * N + n;
+                    *dst = epilogue == LDK_ADD ? *dst + out : out;
                 }
             }
-            const int g = kt * PER + p;
-            float sum[CT];
-#pragma unroll
-            for (int c = 0; c < CT; c++) {
-                sum[c] = 0.f;
-                if (PACKED) {
-                    if ((col & 7) < T) sum[c] = r.sums[(int64_t)g * 16 + col];
-                } else {
-                    const float *p = r.sums + ((int64_t)min(ct0 + c, ct_all - 1) * w.groups + g) * 32 + col;
-                    sum[c] = p[0] + p[16];
-                }
-            }
-#pragma unroll
-            for (int i = 0; i < R; i++) {
-                const int64_t at = (group0[i] + g) * 16 + 4 * h;
-                float s[4], z[4];
-                if (scale_dtype == LD_BF16) {
-                    const uint2 v = *reinterpret_cast<const uint2 *>((const bf16_t *)w.scales + at);
-                    s[0] = __uint_as_float(v.x << 16); s[1] = __uint_as_float(v.x & 0xffff0000u);
-                    s[2] = __uint_as_float(v.y << 16); s[3] = __uint_as_float(v.y & 0xffff0000u);
-                } else {
-                    const float4 v = *reinterpret_cast<const float4 *>((const float *)w.scales + at);
-                    s[0] = v.x; s[1] = v.y; s[2] = v.z; s[3] = v.w;
-                }
-                uint32_t zw = 0x08080808u;
-                if (w.zeros) zw = *reinterpret_cast<const uint32_t *>(w.zeros + at);
-#pragma unroll
-                for (int e = 0; e < 4; e++) z[e] = (float)((zw >> (8 * e)) & 255u);
-#pragma unroll
-                for (int c = 0; c < CT; c++)
-#pragma unroll
-                    for (int e = 0; e < 4; e++) {
-                        float d = acc[i][c][0][e] - z[e] * sum[c];
-                        if (TERMS == 2) d += acc[i][c][TERMS - 1][e];
-                        total[i][c][e] += s[e] * d;
-                    }
-            }
-        }
-    }
-
-    __shared__ f32x4 sm[WAVES][R][CT][64];
-#pragma unroll
-    for (int i = 0; i < R; i++)
-#pragma unroll
-        for (int c = 0; c < CT; c++) sm[wave][i][c][lane] = total[i][c];
-    __syncthreads();
-    for (int idx = threadIdx.x; idx < (pair ? 1 : R) * CT * 64; idx += WAVES * 64) {
-        const int l = idx & 63, c = (idx >> 6) % CT, i = (idx >> 6) / CT;
-        const int t = (ct0 + c) * 16 + (l & 15), n = (rt0 + i) * 16 + 4 * (l >> 4);
-        if (t >= T || n >= N || (PACKED && (l & 15) >= 8)) continue;
-        f32x4 v[2];
-#pragma unroll
-        for (int u = 0; u < 2; u++) {
-            if (u == 1 && !pair) break;
-            const int tile = pair ? u : i;
-            f32x4 a = (f32x4){0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-            for (int q = 0; q < WAVES; q++) {
-                a += sm[q][tile][c][l];
-                if (PACKED) a += sm[q][tile][c][l + 8];
-            }
-            v[u] = a;
-        }
-        const int expo = r.expo[t];
-        float *dst = y + (int64_t)t * N + n;
-        float out[4];
-#pragma unroll
-        for (int e = 0; e < 4; e++) {
-            out[e] = ld::w4_finish(v[0][e], expo);
-            if (pair) out[e] = ld::w4_gated(out[e], ld::w4_finish(v[1][e], expo));
-        }
-        const int m = min(4, N - n);
-        for (int e = 0; e < m; e++) dst[e] = epilogue == LDK_ADD ? dst[e] + out[e] : out[e];
     }
 }
 
-template <int CT, bool PACKED, int G>
-void launch_rows(const ld::W4Image &w, int scale_dtype, const ld::W4Rows &r, int T, int N, int epilogue, float *y, hipStream_t s) {
-    const int tiles = epilogue == LDK_SWIGLU ? w.row_tiles : (w.row_tiles + 1) / 2;
-    const dim3 grid(tiles, PACKED ? 1 : (T + 16 * CT - 1) / (16 * CT)), block(512);
-    LD_LAUNCH((k_w4_rows<CT, PACKED, G, 2>), grid, block, 0, s, w, scale_dtype, r, T, N, epilogue, y);
-}
+struct Few { const float *x, *g; float eps; int T, N, K, epilogue; float *y; };
 
+template <int G, int R, int T, int NC>
+void launch_rows(const ld::W4Image &w, int scale_dtype, const Few &a, hipStream_t s) {
+    // two workgroups a CU, each with the same number of units
+    const int units = a.epilogue == LDK_SWIGLU ? w.row_tiles : (w.row_tiles + R - 1) / R, each = (units + 511) / 512;
+    const dim3 grid((units + each - 1) / each), block(512);
+    const size_t lds = (size_t)T * (2 * (w.k_tiles * 256 + 64) + w.groups * 8);
+    if (scale_dtype == LD_BF16) LD_LAUNCH((k_w4_rows<G, R, T, NC, bf16_t>), grid, block, lds, s, w, a.x, a.g, a.eps, a.N, a.K, a.epilogue, a.y);
+    else LD_LAUNCH((k_w4_rows<G, R, T, NC, float>), grid, block, lds, s, w, a.x, a.g, a.eps, a.N, a.K, a.epilogue, a.y);
+}
+template <int G, int R>
+void launch_rows(const ld::W4Image &w, int scale_dtype, const Few &a, hipStream_t s) {
+    if (a.T == 2) launch_rows<G, R, 2, 2>(w, scale_dtype, a, s);
+    else if (a.K <= 4096) launch_rows<G, R, 1, 2>(w, scale_dtype, a, s);
+    else if (a.K <= 6144) launch_rows<G, R, 1, 3>(w, scale_dtype, a, s);
+    else launch_rows<G, R, 1, 7>(w, scale_dtype, a, s);
+}
 template <int G>
-void launch_group(const ld::W4Image &w, int scale_dtype, const ld::W4Rows &r, int T, int N, int epilogue, float *y, hipStream_t s) {
-    if (T <= 8) launch_rows<1, true, G>(w, scale_dtype, r, T, N, epilogue, y, s);
-    else if (T <= 16) launch_rows<1, false, G>(w, scale_dtype, r, T, N, epilogue, y, s);
-    else if (T <= 32) launch_rows<2, false, G>(w, scale_dtype, r, T, N, epilogue, y, s);
-    else launch_rows<4, false, G>(w, scale_dtype, r, T, N, epilogue, y, s);
+void launch_group(const ld::W4Image &w, int scale_dtype, const Few &a, hipStream_t s) {
+    if (a.epilogue != LDK_SWIGLU && w.row_tiles <= 512) launch_rows<G, 1>(w, scale_dtype, a, s);      // a tile a unit where there are few: more CUs
+    else launch_rows<G, 2>(w, scale_dtype, a, s);
 }
 
-constexpr int TILE_ROWS = 65;      // rows from which the tiled product takes over
+// Rows that a workgroup splits by itself: as many as its threads hold in registers.
+bool few_rows(int T, int K) { return (T == 1 && K <= 7 * 2048) || (T == 2 && K <= 2 * 2048); }
 
 bool bad_shape(int N, int K, int group, int parts, int scale_dtype) {
     return N <= 0 || K <= 0 || N > (1 << 28) || K > (1 << 28) || (group != 32 && group != 64 && group != 128) || (parts != 1 && parts != 2) ||
@@ -494,7 +548,7 @@ ld_status ldk_w4_quantize(const void *W, int32_t dtype, int32_t N, int32_t K, in
 size_t ldk_linear_w4_scratch_bytes(int32_t T, int32_t N, int32_t K, int32_t epilogue) {
     if (T <= 0 || N <= 0 || K <= 0) return 0;
     size_t bytes = 0;
-    ld::w4_rows(nullptr, T, K, T >= TILE_ROWS ? ld::w4_part_bound(T, N, epilogue) : 0, &bytes);
+    ld::w4_rows(nullptr, T, K, ld::w4_part_bound(T, N, epilogue), &bytes);
     return bytes;
 }
 
@@ -504,7 +558,8 @@ ld_status ldk_linear_w4(const void *image, int32_t scale_dtype, int32_t zeros, i
     if (!image || ((uintptr_t)image & 15) || !x || !y || T < 0 || epilogue < 0 || epilogue > 2 ||
         bad_shape(N, K, group, epilogue == LDK_SWIGLU ? 2 : 1, scale_dtype))
         return ld::fail(LD_E_INVAL, "ldk_linear_w4: bad argument (group 32, 64 or 128; image 16-byte aligned)");
-    const ld::W4Plan plan = T >= TILE_ROWS ? ld::w4_plan(T, N, K, epilogue) : ld::W4Plan{};
+    const bool few = few_rows(T, K);
+    const ld::W4Plan plan = few ? ld::W4Plan{} : ld::w4_plan(T, N, K, epilogue);
     size_t need = 0;
     ld::w4_rows(nullptr, T, K, plan.part_bytes, &need);
     if (!scratch || ((uintptr_t)scratch & 15) || scratch_bytes < need)
@@ -513,15 +568,15 @@ ld_status ldk_linear_w4(const void *image, int32_t scale_dtype, int32_t zeros, i
     hipStream_t s = (hipStream_t)stream;
     const ld::W4Image w = ld::w4_image(image, N, K, group, epilogue == LDK_SWIGLU ? 2 : 1, scale_dtype, zeros != 0, nullptr);
     const ld::W4Rows r = ld::w4_rows(scratch, T, K, 0, nullptr);
-    if (T <= 8) launch_split<true>(x, g, eps, T, K, group, r, s);
-    else launch_split<false>(x, g, eps, T, K, group, r, s);
-    if (T >= TILE_ROWS) {
+    if (!few) {
+        launch_split(x, g, eps, T, K, group, r, s);
         ld::launch_w4_tile(w, scale_dtype, r, group, T, N, epilogue, plan, y, s);
         return launched("k_w4_tile");
     }
-    if (group == 32) launch_group<32>(w, scale_dtype, r, T, N, epilogue, y, s);
-    else if (group == 64) launch_group<64>(w, scale_dtype, r, T, N, epilogue, y, s);
-    else launch_group<128>(w, scale_dtype, r, T, N, epilogue, y, s);
+    const Few a{x, g, eps, T, N, K, epilogue, y};
+    if (group == 32) launch_group<32>(w, scale_dtype, a, s);
+    else if (group == 64) launch_group<64>(w, scale_dtype, a, s);
+    else launch_group<128>(w, scale_dtype, a, s);
     return launched("k_w4_rows");
 }
 

@@ -51,7 +51,7 @@ __global__ __launch_bounds__(256, 2) void k_w4_tile(ld::W4Image w, ld::W4Rows r,
     __shared__ __attribute__((aligned(16))) char sm_x[2][TT * 8192];
     __shared__ float sm_s[2][TT * PER * 32];
     __shared__ __attribute__((aligned(16))) float sm_w[2][PER][ZEROS ? 2 : 1][256];      // scales, 8 - zero point
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int col = lane & 15, h = lane >> 4;
     const bool pair = epilogue == LDK_SWIGLU;
     const int slab = blockIdx.y;
@@ -254,7 +254,8 @@ void launch_tile(const ld::W4Image &w, int scale_dtype, const ld::W4Rows &r, int
 }
 template <int G>
 void launch_group(const ld::W4Image &w, int scale_dtype, const ld::W4Rows &r, int T, int N, int epilogue, const ld::W4Plan &p, float *y, hipStream_t s) {
-    if (p.tt == 2) launch_tile<2, G>(w, scale_dtype, r, T, N, epilogue, p, y, s);
+    if (p.tt == 1) launch_tile<1, G>(w, scale_dtype, r, T, N, epilogue, p, y, s);
+    else if (p.tt == 2) launch_tile<2, G>(w, scale_dtype, r, T, N, epilogue, p, y, s);
     else if (p.tt == 3) launch_tile<3, G>(w, scale_dtype, r, T, N, epilogue, p, y, s);
     else launch_tile<4, G>(w, scale_dtype, r, T, N, epilogue, p, y, s);
 }
@@ -277,7 +278,7 @@ W4Plan w4_plan(int T, int N, int K, int epilogue) {
     W4Plan best{};
     const int row_tiles = (N + 15) / 16, k_tiles = (K + 127) / 128, per_block = epilogue == LDK_SWIGLU ? 8 : 16;
     double cost = 0;
-    for (int tt = 2; tt <= 4; tt++)
+    for (int tt = 1; tt <= 4; tt++)
         for (int slabs = 1; slabs <= MOST_SLABS && slabs <= k_tiles; slabs++) {
             W4Plan p;
             p.tt = tt;
