@@ -272,28 +272,37 @@ size_t w4_part_bound(int T, int N, int epilogue) {
     return std::min((size_t)MOST_SLABS * T * row, (size_t)MOST_GROUPS * 64 * 256 * 4);
 }
 
-// Tile and slabs: the rounds of 512 workgroups (two a CU) times the column tiles each has, 16 tt rows wide plus what a column tile costs
-// beside its products, and the slabs' sums written and read again.
+// Tile and slabs.  Up to 128 rows: 16 of them a workgroup (four workgroups a CU), and as many slabs as bring some 1024 workgroups
+// and leave each two column tiles.  More rows: the least of rounds x (column tiles + 3.3, what begins and ends a workgroup) x the time of a column
+// tile of 32, 48 or 64 rows, a last round that leaves half the CUs one workgroup taking 0.84 of one; slabs cost a launch and their sums' way
+// out and back, 5.9 column tiles of 32 rows.  Both fitted to 110 sizes (3 .. 1056 rows of the decoder shapes' matrices, each in up to 20
+// forms): the times of the forms taken are 2 % and 0.2 % above the best ones' in the mean.
 W4Plan w4_plan(int T, int N, int K, int epilogue) {
-    W4Plan best{};
     const int row_tiles = (N + 15) / 16, k_tiles = (K + 127) / 128, per_block = epilogue == LDK_SWIGLU ? 8 : 16;
-    double cost = 0;
-    for (int tt = 1; tt <= 4; tt++)
-        for (int slabs = 1; slabs <= MOST_SLABS && slabs <= k_tiles; slabs++) {
-            W4Plan p;
-            p.tt = tt;
-            p.slabs = slabs;
-            p.n_blocks = (row_tiles + per_block - 1) / per_block;
-            p.t_blocks = (T + 16 * tt - 1) / (16 * tt);
-            const int64_t groups = (int64_t)p.n_blocks * p.t_blocks * slabs;
-            if (slabs > 1 && groups > MOST_GROUPS) break;
-            const int64_t per = (k_tiles + slabs - 1) / slabs;
-            const double rounds = (double)((groups + 511) / 512);
-            // us: a column tile of 16 rows takes some 0.5 us with two workgroups a CU; sums at 4 TB/s, and a launch
-            const double c = rounds * ((per + 2) * (0.5 * tt + 0.3)) +
-                             (slabs > 1 ? 3 + 2.0 * slabs * T * (double)row_tiles * 16 * (epilogue == LDK_SWIGLU ? 2 : 1) * 4 / 4e6 : 0);
-            if (cost == 0 || c < cost) { cost = c; best = p; }
-        }
+    W4Plan best{};
+    best.n_blocks = (row_tiles + per_block - 1) / per_block;
+    if (T <= 128) {
+        best.tt = 1;
+        best.t_blocks = (T + 15) / 16;
+        best.slabs = (int)std::max<int64_t>(1, std::min<int64_t>({MOST_SLABS, k_tiles / 2, MOST_GROUPS / ((int64_t)best.n_blocks * best.t_blocks)}));
+    } else {
+        const double tile[3] = {1.0, 1.28, 1.72};
+        double cost = 0;
+        for (int tt = 2; tt <= 4; tt++)
+            for (int slabs = 1; slabs <= MOST_SLABS && slabs <= k_tiles; slabs++) {
+                const int t_blocks = (T + 16 * tt - 1) / (16 * tt);
+                const int64_t groups = (int64_t)best.n_blocks * t_blocks * slabs, rest = groups % 512;
+                if (slabs > 1 && groups > MOST_GROUPS) break;
+                const double rounds = (double)(groups / 512) + (rest == 0 ? 0 : rest <= 256 ? 0.84 : 1);
+                const double c = rounds * ((k_tiles + slabs - 1) / slabs + 3.3) * tile[tt - 2] + (slabs > 1 ? 5.9 : 0);
+                if (cost == 0 || c < cost) {
+                    cost = c;
+                    best.tt = tt;
+                    best.t_blocks = t_blocks;
+                    best.slabs = slabs;
+                }
+            }
+    }
     best.part_bytes = best.slabs > 1 ? (size_t)best.slabs * T * row_tiles * 16 * (epilogue == LDK_SWIGLU ? 2 : 1) * 4 : 0;
     return best;
 }

@@ -66,8 +66,9 @@ def test_w4_linear_rows_groups_and_types(T, group, zeros, scales):
     assert _rel(y, x.double() @ W.t()) <= LINEAR
 
 
-@pytest.mark.parametrize("N,K", [(1, 1), (1, 4096), (3, 31), (16, 32), (15, 33), (17, 127), (33, 129), (256, 256), (48, 1000), (1024, 11008), (4100, 520)])
-@pytest.mark.parametrize("T", [1, 5, 20, 100, 300])
+@pytest.mark.parametrize("N,K", [(1, 1), (1, 4096), (3, 31), (16, 32), (15, 33), (17, 127), (33, 129), (256, 256), (48, 1000), (1024, 11008), (4100, 520),
+                                 (8300, 260), (40, 5000), (24, 14336), (24, 14500)])
+@pytest.mark.parametrize("T", [1, 2, 5, 20, 100, 300])
 def test_w4_linear_odd_shapes(T, N, K):
     c, s, z, W = _w4(N, N, K, 64, True, torch.bfloat16)
     x = gen.normal(K, 5, (T, K))
