@@ -106,28 +106,28 @@ __global__ __launch_bounds__(256) void k_kv_summary(const KT *__restrict__ pool,
     uint32_t top = 0;
 #pragma unroll
     for (int e = 0; e < 8; e++) { lo[e] = INFINITY; hi[e] = -INFINITY; }
+    float v[PASSES][8];
 #pragma unroll
-    for (int p = 0; p < PASSES; p++) {
-        const int slot = p * ROWS + lane / LPR;
-        if (slot >= real) continue;
-        float v[8];
-        load8_stream(keys + (int64_t)slot * HD + d, v);
+    for (int p = 0; p < PASSES; p++)      // all in flight; past the last position its key again
+        load8_stream(keys + (int64_t)min(p * ROWS + lane / LPR, real - 1) * HD + d, v[p]);
+#pragma unroll
+    for (int p = 0; p < PASSES; p++)
 #pragma unroll
         for (int e = 0; e < 8; e++) {
-            lo[e] = fminf(lo[e], v[e]);
-            hi[e] = fmaxf(hi[e], v[e]);
-            top = max(top, abs_bits(v[e]));      // compared as bits: a NaN stays
+            lo[e] = fminf(lo[e], v[p][e]);
+            hi[e] = fmaxf(hi[e], v[p][e]);
+            top = max(top, abs_bits(v[p][e]));      // compared as bits: a NaN stays
         }
+    top = wave_max(top);
+#pragma unroll
+    for (int e = 0; e < 8; e++) {      // over the lanes of the same dimensions
+        if (LPR == 8) {
+            lo[e] = fminf(lo[e], row_rotate<8>(lo[e]));
+            hi[e] = fmaxf(hi[e], row_rotate<8>(hi[e]));
+        }
+        lo[e] = across_rows(lo[e], [](float a, float b) { return fminf(a, b); });
+        hi[e] = across_rows(hi[e], [](float a, float b) { return fmaxf(a, b); });
     }
-#pragma unroll
-    for (int off = 1; off < 64; off <<= 1) top = max(top, (uint32_t)__shfl_xor((int)top, off, WAVE));
-#pragma unroll
-    for (int off = LPR; off < 64; off <<= 1)
-#pragma unroll
-        for (int e = 0; e < 8; e++) {
-            lo[e] = fminf(lo[e], __shfl_xor(lo[e], off, WAVE));
-            hi[e] = fmaxf(hi[e], __shfl_xor(hi[e], off, WAVE));
-        }
     const int64_t at = (int64_t)phys * Hkv + kvh;
     const bool finite = top < INF_BITS;
     const int ue = finite ? unit_exponent(top) : 0;
