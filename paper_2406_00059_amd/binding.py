@@ -657,7 +657,7 @@ class KV:
 
     def __init__(self, model: Model, n_blocks, max_tokens, max_seqs, max_blocks_per_seq, device="cuda", pool=None):
         self.model = model
-        self.n_blocks, self.max_blocks = n_blocks, max_blocks_per_seq
+        self.n_blocks, self.max_seqs, self.max_blocks = n_blocks, max_seqs, max_blocks_per_seq
         sh = model.shape
         pdtype = torch.bfloat16 if sh.dtype == "bf16" else torch.float32
         nbytes = ld_kv_bytes(model.h, n_blocks)
