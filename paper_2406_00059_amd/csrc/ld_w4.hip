@@ -16,18 +16,14 @@
 // after the other along K: a wave streams consecutive kilobytes.  Word j of lane l holds the columns 32 j + 8 (l / 16)
 // .. + 8 of row l % 16, column e of the eight in nibble e / 2 + 4 (e % 2).  Behind the codes the scales
 // [row tile][group][16], then (optional) the zero points, one byte each, likewise.
-#include "ld_w4.h"
-#include "ld_device.h"
+#include "ld_w4_device.h"
 
 #include <algorithm>
 
 using namespace ldd;
+using namespace ldw;
 
 namespace {
-
-typedef __attribute__((ext_vector_type(8))) _Float16 f16x8;
-typedef __attribute__((ext_vector_type(4))) float f32x4;
-typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;
 
 inline ld_status launched(const char *what) {
     hipError_t e = hipGetLastError();
@@ -123,36 +119,6 @@ __global__ __launch_bounds__(256) void k_w4_quantize(const WT *__restrict__ W, i
 // each in lane order ([row tile][k / 32][term][lane][8]).  sums [row tile][group][term][16]: 2^-24 times the sums of a group's
 // columns (those of hi are exact).  expo[t]: the exponent that takes a finished sum back, or W4_NOT_FINITE.
 
-// Sum over 8, 16 or 32 neighbouring lanes, maximum over 32, in all of them: exchanges within the row of 16 lanes, then of whole rows.
-template <int CTRL> __device__ __forceinline__ float dpp(float v) {
-    return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), CTRL, 0xf, 0xf, false));
-}
-template <typename F> __device__ __forceinline__ float other_row(float v, F f) {
-    const auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-    return f(__uint_as_float(a[0]), __uint_as_float(a[1]));
-}
-__device__ __forceinline__ float lanes_sum(float v, int lanes) {
-    v += dpp<0xb1>(v);       // quads: 1 0 3 2
-    v += dpp<0x4e>(v);       // quads: 2 3 0 1
-    v += dpp<0x141>(v);      // mirrored halves of a row
-    if (lanes > 8) v += dpp<0x140>(v);      // mirrored rows
-    if (lanes > 16) v = other_row(v, [](float a, float b) { return a + b; });
-    return v;
-}
-__device__ __forceinline__ float max_of_32(float v) {
-    v = fmaxf(v, dpp<0xb1>(v));
-    v = fmaxf(v, dpp<0x4e>(v));
-    v = fmaxf(v, dpp<0x141>(v));
-    v = fmaxf(v, dpp<0x140>(v));
-    return other_row(v, [](float a, float b) { return fmaxf(a, b); });
-}
-
-// The other half's value, for one that is the same in the 32 lanes of each.
-__device__ __forceinline__ float swapped_half(float v) {
-    const auto a = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-    return threadIdx.x & 32 ? __uint_as_float(a[0]) : __uint_as_float(a[1]);
-}
-
 // One row by a workgroup of THREADS threads: a thread takes four columns at a time, NC times, and keeps them (NC = 0: longer rows, read
 // twice).  put(c, hi, lo): columns c .. c + 3 as fp16; put_sums(group, hi, lo), by one thread each.  Returns the row's exponent.
 template <int THREADS, int NC>
@@ -223,32 +189,12 @@ struct SplitRow {
         const float inv = gain ? 1.f / sqrtf(ss / K + eps) : 1.f;
         const float m = __uint_as_float(top) * inv;
         const bool finite = m < INFINITY;      // false for NaN
-        const int k = finite && m > 0.f ? 14 - ilogbf(m) : 0;
+        const int k = row_exponent(m);
         auto part = [&](int c, const f32x4 &raw, const f32x4 &g) {
-            float v[4], sum_hi = 0.f, sum_lo = 0.f, most = 0.f;
-            union { _Float16 h[4]; uint2 u; } hi, lo;
+            float v[4];
 #pragma unroll
-            for (int e = 0; e < 4; e++) {
-                v[e] = ldexpf(finite ? raw[e] * inv * g[e] : 0.f, k);      // in the order of the definition: x / rms, then the gain
-                most = fmaxf(most, fabsf(v[e]));
-            }
-            most = max_of_32(most);      // 128 columns
-            // quantum: 2^-12 of the power of two at or below the largest magnitude, as its bits; at least fp16's least subnormal
-            const float quantum = __uint_as_float(max((int)(__float_as_uint(most) & 0x7f800000u) - (12 << 23), (127 - 24) << 23));
-            const float per_quantum = __uint_as_float((254u << 23) - __float_as_uint(quantum));      // its reciprocal
-#pragma unroll
-            for (int e = 0; e < 4; e++) {
-                const float h = (float)(_Float16)(rintf(v[e] * per_quantum) * quantum);
-                const float f = e < 2 ? 1.f : 0.0625f;      // e >= 2: codes in bits 4 .. 7 (c is a multiple of 4)
-                hi.h[e] = (_Float16)(h * f);
-                lo.h[e] = (_Float16)((v[e] - h) * f);
-                sum_hi += h;
-                sum_lo += v[e] - h;
-            }
-            put(c, hi.u, lo.u);
-            sum_hi = lanes_sum(sum_hi, G / 4);
-            sum_lo = lanes_sum(sum_lo, G / 4);
-            if (c % G == 0) put_sums(c / G, ldexpf(sum_hi, -24), ldexpf(sum_lo, -24));
+            for (int e = 0; e < 4; e++) v[e] = finite ? raw[e] * inv * g[e] : 0.f;      // in the order of the definition: x / rms, then the gain
+            split4(v, k, c, G, put, put_sums);
         };
         if constexpr (NC > 0) {
 #pragma unroll
@@ -297,38 +243,6 @@ void launch_split(const float *x, const float *g, float eps, int T, int K, int G
 }
 
 // ---------------------------------------------------------------- the product, few rows
-
-__device__ __forceinline__ f16x8 codes_as_f16(uint32_t w) {
-    const uint32_t s = w >> 8;
-    return __builtin_bit_cast(f16x8, (u32x4){w & 0x000f000fu, w & 0x00f000f0u, s & 0x000f000fu, s & 0x00f000f0u});
-}
-
-// What a wave reads of a tile of 16 rows x 128 columns: its codes, the scales of its lanes' four rows, the zero points.
-template <int PER, typename ST>
-struct CodeTile {
-    u32x4 code;
-    uint32_t scale[PER][sizeof(ST)], zero[PER];
-    __device__ __forceinline__ void load(const ld::W4Image &w, int64_t tile, int kt, int lane) {
-        code = load_stream16(w.codes + ((tile * w.k_tiles + kt) * 64 + lane) * 4);
-#pragma unroll
-        for (int p = 0; p < PER; p++) {
-            const int64_t at = (tile * w.groups + (int64_t)kt * PER + p) * 16 + 4 * (lane >> 4);
-            if constexpr (sizeof(ST) == 2) {
-                const uint2 v = *reinterpret_cast<const uint2 *>((const bf16_t *)w.scales + at);
-                scale[p][0] = v.x; scale[p][1] = v.y;
-            } else {
-                const uint4 v = *reinterpret_cast<const uint4 *>((const float *)w.scales + at);
-                scale[p][0] = v.x; scale[p][1] = v.y; scale[p][2] = v.z; scale[p][3] = v.w;
-            }
-            zero[p] = w.zeros ? *reinterpret_cast<const uint32_t *>(w.zeros + at) : 0x08080808u;
-        }
-    }
-    __device__ __forceinline__ float s(int p, int e) const {
-        if constexpr (sizeof(ST) == 4) return __uint_as_float(scale[p][e]);
-        else return __uint_as_float((e & 1) ? scale[p][e >> 1] & 0xffff0000u : scale[p][e >> 1] << 16);
-    }
-    __device__ __forceinline__ float z(int p, int e) const { return (float)((zero[p] >> (8 * e)) & 255u); }
-};
 
 // One row, or a few short ones.  A workgroup of eight waves splits the rows into LDS by itself, while its first codes are on their way; a launch
 // ahead would take longer than the product.  It takes units of R tiles of 16 output rows (SwiGLU: the gate tile and its up tile), every

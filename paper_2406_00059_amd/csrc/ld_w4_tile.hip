@@ -6,18 +6,14 @@
 // unpacked once per group and meet TT x 2 operands there: 80 vector instructions for TT x 32 matrix instructions.  What a group's sums
 // owe to the zero point 8 enters as the first matrix instruction's addend, so that a group costs 2 vector instructions a
 // value (add, multiply-add with the scale).
-#include "ld_w4.h"
-#include "ld_device.h"
+#include "ld_w4_device.h"
 
 #include <algorithm>
 
 using namespace ldd;
+using namespace ldw;
 
 namespace {
-
-typedef __attribute__((ext_vector_type(8))) _Float16 f16x8;
-typedef __attribute__((ext_vector_type(4))) float f32x4;
-typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;
 
 constexpr int NT = 4;      // tiles of 16 output rows a wave
 
@@ -50,7 +46,8 @@ __global__ __launch_bounds__(256, 2) void k_w4_tile(ld::W4Image w, ld::W4Rows r,
     constexpr int PER = 128 / G, JG = G / 32;
     __shared__ __attribute__((aligned(16))) char sm_x[2][TT * 8192];
     __shared__ float sm_s[2][TT * PER * 32];
-    __shared__ __attribute__((aligned(16))) float sm_w[2][PER][ZEROS ? 2 : 1][256];      // scales, 8 - zero point
+    __shared__ __attribute__((aligned(16))) float sm_w[2][PER][256];      // scales
+    __shared__ __attribute__((aligned(16))) uint8_t sm_z[2][PER][ZEROS ? 256 : 4];      // zero points
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int col = lane & 15, h = lane >> 4;
     const bool pair = epilogue == LDK_SWIGLU;
@@ -102,9 +99,9 @@ __global__ __launch_bounds__(256, 2) void k_w4_tile(ld::W4Image w, ld::W4Rows r,
             if (u * 256 + (int)threadIdx.x < TT * PER * 32) sm_s[stage][u * 256 + threadIdx.x] = v.sum[u];
 #pragma unroll
         for (int p = 0; p < PER; p++) {
-            if constexpr (sizeof(ST) == 2) sm_w[stage][p][0][threadIdx.x] = bf16_to_f32(v.scale[p]);
-            else sm_w[stage][p][0][threadIdx.x] = v.scale[p];
-            if constexpr (ZEROS) sm_w[stage][p][ZEROS][threadIdx.x] = 8.f - (float)v.zero[p];
+            if constexpr (sizeof(ST) == 2) sm_w[stage][p][threadIdx.x] = bf16_to_f32(v.scale[p]);
+            else sm_w[stage][p][threadIdx.x] = v.scale[p];
+            if constexpr (ZEROS) sm_z[stage][p][threadIdx.x] = v.zero[p];
         }
     };
     auto load_codes = [&](int kt, u32x4 (&c)[NT]) {
@@ -145,8 +142,12 @@ __global__ __launch_bounds__(256, 2) void k_w4_tile(ld::W4Image w, ld::W4Rows r,
             f32x4 sc[NT], sz[NT];
 #pragma unroll
             for (int i = 0; i < NT; i++) {
-                sc[i] = *reinterpret_cast<const f32x4 *>(&sm_w[stage][p][0][(wave * NT + i) * 16 + 4 * h]);
-                if constexpr (ZEROS) sz[i] = *reinterpret_cast<const f32x4 *>(&sm_w[stage][p][ZEROS][(wave * NT + i) * 16 + 4 * h]);
+                sc[i] = *reinterpret_cast<const f32x4 *>(&sm_w[stage][p][(wave * NT + i) * 16 + 4 * h]);
+                if constexpr (ZEROS) {
+                    const uint32_t z = *reinterpret_cast<const uint32_t *>(&sm_z[stage][p][(wave * NT + i) * 16 + 4 * h]);
+#pragma unroll
+                    for (int e = 0; e < 4; e++) sz[i][e] = 8.f - (float)(z >> 8 * e & 255);
+                }
             }
 #pragma unroll
             for (int t = 0; t < TT; t++) {
