@@ -193,7 +193,7 @@ ld_status ldk_w4_quantize(const void *W, int32_t dtype, int32_t N, int32_t K, in
                           int32_t zeros, void *image, size_t image_bytes, void *stream);
 
 /* ldk_linear on such an image (same epilogues, same optional RMS normalisation of the input; the image's parts follow
- * from the epilogue).  x [T, K], y [T, N] dense row-major float32.  The codes are exact in the products; the
+ * from the epilogue).  x [T, K], y [T, N] dense row-major float32, which do not overlap.  The codes are exact in the products; the
  * activations enter as two fp16 terms of a row scaled by a power of two (22 significant bits), sums are float32.
  * A row of x that holds a NaN or an infinity (after the normalisation) gives NaN in all of its outputs; no other row is touched by it.
  * scratch: ldk_linear_w4_scratch_bytes(T, N, K, epilogue) bytes, 16-byte aligned, needed at every T; a buffer for more rows serves fewer. */

@@ -11,6 +11,7 @@
 // exponents were 2.4e-6 off, relative 2-norm).  lo is what is left, rounded to fp16: at worst 2^-23 of the 128 columns' maximum
 // gets lost, 2^-25 for columns below a quarter of it.  The two terms meet the same codes in accumulators of their own.
 // Per group of G columns:  total[n] += s[n] (sum_k c hi + sum_k c lo - z[n] sum_k x), the sums of x formed with the split.
+// (The products of many rows with narrow groups take c - 8 in place of the subnormals, see ld_w4_tile.hip; the exactness of hi is the same.)
 //
 // Image of a matrix: tiles of 16 rows x 128 columns, 1 KB each, lane l's 16 bytes in a row, the tiles of 16 rows one
 // after the other along K: a wave streams consecutive kilobytes.  Word j of lane l holds the columns 32 j + 8 (l / 16)
@@ -160,7 +161,7 @@ struct SplitRow {
             }
         }
     }
-    template <typename Put, typename Sums>
+    template <bool SUBNORMAL, typename Put, typename Sums>
     __device__ __forceinline__ int split(float eps, int Kp, int G, Room &sm, Put put, Sums put_sums) {
         float ss = 0.f;
         uint32_t top = 0;      // largest |x gain|, compared as bits: a NaN stays
@@ -194,7 +195,7 @@ struct SplitRow {
             float v[4];
 #pragma unroll
             for (int e = 0; e < 4; e++) v[e] = finite ? raw[e] * inv * g[e] : 0.f;      // in the order of the definition: x / rms, then the gain
-            split4(v, k, c, G, put, put_sums);
+            split4<SUBNORMAL>(v, k, c, G, put, put_sums);
         };
         if constexpr (NC > 0) {
 #pragma unroll
@@ -203,13 +204,13 @@ struct SplitRow {
         } else {
             for (int c = threadIdx.x * 4; c < Kp; c += STEP) part(c, value(c), gain_at(c));
         }
-        return finite ? 24 - k : ld::W4_NOT_FINITE;
+        return finite ? (SUBNORMAL ? 24 : 0) - k : ld::W4_NOT_FINITE;
     }
 };
 
 // The activations of a product of many rows, a workgroup a row.
 constexpr int SPLIT_THREADS = 512;
-template <int NC>
+template <int NC, bool SUBNORMAL>
 __global__ __launch_bounds__(SPLIT_THREADS) void k_w4_split(const float *__restrict__ x, const float *__restrict__ gain, float eps, int T, int K, int G,
                                                             ld::W4Rows r) {
     // the 16 rows of a tile fill the same lines of the image: they go to one XCD (workgroups take turns over eight), whose L2 puts the lines together
@@ -219,7 +220,7 @@ __global__ __launch_bounds__(SPLIT_THREADS) void k_w4_split(const float *__restr
     SplitRow<SPLIT_THREADS, NC> row;
     row.load(x + (int64_t)t * K, gain, K, K % 4 == 0 && (((uintptr_t)x | (uintptr_t)gain) & 15) == 0);
     const int Kp = r.k_tiles * 128, rt = t >> 4, col = t & 15, groups = Kp / G;
-    const int expo = row.split(
+    const int expo = row.template split<SUBNORMAL>(
         eps, Kp, G, sm,
         [&](int c, uint2 hi, uint2 lo) {
             const int kb = c >> 5, slot = col + 16 * ((c & 31) >> 3), half = (c & 7) * 2;      // half: bytes into the lane's 16
@@ -237,9 +238,15 @@ __global__ __launch_bounds__(SPLIT_THREADS) void k_w4_split(const float *__restr
 
 void launch_split(const float *x, const float *g, float eps, int T, int K, int G, const ld::W4Rows &r, hipStream_t s) {
     const dim3 grid((T + 127) / 128 * 128), block(SPLIT_THREADS);
-    if (K <= 2 * 2048) LD_LAUNCH(k_w4_split<2>, grid, block, 0, s, x, g, eps, T, K, G, r);
-    else if (K <= 7 * 2048) LD_LAUNCH(k_w4_split<7>, grid, block, 0, s, x, g, eps, T, K, G, r);
-    else LD_LAUNCH(k_w4_split<0>, grid, block, 0, s, x, g, eps, T, K, G, r);
+#define LD_SPLIT(NC_)                                                                                          \
+    do {                                                                                                       \
+        if (ld::w4_subnormal(G)) LD_LAUNCH((k_w4_split<NC_, true>), grid, block, 0, s, x, g, eps, T, K, G, r); \
+        else LD_LAUNCH((k_w4_split<NC_, false>), grid, block, 0, s, x, g, eps, T, K, G, r);                    \
+    } while (0)
+    if (K <= 2 * 2048) LD_SPLIT(2);
+    else if (K <= 7 * 2048) LD_SPLIT(7);
+    else LD_SPLIT(0);
+#undef LD_SPLIT
 }
 
 // ---------------------------------------------------------------- the product, few rows
@@ -286,7 +293,7 @@ __global__ __launch_bounds__(512, 4) void k_w4_rows(ld::W4Image w, const float *
         } else {
             lds_barrier();      // everyone has read the room
         }
-        const int e = row.split(
+        const int e = row.template split<true>(
             eps, Kp, G, room,
             [&](int c, uint2 hi, uint2 lo) {
                 *reinterpret_cast<uint2 *>(sm_rows + 2 * t * stride + c * 2) = hi;
@@ -311,7 +318,7 @@ __global__ __launch_bounds__(512, 4) void k_w4_rows(ld::W4Image w, const float *
             for (int j = p * (G / 32); j < (p + 1) * (G / 32); j++) {
                 const f16x8 b = *reinterpret_cast<const f16x8 *>(operand + kt * 256 + 64 * j);
 #pragma unroll
-                for (int i = 0; i < R; i++) acc[i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(codes_as_f16(q[i].code[j]), b, acc[i], 0, 0, 0);
+                for (int i = 0; i < R; i++) acc[i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(codes_as_subnormals(q[i].code[j]), b, acc[i], 0, 0, 0);
             }
             const float sum = my_sums[2 * (kt * PER + p)];
 #pragma unroll

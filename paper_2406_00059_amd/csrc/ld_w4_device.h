@@ -45,8 +45,9 @@ __device__ __forceinline__ float swapped_half(float v) {
 __device__ __forceinline__ int row_exponent(float m) { return m < INFINITY && m > 0.f ? 14 - ilogbf(m) : 0; }
 
 // Columns c .. c + 3 of a row (c a multiple of 4; the 32 lanes of a half wave hold 128 columns), scaled by 2^k, as two fp16 terms:
-// put(c, hi, lo), and the sums of a group of G columns, 2^-24 times: put_sums(group, hi, lo), by one lane each.
-template <typename Put, typename Sums>
+// put(c, hi, lo), and the sums of a group of G columns: put_sums(group, hi, lo), by one lane each.  SUBNORMAL: for codes_as_subnormals, the sums
+// 2^-24 times as large.
+template <bool SUBNORMAL, typename Put, typename Sums>
 __device__ __forceinline__ void split4(float (&v)[4], int k, int c, int G, Put put, Sums put_sums) {
     float sum_hi = 0.f, sum_lo = 0.f, most = 0.f;
     union { _Float16 h[4]; uint2 u; } hi, lo;
@@ -62,7 +63,7 @@ __device__ __forceinline__ void split4(float (&v)[4], int k, int c, int G, Put p
 #pragma unroll
     for (int e = 0; e < 4; e++) {
         const float h = (float)(_Float16)(rintf(v[e] * per_quantum) * quantum);
-        const float f = e < 2 ? 1.f : 0.0625f;      // e >= 2: codes in bits 4 .. 7
+        const float f = SUBNORMAL && e >= 2 ? 0.0625f : 1.f;      // e >= 2: codes in bits 4 .. 7
         hi.h[e] = (_Float16)(h * f);
         lo.h[e] = (_Float16)((v[e] - h) * f);
         sum_hi += h;
@@ -71,12 +72,32 @@ __device__ __forceinline__ void split4(float (&v)[4], int k, int c, int G, Put p
     put(c, hi.u, lo.u);
     sum_hi = lanes_sum(sum_hi, G / 4);
     sum_lo = lanes_sum(sum_lo, G / 4);
-    if (c % G == 0) put_sums(c / G, ldexpf(sum_hi, -24), ldexpf(sum_lo, -24));
+    if (c % G == 0) put_sums(c / G, SUBNORMAL ? ldexpf(sum_hi, -24) : sum_hi, SUBNORMAL ? ldexpf(sum_lo, -24) : sum_lo);
 }
 
-__device__ __forceinline__ f16x8 codes_as_f16(uint32_t w) {
+// A word's codes as eight fp16 operands: 2^-24 c and 2^-20 c, a mask each ..
+__device__ __forceinline__ f16x8 codes_as_subnormals(uint32_t w) {
     const uint32_t s = w >> 8;
     return __builtin_bit_cast(f16x8, (u32x4){w & 0x000f000fu, w & 0x00f000f0u, s & 0x000f000fu, s & 0x00f000f0u});
+}
+// .. and c - 8, under the exponents of 1024 + c and 1024 + 16 c.
+__device__ __forceinline__ f16x8 codes_less_8(uint32_t w) {
+    typedef __attribute__((ext_vector_type(2))) _Float16 f16x2;
+    const uint32_t s = w >> 8, one = 0x64006400u;
+    auto low = [](uint32_t v) { return __builtin_bit_cast(uint32_t, __builtin_bit_cast(f16x2, v) - (f16x2){1032.f16, 1032.f16}); };
+    auto high = [](uint32_t v) {
+        return __builtin_bit_cast(uint32_t, __builtin_elementwise_fma(__builtin_bit_cast(f16x2, v), (f16x2){0.0625f16, 0.0625f16}, (f16x2){-72.f16, -72.f16}));
+    };
+    auto pick = [&](uint32_t v, uint32_t mask) {      // in one instruction, which takes one scalar operand
+        uint32_t r;
+#if defined(__HIP_DEVICE_COMPILE__)
+        asm("v_and_or_b32 %0, %1, %2, %3" : "=v"(r) : "v"(v), "s"(mask), "v"(one));
+#else
+        r = (v & mask) | one;
+#endif
+        return r;
+    };
+    return __builtin_bit_cast(f16x8, (u32x4){low(pick(w, 0x000f000fu)), high(pick(w, 0x00f000f0u)), low(pick(s, 0x000f000fu)), high(pick(s, 0x00f000f0u))});
 }
 
 // What a wave reads of a tile of 16 rows x 128 columns: its codes, the scales of its lanes' four rows, the zero points.

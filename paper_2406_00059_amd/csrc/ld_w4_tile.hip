@@ -3,9 +3,14 @@
 // A workgroup of four waves multiplies 16 tiles of 16 output rows (SwiGLU: 8 gate tiles and their up tiles) with 16 TT activation
 // rows, a wave 4 tiles with all of them.  The activations of 128 columns (8 KB per 16 rows, both terms) are copied straight into
 // LDS in operand order, two stages, and every wave reads them all; codes go from memory into registers, a column tile ahead, are
-// unpacked once per group and meet TT x 2 operands there: 80 vector instructions for TT x 32 matrix instructions.  What a group's sums
-// owe to the zero point 8 enters as the first matrix instruction's addend, so that a group costs 2 vector instructions a
-// value (add, multiply-add with the scale).
+// unpacked once per group and meet TT x 2 operands there.
+// Groups of 128 take the codes as subnormals: 80 vector instructions for TT x 32 matrix instructions; what a group's sums owe to the zero
+// point 8 enters as the first matrix instruction's addend, and a group costs 2 vector instructions a value (add, multiply-add with the scale).
+// Groups of 32 and 64 have that cost four and two times as often, and vector and matrix instructions take turns on a SIMD rather than
+// run at the same time (counters, groups of 32: 86 k cycles of the one, 50 k of the other, in 141 k).  They take c - 8 (64 instructions more a column
+// tile) and add the lo products to the exact sum of the hi products: 1 vector instruction a value, no addend to prepare.
+// At 1056 rows the matrix cores run at what a large library product reaches: 13B gate/up (2 x 13824 x 5120, groups of 128) 500 us, 598 TFLOP/s
+// of the product, two terms executed: 1196 (library, fp16: 1173).  4096 x 11008, groups of 32, 257 rows: 72 us, vector instructions first.
 #include "ld_w4_device.h"
 
 #include <algorithm>
@@ -44,8 +49,9 @@ template <int TT, int G, bool ZEROS, typename ST>
 __global__ __launch_bounds__(256, 2) void k_w4_tile(ld::W4Image w, ld::W4Rows r, int T, int N, int epilogue, int n_blocks, int t_blocks, int slabs,
                                                     float *__restrict__ y, float *__restrict__ part) {
     constexpr int PER = 128 / G, JG = G / 32;
+    constexpr bool SUBNORMAL = ld::w4_subnormal(G), SUMMED = SUBNORMAL || ZEROS;      // SUMMED: the sums of the activations are needed
     __shared__ __attribute__((aligned(16))) char sm_x[2][TT * 8192];
-    __shared__ float sm_s[2][TT * PER * 32];
+    __shared__ float sm_s[2][SUMMED ? TT * PER * 32 : 1];
     __shared__ __attribute__((aligned(16))) float sm_w[2][PER][256];      // scales
     __shared__ __attribute__((aligned(16))) uint8_t sm_z[2][PER][ZEROS ? 256 : 4];      // zero points
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -74,8 +80,8 @@ __global__ __launch_bounds__(256, 2) void k_w4_tile(ld::W4Image w, ld::W4Rows r,
     };
     // What belongs to a column tile beside codes and operands goes through LDS: the sums of the activations, and the scales (and zero points)
     // of 256 output rows, a row a thread.  Nothing else is loaded inside a tile's products, so that no wait there drains the copies.
-    constexpr int SUMS = (TT * PER * 32 + 255) / 256;
-    struct Small { float sum[SUMS]; ST scale[PER]; uint8_t zero[PER]; };
+    constexpr int SUMS = SUMMED ? (TT * PER * 32 + 255) / 256 : 0;
+    struct Small { float sum[SUMS ? SUMS : 1]; ST scale[PER]; uint8_t zero[PER]; };
     const int my = threadIdx.x >> 4;      // row tile of the workgroup's 16: wave my / 4, its tile my % 4
     const int64_t my_tile = pair ? (int64_t)((my & 3) >= 2 ? w.row_tiles : 0) + min(nb * 8 + (my >> 2) * 2 + (my & 1), w.row_tiles - 1)
                                  : min(nb * 16 + my, w.row_tiles - 1);
@@ -135,10 +141,7 @@ __global__ __launch_bounds__(256, 2) void k_w4_tile(ld::W4Image w, ld::W4Rows r,
 #pragma unroll
             for (int i = 0; i < NT; i++)
 #pragma unroll
-                for (int j = 0; j < JG; j++) {
-                    const uint32_t v = code[i][p * JG + j], u = v >> 8;
-                    a[i][j] = __builtin_bit_cast(f16x8, (u32x4){v & 0x000f000fu, v & 0x00f000f0u, u & 0x000f000fu, u & 0x00f000f0u});
-                }
+                for (int j = 0; j < JG; j++) a[i][j] = SUBNORMAL ? codes_as_subnormals(code[i][p * JG + j]) : codes_less_8(code[i][p * JG + j]);
             f32x4 sc[NT], sz[NT];
 #pragma unroll
             for (int i = 0; i < NT; i++) {
@@ -151,30 +154,51 @@ __global__ __launch_bounds__(256, 2) void k_w4_tile(ld::W4Image w, ld::W4Rows r,
             }
 #pragma unroll
             for (int t = 0; t < TT; t++) {
-                const float s_hi = sm_s[stage][(t * PER + p) * 32 + col], s_lo = sm_s[stage][(t * PER + p) * 32 + 16 + col];
-                const float c_hi = -8.f * s_hi, c_lo = -8.f * s_lo;
-                f32x4 hi[NT], lo[NT];
-#pragma unroll
-                for (int i = 0; i < NT; i++) {
-                    hi[i] = (f32x4){c_hi, c_hi, c_hi, c_hi};
-                    lo[i] = (f32x4){c_lo, c_lo, c_lo, c_lo};
+                float s_hi = 0.f, s_lo = 0.f;
+                if constexpr (SUMMED) {
+                    s_hi = sm_s[stage][(t * PER + p) * 32 + col];
+                    s_lo = sm_s[stage][(t * PER + p) * 32 + 16 + col];
                 }
+                auto operand = [&](int j, int term) {
+                    return *reinterpret_cast<const f16x8 *>(sm_x[stage] + (t * 4 + p * JG + j) * 2048 + term * 1024 + lane * 16);
+                };
+                f32x4 d[NT];
+                if constexpr (SUBNORMAL) {
+                    const float c_hi = -8.f * s_hi, c_lo = -8.f * s_lo;      // what the sums owe to the zero point 8
+                    f32x4 lo[NT];
 #pragma unroll
-                for (int j = 0; j < JG; j++) {
-                    const char *q = sm_x[stage] + (t * 4 + p * JG + j) * 2048 + lane * 16;
-                    const f16x8 bh = *reinterpret_cast<const f16x8 *>(q), bl = *reinterpret_cast<const f16x8 *>(q + 1024);
+                    for (int i = 0; i < NT; i++) {
+                        d[i] = (f32x4){c_hi, c_hi, c_hi, c_hi};
+                        lo[i] = (f32x4){c_lo, c_lo, c_lo, c_lo};
+                    }
 #pragma unroll
-                    for (int i = 0; i < NT; i++) hi[i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(a[i][j], bh, hi[i], 0, 0, 0);
+                    for (int j = 0; j < JG; j++) {
+                        const f16x8 bh = operand(j, 0), bl = operand(j, 1);
 #pragma unroll
-                    for (int i = 0; i < NT; i++) lo[i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(a[i][j], bl, lo[i], 0, 0, 0);
+                        for (int i = 0; i < NT; i++) d[i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(a[i][j], bh, d[i], 0, 0, 0);
+#pragma unroll
+                        for (int i = 0; i < NT; i++) lo[i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(a[i][j], bl, lo[i], 0, 0, 0);
+                    }
+#pragma unroll
+                    for (int i = 0; i < NT; i++) d[i] += lo[i];
+                } else {
+#pragma unroll
+                    for (int i = 0; i < NT; i++) d[i] = (f32x4){0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                    for (int term = 0; term < 2; term++)      // all hi products first: their sum is exact, the lo products are added to it
+#pragma unroll
+                        for (int j = 0; j < JG; j++) {
+                            const f16x8 b = operand(j, term);
+#pragma unroll
+                            for (int i = 0; i < NT; i++) d[i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(a[i][j], b, d[i], 0, 0, 0);
+                        }
                 }
 #pragma unroll
                 for (int i = 0; i < NT; i++)
 #pragma unroll
                     for (int e = 0; e < 4; e++) {
-                        float d = hi[i][e] + lo[i][e];
-                        if constexpr (ZEROS) d += sz[i][e] * (s_hi + s_lo);
-                        total[i][t][e] += sc[i][e] * d;
+                        if constexpr (ZEROS) d[i][e] += sz[i][e] * (s_hi + s_lo);
+                        total[i][t][e] += sc[i][e] * d[i][e];
                     }
             }
         }
@@ -207,7 +231,7 @@ __global__ __launch_bounds__(256, 2) void k_w4_tile(ld::W4Image w, ld::W4Rows r,
                 out[e] = ld::w4_finish(total[i][t][e], expo);
                 if (pair) out[e] = ld::w4_gated(out[e], ld::w4_finish(total[(i + 2) % NT][t][e], expo));
             }
-            if (n + 4 <= N && N % 4 == 0) {
+            if (n + 4 <= N && N % 4 == 0 && !((uintptr_t)y & 15)) {
                 float4 v = make_float4(out[0], out[1], out[2], out[3]);
                 if (epilogue == LDK_ADD) {
                     const float4 o = *reinterpret_cast<const float4 *>(dst);
