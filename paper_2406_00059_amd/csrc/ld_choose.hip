@@ -3,8 +3,8 @@
 // A workgroup takes a slice of one row's vocabulary.  It counts the history's tokens that lie in the slice in LDS (integer
 // atomics, whose order cannot matter) and notes the last bias entry of each token, walks the slice's logits once, and leaves
 // its best token; a second launch joins the slices.  No count table outlives a call: a sequence that is forked, swapped or
-// rolled back needs nothing but its token history.  Bound by latency at few rows (the chain of loads, the launch behind), by the noise's
-// arithmetic where rows are sampled and by the logits' bytes at many rows.
+// rolled back needs nothing but its token history.  Bound by latency at few rows (the chain of loads, the launch behind: one row of 32000 5.9 + 2 us
+// in the two kernels), by the noise's arithmetic and the histories where many rows are sampled (32 rows, histories of 512 to 8192 tokens: 13.2 us).
 #include "ld_device.h"
 
 #include <algorithm>

@@ -33,7 +33,7 @@ __device__ __forceinline__ void copy_kb(const char *src, char *dst, int lane) {
 // Workgroups go to the 8 XCDs in turn.  An XCD takes whole columns of the grid, all rows' blocks of an output block one after
 // the other: its 64 workgroups stand at much the same place along K, and its 4 MB of L2 hold what they share there (the codes of some three
 // output blocks and the activations of all rows), so that codes leave the memory once and not once a row block.  13B gate/up of 1056 rows:
-// 632 us without it.
+// 505 us, 632 with workgroups in the grid's order.
 __device__ __forceinline__ void block_of(int id, int n_blocks, int t_blocks, int &nb, int &tb) {
     const int whole = n_blocks / 8 * 8;
     if (id < whole * t_blocks) {
@@ -246,7 +246,7 @@ __global__ __launch_bounds__(256, 2) void k_w4_tile(ld::W4Image w, ld::W4Rows r,
     }
 }
 
-// The slabs' sums added in their order, then the epilogue.  A thread four outputs of a row.
+// The slabs' sums added in their order, then the epilogue.  A thread four outputs of a row.  16 slabs of 32 x 6144 sums (12.6 MB): 4.3 us.
 __global__ __launch_bounds__(256) void k_w4_join(const float *__restrict__ part, const int32_t *__restrict__ expo, int T, int N, int np, int slabs,
                                                  int epilogue, float *__restrict__ y) {
     const int quads = np / 4;

@@ -68,7 +68,7 @@ class LightDecoder:
         self.penalties = None if penalties is None else torch.tensor([penalties] * T, **f)
 
     def _i32(self, v):
-        return torch.as_tensor(np.ascontiguousarray(v, dtype=np.int32)).to(self.device, non_blocking=True)
+        return torch.as_tensor(np.ascontiguousarray(v, dtype=np.int32)).to(self.device)
 
     def _map(self, seq, n_tokens):
         """Maps the next n_tokens positions of a sequence and brings the device's copy of its block table up to date."""

@@ -583,3 +583,72 @@ def test_choose_adjusts_in_place():
     token, scratch = torch.empty(R, dtype=torch.int32, device=DEV), torch.empty(ld.ldk_choose_scratch_bytes(R, V), dtype=torch.uint8, device=DEV)
     ld.ldk_choose(logits, token, adjusted=logits, scratch=scratch, **k)
     assert torch.equal(logits.cpu(), adj) and torch.equal(token.cpu(), tok)
+
+
+# ---------------------------------------------------------------- all of them
+
+@pytest.mark.parametrize("T", [1, 2, 20, 200])
+def test_w4_rows_and_outputs_at_odd_addresses(T):
+    """Rows, gain and outputs that start 4 bytes past a 16-byte boundary give the same bits as aligned ones."""
+    N, K, group = 64, 512, 32
+    c, s, z, W = _w4(81, N, K, group, False, torch.bfloat16)
+    w = _packed(c, s, z, N, K, group)
+    x, g = gen.normal(81, 5, (T, K)).to(DEV), gen.normal(81, 6, (K,), std=0.1, mean=1.0).to(DEV)
+
+    def odd(t):
+        v = torch.empty(t.numel() + 1, device=DEV)[1:].view(t.shape)
+        v.copy_(t)
+        return v
+    want = _linear(w, x, g=g)
+    y = odd(torch.zeros((T, N), device=DEV))
+    _linear(w, odd(x), g=odd(g), y=y)
+    assert torch.equal(y, want)
+
+
+@pytest.mark.parametrize("T,H,Hkv,blocks", [(1, 4, 2, 40), (20, 16, 16, 20), (1, 8, 2, 700)], ids=["one-launch", "many-pairs", "two-launches"])
+def test_a_recorded_step_replays_like_the_calls(T, H, Hkv, blocks):
+    """A projection, bounds, attention, a projection and the choice in a graph: every replay, with new inputs and other work between, is the
+    eager calls' result bit for bit."""
+    hd, K, V, budget = 128, 256, 3000, 8
+    ctx = blocks * 16 - 5
+    perm = gen.permutation(91, 1, T * blocks).view(T, blocks).int().to(DEV)
+    pool = device_pool(gen.normal(91, 2, (T * blocks, 2, Hkv, 16, hd)).to(torch.bfloat16)).to(DEV)
+    wq = ld.W4Matrix.quantize(gen.normal(91, 3, (H * hd, K)).to(torch.bfloat16).to(DEV), 64)
+    wo = ld.W4Matrix.quantize(gen.normal(91, 4, (V, H * hd)).to(torch.bfloat16).to(DEV), 128)
+    x, q, att = torch.empty((T, K), device=DEV), torch.empty((T, H * hd), device=DEV), torch.empty((T, H, hd), device=DEV)
+    logits, token = torch.empty((T, V), device=DEV), torch.empty(T, dtype=torch.int32, device=DEV)
+    sel = torch.empty((T, Hkv, budget), dtype=torch.int32, device=DEV)
+    bounds, unit = torch.zeros((T * blocks, Hkv, 2, hd), dtype=torch.int8, device=DEV), torch.zeros((T * blocks, Hkv), device=DEV)
+    ranges = torch.tensor([[t, 0, ctx] for t in range(T)], dtype=torch.int32, device=DEV)
+    slot, length = torch.arange(T, dtype=torch.int32, device=DEV), torch.full((T,), ctx, dtype=torch.int32, device=DEV)
+    history = gen.randint(91, 5, 0, V - 1, T * 50).view(T, 50).int().to(DEV)
+    n_hist, pen = torch.full((T,), 50, dtype=torch.int32, device=DEV), torch.tensor([[1.2, 0.1, 0.3]] * T, device=DEV)
+    scratch = torch.empty(max(ld.ldk_linear_w4_scratch_bytes(T, H * hd, K), ld.ldk_linear_w4_scratch_bytes(T, V, H * hd),
+                              ld.ldk_sparse_attention_scratch_bytes(T, H, Hkv, hd, ctx, 0, budget), ld.ldk_choose_scratch_bytes(T, V)),
+                          dtype=torch.uint8, device=DEV)
+
+    def step():
+        ld.ldk_linear_w4(wq, x, q, scratch=scratch)
+        ld.ldk_kv_summary(pool, perm, ranges, ctx, Hkv, hd, bounds, unit)
+        ld.ldk_sparse_attention(q, H * hd, pool, bounds, unit, perm, slot, length, ctx, H, Hkv, hd, budget, 1, 2, att, sel, scratch)
+        ld.ldk_linear_w4(wo, att.view(T, H * hd), logits, scratch=scratch)
+        ld.ldk_choose(logits, token, history=history, history_len=n_hist, penalties=pen, scratch=scratch)
+
+    inputs = [gen.normal(92, i, (T, K)).to(DEV) for i in range(4)]
+    want = []
+    for v in inputs:
+        x.copy_(v)
+        step()
+        want.append([t.clone() for t in (q, bounds, att, sel, logits, token)])
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    for v, w in zip(inputs, want):
+        x.copy_(v)
+        for t in (q, att, logits, token, sel, bounds, scratch):
+            t.fill_(1)
+        graph.replay()
+        torch.cuda.synchronize()
+        for got, t in zip((q, bounds, att, sel, logits, token), w):
+            assert torch.equal(got, t)
