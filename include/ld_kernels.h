@@ -196,7 +196,7 @@ ld_status ldk_w4_quantize(const void *W, int32_t dtype, int32_t N, int32_t K, in
  * from the epilogue).  x [T, K], y [T, N] dense row-major float32, which do not overlap.  The codes are exact in the products; the
  * activations enter as two fp16 terms of a row scaled by a power of two (22 significant bits), sums are float32.
  * A row of x that holds a NaN or an infinity (after the normalisation) gives NaN in all of its outputs; no other row is touched by it.
- * scratch: ldk_linear_w4_scratch_bytes(T, N, K, epilogue) bytes, 16-byte aligned, needed at every T; a buffer for more rows serves fewer. */
+ * scratch: ldk_linear_w4_scratch_bytes(T, N, K, epilogue) bytes, 16-byte aligned, needed at every T (up to 2^20); a buffer for more rows serves fewer. */
 size_t ldk_linear_w4_scratch_bytes(int32_t T, int32_t N, int32_t K, int32_t epilogue);
 ld_status ldk_linear_w4(const void *image, int32_t scale_dtype, int32_t zeros, int32_t group, const float *x, const float *g, float eps,
                         int32_t T, int32_t N, int32_t K, int32_t epilogue, float *y, void *scratch, size_t scratch_bytes, void *stream);
@@ -251,7 +251,7 @@ typedef struct {
 /* Token choice under rules (HOST struct, may be NULL): token[r] = lowest index of the largest adjusted logit or, where temperature[r] > 0, the
  * draw that ldk_sample makes from the adjusted logits (temperature NULL: greedy; seed and pos as there); -1 where every
  * adjusted logit is -infinity or NaN.  adjusted (may be NULL, may be logits itself): the adjusted logits [R, V].
- * scratch: ldk_choose_scratch_bytes(R, V) bytes, 8-byte aligned. */
+ * scratch: ldk_choose_scratch_bytes(R, V) bytes, 8-byte aligned.  R up to 65535, V up to 2^30. */
 size_t ldk_choose_scratch_bytes(int32_t R, int32_t V);
 ld_status ldk_choose(const float *logits, int32_t R, int32_t V, const ld_token_rules *rules, const float *temperature, const uint64_t *seed,
                      const int32_t *pos, float *adjusted, int32_t *token, void *scratch, size_t scratch_bytes, void *stream);

@@ -31,6 +31,7 @@ int slice_tokens(int R, int V) {
 }
 int slices_of(int R, int V) { const int s = slice_tokens(R, V); return (V + s - 1) / s; }
 constexpr uint32_t SEEN = 0x80000000u;
+constexpr int MOST_TOKENS = 1 << 30;
 
 struct Best { float v; int i; };
 // The larger score, the lower index among equal ones; i < 0: nothing yet.
@@ -138,7 +139,7 @@ __global__ __launch_bounds__(64) void k_choose_join(const Best *__restrict__ par
 extern "C" {
 
 size_t ldk_choose_scratch_bytes(int32_t R, int32_t V) {
-    return R > 0 && V > 0 ? (size_t)R * ((V + LEAST - 1) / LEAST) * sizeof(Best) : 0;      // the most slices
+    return R > 0 && V > 0 && V <= MOST_TOKENS ? (size_t)R * ((V + LEAST - 1) / LEAST) * sizeof(Best) : 0;      // the most slices
 }
 
 ld_status ldk_choose(const float *logits, int32_t R, int32_t V, const ld_token_rules *rules, const float *temperature, const uint64_t *seed,
@@ -152,9 +153,9 @@ ld_status ldk_choose(const float *logits, int32_t R, int32_t V, const ld_token_r
         (u.bias && (!u.bias_start || !u.bias_token)) || (u.mask && u.mask_rows <= 0) || (u.mask && !u.mask_row && u.mask_rows < R))
         return ld::fail(LD_E_INVAL, "ldk_choose: bad argument (history comes with history_len and penalties, bias with bias_start and "
                                     "bias_token, mask with mask_rows and, unless it has a row for each of the logits', mask_row)");
+    if (R > 65535 || V > MOST_TOKENS) return ld::fail(LD_E_RANGE, "ldk_choose: more than 65535 rows or 2^30 tokens");
     if (!scratch || ((uintptr_t)scratch & 7) || scratch_bytes < ldk_choose_scratch_bytes(R, V))
         return ld::fail(LD_E_INVAL, "ldk_choose: scratch missing, not 8-byte aligned or too small");
-    if (R > 65535) return ld::fail(LD_E_RANGE, "ldk_choose: more than 65535 rows");
     const int slice = slice_tokens(R, V), slices = slices_of(R, V);
     hipStream_t s = (hipStream_t)stream;
     LD_LAUNCH(k_choose_slice, dim3(slices, R), dim3(THREADS), (size_t)slice * 8, s, logits, V, slice, u, temperature, seed, pos, adjusted, (Best *)scratch);

@@ -393,6 +393,8 @@ void launch_group(const ld::W4Image &w, int scale_dtype, const Few &a, hipStream
 // Rows that a workgroup splits by itself: as many as its threads hold in registers.
 bool few_rows(int T, int K) { return (T == 1 && K <= 7 * 2048) || (T == 2 && K <= 2 * 2048); }
 
+constexpr int MOST_ROWS = 1 << 20;
+
 bool bad_shape(int N, int K, int group, int parts, int scale_dtype) {
     return N <= 0 || K <= 0 || N > (1 << 28) || K > (1 << 28) || (group != 32 && group != 64 && group != 128) || (parts != 1 && parts != 2) ||
            (scale_dtype != LD_BF16 && scale_dtype != LD_F32);
@@ -470,7 +472,7 @@ ld_status ldk_w4_quantize(const void *W, int32_t dtype, int32_t N, int32_t K, in
 }
 
 size_t ldk_linear_w4_scratch_bytes(int32_t T, int32_t N, int32_t K, int32_t epilogue) {
-    if (T <= 0 || N <= 0 || K <= 0) return 0;
+    if (T <= 0 || T > MOST_ROWS || N <= 0 || K <= 0 || N > (1 << 28) || K > (1 << 28)) return 0;
     size_t bytes = 0;
     ld::w4_rows(nullptr, T, K, ld::w4_part_bound(T, N, epilogue), &bytes);
     return bytes;
@@ -482,13 +484,13 @@ ld_status ldk_linear_w4(const void *image, int32_t scale_dtype, int32_t zeros, i
     if (!image || ((uintptr_t)image & 15) || !x || !y || T < 0 || epilogue < 0 || epilogue > 2 ||
         bad_shape(N, K, group, epilogue == LDK_SWIGLU ? 2 : 1, scale_dtype))
         return ld::fail(LD_E_INVAL, "ldk_linear_w4: bad argument (group 32, 64 or 128; image 16-byte aligned)");
+    if (T > MOST_ROWS) return ld::fail(LD_E_RANGE, "ldk_linear_w4: more than 1048576 rows");
     const bool few = few_rows(T, K);
     const ld::W4Plan plan = few ? ld::W4Plan{} : ld::w4_plan(T, N, K, epilogue);
     size_t need = 0;
     ld::w4_rows(nullptr, T, K, plan.part_bytes, &need);
     if (!scratch || ((uintptr_t)scratch & 15) || scratch_bytes < need)
         return ld::fail(LD_E_INVAL, "ldk_linear_w4: scratch missing, not 16-byte aligned or too small");
-    if (T > 1 << 20) return ld::fail(LD_E_RANGE, "ldk_linear_w4: more than 1048576 rows");
     hipStream_t s = (hipStream_t)stream;
     const ld::W4Image w = ld::w4_image(image, N, K, group, epilogue == LDK_SWIGLU ? 2 : 1, scale_dtype, zeros != 0, nullptr);
     const ld::W4Rows r = ld::w4_rows(scratch, T, K, 0, nullptr);

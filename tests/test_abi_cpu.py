@@ -551,3 +551,14 @@ def test_choose_refusals():
     _refused(ld.LD_E_RANGE, "ldk_choose", *call(R=70000, b=1 << 40))
     assert ld.lib().ldk_choose(*call(R=0, l=None)) == ld.LD_OK
     assert ld.ldk_choose_scratch_bytes(0, V) == 0 and ld.ldk_choose_scratch_bytes(R, V) > 0
+
+
+def test_light_operators_refuse_sizes_past_their_range():
+    top = (1 << 31) - 1
+    for T in (1 << 20 | 1, top - 20, top):
+        _refused(ld.LD_E_RANGE, "ldk_linear_w4", FAKE, 1, 0, 64, FAKE, None, 0.0, T, 16, 128, 0, FAKE, FAKE, 1 << 60, None)
+        assert ld.ldk_linear_w4_scratch_bytes(T, 16, 128) == 0
+    assert ld.ldk_linear_w4_scratch_bytes(1 << 20, 16, 128) > 0
+    for V in (1 << 30 | 1, top):
+        _refused(ld.LD_E_RANGE, "ldk_choose", FAKE, 2, V, None, None, None, None, None, FAKE, FAKE, 1 << 60, None)
+        assert ld.ldk_choose_scratch_bytes(2, V) == 0
