@@ -11,7 +11,7 @@
 // exponents were 2.4e-6 off, relative 2-norm).  lo is what is left, rounded to fp16: at worst 2^-23 of the 128 columns' maximum
 // gets lost, 2^-25 for columns below a quarter of it.  The two terms meet the same codes in accumulators of their own.
 // Per group of G columns:  total[n] += s[n] (sum_k c hi + sum_k c lo - z[n] sum_k x), the sums of x formed with the split.
-// (The products of many rows with narrow groups take c - 8 in place of the subnormals, see ld_w4_tile.hip; the exactness of hi is the same.)
+// (The products of many rows with narrow groups take c - z in place of the subnormals, see ld_w4_tile.hip; the exactness of hi is the same.)
 //
 // Image of a matrix: tiles of 16 rows x 128 columns, 1 KB each, lane l's 16 bytes in a row, the tiles of 16 rows one
 // after the other along K: a wave streams consecutive kilobytes.  Word j of lane l holds the columns 32 j + 8 (l / 16)

@@ -80,13 +80,14 @@ __device__ __forceinline__ f16x8 codes_as_subnormals(uint32_t w) {
     const uint32_t s = w >> 8;
     return __builtin_bit_cast(f16x8, (u32x4){w & 0x000f000fu, w & 0x00f000f0u, s & 0x000f000fu, s & 0x00f000f0u});
 }
-// .. and c - 8, under the exponents of 1024 + c and 1024 + 16 c.
-__device__ __forceinline__ f16x8 codes_less_8(uint32_t w) {
+// .. and c - z, under the exponents of 1024 + c and 1024 + 16 c (all steps exact).  z: 1024 + z in both halves.
+__device__ __forceinline__ f16x8 codes_less(uint32_t w, uint32_t z) {
     typedef __attribute__((ext_vector_type(2))) _Float16 f16x2;
     const uint32_t s = w >> 8, one = 0x64006400u;
-    auto low = [](uint32_t v) { return __builtin_bit_cast(uint32_t, __builtin_bit_cast(f16x2, v) - (f16x2){1032.f16, 1032.f16}); };
-    auto high = [](uint32_t v) {
-        return __builtin_bit_cast(uint32_t, __builtin_elementwise_fma(__builtin_bit_cast(f16x2, v), (f16x2){0.0625f16, 0.0625f16}, (f16x2){-72.f16, -72.f16}));
+    const f16x2 z0 = __builtin_bit_cast(f16x2, z), z1 = (f16x2){960.f16, 960.f16} - z0;
+    auto low = [&](uint32_t v) { return __builtin_bit_cast(uint32_t, __builtin_bit_cast(f16x2, v) - z0); };
+    auto high = [&](uint32_t v) {
+        return __builtin_bit_cast(uint32_t, __builtin_elementwise_fma(__builtin_bit_cast(f16x2, v), (f16x2){0.0625f16, 0.0625f16}, z1));
     };
     auto pick = [&](uint32_t v, uint32_t mask) {      // in one instruction, which takes one scalar operand
         uint32_t r;

@@ -7,13 +7,14 @@
 // Groups of 128 take the codes as subnormals: 80 vector instructions for TT x 32 matrix instructions; what a group's sums owe to the zero
 // point 8 enters as the first matrix instruction's addend, and a group costs 2 vector instructions a value (add, multiply-add with the scale).
 // Groups of 32 and 64 have that cost four and two times as often, and vector and matrix instructions take turns on a SIMD rather than
-// run at the same time (counters, groups of 32: 86 k cycles of the one, 50 k of the other, in 141 k).  They take c - 8 (64 instructions more a column
+// run at the same time (counters, groups of 32: 86 k cycles of the one, 50 k of the other, in 141 k).  They take c - z (64 instructions more a column
 // tile) and add the lo products to the exact sum of the hi products: 1 vector instruction a value, no addend to prepare.
 // At 1056 rows the matrix cores run at what a large library product reaches: 13B gate/up (2 x 13824 x 5120, groups of 128) 500 us, 598 TFLOP/s
 // of the product, two terms executed: 1196 (library, fp16: 1173).  4096 x 11008, groups of 32, 257 rows: 72 us, vector instructions first.
 #include "ld_w4_device.h"
 
 #include <algorithm>
+#include <type_traits>
 
 using namespace ldd;
 using namespace ldw;
@@ -49,11 +50,12 @@ template <int TT, int G, bool ZEROS, typename ST>
 __global__ __launch_bounds__(256, 2) void k_w4_tile(ld::W4Image w, ld::W4Rows r, int T, int N, int epilogue, int n_blocks, int t_blocks, int slabs,
                                                     float *__restrict__ y, float *__restrict__ part) {
     constexpr int PER = 128 / G, JG = G / 32;
-    constexpr bool SUBNORMAL = ld::w4_subnormal(G), SUMMED = SUBNORMAL || ZEROS;      // SUMMED: the sums of the activations are needed
+    constexpr bool SUBNORMAL = ld::w4_subnormal(G);
+    using Zero = std::conditional_t<SUBNORMAL, uint8_t, uint32_t>;      // z, or 1024 + z as two fp16
     __shared__ __attribute__((aligned(16))) char sm_x[2][TT * 8192];
-    __shared__ float sm_s[2][SUMMED ? TT * PER * 32 : 1];
+    __shared__ float sm_s[2][SUBNORMAL ? TT * PER * 32 : 1];
     __shared__ __attribute__((aligned(16))) float sm_w[2][PER][256];      // scales
-    __shared__ __attribute__((aligned(16))) uint8_t sm_z[2][PER][ZEROS ? 256 : 4];      // zero points
+    __shared__ __attribute__((aligned(16))) Zero sm_z[2][PER][ZEROS ? 256 : 4];      // zero points
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int col = lane & 15, h = lane >> 4;
     const bool pair = epilogue == LDK_SWIGLU;
@@ -80,7 +82,7 @@ __global__ __launch_bounds__(256, 2) void k_w4_tile(ld::W4Image w, ld::W4Rows r,
     };
     // What belongs to a column tile beside codes and operands goes through LDS: the sums of the activations, and the scales (and zero points)
     // of 256 output rows, a row a thread.  Nothing else is loaded inside a tile's products, so that no wait there drains the copies.
-    constexpr int SUMS = SUMMED ? (TT * PER * 32 + 255) / 256 : 0;
+    constexpr int SUMS = SUBNORMAL ? (TT * PER * 32 + 255) / 256 : 0;
     struct Small { float sum[SUMS ? SUMS : 1]; ST scale[PER]; uint8_t zero[PER]; };
     const int my = threadIdx.x >> 4;      // row tile of the workgroup's 16: wave my / 4, its tile my % 4
     const int64_t my_tile = pair ? (int64_t)((my & 3) >= 2 ? w.row_tiles : 0) + min(nb * 8 + (my >> 2) * 2 + (my & 1), w.row_tiles - 1)
@@ -107,7 +109,7 @@ __global__ __launch_bounds__(256, 2) void k_w4_tile(ld::W4Image w, ld::W4Rows r,
         for (int p = 0; p < PER; p++) {
             if constexpr (sizeof(ST) == 2) sm_w[stage][p][threadIdx.x] = bf16_to_f32(v.scale[p]);
             else sm_w[stage][p][threadIdx.x] = v.scale[p];
-            if constexpr (ZEROS) sm_z[stage][p][threadIdx.x] = v.zero[p];
+            if constexpr (ZEROS) sm_z[stage][p][threadIdx.x] = SUBNORMAL ? (Zero)v.zero[p] : (Zero)(0x64006400u | v.zero[p] * 0x10001u);
         }
     };
     auto load_codes = [&](int kt, u32x4 (&c)[NT]) {
@@ -139,14 +141,17 @@ __global__ __launch_bounds__(256, 2) void k_w4_tile(ld::W4Image w, ld::W4Rows r,
         for (int p = 0; p < PER; p++) {
             f16x8 a[NT][JG];
 #pragma unroll
-            for (int i = 0; i < NT; i++)
+            for (int i = 0; i < NT; i++) {
+                uint32_t z = 0x64086408u;      // 8
+                if constexpr (ZEROS && !SUBNORMAL) z = sm_z[stage][p][(wave * NT + i) * 16 + col];
 #pragma unroll
-                for (int j = 0; j < JG; j++) a[i][j] = SUBNORMAL ? codes_as_subnormals(code[i][p * JG + j]) : codes_less_8(code[i][p * JG + j]);
+                for (int j = 0; j < JG; j++) a[i][j] = SUBNORMAL ? codes_as_subnormals(code[i][p * JG + j]) : codes_less(code[i][p * JG + j], z);
+            }
             f32x4 sc[NT], sz[NT];
 #pragma unroll
             for (int i = 0; i < NT; i++) {
                 sc[i] = *reinterpret_cast<const f32x4 *>(&sm_w[stage][p][(wave * NT + i) * 16 + 4 * h]);
-                if constexpr (ZEROS) {
+                if constexpr (ZEROS && SUBNORMAL) {
                     const uint32_t z = *reinterpret_cast<const uint32_t *>(&sm_z[stage][p][(wave * NT + i) * 16 + 4 * h]);
 #pragma unroll
                     for (int e = 0; e < 4; e++) sz[i][e] = 8.f - (float)(z >> 8 * e & 255);
@@ -155,7 +160,7 @@ __global__ __launch_bounds__(256, 2) void k_w4_tile(ld::W4Image w, ld::W4Rows r,
 #pragma unroll
             for (int t = 0; t < TT; t++) {
                 float s_hi = 0.f, s_lo = 0.f;
-                if constexpr (SUMMED) {
+                if constexpr (SUBNORMAL) {
                     s_hi = sm_s[stage][(t * PER + p) * 32 + col];
                     s_lo = sm_s[stage][(t * PER + p) * 32 + 16 + col];
                 }
@@ -197,7 +202,7 @@ __global__ __launch_bounds__(256, 2) void k_w4_tile(ld::W4Image w, ld::W4Rows r,
                 for (int i = 0; i < NT; i++)
 #pragma unroll
                     for (int e = 0; e < 4; e++) {
-                        if constexpr (ZEROS) d[i][e] += sz[i][e] * (s_hi + s_lo);
+                        if constexpr (ZEROS && SUBNORMAL) d[i][e] += sz[i][e] * (s_hi + s_lo);
                         total[i][t][e] += sc[i][e] * d[i][e];
                     }
             }
