@@ -260,7 +260,7 @@ void launch_split(const float *x, const float *g, float eps, int T, int K, int G
 // for one then leaves the younger ones in flight.
 // One row of 4096 columns: 4096 outputs 5.7 us (9 MB), gated 2 x 11008 15.4 us (47 MB: 3.1 TB/s over the call, of which the start and the row's split
 // take some 5 us), 32000 outputs 15.8 us; 11008 columns, 4096 outputs 10.9 us.  With the split in a launch ahead each took 3 - 4 us more.
-template <int G, int R, int T, int NC, typename ST>
+template <int G, int R, int T, int NC, typename ST, bool ZEROS>
 __global__ __launch_bounds__(512, 4) void k_w4_rows(ld::W4Image w, const float *__restrict__ x, const float *__restrict__ gain, float eps, int N, int K,
                                                     int epilogue, float *__restrict__ y) {
     constexpr int WAVES = 8, PER = 128 / G;
@@ -277,9 +277,9 @@ __global__ __launch_bounds__(512, 4) void k_w4_rows(ld::W4Image w, const float *
     const int Kp = w.k_tiles * 128, stride = Kp * 2 + 64;      // 64: neighbouring rows' pieces lie in different banks
     float *sm_sums = reinterpret_cast<float *>(sm_rows + 2 * T * stride);
 
-    CodeTile<PER, ST> ring[AHEAD][R];
+    CodeTile<PER, ST, ZEROS> ring[AHEAD][R];
     // asks for step `at` of a unit, or of the workgroup's next one where the unit ends before it
-    auto fill = [&](CodeTile<PER, ST> (&q)[R], int unit, int at) {
+    auto fill = [&](CodeTile<PER, ST, ZEROS> (&q)[R], int unit, int at) {
         if (at >= steps) { at -= steps; unit += gridDim.x; }
         unit = min(unit, units - 1);
         const int kt = min(wave + at * WAVES, w.k_tiles - 1);
@@ -311,7 +311,7 @@ __global__ __launch_bounds__(512, 4) void k_w4_rows(ld::W4Image w, const float *
     const int t_col = min(col & 7, T - 1);      // columns past the rows repeat the last one's
     const char *operand = sm_rows + (2 * t_col + (col >> 3)) * stride + 16 * h;
     const float *my_sums = sm_sums + 2 * t_col * w.groups + (col >> 3);
-    auto multiply = [&](const CodeTile<PER, ST> (&q)[R], int kt) {
+    auto multiply = [&](const CodeTile<PER, ST, ZEROS> (&q)[R], int kt) {
 #pragma unroll
         for (int p = 0; p < PER; p++) {
             f32x4 acc[R];
@@ -374,8 +374,10 @@ void launch_rows(const ld::W4Image &w, int scale_dtype, const Few &a, hipStream_
     const int units = a.epilogue == LDK_SWIGLU ? w.row_tiles : (w.row_tiles + R - 1) / R, each = (units + 511) / 512;
     const dim3 grid((units + each - 1) / each), block(512);
     const size_t lds = (size_t)T * (2 * (w.k_tiles * 256 + 64) + w.groups * 8);
-    if (scale_dtype == LD_BF16) LD_LAUNCH((k_w4_rows<G, R, T, NC, bf16_t>), grid, block, lds, s, w, a.x, a.g, a.eps, a.N, a.K, a.epilogue, a.y);
-    else LD_LAUNCH((k_w4_rows<G, R, T, NC, float>), grid, block, lds, s, w, a.x, a.g, a.eps, a.N, a.K, a.epilogue, a.y);
+#define LD_ROWS(S_, Z_) LD_LAUNCH((k_w4_rows<G, R, T, NC, S_, Z_>), grid, block, lds, s, w, a.x, a.g, a.eps, a.N, a.K, a.epilogue, a.y)
+    if (scale_dtype == LD_BF16) { if (w.zeros) LD_ROWS(bf16_t, true); else LD_ROWS(bf16_t, false); }
+    else { if (w.zeros) LD_ROWS(float, true); else LD_ROWS(float, false); }
+#undef LD_ROWS
 }
 template <int G, int R>
 void launch_rows(const ld::W4Image &w, int scale_dtype, const Few &a, hipStream_t s) {

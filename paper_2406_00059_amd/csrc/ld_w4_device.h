@@ -102,10 +102,10 @@ __device__ __forceinline__ f16x8 codes_less(uint32_t w, uint32_t z) {
 }
 
 // What a wave reads of a tile of 16 rows x 128 columns: its codes, the scales of its lanes' four rows, the zero points.
-template <int PER, typename ST>
+template <int PER, typename ST, bool ZEROS>
 struct CodeTile {
     u32x4 code;
-    uint32_t scale[PER][sizeof(ST)], zero[PER];
+    uint32_t scale[PER][sizeof(ST)], zero[ZEROS ? PER : 1];
     __device__ __forceinline__ void load(const ld::W4Image &w, int64_t tile, int kt, int lane) {
         code = load_stream16(w.codes + ((tile * w.k_tiles + kt) * 64 + lane) * 4);
 #pragma unroll
@@ -118,14 +118,17 @@ struct CodeTile {
                 const uint4 v = *reinterpret_cast<const uint4 *>((const float *)w.scales + at);
                 scale[p][0] = v.x; scale[p][1] = v.y; scale[p][2] = v.z; scale[p][3] = v.w;
             }
-            zero[p] = w.zeros ? *reinterpret_cast<const uint32_t *>(w.zeros + at) : 0x08080808u;
+            if constexpr (ZEROS) zero[p] = *reinterpret_cast<const uint32_t *>(w.zeros + at);
         }
     }
     __device__ __forceinline__ float s(int p, int e) const {
         if constexpr (sizeof(ST) == 4) return __uint_as_float(scale[p][e]);
         else return __uint_as_float((e & 1) ? scale[p][e >> 1] & 0xffff0000u : scale[p][e >> 1] << 16);
     }
-    __device__ __forceinline__ float z(int p, int e) const { return (float)((zero[p] >> (8 * e)) & 255u); }
+    __device__ __forceinline__ float z(int p, int e) const {
+        if constexpr (ZEROS) return (float)((zero[p] >> (8 * e)) & 255u);
+        else return 8.f;
+    }
 };
 
 }  // namespace ldw
