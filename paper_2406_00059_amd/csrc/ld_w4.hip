@@ -258,8 +258,8 @@ void launch_split(const float *x, const float *g, float eps, int T, int K, int G
 // operand: columns 0 .. 7 are their hi terms, 8 .. 15 the lo terms, so that both cost what one does.
 // AHEAD column tiles are asked for at any time, also over the end of a unit, and without a condition (past an end the last one again): a wait
 // for one then leaves the younger ones in flight.
-// One row of 4096 columns: 4096 outputs 5.7 us (9 MB), gated 2 x 11008 15.4 us (47 MB: 3.1 TB/s over the call, of which the start and the row's split
-// take some 5 us), 32000 outputs 15.8 us; 11008 columns, 4096 outputs 10.9 us.  With the split in a launch ahead each took 3 - 4 us more.
+// One row of 4096 columns: 4096 outputs 5.7 us (9 MB), gated 2 x 11008 14.4 us (47 MB: 3.3 TB/s over the call, of which the start and the row's split
+// take some 5 us), 32000 outputs 15.0 us; 11008 columns, 4096 outputs 10.4 us.  With the split in a launch ahead each took 3 - 4 us more.
 template <int G, int R, int T, int NC, typename ST, bool ZEROS>
 __global__ __launch_bounds__(512, 4) void k_w4_rows(ld::W4Image w, const float *__restrict__ x, const float *__restrict__ gain, float eps, int N, int K,
                                                     int epilogue, float *__restrict__ y) {
@@ -381,7 +381,8 @@ void launch_rows(const ld::W4Image &w, int scale_dtype, const Few &a, hipStream_
 }
 template <int G, int R>
 void launch_rows(const ld::W4Image &w, int scale_dtype, const Few &a, hipStream_t s) {
-    if (a.T == 2) launch_rows<G, R, 2, 2>(w, scale_dtype, a, s);
+    if (a.T == 2 && a.K <= 4096) launch_rows<G, R, 2, 2>(w, scale_dtype, a, s);
+    else if (a.T == 2) launch_rows<G, R, 2, 3>(w, scale_dtype, a, s);
     else if (a.K <= 4096) launch_rows<G, R, 1, 2>(w, scale_dtype, a, s);
     else if (a.K <= 6144) launch_rows<G, R, 1, 3>(w, scale_dtype, a, s);
     else launch_rows<G, R, 1, 7>(w, scale_dtype, a, s);
@@ -392,8 +393,9 @@ void launch_group(const ld::W4Image &w, int scale_dtype, const Few &a, hipStream
     else launch_rows<G, 2>(w, scale_dtype, a, s);
 }
 
-// Rows that a workgroup splits by itself: as many as its threads hold in registers.
-bool few_rows(int T, int K) { return (T == 1 && K <= 7 * 2048) || (T == 2 && K <= 2 * 2048); }
+// Rows that a workgroup splits by itself: one as long as its threads hold it in registers, two up to 6144 columns.  us, by itself / in a launch ahead
+// of the tiles, two rows: gated 2 x 13824 x 5120 21 / 27, 15360 x 5120 16 / 19; 4096 x 11008 24 / 21, 4096 x 14336 27 / 24.
+bool few_rows(int T, int K) { return (T == 1 && K <= 7 * 2048) || (T == 2 && K <= 3 * 2048); }
 
 constexpr int MOST_ROWS = 1 << 20;
 
