@@ -924,15 +924,16 @@ int visible_blocks(int max_ctx, int window) {
 }
 
 // One launch or two.  A CU alone draws some 50 GB/s, so one workgroup a (row, KV head) is slow where there are few of them and each has much to
-// read; two launches and the meeting of the shares cost 4 - 5 us.  us, one / two launches: 32 pairs of 280 KB each 13.4 / 12.5, 24 of 336 KB
-// 16.2 / 13.3; 56 of 238 KB 19 / 24, 96 of 188 KB 18.3 / 23.3, 64 of 50 KB 14.2 / 15.2; 1024 of 580 KB 104 / 127.
+// read; two launches and the meeting of the shares cost 4 - 5 us.  us, one / two launches: 32 pairs of 160 KB each 11.5 / 13.0, 40 of 192 KB 15.5 / 16.7, 32 of
+// 192 KB 15.1 / 14.7, 80 of 192 KB 18.1 / 17.2, 32 of 256 KB 21.7 / 16.2, 80 of 280 KB 21.6 / 16.4, 192 of 256 KB 26.0 / 21.9; 1024 of 580 KB 104 / 127.
 bool fused_form(int T, int Hkv, int hd, int el, int nb, int budget) {
     const int n = std::min(nb, budget);
     if (nb > FUSED_BLOCKS || n > FUSED_BUDGET) return false;
-    return (int64_t)T * Hkv >= 256 || (int64_t)(nb > budget ? nb : 0) * 2 * hd + (int64_t)n * 32 * hd * el <= 256 << 10;
+    return (int64_t)T * Hkv >= 256 || (int64_t)(nb > budget ? nb : 0) * 2 * hd + (int64_t)n * 32 * hd * el <= 176 << 10;
 }
 
-// Split form: as many chunks a (row, KV head) as bring a workgroup to every CU, of two blocks at least.  The scratch holds scores, shares
+// Split form: as many chunks a (row, KV head) as bring a workgroup to every CU and no CU a second one (80 pairs, 280 KB each: 16 us with 240 workgroups,
+// 22 with 320), of two blocks at least.  The scratch holds scores, shares
 // and tickets.
 struct SparsePlan { int nb, stride, cb, chunks; size_t scores, part_o, part_ml, total; };
 SparsePlan sparse_plan(int T, int H, int Hkv, int hd, int max_ctx, int window, int budget) {
@@ -940,7 +941,7 @@ SparsePlan sparse_plan(int T, int H, int Hkv, int hd, int max_ctx, int window, i
     p.nb = visible_blocks(max_ctx, window);
     p.stride = (p.nb + 31) / 32 * 32;      // the choice reads whole vectors
     const int n = std::max(1, std::min(p.nb, budget));
-    const int64_t pairs = (int64_t)T * Hkv, want = std::max<int64_t>(1, (256 + pairs - 1) / pairs);
+    const int64_t pairs = (int64_t)T * Hkv, want = std::max<int64_t>(1, 256 / pairs);
     p.cb = (int)std::min<int64_t>(std::max<int64_t>(2, (n + want - 1) / want), SPLIT_BUDGET);      // a chunk's list fits the LDS
     p.chunks = (n + p.cb - 1) / p.cb;
     const size_t shares = (size_t)H / Hkv * (256 + pairs * ((n + SPLIT_BUDGET - 1) / SPLIT_BUDGET));
