@@ -137,19 +137,16 @@ class LightDecoder:
         """Feeds [pending?] ++ tokens and returns the token chosen after the last one.  rules: as in step."""
         tokens = np.asarray(tokens, np.int32)
         first = ld.ld_kv_len(self.kv.h, seq)
-        if first == 0:
-            self.length[seq] = 0
-        at = self.length[seq]
+        at = self.length[seq] if first else 0
+        if at + tokens.size <= first:
+            raise ValueError("prefill: no token to feed")
+        self._map(seq, at + tokens.size - first)      # of the whole prompt: a shortage changes nothing
         self.history[seq, at:at + tokens.size] = self._i32(tokens)
         self.length[seq] = self.prompt[seq] = at + tokens.size
-        x = None
         while first < self.length[seq]:
             n = min(self.max_rows, self.length[seq] - first)
-            self._map(seq, n)
             x = self._pass(self.history[seq, first:first + n], [seq], [first], [n], False)[n - 1:n]
             first += n
-        if x is None:
-            raise ValueError("prefill: no token to feed")
         return self._choose(x, [seq], rules)[0]
 
     def refresh(self, seq, tokens, pending=None):

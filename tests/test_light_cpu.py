@@ -1,0 +1,70 @@
+"""The light decoder's bookkeeping (what is fed, which positions and blocks a sequence holds, what a refusal leaves behind) on the host, with the
+kernels left out: the cache's allocator and state machine are the library's own."""
+import ctypes as C
+from types import SimpleNamespace
+
+import numpy as np
+import pytest
+import torch
+
+import paper_2406_00059_amd as ld
+from paper_2406_00059_amd import binding
+from paper_2406_00059_amd.light import LightDecoder
+from workloads import TINY, make_weights
+
+FAKE = 1 << 20     # an aligned non-null "device address" that is never dereferenced on the CPU
+KERNELS = ("ldk_embed", "ldk_rope_table", "ldk_linear_w4", "ldk_rope_kv_write", "ldk_kv_summary", "ldk_sparse_attention", "ldk_prefill_attention",
+           "ldk_paged_attention", "ldk_w4_quantize")
+
+
+@pytest.fixture
+def decoder(monkeypatch):
+    """make(n_blocks, ...) -> a LightDecoder whose kernels do nothing; .fed: the tokens of every pass, .summed: the ranges whose key bounds were
+    formed, .chosen: the tokens that the next choices give, one list a choice (rows of 5 where it is empty)."""
+    made = []
+
+    def make(n_blocks=40, max_seqs=3, max_blocks=12, **kw):
+        m = ld.Model(TINY, make_weights(TINY, 1))
+        ws = ld.ld_workspace_bytes(m.h, 64, max_seqs, max_blocks)
+        kv = SimpleNamespace(h=ld.ld_kv_create(m.h, FAKE, n_blocks, FAKE, ws, 64, max_seqs, max_blocks), n_blocks=n_blocks, max_seqs=max_seqs,
+                             max_blocks=max_blocks, pool=[None] * TINY.n_layers)
+        light = LightDecoder(m, kv, device="cpu", **{**dict(group=64, budget=8, max_rows=32), **kw})
+        light.fed, light.summed, light.chosen = [], [], []
+        monkeypatch.setattr(binding, "ldk_embed", lambda e, tok, x: light.fed.append(tok.tolist()))
+        monkeypatch.setattr(binding, "ldk_kv_summary", lambda pool, table, ranges, *a: light.summed.append(ranges.tolist()))
+
+        def choose(logits, token, **rules):
+            light.rules = rules
+            token.copy_(torch.tensor(light.chosen.pop(0) if light.chosen else [5] * token.numel()))
+        monkeypatch.setattr(binding, "ldk_choose", choose)
+        made.append((light, m))
+        return light
+    for name in KERNELS:
+        monkeypatch.setattr(binding, name, lambda *a, **k: None)
+    return make
+
+
+def _state(light, seq):
+    return ld.ld_kv_len(light.kv.h, seq), ld.ld_kv_block_table(light.kv.h, seq).tolist(), ld.ld_kv_free_blocks(light.kv.h), light.length[seq]
+
+
+def test_a_prompt_that_finds_no_blocks_changes_nothing(decoder):
+    """40 tokens in chunks of 32 with room for 32: refused as a whole; when blocks have become free the same call feeds every token once."""
+    light = decoder(n_blocks=3)
+    other, seq = ld.ld_kv_alloc(light.kv.h, 16), ld.ld_kv_alloc(light.kv.h)
+    before = _state(light, seq)
+    prompt = list(range(100, 140))
+    with pytest.raises(ld.LdError):
+        light.prefill(seq, prompt)
+    assert light.fed == [] and _state(light, seq) == before
+    ld.ld_kv_free(light.kv.h, other)
+    assert light.prefill(seq, prompt) == 5
+    assert sum(light.fed, []) == prompt and ld.ld_kv_len(light.kv.h, seq) == 40
+    # and one that is appended behind a pending token
+    light.fed.clear()
+    before = _state(light, seq)
+    with pytest.raises(ld.LdError):
+        light.prefill(seq, list(range(200, 209)))
+    assert light.fed == [] and _state(light, seq) == before
+    light.prefill(seq, list(range(200, 207)))
+    assert sum(light.fed, []) == [5] + list(range(200, 207)) and ld.ld_kv_len(light.kv.h, seq) == 48
