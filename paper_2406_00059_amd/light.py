@@ -79,6 +79,19 @@ class LightDecoder:
             self.table[seq, :t.size] = self._i32(t)
         return first
 
+    def _check_room(self, seqs):
+        """Raises what _map of one position for each of these sequences would end in, before any of them is mapped."""
+        need = 0
+        for s in seqs:
+            n, t = ld.ld_kv_len(self.kv.h, s), ld.ld_kv_block_table(self.kv.h, s)
+            if t.size * 16 < n:
+                raise ld.LdError(ld.LD_E_STATE, f"sequence {s} is swapped out")
+            if n // 16 >= self.kv.max_blocks:
+                raise ld.LdError(ld.LD_E_RANGE, f"sequence {s} is as long as its block table allows")
+            need += n % 16 == 0 and (n // 16 >= t.size or t[n // 16] < 0)
+        if need > ld.ld_kv_free_blocks(self.kv.h):
+            raise ld.LdError(ld.LD_E_NOMEM, "out of KV blocks")
+
     def _pass(self, tok, seqs, first, count, decode):
         """Rows of sequences seqs (count[i] rows each from position first[i]) through all layers; the residual stream is left in x."""
         sh, h, hkv, hd = self.shape, self.shape.n_heads, self.shape.n_kv_heads, self.shape.head_dim
@@ -172,6 +185,7 @@ class LightDecoder:
             raise ValueError(f"step: between one and {self.max_rows} distinct sequences")
         if any(self.length[s] != ld.ld_kv_len(self.kv.h, s) + 1 for s in seqs):
             raise ValueError("step: a sequence without a pending token (prefill it, or refresh it first)")
+        self._check_room(seqs)
         first = [self._map(s, 1) for s in seqs]
         tok = self.history[self._i32(seqs).long(), self._i32(first).long()]
         return self._choose(self._pass(tok, list(seqs), first, [1] * len(first), True), seqs, rules)

@@ -68,3 +68,33 @@ def test_a_prompt_that_finds_no_blocks_changes_nothing(decoder):
     assert light.fed == [] and _state(light, seq) == before
     light.prefill(seq, list(range(200, 207)))
     assert sum(light.fed, []) == [5] + list(range(200, 207)) and ld.ld_kv_len(light.kv.h, seq) == 48
+
+
+def test_a_step_that_finds_no_blocks_changes_nothing(decoder):
+    """Two sequences at the end of a block and one block left: neither moves; when a block has become free both do."""
+    light = decoder(n_blocks=4)
+    a, b, other = (ld.ld_kv_alloc(light.kv.h) for _ in range(3))
+    for s in (a, b):
+        light.prefill(s, list(range(16)))
+    ld.ld_kv_assume(light.kv.h, other, 1)
+    before = _state(light, a), _state(light, b)
+    light.fed.clear()
+    with pytest.raises(ld.LdError) as e:
+        light.step([a, b])
+    assert e.value.status == ld.LD_E_NOMEM
+    assert light.fed == [] and (_state(light, a), _state(light, b)) == before
+    ld.ld_kv_free(light.kv.h, other)
+    assert light.step([a, b]) == [5, 5] and light.fed == [[5, 5]]
+    assert [_state(light, s)[0] for s in (a, b)] == [17, 17]
+
+
+def test_a_step_past_the_longest_context_changes_nothing(decoder):
+    light = decoder(max_blocks=2)
+    a, b = (ld.ld_kv_alloc(light.kv.h) for _ in range(2))
+    light.prefill(a, [1])
+    light.prefill(b, list(range(32)))
+    before = _state(light, a), _state(light, b)
+    with pytest.raises(ld.LdError) as e:
+        light.step([a, b])
+    assert e.value.status == ld.LD_E_RANGE and (_state(light, a), _state(light, b)) == before
+    assert light.step([a]) == [5]
