@@ -3,6 +3,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+import struct
 import threading
 import weakref
 
@@ -138,7 +139,7 @@ _SIGS = {
     "ldk_sparse_attention": (C.c_int, [_vp, C.c_int32, _vp, C.c_int32, _vp, _vp, _vp, C.c_int32, _vp, _vp] + [C.c_int32] * 9 +
                              [_vp, _vp, _vp, C.c_size_t, _vp]),
     "ldk_choose_scratch_bytes": (C.c_size_t, [C.c_int32, C.c_int32]),
-    "ldk_choose": (C.c_int, [_vp, C.c_int32, C.c_int32, C.POINTER(ld_token_rules), _vp, _vp, _vp, _vp, _vp, _vp, C.c_size_t, _vp]),
+    "ldk_choose": (C.c_int, [_vp, C.c_int32, C.c_int32, _vp, _vp, _vp, _vp, _vp, _vp, _vp, C.c_size_t, _vp]),
 }
 EXPORTS = tuple(_SIGS)
 
@@ -180,12 +181,16 @@ def _ptr(t):
     return int(t)
 
 
+_cuda_up = torch.cuda.is_initialized
+_raw_stream, _current_device = (getattr(torch._C, n, None) for n in ("_cuda_getCurrentRawStream", "_cuda_getDevice"))
+
+
 def _stream(stream):
     if stream is None:
         # the handle itself: the Stream object that current_stream() builds around it takes 2.7 us a call, 120 of the 165 us in which
         # a caller forks, feeds and frees the 32 sequences of a step
-        if torch.cuda.is_initialized():
-            return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
+        if _cuda_up():
+            return _raw_stream(_current_device())
         stream = torch.cuda.current_stream()
     return stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
 
@@ -417,7 +422,7 @@ def ldk_rmsnorm(x, g, out, eps, row_idx=None, stream=None):
 
 
 def _nbytes(t):
-    return 0 if t is None else t.numel() * t.element_size()
+    return 0 if t is None else t.nbytes
 
 
 def ldk_linear_scratch_bytes(T, N, K, epilogue=LDK_STORE):
@@ -560,15 +565,43 @@ def ldk_choose_scratch_bytes(R, V):
     return lib().ldk_choose_scratch_bytes(R, V)
 
 
+def _at(name, t, dtype, n):
+    """Address of a contiguous tensor of n elements of a type; 0 for None."""
+    if t is None:
+        return 0
+    if t.dtype is not dtype or t.numel() != n or not t.is_contiguous():
+        raise LdError(LD_E_INVAL, f"{name} has to be {n} elements of {dtype}, contiguous, not {t.dtype} {tuple(t.shape)}")
+    return t.data_ptr()
+
+
+def _nothing(*_):
+    return LD_OK
+
+
+_pack_rules = struct.Struct("9Pii").pack      # an ld_token_rules, faster than filling in the structure
+
+
 def ldk_choose(logits, token, history=None, history_len=None, n_prompt=None, penalties=None, bias_start=None, bias_token=None, bias=None,
-               mask=None, mask_row=None, temperature=None, seed=None, pos=None, adjusted=None, scratch=None, stream=None):
-    """Device tensors: history int32 [R, n], history_len, n_prompt, mask_row, pos, token int32 [R], penalties float32 [R, 3] (repetition,
-    presence, frequency), bias_start int32 [R + 1], mask int32 [rows, ceil(V / 32)] (bit patterns), seed int64 [R] (bit patterns)."""
-    R, V = logits.shape
-    rules = ld_token_rules(_ptr(history), _ptr(history_len), _ptr(n_prompt), _ptr(penalties), _ptr(bias_start), _ptr(bias_token), _ptr(bias),
-                           _ptr(mask), _ptr(mask_row), 0 if history is None else history.shape[1], 0 if mask is None else mask.shape[0])
-    _check(lib().ldk_choose(_ptr(logits), R, V, C.byref(rules), _ptr(temperature), _ptr(seed), _ptr(pos), _ptr(adjusted), _ptr(token),
-                            _ptr(scratch), _nbytes(scratch), _stream(stream)))
+               mask=None, mask_row=None, temperature=None, seed=None, pos=None, adjusted=None, scratch=None, stream=None, check_only=False):
+    """Device tensors: logits float32 [R, V], history int32 [R, n], history_len, n_prompt, mask_row, pos, token int32 [R], penalties float32 [R, 3]
+    (repetition, presence, frequency), bias_start int32 [R + 1], bias_token int32 and bias float32 of one length, mask int32 [rows, ceil(V / 32)] (bit
+    patterns), temperature float32 [R], seed int64 [R] (bit patterns), adjusted float32 [R, V].  Types and lengths are checked, for the kernels read by the
+    lengths that the logits imply; check_only: nothing else is done."""
+    try:
+        R, V = logits.shape
+        _, stride = (0, 0) if history is None else history.shape
+        rows, _ = (0, 0) if mask is None else mask.shape
+    except ValueError:
+        raise LdError(LD_E_INVAL, "ldk_choose: logits [R, V], history [R, n] and mask [rows, ceil(V / 32)] have two dimensions") from None
+    n = 0 if bias is None else bias.numel()
+    call = _nothing if check_only else (_lib or lib()).ldk_choose
+    i32, f32 = torch.int32, torch.float32
+    rules = _pack_rules(_at("history", history, i32, R * stride), _at("history_len", history_len, i32, R), _at("n_prompt", n_prompt, i32, R),
+                        _at("penalties", penalties, f32, 3 * R), _at("bias_start", bias_start, i32, R + 1), _at("bias_token", bias_token, i32, n),
+                        _at("bias", bias, f32, n), _at("mask", mask, i32, rows * ((V + 31) // 32)), _at("mask_row", mask_row, i32, R), stride, rows)
+    _check(call(_at("logits", logits, f32, R * V), R, V, rules, _at("temperature", temperature, f32, R), _at("seed", seed, torch.int64, R),
+                _at("pos", pos, i32, R), _at("adjusted", adjusted, f32, R * V), _at("token", token, i32, R), _ptr(scratch), _nbytes(scratch),
+                _stream(stream)))
 
 
 # ------------------------------------------------------------------ owners of handles + device memory

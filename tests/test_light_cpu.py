@@ -98,3 +98,35 @@ def test_a_step_past_the_longest_context_changes_nothing(decoder):
         light.step([a, b])
     assert e.value.status == ld.LD_E_RANGE and (_state(light, a), _state(light, b)) == before
     assert light.step([a]) == [5]
+
+
+# ---------------------------------------------------------------- what the wrappers refuse before the library is called
+
+def _choice(R=3, V=1000):
+    """Arguments of a choice under every rule."""
+    i, f = dict(dtype=torch.int32), dict(dtype=torch.float32)
+    return dict(logits=torch.zeros(R, V, **f), token=torch.zeros(R, **i), history=torch.zeros(R, 7, **i), history_len=torch.zeros(R, **i),
+                n_prompt=torch.zeros(R, **i), penalties=torch.ones(R, 3, **f), bias_start=torch.zeros(R + 1, **i), bias_token=torch.zeros(4, **i),
+                bias=torch.zeros(4, **f), mask=torch.zeros(2, -(-V // 32), **i), mask_row=torch.zeros(R, **i), temperature=torch.ones(R, **f),
+                seed=torch.zeros(R, dtype=torch.int64), pos=torch.zeros(R, **i), adjusted=torch.zeros(R, V, **f), scratch=torch.zeros(1 << 12, dtype=torch.uint8))
+
+
+@pytest.mark.parametrize("name,bad", [
+    ("mask", torch.zeros(2, 31, dtype=torch.int32)),      # 1000 // 32 words: the last tokens' bits would lie past the end
+    ("mask", torch.zeros(2, 32, dtype=torch.int64)), ("mask", torch.zeros(64, dtype=torch.int32)), ("mask_row", torch.zeros(2, dtype=torch.int32)),
+    ("mask_row", torch.zeros(3, dtype=torch.int64)), ("history", torch.zeros(2, 7, dtype=torch.int32)), ("history", torch.zeros(3, 7, dtype=torch.int64)),
+    ("history", torch.zeros(7, 3, dtype=torch.int32).t()), ("history_len", torch.zeros(1, dtype=torch.int32)), ("n_prompt", torch.zeros(4, dtype=torch.int32)),
+    ("penalties", torch.ones(3)), ("penalties", torch.ones(3, 3, dtype=torch.float64)), ("bias_start", torch.zeros(3, dtype=torch.int32)),
+    ("bias_token", torch.zeros(3, dtype=torch.int32)), ("bias", torch.zeros(4, dtype=torch.bfloat16)), ("temperature", torch.ones(1)),
+    ("seed", torch.zeros(3, dtype=torch.int32)), ("pos", torch.zeros(3, dtype=torch.int64)), ("token", torch.zeros(3, dtype=torch.int64)),
+    ("token", torch.zeros(2, dtype=torch.int32)), ("adjusted", torch.zeros(3, 999)), ("logits", torch.zeros(3, 1000, dtype=torch.bfloat16)),
+    ("logits", torch.zeros(1000))])
+def test_choice_refuses_tensors_that_do_not_fit(name, bad, monkeypatch):
+    calls = []
+    monkeypatch.setattr(binding.lib(), "ldk_choose", lambda *a: calls.append(a) or ld.LD_OK)
+    kw = _choice()
+    ld.ldk_choose(stream=0, **kw)
+    assert len(calls) == 1
+    with pytest.raises(ld.LdError) as e:
+        ld.ldk_choose(stream=0, **{**kw, name: bad})
+    assert e.value.status == ld.LD_E_INVAL and name in str(e.value) and len(calls) == 1
