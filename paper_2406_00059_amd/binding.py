@@ -520,12 +520,21 @@ def ldk_w4_image_bytes(N, K, group, parts, scale_dtype, zeros):
     return lib().ldk_w4_image_bytes(N, K, group, parts, _dt(scale_dtype), int(bool(zeros)))
 
 
+_W4_FLOATS = (torch.bfloat16, torch.float32)
+
+
 def ldk_w4_pack(codes, scales, zeros, image, N, K, group, parts=1, stream=None):
+    groups = parts * N * -(-K // group)
+    if codes.dtype != torch.uint8 or codes.numel() != parts * N * ((K + 1) // 2) or scales.dtype not in _W4_FLOATS or scales.numel() != groups or \
+            (zeros is not None and (zeros.dtype != torch.uint8 or zeros.numel() != groups)):
+        raise LdError(LD_E_INVAL, "ldk_w4_pack: sizes or types of codes, scales and zeros do not fit")
     _check(lib().ldk_w4_pack(_ptr(codes), _ptr(scales), _dt(scales.dtype), _ptr(zeros), N, K, group, parts, _ptr(image), _nbytes(image),
                              _stream(stream)))
 
 
 def ldk_w4_quantize(W, image, N, K, group, parts=1, scale_dtype=torch.bfloat16, zeros=False, stream=None):
+    if W.dtype not in _W4_FLOATS or scale_dtype not in _W4_FLOATS or W.numel() != parts * N * K:
+        raise LdError(LD_E_INVAL, f"ldk_w4_quantize: {parts * N} x {K} entries, bf16 or float32, not {W.dtype} {tuple(W.shape)}; scales bf16 or float32")
     _check(lib().ldk_w4_quantize(_ptr(W), _dt(W.dtype), N, K, group, parts, _dt(scale_dtype), int(bool(zeros)), _ptr(image), _nbytes(image),
                                  _stream(stream)))
 
@@ -611,7 +620,7 @@ class W4Matrix:
 
     def __init__(self, N, K, group=128, parts=1, scale_dtype=torch.bfloat16, zeros=False, device="cuda"):
         self.N, self.K, self.group, self.parts, self.scale_dtype, self.zeros = N, K, group, parts, scale_dtype, bool(zeros)
-        n = ldk_w4_image_bytes(N, K, group, parts, scale_dtype, zeros) if scale_dtype in (torch.bfloat16, torch.float32) else 0
+        n = ldk_w4_image_bytes(N, K, group, parts, scale_dtype, zeros) if scale_dtype in _W4_FLOATS else 0
         if n == 0:
             raise LdError(LD_E_INVAL, f"no 4-bit image has {parts} x {N} x {K} weights in groups of {group} with {scale_dtype} scales")
         self.image = torch.empty(n, dtype=torch.uint8, device=device)
@@ -631,6 +640,8 @@ class W4Matrix:
     @classmethod
     def quantize(cls, W, group=128, parts=1, scale_dtype=torch.bfloat16, zeros=False, stream=None):
         """W [parts N, K], bf16 or float32, rounded to nearest."""
+        if W.dim() != 2 or W.dtype not in _W4_FLOATS:
+            raise LdError(LD_E_INVAL, f"W4Matrix.quantize: a bf16 or float32 matrix, not {W.dtype} {tuple(W.shape)}")
         N, K = W.shape[0] // parts, W.shape[1]
         if W.shape[0] != parts * N:
             raise LdError(LD_E_INVAL, "W4Matrix.quantize: rows are not a multiple of parts")

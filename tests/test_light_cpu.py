@@ -130,3 +130,28 @@ def test_choice_refuses_tensors_that_do_not_fit(name, bad, monkeypatch):
     with pytest.raises(ld.LdError) as e:
         ld.ldk_choose(stream=0, **{**kw, name: bad})
     assert e.value.status == ld.LD_E_INVAL and name in str(e.value) and len(calls) == 1
+
+
+@pytest.mark.parametrize("W", [torch.zeros(4, 64, dtype=torch.float16), torch.zeros(4, 64, dtype=torch.float64), torch.zeros(4, 64, dtype=torch.int32),
+                               torch.zeros(256), torch.zeros(2, 2, 64)], ids=["fp16", "float64", "int32", "one-dimensional", "three-dimensional"])
+def test_quantise_refuses_matrices_of_other_types(W, monkeypatch):
+    """An fp16 matrix would be read as float32, past its end."""
+    monkeypatch.setattr(binding, "ldk_w4_quantize", lambda *a, **k: pytest.fail("the matrix got as far as the kernel"))
+    with pytest.raises(ld.LdError) as e:
+        ld.W4Matrix.quantize(W, 64)
+    assert e.value.status == ld.LD_E_INVAL
+
+
+def test_pack_and_quantise_wrappers_refuse_what_the_kernels_would_misread(monkeypatch):
+    for name in ("ldk_w4_pack", "ldk_w4_quantize"):
+        monkeypatch.setattr(binding.lib(), name, lambda *a: ld.LD_OK)
+    codes, scales, image = torch.zeros(8, 32, dtype=torch.uint8), torch.zeros(8, 1), torch.zeros(1 << 16, dtype=torch.uint8)
+    ld.ldk_w4_pack(codes, scales, None, image, 8, 64, 64, stream=0)
+    for c, s, z in [(codes[:7], scales, None), (codes, scales.half(), None), (codes, scales[:7], None), (codes, scales, torch.zeros(8, 1)),
+                    (codes, scales, codes[:7, :1]), (codes.int(), scales, None)]:
+        with pytest.raises(ld.LdError):
+            ld.ldk_w4_pack(c, s, z, image, 8, 64, 64, stream=0)
+    ld.ldk_w4_quantize(torch.zeros(8, 64), image, 8, 64, 64, stream=0)
+    for W in (torch.zeros(8, 64).half(), torch.zeros(7, 64), torch.zeros(8, 64).double()):
+        with pytest.raises(ld.LdError):
+            ld.ldk_w4_quantize(W, image, 8, 64, 64, stream=0)
