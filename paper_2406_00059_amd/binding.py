@@ -544,13 +544,16 @@ def ldk_linear_w4_scratch_bytes(T, N, K, epilogue=LDK_STORE):
 
 
 def ldk_linear_w4(w, x, y, epilogue=LDK_STORE, g=None, eps=0.0, scratch=None, stream=None):
-    """w: a W4Matrix whose parts fit the epilogue (two for LDK_SWIGLU)."""
+    """w: a W4Matrix whose parts fit the epilogue (two for LDK_SWIGLU); x [T, K], y [T, N] and g [K] float32."""
+    f32 = torch.float32
+    if x.dim() != 2 or x.dtype is not f32 or y.dtype is not f32 or (g is not None and (g.dtype is not f32 or g.numel() != w.K)):
+        raise LdError(LD_E_INVAL, f"ldk_linear_w4: x [rows, {w.K}], y and g have to be float32")
     T, K = x.shape
     if K != w.K or y.shape != (T, w.N) or w.parts != (2 if epilogue == LDK_SWIGLU else 1):
         raise LdError(LD_E_INVAL, f"ldk_linear_w4: x {tuple(x.shape)}, y {tuple(y.shape)} and epilogue {epilogue} do not fit {w.parts} x "
                                   f"{w.N} x {w.K} weights")
-    _check(lib().ldk_linear_w4(_ptr(w.image), _dt(w.scale_dtype), int(w.zeros), w.group, _ptr(x), _ptr(g), eps, T, w.N, K, epilogue, _ptr(y),
-                               _ptr(scratch), _nbytes(scratch), _stream(stream)))
+    _check((_lib or lib()).ldk_linear_w4(_ptr(w.image), _dt(w.scale_dtype), int(w.zeros), w.group, _ptr(x), _ptr(g), eps, T, w.N, K, epilogue, _ptr(y),
+                                         _ptr(scratch), _nbytes(scratch), _stream(stream)))
 
 
 def ldk_kv_summary(pool_layer, table, ranges, max_len, Hkv, hd, bounds, unit, stream=None):

@@ -155,3 +155,18 @@ def test_pack_and_quantise_wrappers_refuse_what_the_kernels_would_misread(monkey
     for W in (torch.zeros(8, 64).half(), torch.zeros(7, 64), torch.zeros(8, 64).double()):
         with pytest.raises(ld.LdError):
             ld.ldk_w4_quantize(W, image, 8, 64, 64, stream=0)
+
+
+@pytest.mark.parametrize("name,bad", [("x", torch.zeros(3, 64, dtype=torch.bfloat16)), ("x", torch.zeros(3, 64, dtype=torch.float64)),
+                                      ("y", torch.zeros(3, 8, dtype=torch.bfloat16)), ("y", torch.zeros(3, 8, dtype=torch.float16)),
+                                      ("g", torch.zeros(64, dtype=torch.bfloat16)), ("g", torch.zeros(63)), ("x", torch.zeros(64))])
+def test_linear_refuses_activations_of_other_types(name, bad, monkeypatch):
+    calls = []
+    monkeypatch.setattr(binding.lib(), "ldk_linear_w4", lambda *a: calls.append(a) or ld.LD_OK)
+    w = ld.W4Matrix(8, 64, 64, device="cpu")
+    kw = dict(x=torch.zeros(3, 64), y=torch.zeros(3, 8), g=torch.ones(64))
+    ld.ldk_linear_w4(w, stream=0, **kw)
+    assert len(calls) == 1
+    with pytest.raises(ld.LdError) as e:
+        ld.ldk_linear_w4(w, stream=0, **{**kw, name: bad})
+    assert e.value.status == ld.LD_E_INVAL and len(calls) == 1
