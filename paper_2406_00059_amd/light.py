@@ -79,6 +79,24 @@ class LightDecoder:
             self.table[seq, :t.size] = self._i32(t)
         return first
 
+    RULES = ("bias_start", "bias_token", "bias", "mask", "mask_row", "temperature", "seed")
+
+    def _check_rules(self, R, rules):
+        """Raises what _choose for R rows would refuse, before anything is fed."""
+        if not rules:
+            return
+        for name in rules:
+            if name not in self.RULES:
+                raise TypeError(f"no rule is named {name} (histories, positions and penalties are the decoder's own)")
+        ld.ldk_choose(self.logits[:R], self.sel.view(-1)[:R], check_only=True, stream=0, **rules)
+        given = {name for name in rules if rules[name] is not None}
+        if "temperature" in given and "seed" not in given:
+            raise ld.LdError(ld.LD_E_INVAL, "a temperature needs a seed")
+        if given & {"bias", "bias_start", "bias_token"} and not {"bias", "bias_start", "bias_token"} <= given:
+            raise ld.LdError(ld.LD_E_INVAL, "bias comes with bias_start and bias_token")
+        if "mask" in given and "mask_row" not in given and rules["mask"].shape[0] < R:
+            raise ld.LdError(ld.LD_E_INVAL, f"a mask of {R} rows, or a mask_row for each of the {R} sequences")
+
     def _check_room(self, seqs):
         """Raises what _map of one position for each of these sequences would end in, before any of them is mapped."""
         need = 0
@@ -153,6 +171,7 @@ class LightDecoder:
         at = self.length[seq] if first else 0
         if at + tokens.size <= first:
             raise ValueError("prefill: no token to feed")
+        self._check_rules(1, rules)
         self._map(seq, at + tokens.size - first)      # of the whole prompt: a shortage changes nothing
         self.history[seq, at:at + tokens.size] = self._i32(tokens)
         self.length[seq] = self.prompt[seq] = at + tokens.size
@@ -185,6 +204,7 @@ class LightDecoder:
             raise ValueError(f"step: between one and {self.max_rows} distinct sequences")
         if any(self.length[s] != ld.ld_kv_len(self.kv.h, s) + 1 for s in seqs):
             raise ValueError("step: a sequence without a pending token (prefill it, or refresh it first)")
+        self._check_rules(len(seqs), rules)
         self._check_room(seqs)
         first = [self._map(s, 1) for s in seqs]
         tok = self.history[self._i32(seqs).long(), self._i32(first).long()]

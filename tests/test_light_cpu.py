@@ -33,7 +33,12 @@ def decoder(monkeypatch):
         monkeypatch.setattr(binding, "ldk_embed", lambda e, tok, x: light.fed.append(tok.tolist()))
         monkeypatch.setattr(binding, "ldk_kv_summary", lambda pool, table, ranges, *a: light.summed.append(ranges.tolist()))
 
-        def choose(logits, token, **rules):
+        real = ld.ldk_choose
+
+        def choose(logits, token, scratch=None, **rules):
+            real(logits, token, **{**rules, "stream": 0, "check_only": True})
+            if rules.get("check_only"):
+                return
             light.rules = rules
             token.copy_(torch.tensor(light.chosen.pop(0) if light.chosen else [5] * token.numel()))
         monkeypatch.setattr(binding, "ldk_choose", choose)
@@ -98,6 +103,25 @@ def test_a_step_past_the_longest_context_changes_nothing(decoder):
         light.step([a, b])
     assert e.value.status == ld.LD_E_RANGE and (_state(light, a), _state(light, b)) == before
     assert light.step([a]) == [5]
+
+
+@pytest.mark.parametrize("rules", [dict(mask=torch.zeros(2, 31, dtype=torch.int32)), dict(mask=torch.zeros(1, 32, dtype=torch.int32)), dict(temperature=torch.ones(2)),
+                                   dict(temperature=torch.ones(1), seed=torch.zeros(2, dtype=torch.int64)), dict(bias=torch.zeros(2)),
+                                   dict(bias_start=torch.zeros(3, dtype=torch.int32), bias_token=torch.zeros(1, dtype=torch.int32), bias=torch.zeros(2)),
+                                   dict(history=torch.zeros(2, 4, dtype=torch.int32)), dict(bais=None)],
+                         ids=["mask-words", "mask-rows", "no-seed", "temperature-rows", "bias-alone", "bias-lengths", "own-history", "unknown"])
+def test_rules_that_do_not_fit_are_refused_before_anything_is_fed(decoder, rules):
+    light = decoder()
+    a, b = (ld.ld_kv_alloc(light.kv.h) for _ in range(2))
+    for s in (a, b):
+        light.prefill(s, [1, 2, 3])
+    before = _state(light, a), _state(light, b)
+    light.fed.clear()
+    for call in (lambda: light.step([a, b], **rules), lambda: light.prefill(a, [4], **{**rules, "temperature": torch.ones(2)})):
+        with pytest.raises((ld.LdError, TypeError)):
+            call()
+        assert light.fed == [] and (_state(light, a), _state(light, b)) == before
+    assert light.step([a, b]) == [5, 5]
 
 
 # ---------------------------------------------------------------- what the wrappers refuse before the library is called
