@@ -146,7 +146,7 @@ class LightDecoder:
         return x
 
     def _choose(self, x, seqs, rules):
-        """Logits of the rows of x and one token each, which becomes the sequence's pending one."""
+        """Logits of the rows of x and one token each, which becomes the sequence's pending one; -1 and none where the rules leave no token."""
         R = x.shape[0]
         logits, token = self.logits[:R], torch.empty(R, dtype=torch.int32, device=self.device)
         ld.ldk_linear_w4(self.lm_head, x, logits, g=self.final_norm, eps=self.shape.rms_eps, scratch=self.scratch)
@@ -158,11 +158,12 @@ class LightDecoder:
         if rules.get("temperature") is not None:
             rules = dict(rules, pos=length)
         ld.ldk_choose(logits, token, scratch=self.scratch, **rules)
-        # a row that the rules leave no token stays without a pending one: -1 is reported, and token 0 stands in its history
-        self.history[rows, length.long()] = token.clamp(min=0)
-        for s in seqs:
-            self.length[s] += 1
-        return token.tolist()
+        self.history[rows, length.long()] = token      # behind the end of a row that gets no token
+        token = token.tolist()
+        for s, t in zip(seqs, token):
+            if t >= 0:
+                self.length[s] += 1
+        return token
 
     def prefill(self, seq, tokens, **rules):
         """Feeds [pending?] ++ tokens and returns the token chosen after the last one.  rules: as in step."""
@@ -198,7 +199,8 @@ class LightDecoder:
             ld.ldk_kv_summary(self.kv.pool[l], self.table, ranges, n, sh.n_kv_heads, sh.head_dim, self.bounds[l], self.unit[l])
 
     def step(self, seqs, **rules):
-        """One decode iteration: feeds every sequence's pending token and returns the tokens chosen after them.  rules: ldk_choose's bias_start,
+        """One decode iteration: feeds every sequence's pending token and returns the tokens chosen after them (-1 where no token is allowed: that
+        sequence then has none pending, and goes on with a prefill).  rules: ldk_choose's bias_start,
         bias_token, bias, mask, mask_row, temperature and seed, a row per sequence (the histories are the decoder's own)."""
         if not 0 < len(seqs) <= self.max_rows or len(set(seqs)) != len(seqs):
             raise ValueError(f"step: between one and {self.max_rows} distinct sequences")

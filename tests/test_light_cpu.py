@@ -124,6 +124,29 @@ def test_rules_that_do_not_fit_are_refused_before_anything_is_fed(decoder, rules
     assert light.step([a, b]) == [5, 5]
 
 
+def test_a_row_without_an_allowed_token_has_no_pending_one(decoder):
+    """-1 is no token: the sequence cannot be stepped until tokens are fed again, and nothing but those is fed then."""
+    light = decoder()
+    a, b = (ld.ld_kv_alloc(light.kv.h) for _ in range(2))
+    for s in (a, b):
+        light.prefill(s, [1, 2, 3])
+    light.chosen = [[7, -1]]
+    assert light.step([a, b]) == [7, -1]
+    before = _state(light, a), _state(light, b)
+    light.fed.clear()
+    with pytest.raises(ValueError):
+        light.step([b])
+    with pytest.raises(ValueError):
+        light.step([a, b])
+    assert light.fed == [] and (_state(light, a), _state(light, b)) == before
+    assert light.step([a]) == [5] and light.prefill(b, [40, 41]) == 5
+    assert light.fed == [[7], [40, 41]] and light.history[b, :7].tolist() == [1, 2, 3, 5, 40, 41, 5]
+    light.chosen = [[-1]]
+    assert light.prefill(a, [9]) == -1
+    with pytest.raises(ValueError):
+        light.step([a])
+
+
 # ---------------------------------------------------------------- what the wrappers refuse before the library is called
 
 def _choice(R=3, V=1000):
