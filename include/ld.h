@@ -200,9 +200,10 @@ ld_status ld_kv_trim(ld_kv *kv, ld_seq seq, int32_t *released);
  * the emitted token will take as the counter, so a run is reproducible from (seed, tokens fed). */
 ld_status ld_kv_set_sampling(ld_kv *kv, ld_seq seq, float temperature, uint64_t seed);
 
-/* Test / benchmark hook: declare that the next n_tokens positions of a sequence are already
- * cached (their blocks are mapped; the caller has written, or will write, their keys and values
- * straight into the pool using the layout above), and set the pending token (none if < 0). */
+/* For callers that write keys and values themselves (a decoder made of the calls of ld_kernels.h, tests, benchmarks): declares
+ * that the next n_tokens positions of a sequence are already cached (their blocks are mapped; the caller has written, or will
+ * write, their keys and values straight into the pool using the layout above), and sets the pending token (< 0: the sequence has
+ * none afterwards, whatever it had). */
 ld_status ld_kv_assume(ld_kv *kv, ld_seq seq, int64_t n_tokens, int32_t pending);
 
 /* Prefill (prompt, or a tool observation appended to a live sequence): feeds

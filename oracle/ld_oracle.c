@@ -566,7 +566,7 @@ int64_t orc_kv_free_blocks(const orc_kv *kv) { return kv->n_free; }
 int64_t orc_kv_len(orc_kv *kv, int32_t s) { orc_seq *q = get_seq(kv, s); return q ? q->n_cached : -1; }
 
 /* Test hook: declare that the next n positions of a sequence are already cached, with keys and
- * values given as [n, layers, 2, kv_heads, hd] doubles (stored as given), and set the pending token. */
+ * values given as [n, layers, 2, kv_heads, hd] doubles (stored as given), and set the pending token (< 0: none). */
 int32_t orc_kv_inject(orc_kv *kv, int32_t s, const double *kvdata, int64_t n, int32_t pending)
 {
     orc_seq *q = get_seq(kv, s);
@@ -585,7 +585,8 @@ int32_t orc_kv_inject(orc_kv *kv, int32_t s, const double *kvdata, int64_t n, in
                     memcpy(kv_row(c, &v, l, w, hh, q->n_cached + p),
                            kvdata + ((((p * c->n_layers + l) * 2 + w) * Hk) + hh) * hd, sizeof(double) * hd);
     q->n_cached += n;
-    if (pending >= 0) { q->has_pending = 1; q->pending = pending; }
+    q->has_pending = pending >= 0;
+    if (pending >= 0) q->pending = pending;
     return ORC_OK;
 }
 

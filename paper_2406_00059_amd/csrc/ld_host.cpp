@@ -927,7 +927,8 @@ ld_status ld_kv_assume(ld_kv *kv, ld_seq seq, int64_t n_tokens, int32_t pending)
     if (count_missing(kv, seq, need) > (int64_t)kv->free_stack.size()) return fail(LD_E_NOMEM, "ld_kv_assume: out of KV blocks");
     map_blocks(kv, seq, need);
     q->n_cached += n_tokens;
-    if (pending >= 0) { q->pending = pending; q->has_pending = true; }
+    q->has_pending = pending >= 0;
+    if (pending >= 0) q->pending = pending;
     return LD_OK;
 }
 

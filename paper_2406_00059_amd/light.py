@@ -163,6 +163,7 @@ class LightDecoder:
         for s, t in zip(seqs, token):
             if t >= 0:
                 self.length[s] += 1
+                ld.ld_kv_assume(self.kv.h, s, 0, t)      # the engine's pending token (none since _map), should it carry the sequence on
         return token
 
     def prefill(self, seq, tokens, **rules):

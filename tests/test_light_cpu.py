@@ -147,6 +147,36 @@ def test_a_row_without_an_allowed_token_has_no_pending_one(decoder):
         light.step([a])
 
 
+def test_assume_without_a_pending_token_leaves_none(decoder):
+    kv = decoder().kv.h
+    s = ld.ld_kv_alloc(kv)
+    ld.ld_kv_assume(kv, s, 5, pending=7)
+    ld.ld_kv_assume(kv, s, 1)
+    rc, _ = ld.ld_decode_step(kv, [s], stream=0, check=False)
+    assert rc == ld.LD_E_STATE and "pending" in ld.ld_last_error() and ld.ld_kv_len(kv, s) == 6
+
+
+def test_the_engine_is_told_the_pending_token(decoder, monkeypatch):
+    """The engine's own pending token is the one chosen here, or none, so that its calls can carry a sequence on."""
+    light = decoder()
+    told = {}
+    real = ld.ld_kv_assume
+
+    def assume(kv, seq, n, pending=-1, check=True):
+        told[seq] = pending
+        return real(kv, seq, n, pending, check)
+    monkeypatch.setattr(binding, "ld_kv_assume", assume)
+    a, b = (ld.ld_kv_alloc(light.kv.h) for _ in range(2))
+    real(light.kv.h, a, 20, 900)      # fed by the engine, which holds token 900 back
+    light.refresh(a, range(20), 900)
+    light.prefill(b, [1, 2])
+    light.chosen = [[70, -1]]
+    light.step([a, b])
+    assert light.fed[-1] == [900, 5] and told == {a: 70, b: -1}
+    rc, _ = ld.ld_decode_step(light.kv.h, [b], stream=0, check=False)
+    assert rc == ld.LD_E_STATE and "pending" in ld.ld_last_error()
+
+
 # ---------------------------------------------------------------- what the wrappers refuse before the library is called
 
 def _choice(R=3, V=1000):
