@@ -158,6 +158,10 @@ ld_status ld_kv_free(ld_kv *kv, ld_seq seq);
 ld_status ld_kv_block_table(const ld_kv *kv, ld_seq seq, int32_t *out, int32_t cap, int32_t *n);
 /* Number of cached tokens of a sequence (-1 for a bad handle); number of free blocks. */
 int64_t ld_kv_len(const ld_kv *kv, ld_seq seq);
+/* A number > 0 (-1 for a bad handle) that no other sequence of the cache has had and that changes whenever the sequence gets other
+ * blocks than it had (ld_kv_alloc, ld_kv_fork for the child, ld_kv_swap_out, ld_kv_swap_in); positions that are added and blocks that
+ * ld_kv_trim gives up leave it.  For callers that keep something of their own about a sequence's blocks. */
+int64_t ld_kv_generation(const ld_kv *kv, ld_seq seq);
 int64_t ld_kv_free_blocks(const ld_kv *kv);
 /* KV retention across a tool call (section 2.2: a request that waits for a tool can keep its cache
  * on the GPU, swap it to host memory, or discard it and prefill again).  Discarding is ld_kv_free

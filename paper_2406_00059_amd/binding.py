@@ -23,7 +23,7 @@ __all__ = [
     "LD_CB_CONTINUE", "LD_CB_ABORT", "LD_CB_PAUSE",
     "LDK_STORE", "LDK_ADD", "LDK_SWIGLU", "LIB_PATH", "lib", "LdError", "ld_model_config", "ld_weights",
     "ld_token_cb", "ld_model_create", "ld_model_destroy", "ld_model_f16_image_bytes", "ld_model_attach_f16_image", "ld_kv_bytes", "ld_workspace_bytes", "ld_kv_create",
-    "ld_kv_destroy", "ld_kv_alloc", "ld_kv_map", "ld_kv_free", "ld_kv_block_table", "ld_kv_len",
+    "ld_kv_destroy", "ld_kv_alloc", "ld_kv_map", "ld_kv_free", "ld_kv_block_table", "ld_kv_len", "ld_kv_generation",
     "ld_kv_free_blocks", "ld_kv_assume", "ld_kv_swap_bytes", "ld_kv_swap_out", "ld_kv_swap_in", "ld_kv_fork", "ld_kv_trim", "ld_kv_set_sampling", "ld_prefill", "ld_decode_step", "ld_decode_run", "ld_step_mixed", "ld_last_error", "ld_kv_profile", "ld_kv_profile_read", "ld_profile", "LD_PROF_NAMES",
     "ldk_embed", "ldk_rmsnorm", "ldk_linear", "ldk_linear_f16", "ldk_weights_to_f16", "ldk_prefill_attention_f16", "ldk_linear_scratch_bytes", "ldk_rope_table", "ldk_rope_kv_write", "ldk_qkv_rope",
     "ldk_attention_scratch_bytes", "ldk_paged_attention", "ldk_static_scratch_bytes", "ldk_paged_attention_static",
@@ -85,6 +85,7 @@ _SIGS = {
     "ld_kv_free": (C.c_int, [_vp, C.c_int32]),
     "ld_kv_block_table": (C.c_int, [_vp, C.c_int32, _i32p, C.c_int32, _i32p]),
     "ld_kv_len": (C.c_int64, [_vp, C.c_int32]),
+    "ld_kv_generation": (C.c_int64, [_vp, C.c_int32]),
     "ld_kv_free_blocks": (C.c_int64, [_vp]),
     "ld_kv_assume": (C.c_int, [_vp, C.c_int32, C.c_int64, C.c_int32]),
     "ld_kv_set_sampling": (C.c_int, [_vp, C.c_int32, C.c_float, C.c_uint64]),
@@ -264,6 +265,10 @@ def ld_kv_block_table(kv, seq, cap=1 << 16):
 
 def ld_kv_len(kv, seq):
     return lib().ld_kv_len(kv, seq)
+
+
+def ld_kv_generation(kv, seq):
+    return lib().ld_kv_generation(kv, seq)
 
 
 def ld_kv_free_blocks(kv):

@@ -58,6 +58,7 @@ struct Seq {
     uint64_t seed = 0;
     int32_t pending = -1;
     int64_t n_cached = 0;
+    int64_t generation = 0;        // changes when the sequence gets other blocks than it had
     int32_t n_mapped = 0;          // logical blocks 0..n_mapped-1 may be mapped (holes possible via ld_kv_map)
     int32_t first_block = 0;       // logical blocks below it were released by ld_kv_trim (attention band)
     int32_t dirty_lo = 0, dirty_hi = 0;  // table entries [lo, hi) not yet copied to the device
@@ -140,6 +141,7 @@ struct ld_kv {
     std::vector<int32_t> free_stack;
     std::vector<int32_t> refs;   // sequences holding each block (prefix sharing); 0 = on the free stack
     std::vector<Seq> seqs;
+    int64_t generations = 0;
     std::vector<int32_t> table;  // host copy [max_seqs][max_blocks], -1 = unmapped
     // pinned staging, created by the first pass.  Metadata and emitted tokens are double-buffered (two
     // slots) so that a step can be prepared while the previous one is still in flight; step_ev[slot] marks
@@ -746,6 +748,7 @@ ld_status ld_kv_alloc(ld_kv *kv, int64_t reserve_tokens, ld_seq *out) {
     if (need > (int64_t)kv->free_stack.size()) return fail(LD_E_NOMEM, "ld_kv_alloc: out of KV blocks");
     kv->seqs[s] = Seq();
     kv->seqs[s].active = true;
+    kv->seqs[s].generation = ++kv->generations;
     map_blocks(kv, s, need);
     *out = s;
     return LD_OK;
@@ -790,6 +793,11 @@ int64_t ld_kv_len(const ld_kv *kv, ld_seq seq) {
     return q ? q->n_cached : -1;
 }
 
+int64_t ld_kv_generation(const ld_kv *kv, ld_seq seq) {
+    const Seq *q = get_seq(const_cast<ld_kv *>(kv), seq);
+    return q ? q->generation : -1;
+}
+
 int64_t ld_kv_free_blocks(const ld_kv *kv) { return kv ? (int64_t)kv->free_stack.size() : -1; }
 
 // Bytes of one block over all layers is n_layers pieces of block_bytes, one per layer slice of the pool.
@@ -823,6 +831,7 @@ ld_status ld_kv_swap_out(ld_kv *kv, ld_seq seq, void *host_buf, size_t bytes, vo
         }
     release_blocks(kv, seq);
     q->swapped = true;
+    q->generation = ++kv->generations;
     return LD_OK;
 }
 
@@ -846,6 +855,7 @@ ld_status ld_kv_swap_in(ld_kv *kv, ld_seq seq, const void *host_buf, size_t byte
             return fail(LD_E_HIP, "ld_kv_swap_in: hipMemcpy2DAsync failed");
         }
     q->swapped = false;
+    q->generation = ++kv->generations;
     return LD_OK;
 }
 
@@ -897,6 +907,7 @@ ld_status ld_kv_fork(ld_kv *kv, ld_seq parent, int64_t n_tokens, void *stream, l
     Seq &q = kv->seqs[s];
     q = Seq();
     q.active = true;
+    q.generation = ++kv->generations;
     q.n_cached = n_tokens;
     const int32_t fb = p->first_block;
     q.first_block = fb;

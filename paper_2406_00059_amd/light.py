@@ -4,7 +4,7 @@ The engine's calls (ld_prefill, ld_decode_step, ..) stream every bf16 matrix and
 LightDecoder runs the same decoder on the same paged cache with the kernel-level operators for that: ldk_linear_w4 for
 all matrices, ldk_kv_summary + ldk_sparse_attention for decode rows (prompt rows attend to everything before them), and
 ldk_choose, which keeps a tool call inside its grammar.  Blocks, sequences and positions are the KV object's: sequences are allocated, freed,
-swapped and forked there, and refresh() takes over one whose blocks were not filled here.
+swapped and forked there, and refresh() takes over one whose blocks were not filled here or have moved since.
 
     light = LightDecoder(model, kv, budget=64)
     seq = ld_kv_alloc(kv.h)
@@ -65,6 +65,7 @@ class LightDecoder:
         self.history = torch.zeros((n_seqs, max_ctx + 1), dtype=torch.int32, device=device)
         self.length = [0] * n_seqs           # tokens of the history: the cached ones and the pending one
         self.prompt = [0] * n_seqs
+        self.generation = [0] * n_seqs       # of the blocks that table and bounds are of
         self.penalties = None if penalties is None else torch.tensor([penalties] * T, **f)
 
     def _i32(self, v):
@@ -78,6 +79,13 @@ class LightDecoder:
             t = ld.ld_kv_block_table(self.kv.h, seq)
             self.table[seq, :t.size] = self._i32(t)
         return first
+
+    def _check_own(self, seq, new=False):
+        """Raises where the sequence holds blocks that the decoder has not filled or been shown (table and bounds are of others); new: it may hold none."""
+        if not 0 <= seq < len(self.length) or ld.ld_kv_len(self.kv.h, seq) < 0:
+            raise ValueError(f"no sequence {seq}")
+        if self.generation[seq] != ld.ld_kv_generation(self.kv.h, seq) and not (new and ld.ld_kv_len(self.kv.h, seq) == 0):
+            raise ValueError(f"the blocks of sequence {seq} were replaced (freed, forked or swapped): refresh it first")
 
     RULES = ("bias_start", "bias_token", "bias", "mask", "mask_row", "temperature", "seed")
 
@@ -101,12 +109,12 @@ class LightDecoder:
         """Raises what _map of one position for each of these sequences would end in, before any of them is mapped."""
         need = 0
         for s in seqs:
-            n, t = ld.ld_kv_len(self.kv.h, s), ld.ld_kv_block_table(self.kv.h, s)
-            if t.size * 16 < n:
-                raise ld.LdError(ld.LD_E_STATE, f"sequence {s} is swapped out")
+            n = ld.ld_kv_len(self.kv.h, s)
             if n // 16 >= self.kv.max_blocks:
                 raise ld.LdError(ld.LD_E_RANGE, f"sequence {s} is as long as its block table allows")
-            need += n % 16 == 0 and (n // 16 >= t.size or t[n // 16] < 0)
+            if n % 16 == 0:
+                t = ld.ld_kv_block_table(self.kv.h, s, self.kv.max_blocks)
+                need += n // 16 >= t.size or t[n // 16] < 0
         if need > ld.ld_kv_free_blocks(self.kv.h):
             raise ld.LdError(ld.LD_E_NOMEM, "out of KV blocks")
 
@@ -169,6 +177,7 @@ class LightDecoder:
     def prefill(self, seq, tokens, **rules):
         """Feeds [pending?] ++ tokens and returns the token chosen after the last one.  rules: as in step."""
         tokens = np.asarray(tokens, np.int32)
+        self._check_own(seq, new=True)
         first = ld.ld_kv_len(self.kv.h, seq)
         at = self.length[seq] if first else 0
         if at + tokens.size <= first:
@@ -177,6 +186,7 @@ class LightDecoder:
         self._map(seq, at + tokens.size - first)      # of the whole prompt: a shortage changes nothing
         self.history[seq, at:at + tokens.size] = self._i32(tokens)
         self.length[seq] = self.prompt[seq] = at + tokens.size
+        self.generation[seq] = ld.ld_kv_generation(self.kv.h, seq)
         while first < self.length[seq]:
             n = min(self.max_rows, self.length[seq] - first)
             x = self._pass(self.history[seq, first:first + n], [seq], [first], [n], False)[n - 1:n]
@@ -195,6 +205,7 @@ class LightDecoder:
         self.table[seq, :t.size] = self._i32(t)
         self.history[seq, :len(tokens)] = self._i32(tokens)
         self.length[seq], self.prompt[seq] = len(tokens), n
+        self.generation[seq] = ld.ld_kv_generation(self.kv.h, seq)
         ranges = self._i32([[seq, 0, n]])
         for l in range(sh.n_layers):
             ld.ldk_kv_summary(self.kv.pool[l], self.table, ranges, n, sh.n_kv_heads, sh.head_dim, self.bounds[l], self.unit[l])
@@ -205,6 +216,8 @@ class LightDecoder:
         bias_token, bias, mask, mask_row, temperature and seed, a row per sequence (the histories are the decoder's own)."""
         if not 0 < len(seqs) <= self.max_rows or len(set(seqs)) != len(seqs):
             raise ValueError(f"step: between one and {self.max_rows} distinct sequences")
+        for s in seqs:
+            self._check_own(s)
         if any(self.length[s] != ld.ld_kv_len(self.kv.h, s) + 1 for s in seqs):
             raise ValueError("step: a sequence without a pending token (prefill it, or refresh it first)")
         self._check_rules(len(seqs), rules)

@@ -177,6 +177,53 @@ def test_the_engine_is_told_the_pending_token(decoder, monkeypatch):
     assert rc == ld.LD_E_STATE and "pending" in ld.ld_last_error()
 
 
+@pytest.mark.parametrize("same", [False, True], ids=["other-blocks", "same-blocks"])
+def test_a_sequence_whose_blocks_were_replaced_has_to_be_refreshed(decoder, same):
+    """A handle that was freed and filled again elsewhere, to the same length: neither its block table nor its key bounds are the decoder's,
+    even where the blocks are the same ones.  Nothing is read or written before refresh."""
+    light = decoder()
+    h = light.kv.h
+    seq = ld.ld_kv_alloc(h)
+    light.prefill(seq, list(range(20)))
+    old = light.table[seq, :2].tolist()
+    ld.ld_kv_free(h, seq)
+    assert ld.ld_kv_alloc(h) == seq
+    if not same:
+        ld.ld_kv_assume(h, ld.ld_kv_alloc(h), 1)
+    ld.ld_kv_assume(h, seq, 20)
+    assert light.length[seq] == ld.ld_kv_len(h, seq) + 1 and (ld.ld_kv_block_table(h, seq).tolist() == old) == same
+    light.fed.clear()
+    before = _state(light, seq)
+    for call in (lambda: light.step([seq]), lambda: light.prefill(seq, [7])):
+        with pytest.raises(ValueError):
+            call()
+        assert light.fed == [] and _state(light, seq) == before
+    light.summed.clear()
+    light.refresh(seq, range(300, 320), 9)
+    assert light.table[seq, :2].tolist() == ld.ld_kv_block_table(h, seq).tolist() and light.summed == [[[seq, 0, 20]]] * TINY.n_layers
+    assert light.step([seq]) == [5] and light.fed == [[9]]
+
+
+def test_generation_of_a_sequence(decoder):
+    """A number of its own whenever a sequence gets other blocks than it had, the same one while blocks are only added or given up."""
+    h = decoder().kv.h
+    assert ld.ld_kv_generation(h, 0) == ld.ld_kv_generation(h, -1) == ld.ld_kv_generation(h, 99) == -1
+    a, b = ld.ld_kv_alloc(h, 40), ld.ld_kv_alloc(h)
+    seen = [ld.ld_kv_generation(h, a), ld.ld_kv_generation(h, b)]
+    ld.ld_kv_assume(h, b, 50)
+    ld.ld_kv_trim(h, b)
+    assert ld.ld_kv_generation(h, b) == seen[1]
+    ld.ld_kv_swap_out(h, a, None, stream=0)
+    seen.append(ld.ld_kv_generation(h, a))
+    ld.ld_kv_swap_in(h, a, None, stream=0)
+    seen.append(ld.ld_kv_generation(h, a))
+    ld.ld_kv_free(h, a)
+    assert ld.ld_kv_generation(h, a) == -1
+    assert ld.ld_kv_fork(h, b, 48, stream=0) == a      # whole blocks: nothing to copy
+    seen += [ld.ld_kv_generation(h, a)]
+    assert len(set(seen)) == len(seen) and min(seen) > 0 and ld.ld_kv_generation(h, b) == seen[1]
+
+
 # ---------------------------------------------------------------- what the wrappers refuse before the library is called
 
 def _choice(R=3, V=1000):

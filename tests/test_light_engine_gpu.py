@@ -45,3 +45,36 @@ def test_sequences_go_to_the_engine_and_back():
     light.refresh(fork, hist[:-2])
     light.prefill(fork, hist[-2:-1])
     assert ld.ld_kv_len(h, fork) == len(hist) - 1
+
+
+@pytest.mark.parametrize("shape", [TINY, replace(TINY, dtype="bf16", n_heads=4, n_kv_heads=2, head_dim=128, name="tiny-bf16-hd128-gqa")],
+                         ids=["f32", "bf16-gqa"])
+def test_a_swapped_sequence_goes_on_as_an_undisturbed_one(shape):
+    """Swapped out, its blocks taken and described by another sequence, swapped in on other blocks and on the same ones: refused until it is
+    refreshed, then token for token what a decoder without the swap gives."""
+    light = _light(shape, 13, n_blocks=60, group=64, budget=5, keep_last=2)
+    h, p = light.kv.h, prompt(13, 1, 150, shape.vocab)
+    s = ld.ld_kv_alloc(h)
+    want = [light.prefill(s, p)] + [light.step([s])[0] for _ in range(30)]
+    ld.ld_kv_free(h, s)
+    assert ld.ld_kv_alloc(h) == s
+    got = [light.prefill(s, p)] + [light.step([s])[0] for _ in range(10)]
+    for keep in (True, False):      # the other sequence keeps the blocks, or has freed them again
+        buf = torch.empty(ld.ld_kv_swap_bytes(h, s), dtype=torch.uint8, pin_memory=True)
+        ld.ld_kv_swap_out(h, s, buf)
+        other = ld.ld_kv_alloc(h)
+        light.prefill(other, prompt(13, 2, 170, shape.vocab))
+        if not keep:
+            ld.ld_kv_free(h, other)
+        old = light.table[s].tolist()
+        ld.ld_kv_swap_in(h, s, buf)
+        torch.cuda.synchronize()
+        n = ld.ld_kv_len(h, s)
+        with pytest.raises(ValueError):
+            light.step([s])
+        assert ld.ld_kv_len(h, s) == n
+        hist = p.tolist() + got
+        light.refresh(s, hist[:-1], hist[-1])
+        assert (light.table[s].tolist() != old) == keep
+        got += [light.step([s])[0] for _ in range(10)]
+    assert got == want
