@@ -180,6 +180,8 @@ class LightDecoder:
         self._check_own(seq, new=True)
         first = ld.ld_kv_len(self.kv.h, seq)
         at = self.length[seq] if first else 0
+        if not first <= at <= first + 1:
+            raise ValueError(f"prefill: sequence {seq} has positions that were fed elsewhere (refresh it first)")
         if at + tokens.size <= first:
             raise ValueError("prefill: no token to feed")
         self._check_rules(1, rules)

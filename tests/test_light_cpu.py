@@ -224,6 +224,23 @@ def test_generation_of_a_sequence(decoder):
     assert len(set(seen)) == len(seen) and min(seen) > 0 and ld.ld_kv_generation(h, b) == seen[1]
 
 
+def test_a_prompt_behind_positions_fed_elsewhere_is_refused(decoder):
+    """The engine has fed three more tokens: the decoder does not know them, so a prompt goes behind them only after refresh."""
+    light = decoder()
+    seq = ld.ld_kv_alloc(light.kv.h)
+    light.prefill(seq, list(range(20)))
+    ld.ld_kv_assume(light.kv.h, seq, 3, 77)
+    light.fed.clear()
+    before = _state(light, seq)
+    for tokens in ([7], list(range(100, 130))):
+        with pytest.raises(ValueError):
+            light.prefill(seq, tokens)
+        assert light.fed == [] and _state(light, seq) == before
+    light.refresh(seq, list(range(20)) + [5, 6, 7], 77)
+    light.prefill(seq, [8])
+    assert light.fed == [[77, 8]] and light.history[seq, :26].tolist() == list(range(20)) + [5, 6, 7, 77, 8, 5]
+
+
 # ---------------------------------------------------------------- what the wrappers refuse before the library is called
 
 def _choice(R=3, V=1000):
