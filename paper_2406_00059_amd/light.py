@@ -195,18 +195,28 @@ class LightDecoder:
             first += n
         return self._choose(x, [seq], rules)[0]
 
-    def refresh(self, seq, tokens, pending=None):
-        """Takes over a sequence whose cached positions were filled elsewhere (by the engine, a fork, a swap): its block table, its history
-        (tokens: those of the cached positions; pending: the one to be fed next) and the bounds of all its blocks."""
+    def refresh(self, seq, tokens=None, pending=None, n_prompt=None):
+        """Takes over a sequence whose cached positions were filled elsewhere (by the engine, a fork): its block table, its history (tokens: those of
+        the cached positions; pending: the one to be fed next; n_prompt: how many of them are prompt, all cached ones if not given) and the bounds of
+        all its blocks.  Without tokens: a sequence that was fed here and has only moved (a swap); its history stays."""
         n, sh = ld.ld_kv_len(self.kv.h, seq), self.shape
-        tokens = list(tokens) + ([] if pending is None else [pending])
-        if len(tokens) != n + (pending is not None):
-            raise ValueError(f"refresh: {n} cached positions")
+        if tokens is None:
+            if n < 0 or not n <= self.length[seq] <= n + 1 or pending is not None:
+                raise ValueError(f"refresh: the tokens of the {n} cached positions of sequence {seq} are not known here")
+            length, n_prompt = self.length[seq], self.prompt[seq] if n_prompt is None else n_prompt
+        else:
+            tokens = list(tokens) + ([] if pending is None else [pending])
+            length, n_prompt = len(tokens), n if n_prompt is None else n_prompt
+            if length != n + (pending is not None):
+                raise ValueError(f"refresh: {n} cached positions")
+        if not 0 <= n_prompt <= n:
+            raise ValueError(f"refresh: a prompt of {n_prompt} of {n} cached tokens")
         t = ld.ld_kv_block_table(self.kv.h, seq)
         self.table[seq] = -1
         self.table[seq, :t.size] = self._i32(t)
-        self.history[seq, :len(tokens)] = self._i32(tokens)
-        self.length[seq], self.prompt[seq] = len(tokens), n
+        if tokens is not None:
+            self.history[seq, :length] = self._i32(tokens)
+        self.length[seq], self.prompt[seq] = length, n_prompt
         self.generation[seq] = ld.ld_kv_generation(self.kv.h, seq)
         ranges = self._i32([[seq, 0, n]])
         for l in range(sh.n_layers):

@@ -241,6 +241,36 @@ def test_a_prompt_behind_positions_fed_elsewhere_is_refused(decoder):
     assert light.fed == [[77, 8]] and light.history[seq, :26].tolist() == list(range(20)) + [5, 6, 7, 77, 8, 5]
 
 
+def test_refresh_keeps_or_is_told_where_the_answer_begins(decoder):
+    """Presence and frequency count the answer's tokens: moving a sequence or taking over a fork does not turn them into prompt."""
+    light = decoder(penalties=(1.1, 0.5, 0.25))
+    h = light.kv.h
+    a = ld.ld_kv_alloc(h)
+    light.prefill(a, list(range(13)))
+    for _ in range(3):
+        light.step([a])
+    assert light.rules["n_prompt"].tolist() == [13] and light.rules["history_len"].tolist() == [16]
+    b = ld.ld_kv_fork(h, a, 16, stream=0)
+    hist = light.history[a, :17].tolist()
+    light.refresh(b, hist[:16], hist[16], n_prompt=13)
+    light.step([a, b])
+    assert light.rules["n_prompt"].tolist() == [13, 13] and light.rules["history"][0, :17].tolist() == light.rules["history"][1, :17].tolist() == hist
+    for bad in (-1, 18):
+        with pytest.raises(ValueError):
+            light.refresh(b, hist, 5, n_prompt=bad)
+    light.generation[a] = -1      # as a swap leaves it
+    light.summed.clear()
+    with pytest.raises(ValueError):
+        light.step([a])
+    light.refresh(a)              # the decoder's own tokens
+    assert light.summed == [[[a, 0, 17]]] * TINY.n_layers
+    light.step([a])
+    assert light.rules["n_prompt"].tolist() == [13] and light.rules["history"][0, :18].tolist() == hist + [5]
+    ld.ld_kv_assume(h, a, 2)
+    with pytest.raises(ValueError):
+        light.refresh(a)          # positions whose tokens the decoder does not know
+
+
 # ---------------------------------------------------------------- what the wrappers refuse before the library is called
 
 def _choice(R=3, V=1000):
