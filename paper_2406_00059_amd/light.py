@@ -71,6 +71,15 @@ class LightDecoder:
     def _i32(self, v):
         return torch.as_tensor(np.ascontiguousarray(v, dtype=np.int32)).to(self.device)
 
+    def _tokens(self, v):
+        """Token ids as an int32 array; the embedding is read by them."""
+        a = np.asarray(v)
+        if a.size == 0:
+            return np.empty(0, np.int32)
+        if a.ndim != 1 or a.dtype.kind not in "iu" or a.min() < 0 or a.max() >= self.shape.vocab:
+            raise ValueError(f"tokens have to be a sequence of whole numbers in 0 .. {self.shape.vocab - 1}")
+        return a.astype(np.int32)
+
     def _map(self, seq, n_tokens):
         """Maps the next n_tokens positions of a sequence and brings the device's copy of its block table up to date."""
         first = ld.ld_kv_len(self.kv.h, seq)
@@ -176,7 +185,7 @@ class LightDecoder:
 
     def prefill(self, seq, tokens, **rules):
         """Feeds [pending?] ++ tokens and returns the token chosen after the last one.  rules: as in step."""
-        tokens = np.asarray(tokens, np.int32)
+        tokens = self._tokens(tokens)
         self._check_own(seq, new=True)
         first = ld.ld_kv_len(self.kv.h, seq)
         at = self.length[seq] if first else 0
@@ -205,7 +214,7 @@ class LightDecoder:
                 raise ValueError(f"refresh: the tokens of the {n} cached positions of sequence {seq} are not known here")
             length, n_prompt = self.length[seq], self.prompt[seq] if n_prompt is None else n_prompt
         else:
-            tokens = list(tokens) + ([] if pending is None else [pending])
+            tokens = self._tokens(list(tokens) + ([] if pending is None else [pending]))
             length, n_prompt = len(tokens), n if n_prompt is None else n_prompt
             if length != n + (pending is not None):
                 raise ValueError(f"refresh: {n} cached positions")

@@ -271,6 +271,25 @@ def test_refresh_keeps_or_is_told_where_the_answer_begins(decoder):
         light.refresh(a)          # positions whose tokens the decoder does not know
 
 
+@pytest.mark.parametrize("bad", [[3, TINY.vocab], [-1], [1 << 40], [2.5], [[1, 2], [3, 4]]], ids=["vocabulary", "negative", "64-bit", "float", "two-dimensional"])
+def test_tokens_outside_the_vocabulary_are_refused(decoder, bad):
+    """The embedding's row of such a token would lie outside the matrix."""
+    light = decoder()
+    seq = ld.ld_kv_alloc(light.kv.h)
+    before = _state(light, seq)
+    with pytest.raises(ValueError):
+        light.prefill(seq, bad)
+    assert light.fed == [] and _state(light, seq) == before
+    ld.ld_kv_assume(light.kv.h, seq, 1)
+    with pytest.raises(ValueError):
+        light.refresh(seq, [3], bad[-1])
+    with pytest.raises(ValueError):
+        light.refresh(seq, bad[-1:])
+    assert light.length[seq] == 0
+    light.refresh(seq, [3], TINY.vocab - 1)
+    assert light.step([seq]) == [5] and light.fed == [[TINY.vocab - 1]]
+
+
 # ---------------------------------------------------------------- what the wrappers refuse before the library is called
 
 def _choice(R=3, V=1000):
