@@ -218,8 +218,8 @@ ld_status ldk_kv_summary(const void *pool_layer, int32_t dtype, const int32_t *t
  * index first among equal scores.  With q'_h the query head rounded to integers of v_h = 2^(floor(log2 max |q_h|) - 6),
  * clamped to +-127,
  *   score(b) = max over the KV head's query heads of v_h unit[b] sum_i (q'_i >= 0 ? q'_i bounds[b][0][i] : q'_i bounds[b][1][i]).
- * Sums of integers and powers of two: the choice depends on nothing but the row and the bounds (which every visible block must have).  A query
- * head with a NaN or an infinity scores 0 everywhere.
+ * Sums of integers and powers of two, rounded once, to float32 (beyond its range: an infinity): the choice depends on nothing but the row and the
+ * bounds (which every visible block must have).  A query head with a NaN or an infinity scores 0 everywhere.
  * out [T, H, hd]: softmax attention over the selected blocks' visible positions, arguments as in
  * ldk_paged_attention; ctx_len[t] may be 0: the row's out is 0 and it selects nothing.  max_ctx (HOST) >= every ctx_len.
  * sel (DEVICE, int32 [T, Hkv, budget]): the selected logical blocks, ascending, then -1.

@@ -159,11 +159,11 @@ __device__ __forceinline__ Visible visible(int ctx, int window) {
 // ---------------------------------------------------------------- scores
 
 // Up to 16 query heads of a KV head as operand columns of the integer matrix instructions: [head][positive parts, negative parts][hd]
-// bytes, and the units.  The positive parts meet the upper bounds, the negative ones the lower.
+// bytes, and the units' exponents.  The positive parts meet the upper bounds, the negative ones the lower.
 template <int HD>
 struct ScoreQueries {
     int8_t c[16][2 * HD + 16];      // rows 16 bytes apart from a multiple of the banks
-    float unit[16];
+    int unit[16];
 };
 // A wave a head (q: the first head's); a barrier has to follow.
 template <int HD>
@@ -186,14 +186,14 @@ __device__ __forceinline__ void quantise_queries(const float *__restrict__ q, in
             sq.c[g][lane + 64 * u] = (int8_t)max(c, 0);
             sq.c[g][HD + lane + 64 * u] = (int8_t)min(c, 0);
         }
-        if (lane == 0) sq.unit[g] = ldexpf(1.f, e);
+        if (lane == 0) sq.unit[g] = e;
     }
 }
 // A wave's operands: lane l holds head l % 16, bytes 64 j + 16 (l / 16) .. + 16.
 template <int HD>
 struct ScoreOperand {
     i32x4 b[HD / 32];
-    float unit;
+    int unit;
     bool real;
     __device__ __forceinline__ ScoreOperand(const ScoreQueries<HD> &sq, int heads, int lane) {
         const int g = min(lane & 15, heads - 1);
@@ -213,15 +213,16 @@ __device__ __forceinline__ float score_tile(const ScoreOperand<HD> &q, const int
     i32x4 a[HD / 32];
 #pragma unroll
     for (int j = 0; j < HD / 32; j++) a[j] = *reinterpret_cast<const i32x4 *>(rec + 64 * j);
-    const float un = unit[phys * Hkv + kvh];
+    const int un = (int)(__float_as_uint(unit[phys * Hkv + kvh]) >> 23) - 127;      // exponent of a power of two; 128: infinity
     i32x4 acc = (i32x4){0, 0, 0, 0};
 #pragma unroll
     for (int j = 0; j < HD / 32; j++) acc = __builtin_amdgcn_mfma_i32_16x16x64_i8(a[j], q.b[j], acc, 0, 0, 0);
     float s[4];
 #pragma unroll
     for (int i = 0; i < 4; i++) {
-        const float u = __shfl(un, 4 * h + i, WAVE);
-        s[i] = row_max(q.real ? (u < INFINITY ? (float)acc[i] * q.unit * u : INFINITY) : -INFINITY);
+        const int u = __shfl(un, 4 * h + i, WAVE);
+        // one scaling by both exponents: after the query's alone a score may lie outside the range that it ends in
+        s[i] = row_max(q.real ? (u < 128 ? ldexpf((float)acc[i], q.unit + u) : INFINITY) : -INFINITY);
     }
     const int i = lane & 3;
     return i == 0 ? s[0] : i == 1 ? s[1] : i == 2 ? s[2] : s[3];
