@@ -505,6 +505,8 @@ template <int HD, int NS>
 struct OnMatrixCores {
     typedef bf16_t KT;
     static constexpr int HEADS = 4 * NS;
+    static constexpr bool TERMS = true;
+    static constexpr int WORKGROUPS = NS == 2 ? 2 : HD == 64 ? 5 : 3;      // of k_sparse_row a CU, by registers
     struct Pair { u32x4 k[2][HD / 32], v[HD / 16]; };
     typedef uint16_t Queries[HEADS][3][HD];      // in LDS: the three terms
     bf16x8 q[NS][HD / 32];
@@ -611,6 +613,23 @@ struct OnMatrixCores {
             }
         }
     }
+    // Whether the wave's sums are numbers.  An infinite key or value times the terms of unlike sign, or the zero columns, is NaN, where the product
+    // itself may be -infinity (no weight) or infinite: attend_plainly then.  (A sum of everything times 0, 0 or NaN: an instruction a value.)
+    __device__ __forceinline__ bool finite() const {
+        float z = 0.f;
+#pragma unroll
+        for (int n = 0; n < NS; n++) {
+            z = fmaf(l[n], 0.f, z);
+#pragma unroll
+            for (int t = 0; t < HD / 16; t++)
+#pragma unroll
+                for (int i = 0; i < 4; i++) z = fmaf(o[n][t][i], 0.f, z);
+        }
+        return !__any(z != 0.f);
+    }
+    static __device__ __forceinline__ float query(const Queries &qs, int g, int d) {      // the three terms are the float
+        return bf16_to_f32(qs[g][0][d]) + bf16_to_f32(qs[g][1][d]) + bf16_to_f32(qs[g][2][d]);
+    }
     __device__ __forceinline__ void put(float *so, float *ml, int waves, int wave, int lane) const {
         const int g = lane & 15, h = lane >> 4;
 #pragma unroll
@@ -640,6 +659,8 @@ template <int HD>
 struct OnVectorUnits {
     typedef float KT;
     static constexpr int HEADS = 1;
+    static constexpr bool TERMS = false;
+    static constexpr int WORKGROUPS = 3;
     struct Block { float k[HD / 32][8], v[HD / 32][8]; };
     struct Pair { Block b[2]; };
     typedef float Queries[HD];
@@ -676,8 +697,8 @@ struct OnVectorUnits {
             for (int e = 0; e < 8; e++) s += qs[32 * j + 8 * (lane >> 4) + e] * d.k[j][e];
         s = across_rows(s, [](float a, float b) { return a + b; });
         if (!ok) s = -INFINITY;
-        const float m_new = fmaxf(m, row_max(s));      // a selected block holds a visible position
-        const float corr = fast_exp2(m - m_new), p = ok ? fast_exp2(s - m_new) : 0.f;
+        const float m_new = fmaxf(m, row_max(s)), at = m_new > -INFINITY ? m_new : 0.f;      // -inf: keys of -infinity so far, which have no weight
+        const float corr = fast_exp2(m - at), p = ok ? fast_exp2(s - at) : 0.f;
         m = m_new;
         l = l * corr + p;
         if (lane < 16) pl[lane] = p;
@@ -711,17 +732,78 @@ struct OnVectorUnits {
     }
 };
 
+// A wave's share again, product by product in float32, for what the terms cannot express (see finite): lane l has position l % 16 of a block and the
+// l / 16-th quarter of the dimensions for the scores, the dimensions l + 64 u for the values.  block(i, b, p): logical and physical block i < n.
+template <typename A, int HD, int W, typename Block>
+__device__ __forceinline__ void attend_plainly(const typename A::Queries &qs, int heads, const typename A::KT *__restrict__ pool, int64_t bs, int Hkv, int kvh,
+                                               int n, Block block, int start, int ctx, float *so, float *ml) {
+    int tid = threadIdx.x;
+    asm volatile("" : "+v"(tid));      // nothing of this rare path is computed ahead and kept in registers
+    const int lane = tid & 63, wave = tid >> 6;
+#pragma unroll 1
+    for (int g = 0; g < heads; g++) {
+        float m = -INFINITY, l = 0.f, o[HD / 64];
+        for (int u = 0; u < HD / 64; u++) o[u] = 0.f;
+#pragma unroll 1
+        for (int i = 2 * wave; i < n; i = (i & 1) ? i + 2 * W - 1 : i + 1) {
+            int b;
+            int64_t p;
+            block(i, b, p);
+            const typename A::KT *blk = pool + p * bs;
+            const int pos = b * 16 + (lane & 15);
+            const bool ok = pos >= start && pos < ctx;
+            float s = 0.f;
+#pragma unroll 1
+            for (int d = (lane >> 4) * (HD / 4); d < ((lane >> 4) + 1) * (HD / 4); d += 8) {
+                float v[8];
+                load8(blk + kv_k_offset(HD, kvh, lane & 15, d), v);
+                for (int e = 0; e < 8; e++) s += A::query(qs, g, d + e) * v[e];
+            }
+            s = across_rows(s, [](float a, float c) { return a + c; });
+            if (!ok) s = -INFINITY;
+            const float m_new = fmaxf(m, row_max(s)), at = m_new > -INFINITY ? m_new : 0.f;
+            const float corr = fast_exp2(m - at), w = ok ? fast_exp2(s - at) : 0.f;
+            m = m_new;
+            l = l * corr + w;
+            for (int u = 0; u < HD / 64; u++) {
+                o[u] *= corr;
+                const typename A::KT *vp = blk + kv_v_offset(Hkv, HD, kvh, 0, lane + 64 * u);
+#pragma unroll 1
+                for (int e = 0; e < 16; e++) {
+                    const float we = __shfl(w, e, WAVE);
+                    if (b * 16 + e >= start && b * 16 + e < ctx) o[u] += we * bf16_to_f32(vp[e]);
+                }
+            }
+        }
+        l = row_sum(l);
+        for (int u = 0; u < HD / 64; u++) so[(wave * A::HEADS + g) * HD + lane + 64 * u] = o[u];
+        if (lane == 0) {
+            ml[wave * A::HEADS + g] = m;
+            ml[(W + wave) * A::HEADS + g] = l;
+        }
+    }
+}
+
+template <typename A, int HD, int W, typename Block>
+__device__ __forceinline__ void put_wave(const A &a, const typename A::Queries &qs, int heads, const typename A::KT *__restrict__ pool, int64_t bs, int Hkv,
+                                         int kvh, int n, Block block, int start, int ctx, float *so, float *ml, int wave, int lane) {
+    if constexpr (A::TERMS)
+        if (__builtin_expect(!a.finite(), 0)) return attend_plainly<A, HD, W>(qs, heads, pool, bs, Hkv, kvh, n, block, start, ctx, so, ml);
+    a.put(so, ml, W, wave, lane);
+}
+
 // Output (d of head g) of a workgroup's waves, their sum and their common maximum.
 template <int HD, int HEADS, int W>
 __device__ __forceinline__ float join_waves(const float *so, const float *ml, int g, int d, float &M, float &L) {
     M = ml[g];
 #pragma unroll
     for (int w = 1; w < W; w++) M = fmaxf(M, ml[w * HEADS + g]);      // a wave that had no block: -inf, and its weight 0
+    const float at = M > -INFINITY ? M : 0.f;
     float o = 0.f;
     L = 0.f;
 #pragma unroll
     for (int w = 0; w < W; w++) {
-        const float a = fast_exp2(ml[w * HEADS + g] - M);
+        const float a = fast_exp2(ml[w * HEADS + g] - at);
         o += a * so[(w * HEADS + g) * HD + d];
         L += a * ml[(W + w) * HEADS + g];
     }
@@ -799,7 +881,8 @@ __global__ __launch_bounds__(64 * SPLIT_WAVES) void k_sparse_attend(const float 
             A::load(d, pool + p0 * bs, pool + p1 * bs, Hkv, kvh, lane);
             a.add(d, (v.b0 + b0) * 16, b1 >= 0 ? (v.b0 + b1) * 16 : -16, v.start, ctx, pl[wave], lane);
         }
-        a.put(so, ml, W, wave, lane);
+        put_wave<A, HD, W>(a, qs, heads, pool, bs, Hkv, kvh, i1 - i0, [&](int i, int &b, int64_t &p) { b = v.b0 + mine[i]; p = trow[mine[i]]; },
+                           v.start, ctx, so, ml, wave, lane);
         __syncthreads();
         for (int i = threadIdx.x; i < heads * HD; i += TH) {
             float M, L;
@@ -824,6 +907,7 @@ __global__ __launch_bounds__(64 * SPLIT_WAVES) void k_sparse_attend(const float 
         float M = -INFINITY, o = 0.f, L = 0.f;
 #pragma unroll 8
         for (int k = 0; k < real; k++) M = fmaxf(M, load_shared(part_ml + (base + k) * 2));
+        M = M > -INFINITY ? M : 0.f;
 #pragma unroll 8
         for (int k = 0; k < real; k++) {
             const float w = fast_exp2(load_shared(part_ml + (base + k) * 2) - M);
@@ -845,7 +929,7 @@ __global__ __launch_bounds__(256) void k_sparse_clear(int32_t *__restrict__ tick
 constexpr int FUSED_BLOCKS = 2048, FUSED_BUDGET = 1024, FUSED_WAVES = 4;
 
 template <typename A, int HD>
-__global__ __launch_bounds__(64 * FUSED_WAVES, A::HEADS <= 4 ? 3 : 2) void k_sparse_row(const float *__restrict__ q, int q_stride, const typename A::KT *__restrict__ pool,
+__global__ __launch_bounds__(64 * FUSED_WAVES, A::WORKGROUPS) void k_sparse_row(const float *__restrict__ q, int q_stride, const typename A::KT *__restrict__ pool,
                                                                  const int8_t *__restrict__ bounds, const float *__restrict__ unit, int Hkv,
                                                                  const int32_t *__restrict__ table, int table_stride,
                                                                  const int32_t *__restrict__ seq_slot, const int32_t *__restrict__ ctx_len,
@@ -908,7 +992,8 @@ __global__ __launch_bounds__(64 * FUSED_WAVES, A::HEADS <= 4 ? 3 : 2) void k_spa
             A::load(d, pool + p0 * bs, pool + p1 * bs, Hkv, kvh, lane);
             a.add(d, (v.b0 + b0) * 16, b1 >= 0 ? (v.b0 + b1) * 16 : -16, v.start, ctx, pl[wave], lane);
         }
-        a.put(so, ml, W, wave, lane);
+        put_wave<A, HD, W>(a, qs, heads, pool, bs, Hkv, kvh, n, [&](int i, int &b, int64_t &p) { b = v.b0 + list[i]; p = phys[list[i]]; },
+                           v.start, ctx, so, ml, wave, lane);
         __syncthreads();
         for (int i = threadIdx.x; i < heads * HD; i += 64 * W) {
             float M, L;
