@@ -194,7 +194,10 @@ ld_status ldk_w4_quantize(const void *W, int32_t dtype, int32_t N, int32_t K, in
 
 /* ldk_linear on such an image (same epilogues, same optional RMS normalisation of the input; the image's parts follow
  * from the epilogue).  x [T, K], y [T, N] dense row-major float32, which do not overlap.  The codes are exact in the products; the
- * activations enter as two fp16 terms of a row scaled by a power of two (22 significant bits), sums are float32.
+ * activations enter as two fp16 terms under a power of two of the row, sums are float32.  Of an activation at most 2^-22 of the largest of its
+ * 128 columns (128 j .. + 128) gets lost, 2^-25 where it is below a quarter of that, in either case no more than 2^-11 of itself; on top of it up to
+ * 2^-35 of the row's largest.  So columns beside one 2^12 and more times as large keep 11 bits of their own; where the large one's weight is zero (its
+ * code the zero point), nothing of it enters and the result shows that.
  * A row of x that holds a NaN or an infinity (after the normalisation) gives NaN in all of its outputs; no other row is touched by it.
  * scratch: ldk_linear_w4_scratch_bytes(T, N, K, epilogue) bytes, 16-byte aligned, needed at every T (up to 2^20); a buffer for more rows serves fewer. */
 size_t ldk_linear_w4_scratch_bytes(int32_t T, int32_t N, int32_t K, int32_t epilogue);

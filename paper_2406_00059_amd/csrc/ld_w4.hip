@@ -8,9 +8,10 @@
 // fp16 terms.  hi is a whole number of a quantum that 128 columns share, 2^-12 of the power of two below their largest magnitude:
 // |hi| <= 2^13 quanta, so the sum of 128 products with a code stays below 15 / 16 of 2^24 quanta and is exact in a float32
 // accumulator, in any order (the matrix cores cut what an addition shifts out, always downwards in magnitude: sums of unlike
-// exponents were 2.4e-6 off, relative 2-norm).  lo is what is left, rounded to fp16: at worst 2^-23 of the 128 columns' maximum
-// gets lost, 2^-25 for columns below a quarter of it.  The two terms meet the same codes in accumulators of their own.
-// Per group of G columns:  total[n] += s[n] (sum_k c hi + sum_k c lo - z[n] sum_k x), the sums of x formed with the split.
+// exponents were 2.4e-6 off, relative 2-norm).  lo is what is left (up to 2.5 quanta, half of one for columns below a quarter of the 128's
+// maximum), rounded to fp16: 2^-11 of it gets lost at most, that is 2^-22 and 2^-25 of the maximum, or, below fp16's normal numbers, 2^-25 of a unit, 16
+// times that for the columns divided by 16: 2^-35 of the row's largest magnitude.  The two terms meet the same codes in accumulators of their own.
+// Per group of G columns:  total[n] += s[n] (sum_k c hi + sum_k c lo - z[n] sum_k (hi + lo)), the sums formed with the split.
 // (The products of many rows with narrow groups take c - z in place of the subnormals, see ld_w4_tile.hip; the exactness of hi is the same.)
 //
 // Image of a matrix: tiles of 16 rows x 128 columns, 1 KB each, lane l's 16 bytes in a row, the tiles of 16 rows one

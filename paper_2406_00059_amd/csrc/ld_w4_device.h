@@ -45,8 +45,8 @@ __device__ __forceinline__ float swapped_half(float v) {
 __device__ __forceinline__ int row_exponent(float m) { return m < INFINITY && m > 0.f ? 14 - ilogbf(m) : 0; }
 
 // Columns c .. c + 3 of a row (c a multiple of 4; the 32 lanes of a half wave hold 128 columns), scaled by 2^k, as two fp16 terms:
-// put(c, hi, lo), and the sums of a group of G columns: put_sums(group, hi, lo), by one lane each.  SUBNORMAL: for codes_as_subnormals, the sums
-// 2^-24 times as large.
+// put(c, hi, lo), and the sums of a group of G columns: put_sums(group, hi, lo), by one lane each, of the terms as they are stored, so that a column
+// whose code is the zero point leaves nothing behind.  SUBNORMAL: for codes_as_subnormals, the sums 2^-24 times as large.
 template <bool SUBNORMAL, typename Put, typename Sums>
 __device__ __forceinline__ void split4(float (&v)[4], int k, int c, int G, Put put, Sums put_sums) {
     float sum_hi = 0.f, sum_lo = 0.f, most = 0.f;
@@ -62,12 +62,12 @@ __device__ __forceinline__ void split4(float (&v)[4], int k, int c, int G, Put p
     const float per_quantum = __uint_as_float((254u << 23) - __float_as_uint(quantum));      // its reciprocal
 #pragma unroll
     for (int e = 0; e < 4; e++) {
-        const float h = (float)(_Float16)(rintf(v[e] * per_quantum) * quantum);
         const float f = SUBNORMAL && e >= 2 ? 0.0625f : 1.f;      // e >= 2: codes in bits 4 .. 7
-        hi.h[e] = (_Float16)(h * f);
+        hi.h[e] = (_Float16)(rintf(v[e] * per_quantum) * quantum * f);
+        const float h = (float)hi.h[e] / f;
         lo.h[e] = (_Float16)((v[e] - h) * f);
         sum_hi += h;
-        sum_lo += v[e] - h;
+        sum_lo += (float)lo.h[e] / f;
     }
     put(c, hi.u, lo.u);
     sum_hi = lanes_sum(sum_hi, G / 4);

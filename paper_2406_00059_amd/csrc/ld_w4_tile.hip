@@ -184,6 +184,15 @@ __global__ __launch_bounds__(256, 2) void k_w4_tile(ld::W4Image w, ld::W4Rows r,
 #pragma unroll
                         for (int i = 0; i < NT; i++) lo[i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(a[i][j], bl, lo[i], 0, 0, 0);
                     }
+                    if constexpr (ZEROS) {      // on the exact sums, before the lo terms round them
+#pragma unroll
+                        for (int i = 0; i < NT; i++)
+#pragma unroll
+                            for (int e = 0; e < 4; e++) {
+                                d[i][e] += sz[i][e] * s_hi;
+                                lo[i][e] += sz[i][e] * s_lo;
+                            }
+                    }
 #pragma unroll
                     for (int i = 0; i < NT; i++) d[i] += lo[i];
                 } else {
@@ -201,10 +210,7 @@ __global__ __launch_bounds__(256, 2) void k_w4_tile(ld::W4Image w, ld::W4Rows r,
 #pragma unroll
                 for (int i = 0; i < NT; i++)
 #pragma unroll
-                    for (int e = 0; e < 4; e++) {
-                        if constexpr (ZEROS && SUBNORMAL) d[i][e] += sz[i][e] * (s_hi + s_lo);
-                        total[i][t][e] += sc[i][e] * d[i][e];
-                    }
+                    for (int e = 0; e < 4; e++) total[i][t][e] += sc[i][e] * d[i][e];
             }
         }
 #pragma unroll
