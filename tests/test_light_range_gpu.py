@@ -69,3 +69,78 @@ def test_a_row_whose_only_key_has_no_weight_is_nan(H, Hkv, hd, dtype):
         ref, want = _sparse64(q.numpy(), logical.double().numpy(), bounds, unit, *args)
     np.testing.assert_array_equal(sel.cpu().numpy(), want)
     assert torch.isnan(out[0]).all() and np.isnan(ref[0]).all() and _rel(out[1], torch.from_numpy(ref[1])) <= ATTENTION
+
+
+def _bf16(x):
+    return torch.from_numpy(np.asarray(x, np.float32)).bfloat16().float().numpy()
+
+
+def _third(x):
+    """What is left of float32 numbers behind two bf16 terms, and the two terms' sum."""
+    x = np.asarray(x, np.float32)
+    a = _bf16(x)
+    b = _bf16(x - a)
+    return (x - a) - b, a.astype(np.float64) + b
+
+
+@pytest.mark.parametrize("H,Hkv,hd", [(1, 1, 128), (2, 2, 64), (8, 1, 128), (6, 1, 64)])
+@pytest.mark.parametrize("blocks", [24, 700], ids=["one-launch", "two-launches"])
+def test_queries_keep_their_last_bits(H, Hkv, hd, blocks):
+    """Keys whose products with a query cancel while those with its bits behind the 16th add up.  A score is held to five roundings of 2^-23 of the
+    products' mass: up to four steps of 32 dimensions, each of which may cut 2^-23 of a partial sum of half the mass twice, and the query's scaling.
+    A query of two bf16 terms would be off by more than twice that, which the oracle with such queries shows."""
+    ctx = [16 * blocks - 3]
+    q, logical, table, slot = _sparse_case(104, torch.bfloat16, H, Hkv, hd, ctx)
+    scale = np.float32(np.float32(1.4426950408889634) / np.sqrt(np.float32(hd)))
+    q = (1.0 + q.abs() * 0.2) * q.sign()
+    q[0, 1:] = q[0, 0]      # one query: the keys are made for it
+    rest, two = _third(q[0, 0].numpy() * scale)
+    u = np.sign(rest) + (rest == 0)
+    side = q[0, 0].numpy() * u > 0
+    u[side] *= np.abs(q[0, 0].numpy()[~side]).sum() / np.abs(q[0, 0].numpy()[side]).sum()
+    sign = torch.where(torch.arange(16) % 2 == 0, 1.0, -1.0)
+    logical = logical.clone()
+    logical[:, 0] = (torch.from_numpy(u).float() * 16 * sign[:, None]).bfloat16()
+    logical[:, 1] = sign[:, None].bfloat16()
+    args = (table, slot, ctx, H, Hkv, hd, 0, 9, 1, 2)
+    out, sel, bounds, unit = _run_sparse(q, logical, *args)
+    keys = logical.double().numpy()
+    ref, want = _sparse64(q.numpy(), keys, bounds, unit, *args)
+    np.testing.assert_array_equal(sel.cpu().numpy(), want)
+    mass = np.abs(q[0, 0].double().numpy()) @ np.abs(keys[0, 0, 0, 0]) / np.sqrt(hd)
+    tol = 2.0 ** -23 * 5 * mass      # of the result too: two groups of positions whose scores are off in opposite directions weigh +1 and -1
+    planted = np.broadcast_to(two / (1.4426950408889634 / np.sqrt(hd)), (1, H, hd))
+    wrong, same = _sparse64(planted, keys, bounds, unit, *args)
+    np.testing.assert_array_equal(same, want)
+    assert np.abs(wrong - ref).min() > 2 * tol
+    assert np.abs(out.cpu().double().numpy() - ref).max() <= tol
+
+
+@pytest.mark.parametrize("H,Hkv,hd", [(1, 1, 128), (2, 2, 64), (8, 1, 128), (6, 1, 64)])
+@pytest.mark.parametrize("blocks", [24, 700], ids=["one-launch", "two-launches"])
+def test_probabilities_keep_their_last_bits(H, Hkv, hd, blocks):
+    """One position of a block has the maximum, the other fifteen a probability with a long third term; the values cancel.  The result is held to
+    eight roundings of 2^-23 of the values' mass; probabilities of two bf16 terms are off by more than twice that."""
+    ctx = [16 * blocks]
+    q, logical, table, slot = _sparse_case(105, torch.bfloat16, H, Hkv, hd, ctx)
+    q[:] = 0
+    q[..., 0] = 1
+    steps = np.arange(1, 200) / 16.0      # differences of the first key entry: exact in bf16
+    p = np.exp(-steps / np.sqrt(hd))
+    rest, _ = _third(p)
+    best = int(np.argmax(np.abs(rest) / p))
+    d, p, rest = steps[best], p[best], rest[best]
+    logical = logical.clone()
+    logical[:, 0] = 0
+    logical[:, 0, :, 1:, 0] = -d
+    low = float(torch.tensor(15 * p * 32).bfloat16())
+    logical[:, 1] = 32.0
+    logical[:, 1, :, 0] = -low
+    args = (table, slot, ctx, H, Hkv, hd, 0, 9, 1, 2)
+    out, sel, bounds, unit = _run_sparse(q, logical, *args)
+    ref, want = _sparse64(q.numpy(), logical.double().numpy(), bounds, unit, *args)
+    np.testing.assert_array_equal(sel.cpu().numpy(), want)
+    total = 1 + 15 * p
+    tol = 2.0 ** -23 * 8 * (low + 15 * p * 32) / total
+    assert abs(15 * rest * 32 / total) > 2 * tol
+    assert np.abs(out.cpu().double().numpy() - ref).max() <= tol
