@@ -177,7 +177,7 @@ ld_status ldk_sample(const float *logits, int32_t R, int32_t V, const float *tem
 
 /* 4-bit weights with group scales: W[n, k] = (c[n, k] - z[n, k / group]) * s[n, k / group], codes c in 0..15, group 32,
  * 64 or 128 input columns, scales s of scale_dtype (LD_F32 | LD_BF16), zero points z in 0..15 or, without them
- * (zeros NULL / 0), z = 8 everywhere.  Any N >= 1 and K >= 1; a last group may be short.
+ * (zeros NULL / 0), z = 8 everywhere.  Any N from 1 to 1048560 and K >= 1; a last group may be short.
  * ldk_linear_w4 reads a matrix from an image that is laid out once: `parts` matrices of N rows each (1; 2 for
  * LDK_SWIGLU: the gate rows, then the up rows), ldk_w4_image_bytes(...) bytes of DEVICE memory, 16-byte aligned.
  * ldk_w4_image_bytes returns 0 for arguments that no image has.

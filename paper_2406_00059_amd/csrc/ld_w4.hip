@@ -398,7 +398,7 @@ void launch_group(const ld::W4Image &w, int scale_dtype, const Few &a, hipStream
 // of the tiles, two rows: gated 2 x 13824 x 5120 21 / 27, 15360 x 5120 16 / 19; 4096 x 11008 24 / 21, 4096 x 14336 27 / 24.
 bool few_rows(int T, int K) { return (T == 1 && K <= 7 * 2048) || (T == 2 && K <= 3 * 2048); }
 
-constexpr int MOST_ROWS = 1 << 20;
+constexpr int MOST_ROWS = 1 << 20, MOST_OUTPUTS = 65535 * 16;      // of a call, of a part of an image
 
 bool bad_shape(int N, int K, int group, int parts, int scale_dtype) {
     return N <= 0 || K <= 0 || N > (1 << 28) || K > (1 << 28) || (group != 32 && group != 64 && group != 128) || (parts != 1 && parts != 2) ||
@@ -443,7 +443,7 @@ W4Rows w4_rows(void *scratch, int T, int K, size_t part_bytes, size_t *bytes) {
 extern "C" {
 
 size_t ldk_w4_image_bytes(int32_t N, int32_t K, int32_t group, int32_t parts, int32_t scale_dtype, int32_t zeros) {
-    if (bad_shape(N, K, group, parts, scale_dtype)) return 0;
+    if (bad_shape(N, K, group, parts, scale_dtype) || N > MOST_OUTPUTS) return 0;
     size_t bytes = 0;
     ld::w4_image(nullptr, N, K, group, parts, scale_dtype, zeros != 0, &bytes);
     return bytes;
@@ -456,7 +456,7 @@ ld_status ldk_w4_pack(const uint8_t *codes, const void *scales, int32_t scale_dt
     size_t need = 0;
     const ld::W4Image w = ld::w4_image(image, N, K, group, parts, scale_dtype, zeros != nullptr, &need);
     if (image_bytes < need) return ld::fail(LD_E_INVAL, "ldk_w4_pack: image too small");
-    if (w.row_tiles > 65535) return ld::fail(LD_E_RANGE, "ldk_w4_pack: more than 1048560 rows");
+    if (N > MOST_OUTPUTS) return ld::fail(LD_E_RANGE, "ldk_w4_pack: more than 1048560 rows");
     LD_LAUNCH(k_w4_pack, dim3(w.k_tiles, w.row_tiles, parts), dim3(256), 0, (hipStream_t)stream, codes, scales, scale_dtype, zeros, N, K, group, w);
     return launched("k_w4_pack");
 }
@@ -468,7 +468,7 @@ ld_status ldk_w4_quantize(const void *W, int32_t dtype, int32_t N, int32_t K, in
     size_t need = 0;
     const ld::W4Image w = ld::w4_image(image, N, K, group, parts, scale_dtype, zeros != 0, &need);
     if (image_bytes < need) return ld::fail(LD_E_INVAL, "ldk_w4_quantize: image too small");
-    if (w.row_tiles > 65535) return ld::fail(LD_E_RANGE, "ldk_w4_quantize: more than 1048560 rows");
+    if (N > MOST_OUTPUTS) return ld::fail(LD_E_RANGE, "ldk_w4_quantize: more than 1048560 rows");
     const dim3 grid(w.k_tiles, w.row_tiles, parts), block(256);
     hipStream_t s = (hipStream_t)stream;
     if (dtype == LD_BF16) LD_LAUNCH(k_w4_quantize<bf16_t>, grid, block, 0, s, (const bf16_t *)W, scale_dtype, N, K, group, w);

@@ -360,3 +360,12 @@ def test_linear_refuses_activations_of_other_types(name, bad, monkeypatch):
     with pytest.raises(ld.LdError) as e:
         ld.ldk_linear_w4(w, stream=0, **{**kw, name: bad})
     assert e.value.status == ld.LD_E_INVAL and len(calls) == 1
+
+
+def test_images_that_no_matrix_can_be_laid_out_in_have_no_size():
+    top, big = 65535 * 16, 1 << 60
+    assert ld.ldk_w4_image_bytes(top, 64, 64, 1, torch.float32, False) > 0
+    assert ld.ldk_w4_image_bytes(top + 1, 64, 64, 1, torch.float32, False) == 0
+    for call, args in (("ldk_w4_pack", (FAKE, FAKE, 0, None, top + 1, 64, 64, 1, FAKE, big, None)),
+                       ("ldk_w4_quantize", (FAKE, 1, top + 1, 64, 64, 1, 1, 0, FAKE, big, None))):
+        assert getattr(ld.lib(), call)(*args) == ld.LD_E_RANGE and call in ld.ld_last_error()
