@@ -582,11 +582,14 @@ def ldk_choose_scratch_bytes(R, V):
     return lib().ldk_choose_scratch_bytes(R, V)
 
 
+_BITS = {torch.int32: torch.uint32, torch.int64: torch.uint64}      # what else may hold bit patterns
+
+
 def _at(name, t, dtype, n):
     """Address of a contiguous tensor of n elements of a type; 0 for None."""
     if t is None:
         return 0
-    if t.dtype is not dtype or t.numel() != n or not t.is_contiguous():
+    if (t.dtype is not dtype and t.dtype is not _BITS.get(dtype)) or t.numel() != n or not t.is_contiguous():
         raise LdError(LD_E_INVAL, f"{name} has to be {n} elements of {dtype}, contiguous, not {t.dtype} {tuple(t.shape)}")
     return t.data_ptr()
 

@@ -322,6 +322,14 @@ def test_choice_refuses_tensors_that_do_not_fit(name, bad, monkeypatch):
     assert e.value.status == ld.LD_E_INVAL and name in str(e.value) and len(calls) == 1
 
 
+def test_choice_takes_bit_patterns_as_unsigned_numbers_too(monkeypatch):
+    calls = []
+    monkeypatch.setattr(binding.lib(), "ldk_choose", lambda *a: calls.append(a) or ld.LD_OK)
+    kw = _choice()
+    ld.ldk_choose(stream=0, **{**kw, "mask": kw["mask"].view(torch.uint32), "seed": kw["seed"].view(torch.uint64)})
+    assert len(calls) == 1
+
+
 @pytest.mark.parametrize("W", [torch.zeros(4, 64, dtype=torch.float16), torch.zeros(4, 64, dtype=torch.float64), torch.zeros(4, 64, dtype=torch.int32),
                                torch.zeros(256), torch.zeros(2, 2, 64)], ids=["fp16", "float64", "int32", "one-dimensional", "three-dimensional"])
 def test_quantise_refuses_matrices_of_other_types(W, monkeypatch):
