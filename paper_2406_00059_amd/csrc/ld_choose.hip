@@ -13,15 +13,6 @@ using namespace ldd;
 
 namespace {
 
-inline ld_status launched(const char *what) {
-    hipError_t e = hipGetLastError();
-    if (e != hipSuccess) {
-        ld::set_error("launch of %s failed: %s", what, hipGetErrorString(e));
-        return LD_E_HIP;
-    }
-    return LD_OK;
-}
-
 constexpr int THREADS = 1024, PER = 4;                        // tokens a thread has at once
 constexpr int LEAST = 2048, MOST = 8192;                      // tokens of a slice: 16 - 64 KB of LDS
 // Slices of a row, of whole thousands: as many as bring a workgroup to every CU.  A history is read once a slice.

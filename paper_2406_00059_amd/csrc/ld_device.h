@@ -9,6 +9,16 @@ namespace ldd {
 constexpr int WAVE = 64;
 typedef uint16_t bf16_t;
 
+// Status of the launches just made.
+inline ld_status launched(const char *what) {
+    hipError_t e = hipGetLastError();
+    if (e != hipSuccess) {
+        ld::set_error("launch of %s failed: %s", what, hipGetErrorString(e));
+        return LD_E_HIP;
+    }
+    return LD_OK;
+}
+
 // ---------------------------------------------------------------- element helpers
 
 __device__ __forceinline__ float bf16_to_f32(bf16_t b) { return __uint_as_float((uint32_t)b << 16); }

@@ -541,15 +541,6 @@ __global__ __launch_bounds__(1024) void k_sample(const float *__restrict__ logit
 
 // ---------------------------------------------------------------- launch helpers
 
-inline ld_status launched(const char *what) {
-    hipError_t e = hipGetLastError();
-    if (e != hipSuccess) {
-        ld::set_error("launch of %s failed: %s", what, hipGetErrorString(e));
-        return LD_E_HIP;
-    }
-    return LD_OK;
-}
-
 template <typename WT, int TT, int R, bool NORM>
 void launch_linear_epi(const WT *W, const float *x, const float *g, float eps, int T, int N, int K, int epi,
                        float *y, hipStream_t s) {

@@ -20,15 +20,6 @@ typedef __attribute__((ext_vector_type(4))) int32_t i32x4;
 typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;
 typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8;
 
-inline ld_status launched(const char *what) {
-    hipError_t e = hipGetLastError();
-    if (e != hipSuccess) {
-        ld::set_error("launch of %s failed: %s", what, hipGetErrorString(e));
-        return LD_E_HIP;
-    }
-    return LD_OK;
-}
-
 __device__ __forceinline__ uint32_t abs_bits(float v) { return __float_as_uint(v) & 0x7fffffffu; }
 constexpr uint32_t INF_BITS = 0x7f800000u;
 

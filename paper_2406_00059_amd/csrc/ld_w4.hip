@@ -27,15 +27,6 @@ using namespace ldw;
 
 namespace {
 
-inline ld_status launched(const char *what) {
-    hipError_t e = hipGetLastError();
-    if (e != hipSuccess) {
-        ld::set_error("launch of %s failed: %s", what, hipGetErrorString(e));
-        return LD_E_HIP;
-    }
-    return LD_OK;
-}
-
 // ---------------------------------------------------------------- laying a matrix out
 
 __device__ __forceinline__ int nibble_of(int e) { return (e >> 1) + 4 * (e & 1); }
