@@ -3,9 +3,9 @@
 // A block of 16 positions is described, per KV head, by the largest and the smallest value of its keys in every
 // dimension, as 8-bit integers of a power of two: with q rounded to 8-bit integers the same way,
 //   score = sum_i (q_i >= 0 ? q_i hi_i : q_i lo_i)
-// bounds q.k over the block's positions (up to the rounding of q).  Integer sums and powers of two: a score has one
-// value, however the work is cut, and so has the choice.  A block and head cost 2 hd + 4 bytes to score against
-// 64 hd to attend to (bf16).
+// is the most that q.k can be over the block's positions, up to the rounding of q and to a magnitude between 127 and 128 units, which counts as 127.
+// Integer sums and powers of two, rounded once: a score has one value, however the work is cut, and so has the choice.  A block and head cost 2 hd + 4
+// bytes to score against 64 hd to attend to (bf16).
 #include "ld_device.h"
 
 #include <algorithm>
@@ -810,7 +810,7 @@ __device__ __forceinline__ float load_shared(const float *p) { return __hip_atom
 // Second launch of the split form: gridDim.x workgroups a (row, KV head).  Each makes the choice by itself (it is the same in all of them,
 // and cheaper than a launch between), attends to its chunk of cb blocks and leaves its share; the one that draws the last ticket
 // joins the shares in their order.  chosen: the choice is in sel already (k_sparse_select_long).
-// 256 of 8192 blocks of 8 KV heads: 18 us, some 5 of them the choice and 4 the 17 MB of keys and values; both launches 24.
+// 256 of 8192 blocks of 8 KV heads: 18 us, some 5 of them the choice and 4 the 17 MB of keys and values (the rest not measured apart); both launches 24.
 constexpr int SPLIT_WAVES = 8, SPLIT_BLOCKS = 16384, SPLIT_BUDGET = 4096;
 template <typename A, int HD>
 __global__ __launch_bounds__(64 * SPLIT_WAVES) void k_sparse_attend(const float *__restrict__ q, int q_stride, const typename A::KT *__restrict__ pool,
@@ -1009,9 +1009,8 @@ bool fused_form(int T, int Hkv, int hd, int el, int nb, int budget) {
     return (int64_t)T * Hkv >= 256 || (int64_t)(nb > budget ? nb : 0) * 2 * hd + (int64_t)n * 32 * hd * el <= 176 << 10;
 }
 
-// Split form: as many chunks a (row, KV head) as bring a workgroup to every CU and no CU a second one (80 pairs, 280 KB each: 16 us with 240 workgroups,
-// 22 with 320), of two blocks at least.  The scratch holds scores, shares
-// and tickets.
+// Split form: as many chunks a (row, KV head) as bring a workgroup to every CU and, where the pairs alone do not, no CU a second one (80 pairs, 280 KB
+// each: 16 us with 240 workgroups, 22 with 320), of two blocks at least.  The scratch holds scores, shares and tickets.
 struct SparsePlan { int nb, stride, cb, chunks; size_t scores, part_o, part_ml, total; };
 SparsePlan sparse_plan(int T, int H, int Hkv, int hd, int max_ctx, int window, int budget) {
     SparsePlan p;

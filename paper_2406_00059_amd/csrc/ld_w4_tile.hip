@@ -6,11 +6,12 @@
 // unpacked once per group and meet TT x 2 operands there.
 // Groups of 128 take the codes as subnormals: 80 vector instructions for TT x 32 matrix instructions; what a group's sums owe to the zero
 // point 8 enters as the first matrix instruction's addend, and a group costs 2 vector instructions a value (add, multiply-add with the scale).
-// Groups of 32 and 64 have that cost four and two times as often, and vector and matrix instructions take turns on a SIMD rather than
-// run at the same time (counters, groups of 32: 86 k cycles of the one, 50 k of the other, in 141 k).  They take c - z (64 instructions more a column
-// tile) and add the lo products to the exact sum of the hi products: 1 vector instruction a value, no addend to prepare.
-// At 1056 rows the matrix cores run at what a large library product reaches: 13B gate/up (2 x 13824 x 5120, groups of 128) 500 us, 598 TFLOP/s
-// of the product, two terms executed: 1196 (library, fp16: 1173).  4096 x 11008, groups of 32, 257 rows: 72 us, vector instructions first.
+// Groups of 32 and 64 have that cost four and two times as often, and little of it runs beside the matrix instructions of the other wave of a
+// SIMD here (counters of 4096 x 11008, groups of 32, 257 rows: 47 k cycles a SIMD of vector and 50 k of matrix instructions in 114 k that a CU is
+// busy).  They take c - z (64 instructions more a column tile) and add the lo products to the exact sum of the hi products: 1 vector instruction a
+// value, no addend to prepare.  Zero points that are given cost groups of 128 two more: they meet the hi sums while those are exact.
+// At 1056 rows the matrix cores bound it: 13B gate/up (2 x 13824 x 5120, groups of 128) 497 us, 601 TFLOP/s of the product, two terms executed: 1.2 PFLOP/s
+// (a large library product in fp16: 1.1 - 1.5).  4096 x 11008, groups of 32, 257 rows: 72 us with split and join.
 #include "ld_w4_device.h"
 
 #include <algorithm>
