@@ -15,10 +15,10 @@ struct W4Image {
 
 constexpr int W4_NOT_FINITE = 1 << 20;
 
-// How the products of many rows take the codes: as subnormals (fewest instructions a code) with wide groups, as c - z (fewest a group's sum)
-// with narrow ones.  us, subnormals / c - z: 4096 x 11008 with groups of 32, 300 rows 95 / 80; 6144 x 4096 with groups of 64, 512 rows 77 / 71;
-// gated 2 x 13824 x 5120 with groups of 128, 1056 rows 494 / 523.
-constexpr bool w4_subnormal(int group) { return group == 128; }
+// How the products of many rows take the codes: as subnormals (fewest instructions a code) with wide groups and zero points 8, as c - z (fewest a group's
+// sum, and zero points cost nothing more) otherwise.  us, subnormals / c - z: 4096 x 11008 with groups of 32, 300 rows 95 / 80; 6144 x 4096 with groups of 64, 512 rows
+// 77 / 71; gated 2 x 13824 x 5120 with groups of 128, 1056 rows 494 / 523, with zero points given 592 / 528.
+constexpr bool w4_subnormal(int group, bool zeros) { return group == 128 && !zeros; }
 
 struct W4Rows {
     uint16_t *image;       // fp16 operands

@@ -12,7 +12,7 @@
 // maximum), rounded to fp16: 2^-11 of it gets lost at most, that is 2^-22 and 2^-25 of the maximum, or, below fp16's normal numbers, 2^-25 of a unit, 16
 // times that for the columns divided by 16: 2^-35 of the row's largest magnitude.  The two terms meet the same codes in accumulators of their own.
 // Per group of G columns:  total[n] += s[n] (sum_k c hi + sum_k c lo - z[n] sum_k (hi + lo)), the sums formed with the split.
-// (The products of many rows with narrow groups take c - z in place of the subnormals, see ld_w4_tile.hip; the exactness of hi is the same.)
+// (The products of many rows with narrow groups or zero points take c - z in place of the subnormals, see ld_w4_tile.hip; the exactness of hi is the same.)
 //
 // Image of a matrix: tiles of 16 rows x 128 columns, 1 KB each, lane l's 16 bytes in a row, the tiles of 16 rows one
 // after the other along K: a wave streams consecutive kilobytes.  Word j of lane l holds the columns 32 j + 8 (l / 16)
@@ -229,11 +229,11 @@ __global__ __launch_bounds__(SPLIT_THREADS) void k_w4_split(const float *__restr
     if (threadIdx.x == 0) r.expo[t] = expo;
 }
 
-void launch_split(const float *x, const float *g, float eps, int T, int K, int G, const ld::W4Rows &r, hipStream_t s) {
+void launch_split(const float *x, const float *g, float eps, int T, int K, int G, bool zeros, const ld::W4Rows &r, hipStream_t s) {
     const dim3 grid((T + 127) / 128 * 128), block(SPLIT_THREADS);
 #define LD_SPLIT(NC_)                                                                                          \
     do {                                                                                                       \
-        if (ld::w4_subnormal(G)) LD_LAUNCH((k_w4_split<NC_, true>), grid, block, 0, s, x, g, eps, T, K, G, r); \
+        if (ld::w4_subnormal(G, zeros)) LD_LAUNCH((k_w4_split<NC_, true>), grid, block, 0, s, x, g, eps, T, K, G, r); \
         else LD_LAUNCH((k_w4_split<NC_, false>), grid, block, 0, s, x, g, eps, T, K, G, r);                    \
     } while (0)
     if (K <= 2 * 2048) LD_SPLIT(2);
@@ -491,7 +491,7 @@ ld_status ldk_linear_w4(const void *image, int32_t scale_dtype, int32_t zeros, i
     const ld::W4Image w = ld::w4_image(image, N, K, group, epilogue == LDK_SWIGLU ? 2 : 1, scale_dtype, zeros != 0, nullptr);
     const ld::W4Rows r = ld::w4_rows(scratch, T, K, 0, nullptr);
     if (!few) {
-        launch_split(x, g, eps, T, K, group, r, s);
+        launch_split(x, g, eps, T, K, group, zeros != 0, r, s);
         ld::launch_w4_tile(w, scale_dtype, r, group, T, N, epilogue, plan, y, s);
         return launched("k_w4_tile");
     }

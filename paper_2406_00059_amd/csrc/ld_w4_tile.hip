@@ -6,16 +6,16 @@
 // unpacked once per group and meet TT x 2 operands there.
 // Groups of 128 take the codes as subnormals: 80 vector instructions for TT x 32 matrix instructions; what a group's sums owe to the zero
 // point 8 enters as the first matrix instruction's addend, and a group costs 2 vector instructions a value (add, multiply-add with the scale).
-// Groups of 32 and 64 have that cost four and two times as often, and little of it runs beside the matrix instructions of the other wave of a
+// Groups of 32 and 64 have that cost four and two times as often, zero points that are given would meet both terms' sums apart (2 more, for they
+// have to be taken off the hi sums while those are exact), and little of it runs beside the matrix instructions of the other wave of a
 // SIMD here (counters of 4096 x 11008, groups of 32, 257 rows: 47 k cycles a SIMD of vector and 50 k of matrix instructions in 114 k that a CU is
-// busy).  They take c - z (64 instructions more a column tile) and add the lo products to the exact sum of the hi products: 1 vector instruction a
-// value, no addend to prepare.  Zero points that are given cost groups of 128 two more: they meet the hi sums while those are exact.
+// busy).  These take c - z (64 instructions more a column tile) and add the lo products to the exact sum of the hi products: 1 vector instruction a
+// value, no addend to prepare.
 // At 1056 rows the matrix cores bound it: 13B gate/up (2 x 13824 x 5120, groups of 128) 497 us, 601 TFLOP/s of the product, two terms executed: 1.2 PFLOP/s
 // (a large library product in fp16: 1.1 - 1.5).  4096 x 11008, groups of 32, 257 rows: 72 us with split and join.
 #include "ld_w4_device.h"
 
 #include <algorithm>
-#include <type_traits>
 
 using namespace ldd;
 using namespace ldw;
@@ -51,12 +51,11 @@ template <int TT, int G, bool ZEROS, typename ST>
 __global__ __launch_bounds__(256, 2) void k_w4_tile(ld::W4Image w, ld::W4Rows r, int T, int N, int epilogue, int n_blocks, int t_blocks, int slabs,
                                                     float *__restrict__ y, float *__restrict__ part) {
     constexpr int PER = 128 / G, JG = G / 32;
-    constexpr bool SUBNORMAL = ld::w4_subnormal(G);
-    using Zero = std::conditional_t<SUBNORMAL, uint8_t, uint32_t>;      // z, or 1024 + z as two fp16
+    constexpr bool SUBNORMAL = ld::w4_subnormal(G, ZEROS);
     __shared__ __attribute__((aligned(16))) char sm_x[2][TT * 8192];
     __shared__ float sm_s[2][SUBNORMAL ? TT * PER * 32 : 1];
     __shared__ __attribute__((aligned(16))) float sm_w[2][PER][256];      // scales
-    __shared__ __attribute__((aligned(16))) Zero sm_z[2][PER][ZEROS ? 256 : 4];      // zero points
+    __shared__ __attribute__((aligned(16))) uint32_t sm_z[2][PER][ZEROS ? 256 : 4];      // zero points: 1024 + z as two fp16
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int col = lane & 15, h = lane >> 4;
     const bool pair = epilogue == LDK_SWIGLU;
@@ -110,7 +109,7 @@ __global__ __launch_bounds__(256, 2) void k_w4_tile(ld::W4Image w, ld::W4Rows r,
         for (int p = 0; p < PER; p++) {
             if constexpr (sizeof(ST) == 2) sm_w[stage][p][threadIdx.x] = bf16_to_f32(v.scale[p]);
             else sm_w[stage][p][threadIdx.x] = v.scale[p];
-            if constexpr (ZEROS) sm_z[stage][p][threadIdx.x] = SUBNORMAL ? (Zero)v.zero[p] : (Zero)(0x64006400u | v.zero[p] * 0x10001u);
+            if constexpr (ZEROS) sm_z[stage][p][threadIdx.x] = 0x64006400u | v.zero[p] * 0x10001u;
         }
     };
     auto load_codes = [&](int kt, u32x4 (&c)[NT]) {
@@ -144,20 +143,13 @@ __global__ __launch_bounds__(256, 2) void k_w4_tile(ld::W4Image w, ld::W4Rows r,
 #pragma unroll
             for (int i = 0; i < NT; i++) {
                 uint32_t z = 0x64086408u;      // 8
-                if constexpr (ZEROS && !SUBNORMAL) z = sm_z[stage][p][(wave * NT + i) * 16 + col];
+                if constexpr (ZEROS) z = sm_z[stage][p][(wave * NT + i) * 16 + col];
 #pragma unroll
                 for (int j = 0; j < JG; j++) a[i][j] = SUBNORMAL ? codes_as_subnormals(code[i][p * JG + j]) : codes_less(code[i][p * JG + j], z);
             }
-            f32x4 sc[NT], sz[NT];
+            f32x4 sc[NT];
 #pragma unroll
-            for (int i = 0; i < NT; i++) {
-                sc[i] = *reinterpret_cast<const f32x4 *>(&sm_w[stage][p][(wave * NT + i) * 16 + 4 * h]);
-                if constexpr (ZEROS && SUBNORMAL) {
-                    const uint32_t z = *reinterpret_cast<const uint32_t *>(&sm_z[stage][p][(wave * NT + i) * 16 + 4 * h]);
-#pragma unroll
-                    for (int e = 0; e < 4; e++) sz[i][e] = 8.f - (float)(z >> 8 * e & 255);
-                }
-            }
+            for (int i = 0; i < NT; i++) sc[i] = *reinterpret_cast<const f32x4 *>(&sm_w[stage][p][(wave * NT + i) * 16 + 4 * h]);
 #pragma unroll
             for (int t = 0; t < TT; t++) {
                 float s_hi = 0.f, s_lo = 0.f;
@@ -184,15 +176,6 @@ __global__ __launch_bounds__(256, 2) void k_w4_tile(ld::W4Image w, ld::W4Rows r,
                         for (int i = 0; i < NT; i++) d[i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(a[i][j], bh, d[i], 0, 0, 0);
 #pragma unroll
                         for (int i = 0; i < NT; i++) lo[i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(a[i][j], bl, lo[i], 0, 0, 0);
-                    }
-                    if constexpr (ZEROS) {      // on the exact sums, before the lo terms round them
-#pragma unroll
-                        for (int i = 0; i < NT; i++)
-#pragma unroll
-                            for (int e = 0; e < 4; e++) {
-                                d[i][e] += sz[i][e] * s_hi;
-                                lo[i][e] += sz[i][e] * s_lo;
-                            }
                     }
 #pragma unroll
                     for (int i = 0; i < NT; i++) d[i] += lo[i];
