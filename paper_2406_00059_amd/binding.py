@@ -582,7 +582,8 @@ def ldk_choose_scratch_bytes(R, V):
     return lib().ldk_choose_scratch_bytes(R, V)
 
 
-_BITS = {torch.int32: torch.uint32, torch.int64: torch.uint64}      # what else may hold bit patterns
+_I32, _I64, _F32 = torch.int32, torch.int64, torch.float32
+_BITS = {_I32: torch.uint32, _I64: torch.uint64}      # what else may hold bit patterns
 
 
 def _at(name, t, dtype, n):
@@ -615,13 +616,15 @@ def ldk_choose(logits, token, history=None, history_len=None, n_prompt=None, pen
         raise LdError(LD_E_INVAL, "ldk_choose: logits [R, V], history [R, n] and mask [rows, ceil(V / 32)] have two dimensions") from None
     n = 0 if bias is None else bias.numel()
     call = _nothing if check_only else (_lib or lib()).ldk_choose
-    i32, f32 = torch.int32, torch.float32
+    i32, f32 = _I32, _F32
     rules = _pack_rules(_at("history", history, i32, R * stride), _at("history_len", history_len, i32, R), _at("n_prompt", n_prompt, i32, R),
                         _at("penalties", penalties, f32, 3 * R), _at("bias_start", bias_start, i32, R + 1), _at("bias_token", bias_token, i32, n),
                         _at("bias", bias, f32, n), _at("mask", mask, i32, rows * ((V + 31) // 32)), _at("mask_row", mask_row, i32, R), stride, rows)
-    _check(call(_at("logits", logits, f32, R * V), R, V, rules, _at("temperature", temperature, f32, R), _at("seed", seed, torch.int64, R),
-                _at("pos", pos, i32, R), _at("adjusted", adjusted, f32, R * V), _at("token", token, i32, R), _ptr(scratch), _nbytes(scratch),
-                _stream(stream)))
+    rc = call(_at("logits", logits, f32, R * V), R, V, rules, _at("temperature", temperature, f32, R), _at("seed", seed, _I64, R),
+              _at("pos", pos, i32, R), _at("adjusted", adjusted, f32, R * V), _at("token", token, i32, R), _ptr(scratch), 0 if scratch is None else scratch.nbytes,
+              _raw_stream(_current_device()) if stream is None and _cuda_up() else _stream(stream))
+    if rc:
+        _check(rc)
 
 
 # ------------------------------------------------------------------ owners of handles + device memory
