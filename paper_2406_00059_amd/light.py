@@ -188,7 +188,7 @@ class LightDecoder:
         tokens = self._tokens(tokens)
         self._check_own(seq, new=True)
         first = ld.ld_kv_len(self.kv.h, seq)
-        at = self.length[seq] if first else 0
+        at = self.length[seq] if self.generation[seq] == ld.ld_kv_generation(self.kv.h, seq) else 0      # else a new sequence
         if not first <= at <= first + 1:
             raise ValueError(f"prefill: sequence {seq} has positions that were fed elsewhere (refresh it first)")
         if at + tokens.size <= first:

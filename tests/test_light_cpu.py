@@ -290,6 +290,19 @@ def test_tokens_outside_the_vocabulary_are_refused(decoder, bad):
     assert light.step([seq]) == [5] and light.fed == [[TINY.vocab - 1]]
 
 
+def test_a_prompt_behind_a_pending_token_without_cached_positions(decoder):
+    """[pending] ++ tokens, also where refresh has given an empty sequence its first token; a new sequence on the handle has none."""
+    light = decoder()
+    seq = ld.ld_kv_alloc(light.kv.h)
+    light.refresh(seq, [], 9)
+    light.prefill(seq, [6, 7])
+    assert light.fed == [[9, 6, 7]]
+    ld.ld_kv_free(light.kv.h, seq)
+    assert ld.ld_kv_alloc(light.kv.h) == seq
+    light.prefill(seq, [8])
+    assert light.fed[1:] == [[8]] and ld.ld_kv_len(light.kv.h, seq) == 1
+
+
 # ---------------------------------------------------------------- what the wrappers refuse before the library is called
 
 def _choice(R=3, V=1000):
