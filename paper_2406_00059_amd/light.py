@@ -221,6 +221,8 @@ class LightDecoder:
         if not 0 <= n_prompt <= n:
             raise ValueError(f"refresh: a prompt of {n_prompt} of {n} cached tokens")
         t = ld.ld_kv_block_table(self.kv.h, seq)
+        if t.size * 16 < n:
+            raise ValueError(f"refresh: sequence {seq} is swapped out")
         self.table[seq] = -1
         self.table[seq, :t.size] = self._i32(t)
         if tokens is not None:

@@ -303,6 +303,25 @@ def test_a_prompt_behind_a_pending_token_without_cached_positions(decoder):
     assert light.fed[1:] == [[8]] and ld.ld_kv_len(light.kv.h, seq) == 1
 
 
+def test_a_swapped_out_sequence_is_not_taken_over(decoder, monkeypatch):
+    """It holds no blocks: a step would move the sequences ahead of it before the cache refuses it."""
+    light = decoder()
+    a, b = (ld.ld_kv_alloc(light.kv.h) for _ in range(2))
+    for s in (a, b):
+        light.prefill(s, list(range(20)))
+    real = ld.ld_kv_block_table
+    monkeypatch.setattr(binding, "ld_kv_block_table", lambda kv, s, *cap: real(kv, s, *cap)[:0] if s == b else real(kv, s, *cap))      # as a swap leaves it
+    light.generation[b] = -1
+    light.summed.clear()
+    for call in (lambda: light.refresh(b), lambda: light.refresh(b, range(20), 5)):
+        with pytest.raises(ValueError):
+            call()
+    assert light.summed == [] and light.generation[b] == -1
+    with pytest.raises(ValueError):
+        light.step([a, b])
+    assert ld.ld_kv_len(light.kv.h, a) == 20
+
+
 # ---------------------------------------------------------------- what the wrappers refuse before the library is called
 
 def _choice(R=3, V=1000):
