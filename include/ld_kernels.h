@@ -259,6 +259,76 @@ size_t ldk_choose_scratch_bytes(int32_t R, int32_t V);
 ld_status ldk_choose(const float *logits, int32_t R, int32_t V, const ld_token_rules *rules, const float *temperature, const uint64_t *seed,
                      const int32_t *pos, float *adjusted, int32_t *token, void *scratch, size_t scratch_bytes, void *stream);
 
+/* ---- An 8-bit paged cache, and the attention that reads it. ---- */
+
+/* One layer's 8-bit pool.  The vector x[0 .. hd) of one position and KV head, a key or a value, stands as c[i] 2^e:
+ *   e = max(floor(log2 max |x|) - 6, -126) (-126 for a zero vector),  c[i] = x[i] 2^-e rounded to nearest, ties to even, within +-127.
+ * A vector with a NaN or an infinity (or beyond the range of float32) has e = -128, c = 0 and stands for NaN in every entry.
+ *   codes int8 [block][0][Hkv][16][hd] keys, [block][1][Hkv][hd][16] values (transposed, as in ldk_rope_kv_write's pool), 16-byte aligned;
+ *   expo  int8 [block][2][Hkv][16] (keys, values), 16-byte aligned.
+ * c 2^e is exact in bf16 and float32, so positions that go through a bf16 pool and back keep their codes.  What unwritten slots hold never
+ * reaches a result.  Tables, slots and positions as in ldk_rope_kv_write; hd is 64 or 128, H a multiple of Hkv.  In every call of this
+ * section blocks that a table does not map (entry < 0, or positions beyond table_stride blocks) are not touched: nothing is written to them, and no
+ * position of theirs is visible. */
+
+/* ldk_rope_table for any even rot >= 2 (the rotated part of a head; pairs i < rot / 2) and scaled frequencies: with f = rope_base^(-2i/rot),
+ *   r = original f / 2 pi (turns over the original context),  g = clamp((r - low) / (high - low), 0, 1),  f' = f ((1 - g) / factor + g),
+ *   cos_sin[t, i] = attention * (cos, sin)(pos[t] f'), float64 rounded once.
+ * original == 0: g = 0 (all frequencies divided by factor; low and high are not looked at).  scaling (HOST) NULL: f' = f, attention 1. */
+typedef struct {
+    float factor;      /* > 0 */
+    float low, high;   /* turns below which a frequency is divided by factor, above which it is kept; high > low */
+    int32_t original;  /* context length the model was trained on, >= 0 */
+    float attention;   /* on cos and sin, finite */
+} ld_rope_scaling;
+ld_status ldk_rope_table_scaled(const int32_t *pos, int32_t T, int32_t rot, float rope_base, const ld_rope_scaling *scaling, float *cos_sin,
+                                void *stream);
+
+/* ldk_rope_kv_write into an 8-bit pool, with the norms of q and k heads in the same pass.  Row t of qkv starts at qkv + t * qkv_stride (H q heads, Hkv k
+ * heads, Hkv v heads of hd floats).  With q_gain [hd]: every q head x becomes x / sqrt(mean x^2 + eps) * q_gain; k_gain likewise (NULL: none).
+ * Then the first rot (even, 0 .. hd) elements of q and k heads are rotated by cos_sin [T, rot / 2]: pair i = elements (i, i + rot / 2), or with
+ * interleaved != 0 (2i, 2i + 1).  q goes to q_out + t * q_out_stride [H hd]; q_out may be qkv itself with the same stride, otherwise they do not
+ * overlap.  k and v go into the pool.  Norms, rotation and codes are computed in float64: whichever order a sum takes, no code differs.  A row with
+ * pos[t] < 0 is padding: nothing of it is written.  Rows of one call address distinct (sequence, position) pairs. */
+ld_status ldk_rope_kv_write_q8(const float *qkv, int32_t qkv_stride, const float *q_gain, const float *k_gain, float eps, const float *cos_sin,
+                               int32_t rot, int32_t interleaved, const int32_t *pos, const int32_t *seq_slot, const int32_t *table,
+                               int32_t table_stride, int8_t *codes, int8_t *expo, int32_t T, int32_t H, int32_t Hkv, int32_t hd, float *q_out,
+                               int32_t q_out_stride, void *stream);
+
+/* Cached positions from a pool of the model's type (one layer, as ldk_rope_kv_write leaves it) into an 8-bit one, and back: a sequence that
+ * waits can be set aside at half its size.  ranges DEVICE int32 [n_ranges][3] = (block-table row, the same in both tables; first position; end):
+ * positions first .. end - 1 of row table of the source go to the same positions of the destination's table; nothing else is written.  max_len (HOST) >=
+ * end - first of every range, positions beyond it stay behind.  Ranges of one call name distinct positions. */
+ld_status ldk_kv_to_q8(const void *pool_layer, int32_t dtype, const int32_t *table, int32_t table_stride, int8_t *codes, int8_t *expo,
+                       const int32_t *q8_table, int32_t q8_table_stride, const int32_t *ranges, int32_t n_ranges, int32_t max_len, int32_t Hkv,
+                       int32_t hd, void *stream);
+ld_status ldk_kv_from_q8(const int8_t *codes, const int8_t *expo, const int32_t *q8_table, int32_t q8_table_stride, void *pool_layer, int32_t dtype,
+                         const int32_t *table, int32_t table_stride, const int32_t *ranges, int32_t n_ranges, int32_t max_len, int32_t Hkv,
+                         int32_t hd, void *stream);
+
+/* ldk_paged_attention over an 8-bit pool.  Row t, at position p = ctx_len[t] - 1, sees positions max(first[t], ctx_len[t] - window) .. p of its
+ * sequence (first NULL: 0; window 0: no band); ctx_len[t] may be 0, and a row that sees nothing gives 0.
+ *   s_j = q.k_j / sqrt(hd);  softcap > 0: s_j = softcap tanh(s_j / softcap);  slopes (DEVICE [H], may be NULL): s_j += slopes[h] (j - p);
+ *   out = sum_j softmax(s)_j v_j.
+ * A query head with a NaN or an infinity gives NaN, as does a head that sees a key or value that stands for NaN.  max_ctx (HOST) >= every ctx_len.
+ * scratch: ldk_attention_q8_scratch_bytes(...) bytes, 16-byte aligned (may be 0 bytes); a buffer for more rows or longer contexts serves less. */
+size_t ldk_attention_q8_scratch_bytes(int32_t T, int32_t H, int32_t Hkv, int32_t hd, int32_t max_ctx, int32_t window);
+ld_status ldk_paged_attention_q8(const float *q, int32_t q_stride, const int8_t *codes, const int8_t *expo, const int32_t *table,
+                                 int32_t table_stride, const int32_t *seq_slot, const int32_t *first, const int32_t *ctx_len, int32_t max_ctx,
+                                 int32_t T, int32_t H, int32_t Hkv, int32_t hd, int32_t window, float softcap, const float *slopes, float *out,
+                                 void *scratch, size_t scratch_bytes, void *stream);
+
+/* ldk_prefill_attention over an 8-bit pool.  tiles: DEVICE int32 [n_tiles][6] = (first row, number of rows 1 .. 128, position of the first row,
+ * block-table row, first visible position, prefix length).  The row at position p sees positions max(first visible, p - window + 1) ..
+ * max(p, prefix - 1): a band (window 0: none), a document's start and a prefix that sees all of itself; a row that sees nothing gives 0.
+ * Scores as in ldk_paged_attention_q8.  Rows that no tile names are left as they are.  max_pos (HOST) >= every max(p, prefix - 1).
+ * scratch: ldk_prefill_attention_q8_scratch_bytes(...) bytes, 16-byte aligned (may be 0 bytes); a buffer for more tiles or longer contexts serves less. */
+size_t ldk_prefill_attention_q8_scratch_bytes(int32_t n_tiles, int32_t H, int32_t Hkv, int32_t hd, int32_t max_pos, int32_t window);
+ld_status ldk_prefill_attention_q8(const float *q, int32_t q_stride, const int8_t *codes, const int8_t *expo, const int32_t *table,
+                                   int32_t table_stride, const int32_t *tiles, int32_t n_tiles, int32_t H, int32_t Hkv, int32_t hd, int32_t window,
+                                   float softcap, const float *slopes, int32_t max_pos, float *out, void *scratch, size_t scratch_bytes,
+                                   void *stream);
+
 #ifdef __cplusplus
 }
 #endif

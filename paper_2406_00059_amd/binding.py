@@ -30,6 +30,8 @@ __all__ = [
     "ldk_prefill_attention_scratch_bytes",
     "ldk_prefill_attention", "ldk_argmax", "ldk_sample", "Model", "KV",
     "ldk_w4_image_bytes", "ldk_w4_pack", "ldk_w4_quantize", "ldk_linear_w4_scratch_bytes", "ldk_linear_w4", "W4Matrix",
+    "ld_rope_scaling", "ldk_rope_table_scaled", "ldk_rope_kv_write_q8", "ldk_kv_to_q8", "ldk_kv_from_q8", "ldk_attention_q8_scratch_bytes",
+    "ldk_paged_attention_q8", "ldk_prefill_attention_q8_scratch_bytes", "ldk_prefill_attention_q8",
     "ldk_kv_summary", "ldk_sparse_attention_scratch_bytes", "ldk_sparse_attention", "ld_token_rules", "ldk_choose_scratch_bytes", "ldk_choose",
 ]
 
@@ -64,6 +66,10 @@ class ld_profile(C.Structure):
 class ld_token_rules(C.Structure):
     _fields_ = [(n, C.c_void_p) for n in ("history", "history_len", "n_prompt", "penalties", "bias_start", "bias_token", "bias",
                                           "mask", "mask_row")] + [("history_stride", C.c_int32), ("mask_rows", C.c_int32)]
+
+
+class ld_rope_scaling(C.Structure):
+    _fields_ = [("factor", C.c_float), ("low", C.c_float), ("high", C.c_float), ("original", C.c_int32), ("attention", C.c_float)]
 
 
 ld_token_cb = C.CFUNCTYPE(C.c_int, C.c_void_p, C.c_int32, C.c_int32, C.c_int32)
@@ -141,6 +147,17 @@ _SIGS = {
                              [_vp, _vp, _vp, C.c_size_t, _vp]),
     "ldk_choose_scratch_bytes": (C.c_size_t, [C.c_int32, C.c_int32]),
     "ldk_choose": (C.c_int, [_vp, C.c_int32, C.c_int32, _vp, _vp, _vp, _vp, _vp, _vp, _vp, C.c_size_t, _vp]),
+    "ldk_rope_table_scaled": (C.c_int, [_vp, C.c_int32, C.c_int32, C.c_float, _vp, _vp, _vp]),
+    "ldk_rope_kv_write_q8": (C.c_int, [_vp, C.c_int32, _vp, _vp, C.c_float, _vp, C.c_int32, C.c_int32, _vp, _vp, _vp, C.c_int32, _vp, _vp] +
+                             [C.c_int32] * 4 + [_vp, C.c_int32, _vp]),
+    "ldk_kv_to_q8": (C.c_int, [_vp, C.c_int32, _vp, C.c_int32, _vp, _vp, _vp, C.c_int32, _vp] + [C.c_int32] * 4 + [_vp]),
+    "ldk_kv_from_q8": (C.c_int, [_vp, _vp, _vp, C.c_int32, _vp, C.c_int32, _vp, C.c_int32, _vp] + [C.c_int32] * 4 + [_vp]),
+    "ldk_attention_q8_scratch_bytes": (C.c_size_t, [C.c_int32] * 6),
+    "ldk_paged_attention_q8": (C.c_int, [_vp, C.c_int32, _vp, _vp, _vp, C.c_int32, _vp, _vp, _vp] + [C.c_int32] * 6 +
+                               [C.c_float, _vp, _vp, _vp, C.c_size_t, _vp]),
+    "ldk_prefill_attention_q8_scratch_bytes": (C.c_size_t, [C.c_int32] * 6),
+    "ldk_prefill_attention_q8": (C.c_int, [_vp, C.c_int32, _vp, _vp, _vp, C.c_int32, _vp] + [C.c_int32] * 5 +
+                                 [C.c_float, _vp, C.c_int32, _vp, _vp, C.c_size_t, _vp]),
 }
 EXPORTS = tuple(_SIGS)
 
@@ -625,6 +642,121 @@ def ldk_choose(logits, token, history=None, history_len=None, n_prompt=None, pen
               _raw_stream(_current_device()) if stream is None and _cuda_up() else _stream(stream))
     if rc:
         _check(rc)
+
+
+# 8-bit cache.  The kernels read by the lengths that the arguments imply: types and sizes are checked here, where they are known.
+
+def _refuse(what):
+    raise LdError(LD_E_INVAL, what)
+
+
+def _q8_layer(call, codes, expo, Hkv, hd):
+    """Addresses of a layer's codes int8 [blocks, 2, Hkv, 16, hd] and exponents int8 [blocks, 2, Hkv, 16]."""
+    n = expo.numel()
+    if Hkv < 1 or hd < 1 or codes.dtype is not torch.int8 or expo.dtype is not torch.int8 or codes.numel() != n * hd or n % (32 * Hkv) or not codes.is_contiguous() or \
+            not expo.is_contiguous():
+        _refuse(f"{call}: codes int8 [blocks, 2, {Hkv}, 16, {hd}] and expo int8 [blocks, 2, {Hkv}, 16], contiguous, not {codes.dtype} {tuple(codes.shape)} "
+                f"and {expo.dtype} {tuple(expo.shape)}")
+    return codes.data_ptr(), expo.data_ptr()
+
+
+def _q8_table(call, table):
+    if table.dtype is not _I32 or table.dim() != 2 or not table.is_contiguous():
+        _refuse(f"{call}: a block table is int32 [rows, blocks], contiguous, not {table.dtype} {tuple(table.shape)}")
+    return table.data_ptr()
+
+
+def _rows_of(call, t, what, stride, width, n=None):
+    """Address of float32 rows that are `stride` elements apart, `width` of them used, n rows in all (None: as many as the tensor holds)."""
+    if t.dtype is not _F32 or not t.is_contiguous():
+        _refuse(f"{call}: {what} has to be float32, contiguous, not {t.dtype} {tuple(t.shape)}")
+    if stride < width or (n and t.numel() < (n - 1) * stride + width):
+        _refuse(f"{call}: {what} of {t.numel()} elements does not hold {n} rows of {width}, {stride} apart")
+    return t.data_ptr()
+
+
+def ldk_rope_table_scaled(pos, rot, rope_base, cos_sin, factor=1.0, low=0.0, high=0.0, original=0, attention=1.0, stream=None):
+    """pos int32 [T], cos_sin float32 [T, rot / 2, 2]; the other numbers as in ld_rope_scaling."""
+    T = pos.numel()
+    scaling = ld_rope_scaling(factor, low, high, original, attention)
+    _check(lib().ldk_rope_table_scaled(_at("pos", pos, _I32, T), T, rot, rope_base, C.addressof(scaling), _at("cos_sin", cos_sin, _F32, T * max(rot, 0)),
+                                       _stream(stream)))
+
+
+def ldk_rope_kv_write_q8(qkv, cos_sin, pos, seq_slot, table, codes, expo, H, Hkv, hd, q_out, rot=None, interleaved=False, q_gain=None, k_gain=None,
+                         eps=0.0, stream=None):
+    """qkv float32 [T, at least (H + 2 Hkv) hd], q_out float32 [T, at least H hd] (or qkv itself); rot: rotated elements of a head (all of them if not
+    given), cos_sin float32 [T, rot / 2, 2] (None for rot 0); gains float32 [hd] or None; codes and expo: a layer of the 8-bit pool."""
+    call = "ldk_rope_kv_write_q8"
+    rot = hd if rot is None else rot
+    T = pos.numel()
+    if qkv.dim() != 2 or q_out.dim() < 2 or qkv.shape[0] != T or q_out.shape[0] != T:
+        _refuse(f"{call}: qkv and q_out have a row for each of the {T} positions, not {tuple(qkv.shape)} and {tuple(q_out.shape)}")
+    qs, os_ = qkv.shape[1], q_out.numel() // T if T else H * hd
+    c, e = _q8_layer(call, codes, expo, Hkv, hd)
+    _check((_lib or lib()).ldk_rope_kv_write_q8(
+        _rows_of(call, qkv, "qkv", qs, (H + 2 * Hkv) * hd, T), qs, _at("q_gain", q_gain, _F32, hd), _at("k_gain", k_gain, _F32, hd), eps,
+        _at("cos_sin", cos_sin, _F32, T * rot), rot, int(interleaved), _at("pos", pos, _I32, T), _at("seq_slot", seq_slot, _I32, T),
+        _q8_table(call, table), table.shape[1], c, e, T, H, Hkv, hd, _rows_of(call, q_out, "q_out", os_, H * hd, T), os_, _stream(stream)))
+
+
+def _move(call, pool_layer, table, codes, expo, q8_table, ranges, Hkv, hd):
+    """(pool, table), (codes and expo, 8-bit table) and ranges as arguments of the two moves; their types and sizes."""
+    if Hkv < 1 or hd < 1 or pool_layer.dtype not in _W4_FLOATS or not pool_layer.is_contiguous() or pool_layer.numel() % (32 * Hkv * hd):
+        _refuse(f"{call}: a pool is bf16 or float32 [blocks, 2, {Hkv}, 16, {hd}], contiguous, not {pool_layer.dtype} {tuple(pool_layer.shape)}")
+    if ranges.dim() != 2 or ranges.shape[1] != 3:
+        _refuse(f"{call}: ranges int32 [n, 3], not {tuple(ranges.shape)}")
+    return ((pool_layer.data_ptr(), _dt(pool_layer.dtype), _q8_table(call, table), table.shape[1]),
+            (*_q8_layer(call, codes, expo, Hkv, hd), _q8_table(call, q8_table), q8_table.shape[1]),
+            (_at("ranges", ranges, _I32, ranges.numel()), ranges.shape[0]))
+
+
+def ldk_kv_to_q8(pool_layer, table, codes, expo, q8_table, ranges, max_len, Hkv, hd, stream=None):
+    """ranges int32 [n, 3]: (row of both block tables, first position, end)."""
+    src, dst, r = _move("ldk_kv_to_q8", pool_layer, table, codes, expo, q8_table, ranges, Hkv, hd)
+    _check((_lib or lib()).ldk_kv_to_q8(*src, *dst, *r, max_len, Hkv, hd, _stream(stream)))
+
+
+def ldk_kv_from_q8(codes, expo, q8_table, pool_layer, table, ranges, max_len, Hkv, hd, stream=None):
+    dst, src, r = _move("ldk_kv_from_q8", pool_layer, table, codes, expo, q8_table, ranges, Hkv, hd)
+    _check((_lib or lib()).ldk_kv_from_q8(*src, *dst, *r, max_len, Hkv, hd, _stream(stream)))
+
+
+def ldk_attention_q8_scratch_bytes(T, H, Hkv, hd, max_ctx, window=0):
+    return lib().ldk_attention_q8_scratch_bytes(T, H, Hkv, hd, max_ctx, window)
+
+
+def ldk_paged_attention_q8(q, q_stride, codes, expo, table, seq_slot, ctx_len, max_ctx, H, Hkv, hd, out, scratch, window=0, first=None, softcap=0.0,
+                           slopes=None, stream=None):
+    """q float32, rows q_stride elements apart; seq_slot, ctx_len, first int32 [T]; slopes float32 [H]; out float32 [T, H, hd]."""
+    call = "ldk_paged_attention_q8"
+    T = ctx_len.numel()
+    c, e = _q8_layer(call, codes, expo, Hkv, hd)
+    _check((_lib or lib()).ldk_paged_attention_q8(
+        _rows_of(call, q, "q", q_stride, H * hd, T), q_stride, c, e, _q8_table(call, table), table.shape[1], _at("seq_slot", seq_slot, _I32, T),
+        _at("first", first, _I32, T), _at("ctx_len", ctx_len, _I32, T), max_ctx, T, H, Hkv, hd, window, softcap, _at("slopes", slopes, _F32, H),
+        _at("out", out, _F32, T * H * hd), _ptr(scratch), _nbytes(scratch), _stream(stream)))
+
+
+def ldk_prefill_attention_q8_scratch_bytes(n_tiles, H, Hkv, hd, max_pos, window=0):
+    return lib().ldk_prefill_attention_q8_scratch_bytes(n_tiles, H, Hkv, hd, max_pos, window)
+
+
+def ldk_prefill_attention_q8(q, q_stride, codes, expo, table, tiles, H, Hkv, hd, out, max_pos, window=0, softcap=0.0, slopes=None, scratch=None,
+                             stream=None):
+    """q float32, rows q_stride elements apart; tiles int32 [n, 6]: (first row, rows, position of the first row, table row, first visible position,
+    prefix); out float32 [rows, H, hd]."""
+    call = "ldk_prefill_attention_q8"
+    if tiles.dim() != 2 or tiles.shape[1] != 6:
+        _refuse(f"{call}: tiles int32 [n, 6], not {tuple(tiles.shape)}")
+    c, e = _q8_layer(call, codes, expo, Hkv, hd)
+    if H < 1:
+        _refuse(f"{call}: {H} heads")
+    rows = out.numel() // (H * hd)
+    _check((_lib or lib()).ldk_prefill_attention_q8(
+        _rows_of(call, q, "q", q_stride, H * hd, rows), q_stride, c, e, _q8_table(call, table), table.shape[1],
+        _at("tiles", tiles, _I32, tiles.numel()), tiles.shape[0], H, Hkv, hd, window, softcap, _at("slopes", slopes, _F32, H), max_pos,
+        _at("out", out, _F32, rows * H * hd), _ptr(scratch), _nbytes(scratch), _stream(stream)))
 
 
 # ------------------------------------------------------------------ owners of handles + device memory
