@@ -1,5 +1,6 @@
 // The 8-bit cache: layout of a layer, and what its kernels share.
 #pragma once
+#include <cmath>
 #include "ld_device.h"
 
 namespace ldd {
@@ -38,6 +39,12 @@ struct Q8Attention {
     float *out;
 };
 
+inline bool bad_attention(const Q8Attention &a, int hd) {
+    return !a.q || !a.codes || !a.expo || (((uintptr_t)a.codes | (uintptr_t)a.expo) & 15) || !a.table || a.table_stride < 0 || a.H <= 0 || a.Hkv <= 0 ||
+           a.H % a.Hkv || (hd != 64 && hd != 128) || (int64_t)a.q_stride < (int64_t)a.H * hd || a.window < 0 || !(a.softcap >= 0.f) ||
+           !std::isfinite(a.softcap) || !a.out;
+}
+
 // cap tanh(s / cap).  Small arguments by the odd series (next term 2e-9 of the sum at 0.25), the others by the exponential, which would
 // cancel there.
 __device__ __forceinline__ float q8_cap(float s, float cap, float inv_cap) {
@@ -45,6 +52,51 @@ __device__ __forceinline__ float q8_cap(float s, float cap, float inv_cap) {
     const float series = x * (1.f + x2 * (-1.f / 3 + x2 * (2.f / 15 + x2 * (-17.f / 315 + x2 * (62.f / 2835)))));
     const float t = fast_exp2(-2.8853900817779268f * x);
     return copysignf(cap * (x < 0.25f ? series : (1.f - t) / (1.f + t)), s);
+}
+
+typedef int i32x4_t __attribute__((ext_vector_type(4)));
+typedef float f32x4_t __attribute__((ext_vector_type(4)));
+typedef _Float16 f16x2_t __attribute__((ext_vector_type(2)));
+typedef _Float16 f16x8_t __attribute__((ext_vector_type(8)));
+
+// Eight codes (two words) as fp16, exact: a byte c + 128 under the exponent of 1024 is the fp16 number 1152 + c.
+__device__ __forceinline__ f16x8_t q8_halves(uint32_t w0, uint32_t w1) {
+    const f16x2_t bias = {(_Float16)1152.f, (_Float16)1152.f};
+    const uint32_t a = w0 ^ 0x80808080u, b = w1 ^ 0x80808080u;
+    f16x2_t h[4];
+    h[0] = __builtin_bit_cast(f16x2_t, __builtin_amdgcn_perm(0x64646464u, a, 0x04010400u)) - bias;
+    h[1] = __builtin_bit_cast(f16x2_t, __builtin_amdgcn_perm(0x64646464u, a, 0x04030402u)) - bias;
+    h[2] = __builtin_bit_cast(f16x2_t, __builtin_amdgcn_perm(0x64646464u, b, 0x04010400u)) - bias;
+    h[3] = __builtin_bit_cast(f16x2_t, __builtin_amdgcn_perm(0x64646464u, b, 0x04030402u)) - bias;
+    return (f16x8_t){h[0][0], h[0][1], h[1][0], h[1][1], h[2][0], h[2][1], h[3][0], h[3][1]};
+}
+
+// A query as whole numbers n = round(8355711 q / max |q|), three base-256 digits from -128 .. 127 each: q = n unit 2^exp, |n - exact| <= 1/2.
+struct Q8Query {
+    double scale;      // 8355711 / max |q|, 0 for a query that is zero or not finite
+    float unit;        // in 1 .. 2; NaN for a query that is not finite
+    int exp;
+};
+// top: the bits of max |q| (which order as the numbers do; above infinity's: a NaN).  factor: what scores are multiplied by besides.
+__device__ __forceinline__ Q8Query q8_query(uint32_t top, double factor) {
+    Q8Query r{0.0, 1.f, 0};
+    if (top >= 0x7f800000u) {
+        r.unit = __uint_as_float(0x7fc00000u);
+    } else if (top) {
+        const double most = (double)__uint_as_float(top);
+        r.scale = 8355711.0 / most;
+        const double u = most * factor * (1.0 / 8355711.0);
+        r.exp = (int)((__double2hiint(u) >> 20) & 0x7ff) - 1023;
+        r.unit = (float)__longlong_as_double((__double_as_longlong(u) & 0xfffffffffffffll) | 0x3ff0000000000000ll);
+    }
+    return r;
+}
+// Digit 2 (of 65536), 1 (of 256) or 0.
+__device__ __forceinline__ int q8_digit(float q, double scale, int digit) {
+    int n = (int)rint(q * scale);
+    if (scale == 0.0) n = 0;
+    const int d0 = (int8_t)n, n1 = (n - d0) >> 8, d1 = (int8_t)n1, d2 = (n1 - d1) >> 8;
+    return digit == 2 ? d2 : digit == 1 ? d1 : d0;
 }
 
 }  // namespace ldd

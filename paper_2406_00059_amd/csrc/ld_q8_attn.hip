@@ -55,15 +55,6 @@ __device__ void attend(const Q8Attention &a, int row, int h, int p, int lo, int 
 }
 
 template <int HD>
-__global__ __launch_bounds__(64) void k_paged_q8(Q8Attention a, const int32_t *seq_slot, const int32_t *first, const int32_t *ctx_len, int max_ctx) {
-    __shared__ float qs[HD], ws[64];
-    const int t = blockIdx.x, h = blockIdx.y;
-    const int ctx = min(ctx_len[t], max_ctx);
-    const int lo = max(max(first ? first[t] : 0, a.window > 0 ? ctx - a.window : 0), 0);
-    attend<HD>(a, t, h, ctx - 1, lo, ctx - 1, a.table + (int64_t)seq_slot[t] * a.table_stride, qs, ws);
-}
-
-template <int HD>
 __global__ __launch_bounds__(64) void k_prefill_q8(Q8Attention a, const int32_t *tiles, int max_pos) {
     __shared__ float qs[HD], ws[64];
     const int32_t *tile = tiles + 6 * blockIdx.x;
@@ -74,33 +65,9 @@ __global__ __launch_bounds__(64) void k_prefill_q8(Q8Attention a, const int32_t 
     attend<HD>(a, tile[0] + r, h, p, lo, min(max(p, tile[5] - 1), max_pos), a.table + (int64_t)tile[3] * a.table_stride, qs, ws);
 }
 
-bool bad_attention(const float *q, int q_stride, const int8_t *codes, const int8_t *expo, const int32_t *table, int table_stride, int H, int Hkv, int hd,
-                   int window, float softcap, const float *out) {
-    return !q || !codes || !expo || (((uintptr_t)codes | (uintptr_t)expo) & 15) || !table || table_stride < 0 || H <= 0 || Hkv <= 0 || H % Hkv ||
-           (hd != 64 && hd != 128) || (int64_t)q_stride < (int64_t)H * hd || window < 0 || !(softcap >= 0.f) || !std::isfinite(softcap) || !out;
-}
-
 }  // namespace
 
 extern "C" {
-
-size_t ldk_attention_q8_scratch_bytes(int32_t T, int32_t H, int32_t Hkv, int32_t hd, int32_t max_ctx, int32_t window) { return 0; }
-
-ld_status ldk_paged_attention_q8(const float *q, int32_t q_stride, const int8_t *codes, const int8_t *expo, const int32_t *table,
-                                 int32_t table_stride, const int32_t *seq_slot, const int32_t *first, const int32_t *ctx_len, int32_t max_ctx,
-                                 int32_t T, int32_t H, int32_t Hkv, int32_t hd, int32_t window, float softcap, const float *slopes, float *out,
-                                 void *scratch, size_t scratch_bytes, void *stream) {
-    if (T == 0) return LD_OK;
-    if (T < 0 || max_ctx < 0 || !seq_slot || !ctx_len ||
-        bad_attention(q, q_stride, codes, expo, table, table_stride, H, Hkv, hd, window, softcap, out))
-        return ld::fail(LD_E_INVAL, "ldk_paged_attention_q8: bad argument");
-    if (H > 65535) return ld::fail(LD_E_RANGE, "ldk_paged_attention_q8: more than 65535 heads");
-    const Q8Attention a{q, q_stride, codes, expo, table, table_stride, H, Hkv, window, softcap, slopes, out};
-    hipStream_t s = (hipStream_t)stream;
-    if (hd == 128) LD_LAUNCH(k_paged_q8<128>, dim3(T, H), dim3(64), 0, s, a, seq_slot, first, ctx_len, max_ctx);
-    else LD_LAUNCH(k_paged_q8<64>, dim3(T, H), dim3(64), 0, s, a, seq_slot, first, ctx_len, max_ctx);
-    return launched("k_paged_q8");
-}
 
 size_t ldk_prefill_attention_q8_scratch_bytes(int32_t n_tiles, int32_t H, int32_t Hkv, int32_t hd, int32_t max_pos, int32_t window) { return 0; }
 
@@ -109,10 +76,10 @@ ld_status ldk_prefill_attention_q8(const float *q, int32_t q_stride, const int8_
                                    float softcap, const float *slopes, int32_t max_pos, float *out, void *scratch, size_t scratch_bytes,
                                    void *stream) {
     if (n_tiles == 0) return LD_OK;
-    if (n_tiles < 0 || max_pos < 0 || !tiles || bad_attention(q, q_stride, codes, expo, table, table_stride, H, Hkv, hd, window, softcap, out))
+    const Q8Attention a{q, q_stride, codes, expo, table, table_stride, H, Hkv, window, softcap, slopes, out};
+    if (n_tiles < 0 || max_pos < 0 || !tiles || bad_attention(a, hd))
         return ld::fail(LD_E_INVAL, "ldk_prefill_attention_q8: bad argument");
     if (H > 65535) return ld::fail(LD_E_RANGE, "ldk_prefill_attention_q8: more than 65535 heads");
-    const Q8Attention a{q, q_stride, codes, expo, table, table_stride, H, Hkv, window, softcap, slopes, out};
     hipStream_t s = (hipStream_t)stream;
     if (hd == 128) LD_LAUNCH(k_prefill_q8<128>, dim3(n_tiles, H, 128), dim3(64), 0, s, a, tiles, max_pos);
     else LD_LAUNCH(k_prefill_q8<64>, dim3(n_tiles, H, 128), dim3(64), 0, s, a, tiles, max_pos);

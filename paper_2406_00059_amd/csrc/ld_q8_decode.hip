@@ -1,0 +1,389 @@
+// Attention of single tokens over the 8-bit cache on the matrix cores.
+//
+// A workgroup of four waves takes one row, KV head and chunk of the sequence, a wave 64 positions (four blocks) at a time, which it loads
+// straight into operand registers; nothing goes through LDS but the join of the waves.  The G query heads of the KV head, padded to GP = 1, 2, 4, 8 or 16,
+// share the 16 columns of a tile with their terms: column c is head c % GP and term c / GP.
+//
+//   scores   S^T[pos, c] = K[pos, :] . Q[c, :] in whole numbers (16x16x64, 8 bits): a query is three base-256 digits (24 bits under its largest
+//            entry), the keys enter as they lie in the cache.  One product where three terms find room beside the heads (GP <= 4), two or three else; a
+//            rotation within 16 lanes adds the terms, scaled to float32, so that every column of a head holds its score.
+//   sums     O^T[d, c] += V^T[d, pos] W^T[pos, c] (16x16x32, fp16): codes are exact in fp16; W = p 2^(e - k), e the value's exponent and k
+//            the running largest of p 2^e in the column, as two fp16 terms (22 bits) in two columns.
+//
+// Which position a row of the score tile is, is free: row 4 g + i of tile t is slot 4 t + i of block g, so lane (c, g) ends with the scores of
+// block g, slot by slot, which is what it has to bring as the other operand of the sums.
+#include <algorithm>
+#include <cmath>
+#include "ld_q8.h"
+
+using namespace ldd;
+
+namespace {
+
+constexpr int TILE = 64, WAVES = 4;
+
+// Positions lo .. hi that a row sees; hi < lo: none.
+struct Seen { int lo, hi; };
+__device__ __forceinline__ Seen seen_of(int ctx_len, int first, int max_ctx, int window, int table_stride) {
+    const int ctx = (int)min((int64_t)min(ctx_len, max_ctx), (int64_t)table_stride * 16);
+    return {max(max(first, window > 0 ? ctx_len - window : 0), 0), ctx - 1};
+}
+
+// x summed over the lanes of 16 that hold the same head's terms; the same bits in all of them.
+template <int GP>
+__device__ __forceinline__ float sum_terms(float x) {
+#define LD_ROR(N_) __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), 0x120 + N_, 0xf, 0xf, true))
+    if constexpr (GP <= 8) x += LD_ROR(8);
+    if constexpr (GP <= 4) x += LD_ROR(4);
+    if constexpr (GP <= 2) x += LD_ROR(2);
+    if constexpr (GP <= 1) x += LD_ROR(1);
+#undef LD_ROR
+    return x;
+}
+
+template <int HD, int GP, bool EXTRA>
+__global__ __launch_bounds__(64 * WAVES, 2) void k_decode_q8(Q8Attention a, const int32_t *__restrict__ seq_slot, const int32_t *__restrict__ first,
+                                                             const int32_t *__restrict__ ctx_len, int max_ctx, int chunk, int chunks, float *__restrict__ part_o,
+                                                             float2 *__restrict__ part_ml) {
+    constexpr int KS = HD / 64, ND = HD / 16, TERMS = 16 / GP, PASSES = (3 + TERMS - 1) / TERMS;
+    const int t = blockIdx.x / chunks, ch = blockIdx.x % chunks;
+    const int G = a.H / a.Hkv, parts = (G + 15) / 16, j = blockIdx.y / parts, h0 = j * G + blockIdx.y % parts * 16, heads = min(G - (int)(blockIdx.y % parts) * 16, 16);
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = lane & 15, g = lane >> 4, head = c % GP, term = c / GP;
+    const int len = ctx_len[t];
+    const Seen see = seen_of(len, first ? first[t] : 0, max_ctx, a.window, a.table_stride);
+    const int t0 = (see.lo >> 6) + ch * chunk, t1 = min(t0 + chunk, (see.hi >> 6) + 1);
+    if (see.hi < see.lo || t0 >= t1) {
+        if (chunks == 1)
+            for (int i = threadIdx.x; i < heads * HD; i += 64 * WAVES) a.out[((int64_t)t * a.H + h0) * HD + i] = 0.f;
+        return;
+    }
+    const int32_t *trow = a.table + (int64_t)seq_slot[t] * a.table_stride;
+    const int last = see.hi >> 4;      // last visible block
+    const int64_t bs = q8_block(a.Hkv, HD);
+    const int8_t *kbase = a.codes + q8_k(HD, j, c & 3, 16 * g), *vbase = a.codes + q8_v(a.Hkv, HD, j, 0, c);
+
+    // Queries: dims 64 s + 16 g .. + 16 of this lane's head and term
+    i32x4_t qd[PASSES][KS];
+    float weight[PASSES];
+    Q8Query query;
+    {
+        const float *qp = a.q + (int64_t)t * a.q_stride + (h0 + (head < heads ? head : 0)) * HD + 16 * g;
+        float x[KS][16];
+        uint32_t top = 0;
+#pragma unroll
+        for (int s = 0; s < KS; s++)
+#pragma unroll
+            for (int i = 0; i < 16; i++) {
+                x[s][i] = qp[64 * s + i];
+                top = max(top, __float_as_uint(x[s][i]) & 0x7fffffffu);
+            }
+        top = max(top, (uint32_t)__shfl_xor((int)top, 16, WAVE));
+        top = max(top, (uint32_t)__shfl_xor((int)top, 32, WAVE));
+        query = q8_query(top, (EXTRA ? 1.0 : 1.4426950408889634) / sqrt((double)HD));
+#pragma unroll
+        for (int p = 0; p < PASSES; p++) {
+            const int digit = 2 - p * TERMS - term;
+            weight[p] = digit == 2 ? 65536.f : digit == 1 ? 256.f : 1.f;
+#pragma unroll
+            for (int s = 0; s < KS; s++)
+#pragma unroll
+                for (int w = 0; w < 4; w++) {
+                    uint32_t word = 0;
+#pragma unroll
+                    for (int i = 0; i < 4; i++) word |= (uint32_t)(q8_digit(x[s][4 * w + i], query.scale, digit) & 255) << (8 * i);
+                    qd[p][s][w] = digit >= 0 && head < heads ? (int)word : 0;
+                }
+        }
+    }
+    const float slope = EXTRA && a.slopes && head < heads ? a.slopes[h0 + head] * 1.4426950408889634f : 0.f;
+    const float inv_cap = EXTRA && a.softcap > 0.f ? 1.f / a.softcap : 0.f;
+
+    f32x4_t o[ND];
+#pragma unroll
+    for (int n = 0; n < ND; n++) o[n] = (f32x4_t){0.f, 0.f, 0.f, 0.f};
+    float m = -INFINITY, l = 0.f;      // log2 domain; l over this lane's own positions
+    int k = -100000;                   // o is in units of 2^(k - 14)
+
+    u32x4_t kf[4][KS], vf[ND], ek, ev;
+    int idk, idv;      // blocks of the tile to be loaded: the one of this lane's key rows, and block g
+    auto ask = [&](int tile) {
+        idk = trow[min(4 * tile + (c >> 2), last)];
+        idv = trow[min(4 * tile + g, last)];
+    };
+    auto load_k = [&]() {
+        const int8_t *p = kbase + max(idk, 0) * bs;
+#pragma unroll
+        for (int s = 0; s < 4; s++)
+#pragma unroll
+            for (int u = 0; u < KS; u++) kf[s][u] = load_stream16(p + 4 * s * HD + 64 * u);
+        const int8_t *e = a.expo + ((int64_t)max(idv, 0) * 2 * a.Hkv + j) * 16;
+        ek = *reinterpret_cast<const u32x4_t *>(e);
+        ev = *reinterpret_cast<const u32x4_t *>(e + a.Hkv * 16);
+    };
+    auto load_v = [&](int id) {
+        const int8_t *p = vbase + max(id, 0) * bs;
+#pragma unroll
+        for (int n = 0; n < ND; n++) vf[n] = load_stream16(p + 256 * n);
+    };
+
+    const int begin = t0 + wave;
+    if (begin < t1) {
+        ask(begin);
+        load_k();
+        load_v(idv);
+    }
+    for (int tile = begin; tile < t1; tile += WAVES) {
+        const bool more = tile + WAVES < t1;
+        // ---- scores of block g's 16 slots
+        float s[16];
+        const int at = (4 * tile + g) * 16;      // position of slot 0
+        const bool mapped = idv >= 0;
+        const u32x4_t ekn = ek, evn = ev;
+#pragma unroll
+        for (int q = 0; q < 4; q++) {
+            float sum[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int p = 0; p < PASSES; p++) {
+                i32x4_t acc = {0, 0, 0, 0};
+#pragma unroll
+                for (int u = 0; u < KS; u++) acc = __builtin_amdgcn_mfma_i32_16x16x64_i8(__builtin_bit_cast(i32x4_t, kf[q][u]), qd[p][u], acc, 0, 0, 0);
+#pragma unroll
+                for (int i = 0; i < 4; i++) sum[i] = fmaf((float)acc[i], weight[p], sum[i]);
+            }
+#pragma unroll
+            for (int i = 0; i < 4; i++) s[4 * q + i] = sum_terms<GP>(sum[i]);
+        }
+        if (more) {
+            ask(tile + WAVES);
+            load_k();
+        }
+        const int id_next = idv;
+        // ---- online softmax of this lane's column
+        bool all = mapped && at >= see.lo && at + 15 <= see.hi;
+        float mb = -INFINITY;
+        int e[16];      // exponents of the values
+#pragma unroll
+        for (int i = 0; i < 16; i++) {
+            const int kexp = (int)(int8_t)(ekn[i >> 2] >> (8 * (i & 3)));
+            e[i] = (int)(int8_t)(evn[i >> 2] >> (8 * (i & 3)));
+            float x = ldexpf(s[i], kexp + query.exp) * query.unit;
+            if constexpr (EXTRA) {
+                if (a.softcap > 0.f) x = q8_cap(x, a.softcap, inv_cap);
+                x = fmaf(slope, (float)(at + i - (len - 1)), x * 1.4426950408889634f);
+            }
+            x = kexp == Q8_NAN ? __uint_as_float(0x7fc00000u) : x;
+            s[i] = x;
+        }
+        if (!__all(all)) {
+#pragma unroll
+            for (int i = 0; i < 16; i++) {
+                const bool ok = mapped && at + i >= see.lo && at + i <= see.hi;
+                s[i] = ok ? s[i] : -INFINITY;
+                e[i] = ok ? e[i] : -1000;
+            }
+        }
+        float top = -INFINITY;      // of p 2^e
+#pragma unroll
+        for (int i = 0; i < 16; i++) {
+            mb = fmaxf(mb, s[i]);
+            top = fmaxf(top, s[i] + (float)e[i]);
+        }
+        mb = fmaxf(mb, __shfl_xor(mb, 16, WAVE));
+        top = fmaxf(top, __shfl_xor(top, 16, WAVE));
+        mb = fmaxf(mb, __shfl_xor(mb, 32, WAVE));
+        top = fmaxf(top, __shfl_xor(top, 32, WAVE));
+        const float mn = fmaxf(m, mb), ref = mn > -INFINITY ? mn : 0.f;
+        const float keep = fast_exp2(m - ref);
+        // k: at least the largest exponent so far of what a column adds up, in units of the new reference
+        const float lift = m > -INFINITY ? ref - m : 0.f;
+        const int fall = (int)ceilf(fminf(lift, 100000.f));
+        const int kt = top > -INFINITY ? (int)ceilf(fminf(fmaxf(top - ref, -90000.f), 90000.f)) : -100000;
+        const int kn = max(max(k - fall, kt), -100000);
+        const float scale = ldexpf(keep, max(min(k - kn, 300), -300));
+        l *= keep;
+        m = mn;
+        k = kn;
+        if (__any(scale != 1.f)) {
+#pragma unroll
+            for (int n = 0; n < ND; n++)
+#pragma unroll
+                for (int i = 0; i < 4; i++) o[n][i] *= scale;
+        }
+        float hi[16], lo[16];
+#pragma unroll
+        for (int i = 0; i < 16; i++) {
+            const float p = fast_exp2(s[i] - ref);
+            l += p;
+            float w = ldexpf(p, e[i] - k + 14);
+            w = e[i] == Q8_NAN ? __uint_as_float(0x7fc00000u) : w;
+            hi[i] = (float)(_Float16)w;
+            lo[i] = w - hi[i];
+        }
+        f16x8_t wb[2][GP == 16 ? 2 : 1];
+#pragma unroll
+        for (int i = 0; i < 16; i++) {
+            if constexpr (GP == 16) {
+                wb[i >> 3][0][i & 7] = (_Float16)hi[i];
+                wb[i >> 3][1][i & 7] = (_Float16)lo[i];
+            } else {
+                wb[i >> 3][0][i & 7] = (_Float16)(term == 0 ? hi[i] : term == 1 ? lo[i] : 0.f);
+            }
+        }
+        // ---- sums
+#pragma unroll
+        for (int n = 0; n < ND; n++) {
+            const f16x8_t va = q8_halves(vf[n][0], vf[n][1]), vb = q8_halves(vf[n][2], vf[n][3]);
+#pragma unroll
+            for (int p = 0; p < (GP == 16 ? 2 : 1); p++) {
+                o[n] = __builtin_amdgcn_mfma_f32_16x16x32_f16(va, wb[0][p], o[n], 0, 0, 0);
+                o[n] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vb, wb[1][p], o[n], 0, 0, 0);
+            }
+        }
+        if (more) load_v(id_next);
+    }
+
+    l += __shfl_xor(l, 16, WAVE);
+    l += __shfl_xor(l, 32, WAVE);
+    __shared__ __attribute__((aligned(16))) float so[WAVES][GP][HD + 4];
+    __shared__ float2 sml[WAVES][GP];
+    const float inv = l == 0.f ? 0.f : 1.f / l;
+#pragma unroll
+    for (int n = 0; n < ND; n++) {
+        float4 r;
+        float *v = &r.x;
+#pragma unroll
+        for (int i = 0; i < 4; i++) {
+            float x = o[n][i];
+            if constexpr (GP < 16) {      // its two terms
+                const float other = __shfl_xor(x, GP, WAVE);
+                x += other;
+            }
+            v[i] = ldexpf(x * inv, max(min(k - 14, 300), -300));
+        }
+        if (term == 0) *reinterpret_cast<float4 *>(&so[wave][head][16 * n + 4 * g]) = r;
+    }
+    if (lane < GP) sml[wave][lane] = make_float2(m, l);
+    __syncthreads();
+    for (int idx = threadIdx.x; idx < heads * HD; idx += 64 * WAVES) {
+        const int hh = idx / HD, d = idx % HD;
+        float M = -INFINITY, L = 0.f, acc = 0.f;
+#pragma unroll
+        for (int w = 0; w < WAVES; w++) M = fmaxf(M, sml[w][hh].x);
+        const float ref = M > -INFINITY ? M : 0.f;
+#pragma unroll
+        for (int w = 0; w < WAVES; w++) {
+            const float2 ml = sml[w][hh];
+            const float f = fast_exp2(ml.x - ref) * ml.y;
+            L += ml.y == 0.f ? 0.f : f;
+            acc += ml.y == 0.f ? 0.f : f * so[w][hh][d];
+        }
+        const float r = L == 0.f ? 0.f : acc / L;
+        const int64_t item = (int64_t)t * a.H + h0 + hh;
+        if (chunks == 1) {
+            a.out[item * HD + d] = r;
+        } else {
+            part_o[(item * chunks + ch) * HD + d] = r;
+            if (d == 0) part_ml[item * chunks + ch] = make_float2(M, L);
+        }
+    }
+}
+
+// Joins the chunks of a row and head: one wave, in the chunks' order.
+template <int HD>
+__global__ __launch_bounds__(64) void k_join_q8(Q8Attention a, const int32_t *__restrict__ first, const int32_t *__restrict__ ctx_len, int max_ctx, int chunk,
+                                                int chunks, const float *__restrict__ part_o, const float2 *__restrict__ part_ml) {
+    const int t = blockIdx.x, h = blockIdx.y, lane = threadIdx.x;
+    const Seen see = seen_of(ctx_len[t], first ? first[t] : 0, max_ctx, a.window, a.table_stride);
+    const int64_t item = (int64_t)t * a.H + h;
+    const int n = see.hi < see.lo ? 0 : ((see.hi >> 6) - (see.lo >> 6)) / chunk + 1;
+    float M = -INFINITY;
+    for (int i = lane; i < n; i += 64) M = fmaxf(M, part_ml[item * chunks + i].x);
+    for (int off = 32; off > 0; off >>= 1) M = fmaxf(M, __shfl_xor(M, off, WAVE));
+    const float ref = M > -INFINITY ? M : 0.f;
+    float L = 0.f, acc[HD / 64] = {};
+    for (int i = 0; i < n; i++) {
+        const float2 ml = part_ml[item * chunks + i];
+        const float f = ml.y == 0.f ? 0.f : fast_exp2(ml.x - ref) * ml.y;
+        L += f;
+#pragma unroll
+        for (int u = 0; u < HD / 64; u++) acc[u] += ml.y == 0.f ? 0.f : f * part_o[(item * chunks + i) * HD + lane + 64 * u];
+    }
+#pragma unroll
+    for (int u = 0; u < HD / 64; u++) a.out[item * HD + lane + 64 * u] = L == 0.f ? 0.f : acc[u] / L;
+}
+
+struct Plan { int chunk, chunks; size_t rows; };
+
+int visible_tiles(int max_ctx, int window) {
+    const int64_t all = ((int64_t)max_ctx + TILE - 1) / TILE;
+    return (int)(window > 0 ? std::min<int64_t>(all, ((int64_t)window + TILE - 2) / TILE + 1) : all);
+}
+
+constexpr int WANT = 512, CHUNK_TILES = 32;
+
+Plan plan(int T, int H, int Hkv, int max_ctx, int window) {
+    const int tiles = std::max(1, visible_tiles(max_ctx, window)), G = H / Hkv;
+    const int64_t pairs = (int64_t)T * Hkv * ((G + 15) / 16);
+    const int64_t want = std::max<int64_t>((WANT + pairs - 1) / pairs, (tiles + CHUNK_TILES - 1) / CHUNK_TILES);
+    Plan p;
+    p.chunk = (int)std::max<int64_t>(WAVES, (tiles + want - 1) / want);
+    p.chunks = (tiles + p.chunk - 1) / p.chunk;
+    p.rows = (size_t)T * H * (1 + (tiles + CHUNK_TILES - 1) / CHUNK_TILES) + (size_t)WANT * std::min(G, 16);
+    return p;
+}
+
+template <int HD, int GP>
+void launch_decode(const Q8Attention &a, const int32_t *seq_slot, const int32_t *first, const int32_t *ctx_len, int max_ctx, int T, const Plan &p, char *scratch,
+                   hipStream_t s) {
+    float *part_o = (float *)(scratch + ld::align_up(p.rows * 8, 256));
+    float2 *part_ml = (float2 *)scratch;
+    const int parts = (a.H / a.Hkv + 15) / 16;
+    const dim3 grid(T * p.chunks, a.Hkv * parts), block(64 * WAVES);
+    if (a.softcap > 0.f || a.slopes)
+        LD_LAUNCH((k_decode_q8<HD, GP, true>), grid, block, 0, s, a, seq_slot, first, ctx_len, max_ctx, p.chunk, p.chunks, part_o, part_ml);
+    else
+        LD_LAUNCH((k_decode_q8<HD, GP, false>), grid, block, 0, s, a, seq_slot, first, ctx_len, max_ctx, p.chunk, p.chunks, part_o, part_ml);
+    if (p.chunks > 1) LD_LAUNCH(k_join_q8<HD>, dim3(T, a.H), dim3(64), 0, s, a, first, ctx_len, max_ctx, p.chunk, p.chunks, part_o, part_ml);
+}
+
+template <int HD>
+void launch_decode(const Q8Attention &a, const int32_t *seq_slot, const int32_t *first, const int32_t *ctx_len, int max_ctx, int T, const Plan &p, char *scratch,
+                   hipStream_t s) {
+    const int G = a.H / a.Hkv;
+#define LD_DECODE(GP_) launch_decode<HD, GP_>(a, seq_slot, first, ctx_len, max_ctx, T, p, scratch, s)
+    if (G == 1) LD_DECODE(1);
+    else if (G == 2) LD_DECODE(2);
+    else if (G <= 4) LD_DECODE(4);
+    else if (G <= 8) LD_DECODE(8);
+    else LD_DECODE(16);
+#undef LD_DECODE
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t ldk_attention_q8_scratch_bytes(int32_t T, int32_t H, int32_t Hkv, int32_t hd, int32_t max_ctx, int32_t window) {
+    if (T <= 0 || H <= 0 || Hkv <= 0 || H % Hkv || (hd != 64 && hd != 128) || max_ctx < 0 || window < 0) return 0;
+    const size_t rows = plan(T, H, Hkv, max_ctx, window).rows;
+    return ld::align_up(rows * 8, 256) + rows * hd * 4;
+}
+
+ld_status ldk_paged_attention_q8(const float *q, int32_t q_stride, const int8_t *codes, const int8_t *expo, const int32_t *table,
+                                 int32_t table_stride, const int32_t *seq_slot, const int32_t *first, const int32_t *ctx_len, int32_t max_ctx,
+                                 int32_t T, int32_t H, int32_t Hkv, int32_t hd, int32_t window, float softcap, const float *slopes, float *out,
+                                 void *scratch, size_t scratch_bytes, void *stream) {
+    if (T == 0) return LD_OK;
+    const Q8Attention a{q, q_stride, codes, expo, table, table_stride, H, Hkv, window, softcap, slopes, out};
+    if (T < 0 || max_ctx < 0 || !seq_slot || !ctx_len || bad_attention(a, hd)) return ld::fail(LD_E_INVAL, "ldk_paged_attention_q8: bad argument");
+    const Plan p = plan(T, H, Hkv, max_ctx, window);
+    if (H > 65535 || (int64_t)T * p.chunks > INT32_MAX) return ld::fail(LD_E_RANGE, "ldk_paged_attention_q8: more than 65535 heads, or too many rows");
+    if (!scratch || ((uintptr_t)scratch & 15) || scratch_bytes < ldk_attention_q8_scratch_bytes(T, H, Hkv, hd, max_ctx, window))
+        return ld::fail(LD_E_INVAL, "ldk_paged_attention_q8: scratch too small, or not aligned to 16 bytes");
+    hipStream_t s = (hipStream_t)stream;
+    if (hd == 128) launch_decode<128>(a, seq_slot, first, ctx_len, max_ctx, T, p, (char *)scratch, s);
+    else launch_decode<64>(a, seq_slot, first, ctx_len, max_ctx, T, p, (char *)scratch, s);
+    return launched("k_decode_q8");
+}
+
+}  // extern "C"
