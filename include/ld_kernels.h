@@ -312,7 +312,7 @@ ld_status ldk_kv_from_q8(const int8_t *codes, const int8_t *expo, const int32_t 
  *   out = sum_j softmax(s)_j v_j.
  * A query enters as a multiple of 1 / 8355711 of its largest entry, a weight times its value's 2^e with 22 bits, of which at most 2^-38 of the largest such product
  * gets lost besides; codes are exact, sums float32.  A query head with a NaN or an infinity gives NaN, as does a head that sees a key or value that stands for NaN.  max_ctx (HOST) >= every ctx_len.
- * scratch: ldk_attention_q8_scratch_bytes(...) bytes, 16-byte aligned (may be 0 bytes); a buffer for more rows or longer contexts serves less. */
+ * scratch: ldk_attention_q8_scratch_bytes(...) bytes, 16-byte aligned; a buffer for more rows or longer contexts serves less. */
 size_t ldk_attention_q8_scratch_bytes(int32_t T, int32_t H, int32_t Hkv, int32_t hd, int32_t max_ctx, int32_t window);
 ld_status ldk_paged_attention_q8(const float *q, int32_t q_stride, const int8_t *codes, const int8_t *expo, const int32_t *table,
                                  int32_t table_stride, const int32_t *seq_slot, const int32_t *first, const int32_t *ctx_len, int32_t max_ctx,
@@ -323,7 +323,7 @@ ld_status ldk_paged_attention_q8(const float *q, int32_t q_stride, const int8_t 
  * block-table row, first visible position, prefix length).  The row at position p sees positions max(first visible, p - window + 1) ..
  * max(p, prefix - 1): a band (window 0: none), a document's start and a prefix that sees all of itself; a row that sees nothing gives 0.
  * Scores as in ldk_paged_attention_q8.  Rows that no tile names are left as they are.  max_pos (HOST) >= every max(p, prefix - 1).
- * scratch: ldk_prefill_attention_q8_scratch_bytes(...) bytes, 16-byte aligned (may be 0 bytes); a buffer for more tiles or longer contexts serves less. */
+ * scratch: ldk_prefill_attention_q8_scratch_bytes(...) bytes, 16-byte aligned; a buffer for more tiles or longer contexts serves less. */
 size_t ldk_prefill_attention_q8_scratch_bytes(int32_t n_tiles, int32_t H, int32_t Hkv, int32_t hd, int32_t max_pos, int32_t window);
 ld_status ldk_prefill_attention_q8(const float *q, int32_t q_stride, const int8_t *codes, const int8_t *expo, const int32_t *table,
                                    int32_t table_stride, const int32_t *tiles, int32_t n_tiles, int32_t H, int32_t Hkv, int32_t hd, int32_t window,

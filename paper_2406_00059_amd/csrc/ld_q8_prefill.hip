@@ -1,0 +1,393 @@
+// Attention of prompt and chunk rows over the 8-bit cache on the matrix cores.
+//
+// A workgroup takes a tile of up to 128 rows and a query head, each of its four waves 32 rows, and walks the positions 64 (four blocks) at a time.
+// Keys and values go through LDS, the next tile's while one is multiplied: keys as they are, values widened to fp16 once for the four waves.
+//
+//   scores   S^T[pos, row] = K[pos, :] . Q[row, :] in whole numbers (32x32x32, 8 bits): a query is three base-256 digits (24 bits under its largest
+//            entry), kept in registers.
+//   sums     O^T[d, row] += V^T[d, pos] W^T[pos, row] (32x32x16, fp16): codes are exact in fp16; W = p 2^e 2^x, e the value's exponent and 2^x the power
+//            of two that brings the largest p 2^e of the row so far to 2^13 .. 2^15, as two fp16 terms (22 bits).
+//
+// Which position a row of the score tile is, is free: row 8 b + 4 h + i is slot 4 b + i of block h of a pair, so that lane (row, h) ends with the scores of
+// block h, slot by slot, which is what it has to bring as the other operand of the sums.
+//
+// The top m of a row's scores is raised only when one exceeds it by 2^8: p may be up to 256, and the sums are seldom scaled.
+#include <algorithm>
+#include <cmath>
+#include "ld_q8.h"
+
+using namespace ldd;
+
+namespace {
+
+constexpr int TILE = 64, ROWS = 128;
+typedef int i32x16_t __attribute__((ext_vector_type(16)));
+typedef float f32x16_t __attribute__((ext_vector_type(16)));
+
+template <int HD>
+struct Stage {
+    uint4 k[4 * HD];               // [position][piece of 16 dims, swizzled]
+    f16x8_t v[8 * HD];             // [block][half][dim]: eight slots
+    float ku[TILE], vu[TILE];      // units; NaN where a vector is not finite
+    int mapped;                    // bit b: block b
+};
+
+// Piece p of position r (block r / 16, slot r % 16), so that eight lanes' pieces of a score operand lie in different banks.
+template <int HD>
+__device__ __forceinline__ int key_piece(int r, int p) {
+    constexpr int N = HD / 16;
+    return N == 8 ? r * 8 + (p ^ ((r & 3) | ((r >> 2) & 4))) : r * 4 + (p ^ (((r >> 1) & 1) | ((r >> 3) & 2)));
+}
+
+struct TileRows { int row, n, pos, seq, first, prefix; };
+
+// Positions that rows r0 .. r1 - 1 of a tile see at least one of.
+__device__ __forceinline__ int seen_from(const TileRows &t, int r, int window) { return max(max(t.first, window > 0 ? t.pos + r - window + 1 : 0), 0); }
+__device__ __forceinline__ int seen_to(const TileRows &t, int r, int most) { return min(max(t.pos + r, t.prefix - 1), most); }
+
+template <int HD, bool EXTRA>
+__global__ __launch_bounds__(256, 2) void k_prefill_q8(Q8Attention a, const int32_t *__restrict__ tiles, int n_tiles, int max_pos, int splits,
+                                                       float *__restrict__ part_o, float2 *__restrict__ part_ml) {
+    constexpr int KS = HD / 32, ND = HD / 32, NP = HD / 64;
+    // the last tiles first (they see the most); KV heads next to each other, so that one cache's L2 serves one of them where there are eight
+    int idx = blockIdx.x;
+    const int sp = idx % splits;
+    idx /= splits;
+    const int x = idx % a.H, tile_no = n_tiles - 1 - idx / a.H, G = a.H / a.Hkv, j = x % a.Hkv, h = j * G + x / a.Hkv;
+    const int32_t *tp = tiles + 6 * (int64_t)tile_no;
+    const TileRows tr{tp[0], min(tp[1], ROWS), tp[2], tp[3], tp[4], tp[5]};
+    if (tr.n <= 0) return;
+    const int most = (int)min((int64_t)max_pos, (int64_t)a.table_stride * 16 - 1);
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, r32 = lane & 31, hh = lane >> 5;
+    const int wlo = seen_from(tr, 0, a.window), whi = seen_to(tr, tr.n - 1, most);      // of the workgroup
+    int t0 = wlo >> 6, t1 = whi < wlo ? t0 : (whi >> 6) + 1;
+    const int per = (t1 - t0 + splits - 1) / splits;
+    t0 += sp * per;
+    t1 = min(t1, t0 + per);
+
+    const int r = 32 * wave + r32;
+    const bool real = r < tr.n, busy = 32 * wave < tr.n;
+    // lanes past the last row do as the last one does
+    const int rr = min(r, tr.n - 1), nlast = min(tr.n - 1, 32 * wave + 31);
+    const int lo = seen_from(tr, rr, a.window), hi = seen_to(tr, rr, most);
+    const int wave_lo = seen_from(tr, 32 * wave, a.window), wave_hi = seen_to(tr, nlast, most);      // any row of the wave (if busy)
+    const int all_lo = seen_from(tr, nlast, a.window), all_hi = seen_to(tr, 32 * wave, most);        // every row
+
+    __shared__ __attribute__((aligned(16))) Stage<HD> stage[2];
+    const int32_t *trow = a.table + (int64_t)tr.seq * a.table_stride;
+    const int last = whi >> 4;
+    const int64_t bs = q8_block(a.Hkv, HD);
+
+    // ---- what a thread brings of a tile: NP pieces of keys and of values, and one exponent
+    int id[NP], ide;
+    uint4 kr[NP], vr[NP];
+    int er = 0;
+    const int eb = (tid & 63) >> 4;
+    auto ask = [&](int tile) {
+#pragma unroll
+        for (int u = 0; u < NP; u++) id[u] = trow[min(4 * tile + (tid + 256 * u) / HD, last)];
+        ide = trow[min(4 * tile + eb, last)];
+    };
+    auto load = [&]() {
+#pragma unroll
+        for (int u = 0; u < NP; u++) {
+            const int8_t *b = a.codes + max(id[u], 0) * bs + 16 * ((tid + 256 * u) % HD);
+            kr[u] = *reinterpret_cast<const uint4 *>(b + q8_k(HD, j, 0, 0));
+            vr[u] = *reinterpret_cast<const uint4 *>(b + q8_v(a.Hkv, HD, j, 0, 0));
+        }
+        if (tid < 128) er = a.expo[(((int64_t)max(ide, 0) * 2 + (tid >> 6)) * a.Hkv + j) * 16 + (tid & 15)];
+    };
+    auto store = [&](Stage<HD> &s, int ide_of) {
+#pragma unroll
+        for (int u = 0; u < NP; u++) {
+            const int i = tid + 256 * u, b = i / HD, in = i % HD;
+            s.k[key_piece<HD>(b * 16 + in / (HD / 16), in % (HD / 16))] = kr[u];
+            s.v[(2 * b) * HD + in] = q8_halves(vr[u].x, vr[u].y);
+            s.v[(2 * b + 1) * HD + in] = q8_halves(vr[u].z, vr[u].w);
+        }
+        if (tid < 64) {
+            s.ku[tid] = q8_unit(er);
+            const uint64_t ok = __ballot(ide_of >= 0);
+            if (tid == 0) s.mapped = (int)((ok & 1) | (ok >> 15 & 2) | (ok >> 30 & 4) | (ok >> 45 & 8));
+        } else if (tid < 128) {
+            s.vu[tid - 64] = q8_unit(er);
+        }
+    };
+
+    // ---- queries: dims 32 s + 16 hh .. + 16 of this lane's row
+    i32x4_t qd[3][KS];
+    float unit;
+    {
+        const float *qp = a.q + (int64_t)(tr.row + rr) * a.q_stride + h * HD + 16 * hh;
+        float v[KS][16];
+        uint32_t top = 0;
+#pragma unroll
+        for (int s = 0; s < KS; s++)
+#pragma unroll
+            for (int i = 0; i < 16; i++) {
+                v[s][i] = qp[32 * s + i];
+                top = max(top, __float_as_uint(v[s][i]) & 0x7fffffffu);
+            }
+        top = max(top, (uint32_t)__shfl_xor((int)top, 32, WAVE));
+        const Q8Query query = q8_query(top, (EXTRA ? 1.0 : 1.4426950408889634) / sqrt((double)HD));
+        unit = ldexpf(query.unit, query.exp);
+        unit = unit < 0x1p-126f ? 0x1p-126f : unit;      // not zero: it multiplies -infinity
+#pragma unroll
+        for (int s = 0; s < KS; s++)
+#pragma unroll
+            for (int w = 0; w < 4; w++) {
+                uint32_t d[3] = {0, 0, 0};
+#pragma unroll
+                for (int i = 0; i < 4; i++)
+#pragma unroll
+                    for (int n = 0; n < 3; n++) d[n] |= (uint32_t)(q8_digit(v[s][4 * w + i], query.scale, n) & 255) << (8 * i);
+#pragma unroll
+                for (int n = 0; n < 3; n++) qd[n][s][w] = (int)d[n];
+            }
+    }
+    const float rs = EXTRA ? 1.f : unit;
+    const float slope = EXTRA && a.slopes ? a.slopes[h] * 1.4426950408889634f : 0.f, inv_cap = EXTRA && a.softcap > 0.f ? 1.f / a.softcap : 0.f;
+
+    f32x16_t o[ND];
+#pragma unroll
+    for (int n = 0; n < ND; n++)
+#pragma unroll
+        for (int i = 0; i < 16; i++) o[n][i] = 0.f;
+    float m = -INFINITY, M = 0.f, l = 0.f;      // top of the scores (before rs), m rs where there is one, sum over this lane's positions
+    float big = 0.f;                            // largest p 2^e of the row
+    int x2 = 0;                                 // o is in units of 2^-x2
+
+    auto multiply = [&](const Stage<HD> &st, int tile) {
+        const int base = tile * TILE;
+        float s[2][16];
+#pragma unroll
+        for (int u = 0; u < 2; u++) {
+            i32x16_t acc2 = {}, acc = {};
+            const int row = (2 * u + ((r32 >> 2) & 1)) * 16 + (r32 >> 3) * 4 + (r32 & 3);
+            i32x4_t kf[KS];
+#pragma unroll
+            for (int q = 0; q < KS; q++) kf[q] = __builtin_bit_cast(i32x4_t, st.k[key_piece<HD>(row, 2 * q + hh)]);
+#pragma unroll
+            for (int q = 0; q < KS; q++) acc = __builtin_amdgcn_mfma_i32_32x32x32_i8(kf[q], qd[1][q], acc, 0, 0, 0);
+#pragma unroll
+            for (int q = 0; q < KS; q++) acc2 = __builtin_amdgcn_mfma_i32_32x32x32_i8(kf[q], qd[2][q], acc2, 0, 0, 0);
+#pragma unroll
+            for (int i = 0; i < 16; i++) acc[i] <<= 8;
+#pragma unroll
+            for (int q = 0; q < KS; q++) acc = __builtin_amdgcn_mfma_i32_32x32x32_i8(kf[q], qd[0][q], acc, 0, 0, 0);
+            const float4 *ku = reinterpret_cast<const float4 *>(st.ku + 32 * u + 16 * hh);
+#pragma unroll
+            for (int i = 0; i < 16; i++) {
+                const float4 k4 = ku[i >> 2];
+                const float kk = (i & 3) == 0 ? k4.x : (i & 3) == 1 ? k4.y : (i & 3) == 2 ? k4.z : k4.w;
+                s[u][i] = fmaf((float)acc2[i], 65536.f, (float)acc[i]) * kk;
+                if constexpr (EXTRA) {
+                    float y = s[u][i] * unit;
+                    if (a.softcap > 0.f) y = q8_cap(y, a.softcap, inv_cap);
+                    s[u][i] = fmaf(slope, (float)(base + 32 * u + 16 * hh + i - (tr.pos + rr)), y * 1.4426950408889634f);
+                }
+            }
+        }
+        const bool whole = base >= all_lo && base + TILE - 1 <= all_hi && st.mapped == 15;
+        uint32_t ok = 0xffffffffu;
+        if (!whole) {
+            ok = 0;
+#pragma unroll
+            for (int u = 0; u < 2; u++)
+#pragma unroll
+                for (int i = 0; i < 16; i++) {
+                    const int p = base + 32 * u + 16 * hh + i;
+                    const bool see = p >= lo && p <= hi && (st.mapped >> (2 * u + hh) & 1);
+                    ok |= (uint32_t)see << (16 * u + i);
+                    s[u][i] = see ? s[u][i] : -INFINITY;
+                }
+        }
+        float mb = -INFINITY;
+#pragma unroll
+        for (int u = 0; u < 2; u++)
+#pragma unroll
+            for (int i = 0; i < 16; i++) mb = fmaxf(mb, s[u][i]);
+        mb = fmaxf(mb, __shfl_xor(mb, 32, WAVE));
+        float keep = 1.f;
+        if (__any((mb - m) * rs > 8.f || (m == -INFINITY && mb > -INFINITY))) {
+            const float mn = fmaxf(m, mb), Mn = mn > -INFINITY ? mn * rs : 0.f;
+            keep = m > -INFINITY ? fast_exp2(M - Mn) : 0.f;
+            m = mn;
+            M = Mn;
+            l *= keep;
+            big *= keep;
+        }
+        float top = 0.f;
+#pragma unroll
+        for (int u = 0; u < 2; u++) {
+            const float4 *vu = reinterpret_cast<const float4 *>(st.vu + 32 * u + 16 * hh);
+#pragma unroll
+            for (int i = 0; i < 16; i++) {
+                const float4 v4 = vu[i >> 2];
+                const float vv = (i & 3) == 0 ? v4.x : (i & 3) == 1 ? v4.y : (i & 3) == 2 ? v4.z : v4.w;
+                const float p = fast_exp2(fmaf(s[u][i], rs, -M));
+                l += p;
+                s[u][i] = p * vv;
+            }
+        }
+        if (!whole) {      // units of positions that are not seen may be anything
+#pragma unroll
+            for (int u = 0; u < 2; u++)
+#pragma unroll
+                for (int i = 0; i < 16; i++) s[u][i] = ok >> (16 * u + i) & 1 ? s[u][i] : 0.f;
+        }
+#pragma unroll
+        for (int u = 0; u < 2; u++)
+#pragma unroll
+            for (int i = 0; i < 16; i++) top = fmaxf(top, s[u][i]);
+        top = fmaxf(top, __shfl_xor(top, 32, WAVE));
+        const bool grown = top > ldexpf(1.f, 15 - x2) || (big == 0.f && top > 0.f);
+        big = fmaxf(big, top);
+        if (__any(keep != 1.f || grown)) {
+            // big 2^xn in 2^13 .. 2^14
+            const int xn = big > 0.f ? min(13 - ((int)(__float_as_uint(big) >> 23) - 127), 126) : x2;
+            const float scale = ldexpf(keep, xn - x2);
+            x2 = xn;
+#pragma unroll
+            for (int n = 0; n < ND; n++)
+#pragma unroll
+                for (int i = 0; i < 16; i++) o[n][i] *= scale;
+        }
+        const float up = ldexpf(1.f, x2);
+#pragma unroll
+        for (int u = 0; u < 2; u++) {
+            f16x8_t wh[2], wl[2];
+#pragma unroll
+            for (int i = 0; i < 16; i++) {
+                const float w = s[u][i] * up;
+                const _Float16 y = (_Float16)w;
+                wh[i >> 3][i & 7] = y;
+                wl[i >> 3][i & 7] = (_Float16)(w - (float)y);
+            }
+#pragma unroll
+            for (int n = 0; n < ND; n++)
+#pragma unroll
+                for (int q = 0; q < 2; q++) {
+                    const f16x8_t vf = st.v[(2 * (2 * u + hh) + q) * HD + 32 * n + r32];
+                    o[n] = __builtin_amdgcn_mfma_f32_32x32x16_f16(vf, wh[q], o[n], 0, 0, 0);
+                    o[n] = __builtin_amdgcn_mfma_f32_32x32x16_f16(vf, wl[q], o[n], 0, 0, 0);
+                }
+        }
+    };
+
+    if (t0 < t1) {
+        ask(t0);
+        load();
+        int ide_of = ide;
+        if (t0 + 1 < t1) ask(t0 + 1);
+        store(stage[0], ide_of);
+        if (t0 + 1 < t1) {
+            load();
+            ide_of = ide;
+        }
+        if (t0 + 2 < t1) ask(t0 + 2);
+        lds_barrier();
+        for (int tile = t0; tile < t1; tile++) {
+            const int cur = (tile - t0) & 1;
+            if (busy && tile * TILE <= wave_hi && tile * TILE + TILE - 1 >= wave_lo) multiply(stage[cur], tile);
+            if (tile + 1 < t1) {
+                store(stage[cur ^ 1], ide_of);
+                if (tile + 2 < t1) {
+                    load();
+                    ide_of = ide;
+                }
+                if (tile + 3 < t1) ask(tile + 3);
+                lds_barrier();
+            }
+        }
+    }
+
+    l += __shfl_xor(l, 32, WAVE);
+    if (!real) return;
+    const float inv = l == 0.f ? 0.f : 1.f / l;
+    const int64_t item = splits == 1 ? (int64_t)(tr.row + r) * a.H + h : (((int64_t)tile_no * a.H + h) * splits + sp) * ROWS + r;
+    float *dst = (splits == 1 ? a.out : part_o) + item * HD;
+#pragma unroll
+    for (int n = 0; n < ND; n++)
+#pragma unroll
+        for (int b = 0; b < 4; b++) {
+            float4_u y;
+#pragma unroll
+            for (int i = 0; i < 4; i++) y[i] = ldexpf(o[n][4 * b + i] * inv, -x2);
+            *reinterpret_cast<float4_u *>(dst + 32 * n + 8 * b + 4 * hh) = y;
+        }
+    if (splits > 1 && hh == 0) part_ml[item] = make_float2(m > -INFINITY ? M : -INFINITY, l);
+}
+
+// Joins the shares of a row and head, in their order: one wave a row.
+template <int HD>
+__global__ __launch_bounds__(256) void k_join_prefill_q8(Q8Attention a, const int32_t *__restrict__ tiles, int splits, const float *__restrict__ part_o,
+                                                         const float2 *__restrict__ part_ml) {
+    const int tile_no = blockIdx.x, h = blockIdx.y, lane = threadIdx.x & 63, r = blockIdx.z * 4 + (threadIdx.x >> 6);
+    const int32_t *tp = tiles + 6 * (int64_t)tile_no;
+    if (r >= min(tp[1], ROWS)) return;
+    const int64_t first = ((int64_t)tile_no * a.H + h) * splits * ROWS + r;
+    float M = -INFINITY;
+    for (int i = 0; i < splits; i++) M = fmaxf(M, part_ml[first + (int64_t)i * ROWS].x);
+    const float ref = M > -INFINITY ? M : 0.f;
+    float L = 0.f, acc[HD / 64] = {};
+    for (int i = 0; i < splits; i++) {
+        const int64_t at = first + (int64_t)i * ROWS;
+        const float2 ml = part_ml[at];
+        if (ml.y == 0.f) continue;
+        const float f = fast_exp2(ml.x - ref) * ml.y;
+        L += f;
+#pragma unroll
+        for (int u = 0; u < HD / 64; u++) acc[u] += f * part_o[at * HD + lane + 64 * u];
+    }
+#pragma unroll
+    for (int u = 0; u < HD / 64; u++) a.out[((int64_t)(tp[0] + r) * a.H + h) * HD + lane + 64 * u] = L == 0.f ? 0.f : acc[u] / L;
+}
+
+constexpr int WANT = 512, LEAST = 4;      // workgroups, tiles of positions a share
+
+int shares(int n_tiles, int H, int max_pos) {
+    const int64_t pairs = (int64_t)n_tiles * H, kt = ((int64_t)max_pos + TILE) / TILE;
+    return (int)std::max<int64_t>(1, std::min<int64_t>((WANT + pairs - 1) / pairs, kt / LEAST));
+}
+
+template <int HD>
+void launch_prefill(const Q8Attention &a, const int32_t *tiles, int n_tiles, int max_pos, int splits, char *scratch, hipStream_t s) {
+    float2 *part_ml = (float2 *)scratch;
+    float *part_o = (float *)(scratch + ld::align_up((size_t)n_tiles * a.H * splits * ROWS * 8, 256));
+    const dim3 grid((unsigned)((int64_t)n_tiles * a.H * splits)), block(256);
+    if (a.softcap > 0.f || a.slopes) LD_LAUNCH((k_prefill_q8<HD, true>), grid, block, 0, s, a, tiles, n_tiles, max_pos, splits, part_o, part_ml);
+    else LD_LAUNCH((k_prefill_q8<HD, false>), grid, block, 0, s, a, tiles, n_tiles, max_pos, splits, part_o, part_ml);
+    if (splits > 1) LD_LAUNCH(k_join_prefill_q8<HD>, dim3(n_tiles, a.H, ROWS / 4), block, 0, s, a, tiles, splits, part_o, part_ml);
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t ldk_prefill_attention_q8_scratch_bytes(int32_t n_tiles, int32_t H, int32_t Hkv, int32_t hd, int32_t max_pos, int32_t window) {
+    if (n_tiles <= 0 || H <= 0 || Hkv <= 0 || H % Hkv || (hd != 64 && hd != 128) || max_pos < 0 || window < 0) return 0;
+    // no more shares than fill the machine, whatever the number of tiles: pairs * shares < WANT + pairs
+    const size_t rows = ((size_t)n_tiles * H + WANT) * ROWS;
+    return shares(1, 1, max_pos) == 1 ? 256 : ld::align_up(rows * 8, 256) + rows * hd * 4;
+}
+
+ld_status ldk_prefill_attention_q8(const float *q, int32_t q_stride, const int8_t *codes, const int8_t *expo, const int32_t *table,
+                                   int32_t table_stride, const int32_t *tiles, int32_t n_tiles, int32_t H, int32_t Hkv, int32_t hd, int32_t window,
+                                   float softcap, const float *slopes, int32_t max_pos, float *out, void *scratch, size_t scratch_bytes,
+                                   void *stream) {
+    if (n_tiles == 0) return LD_OK;
+    const Q8Attention a{q, q_stride, codes, expo, table, table_stride, H, Hkv, window, softcap, slopes, out};
+    if (n_tiles < 0 || max_pos < 0 || !tiles || bad_attention(a, hd)) return ld::fail(LD_E_INVAL, "ldk_prefill_attention_q8: bad argument");
+    const int splits = shares(n_tiles, H, max_pos);
+    if (H > 65535 || (int64_t)n_tiles * H * splits > INT32_MAX)
+        return ld::fail(LD_E_RANGE, "ldk_prefill_attention_q8: more than 65535 heads, or too many tiles");
+    if (!scratch || ((uintptr_t)scratch & 15) || scratch_bytes < ldk_prefill_attention_q8_scratch_bytes(n_tiles, H, Hkv, hd, max_pos, window))
+        return ld::fail(LD_E_INVAL, "ldk_prefill_attention_q8: scratch too small, or not aligned to 16 bytes");
+    hipStream_t s = (hipStream_t)stream;
+    if (hd == 128) launch_prefill<128>(a, tiles, n_tiles, max_pos, splits, (char *)scratch, s);
+    else launch_prefill<64>(a, tiles, n_tiles, max_pos, splits, (char *)scratch, s);
+    return launched("k_prefill_q8");
+}
+
+}  // extern "C"
