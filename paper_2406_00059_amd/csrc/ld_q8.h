@@ -20,6 +20,23 @@ __device__ __forceinline__ int q8_exponent(uint32_t top) {
     const int e = (int)(top >> 20) - 1023;
     return e > 127 ? Q8_NAN : max(e - 6, -126);
 }
+// The same of floats' bits: only the exponent counts, and subnormals' would be below -126.
+__device__ __forceinline__ int q8_exponent32(uint32_t top) {
+    const int e = (int)(top >> 23) - 127;
+    return e > 127 ? Q8_NAN : max(e - 6, -126);
+}
+// Codes of eight floats under their exponents, packed.  x 2^-e is exact; adding 1.5 2^23 leaves its nearest whole number (ties to even) in the low bits.
+__device__ __forceinline__ uint2 q8_codes8(const float (&x)[8], const int (&e)[8]) {
+    uint32_t n[8];
+#pragma unroll
+    for (int i = 0; i < 8; i++) {
+        const float u = __uint_as_float((uint32_t)(127 - e[i]) << 23);
+        const float c = fminf(fmaxf(x[i] * u, -127.f), 127.f) + 12582912.f;
+        n[i] = e[i] == Q8_NAN ? 0u : __float_as_uint(c) & 255u;
+    }
+    return make_uint2(n[0] | n[1] << 8 | n[2] << 16 | n[3] << 24, n[4] | n[5] << 8 | n[6] << 16 | n[7] << 24);
+}
+
 // Code of x under exponent e.
 __device__ __forceinline__ int8_t q8_code(double x, int e) {
     if (e == Q8_NAN) return 0;

@@ -89,6 +89,111 @@ __global__ __launch_bounds__(64) void k_write_q8(WriteArgs a) {
     if (lane == 0) a.expo[(((int64_t)phys * 2 + value) * a.Hkv + j) * 16 + slot] = (int8_t)e;
 }
 
+// Sixteen rows of a head a workgroup, HD / 8 lanes a row and eight elements a lane: four rotated pairs, or (lanes i >= rot / 8) the elements from 8 i on, of
+// the rest.  rot is a multiple of 8.
+// Values go through LDS, from which neighbouring lanes write neighbouring positions: a position's values lie 16 bytes apart in the cache, and a store of
+// one of them touches a sector for a byte.
+template <int HD, bool INTERLEAVED>
+__global__ __launch_bounds__(2 * HD) void k_write_rows_q8(WriteArgs a, int T) {
+    constexpr int R = 16, LPR = HD / 8;
+    __shared__ __attribute__((aligned(8))) uint8_t vt[R][HD + 8];
+    __shared__ int64_t at[R];      // the row's block, -1: not stored
+    __shared__ int slots[R];
+    const int r = threadIdx.x / LPR, i = threadIdx.x % LPR, t = blockIdx.x * R + r, hh = blockIdx.y;
+    const bool value = hh >= a.H + a.Hkv, keep = hh >= a.H;
+    const int j = value ? hh - a.H - a.Hkv : hh - a.H;
+    const int p = t < T ? a.pos[t] : -1;
+    const bool live = p >= 0;
+    const int half = a.rot / 2;
+    const bool turn = !value && (INTERLEAVED ? 8 * i < a.rot : 4 * i < half);
+    const int i0 = INTERLEAVED || value || !turn ? 8 * i : 4 * i, i1 = INTERLEAVED || value || !turn ? 8 * i + 4 : half + 4 * i;
+    int phys = -1;
+    float4_u x0 = {0.f, 0.f, 0.f, 0.f}, x1 = x0;
+    float4_u c0 = x0, c1 = x0;
+    if (live) {
+        const float *row = a.qkv + t * a.qkv_stride + hh * HD;
+        x0 = *reinterpret_cast<const float4_u *>(row + i0);
+        x1 = *reinterpret_cast<const float4_u *>(row + i1);
+        if (turn) {
+            const float *cs = a.cos_sin + ((int64_t)t * half + 4 * i) * 2;
+            c0 = *reinterpret_cast<const float4_u *>(cs);
+            c1 = *reinterpret_cast<const float4_u *>(cs + 4);
+        }
+        if (keep) {
+            const int b = p >> 4, seq = a.seq_slot[t];
+            phys = b < a.table_stride && seq >= 0 ? a.table[(int64_t)seq * a.table_stride + b] : -1;
+        }
+    }
+    const int slot = p & 15;
+    if (value) {
+        uint32_t top = 0;
+#pragma unroll
+        for (int e = 0; e < 4; e++) top = max(top, max(__float_as_uint(x0[e]) & 0x7f800000u, __float_as_uint(x1[e]) & 0x7f800000u));
+#pragma unroll
+        for (int off = LPR / 2; off > 0; off >>= 1) top = max(top, (uint32_t)__shfl_xor((int)top, off, WAVE));
+        const int e1 = q8_exponent32(top);
+        const float x[8] = {x0[0], x0[1], x0[2], x0[3], x1[0], x1[1], x1[2], x1[3]};
+        const int e[8] = {e1, e1, e1, e1, e1, e1, e1, e1};
+        *reinterpret_cast<uint2 *>(&vt[r][8 * i]) = q8_codes8(x, e);
+        if (i == 0) {
+            at[r] = phys;
+            slots[r] = slot;
+            if (phys >= 0) a.expo[(((int64_t)phys * 2 + 1) * a.Hkv + j) * 16 + slot] = (int8_t)e1;
+        }
+        __syncthreads();
+        const int vr = threadIdx.x % R;
+        const int64_t b = at[vr];
+        if (b < 0) return;
+        int8_t *dst = a.codes + b * q8_block(a.Hkv, HD) + q8_v(a.Hkv, HD, j, slots[vr], 0);
+        for (int d = threadIdx.x / R; d < HD; d += LPR) dst[16 * d] = (int8_t)vt[vr][d];
+        return;
+    }
+    double y[8] = {x0[0], x0[1], x0[2], x0[3], x1[0], x1[1], x1[2], x1[3]};
+    const float *gain = keep ? a.k_gain : a.q_gain;
+    if (gain) {
+        double ss = 0;
+#pragma unroll
+        for (int e = 0; e < 8; e++) ss += y[e] * y[e];
+#pragma unroll
+        for (int off = LPR / 2; off > 0; off >>= 1) ss += __shfl_xor(ss, off, WAVE);
+        const double n = 1.0 / sqrt(ss / HD + a.eps);
+#pragma unroll
+        for (int e = 0; e < 8; e++) y[e] *= n * gain[(e < 4 ? i0 : i1) + (e & 3)];
+    }
+    if (turn) {
+        const float cs[8] = {c0[0], c0[1], c0[2], c0[3], c1[0], c1[1], c1[2], c1[3]};
+#pragma unroll
+        for (int e = 0; e < 4; e++) {
+            const int u = INTERLEAVED ? 2 * e : e, w = INTERLEAVED ? 2 * e + 1 : e + 4;
+            const double c = cs[2 * e], s = cs[2 * e + 1], first = y[u] * c - y[w] * s;
+            y[w] = y[u] * s + y[w] * c;
+            y[u] = first;
+        }
+    }
+    if (!keep) {
+        if (live) {
+            float *q = a.q_out + t * a.q_out_stride + hh * HD;
+            *reinterpret_cast<float4_u *>(q + i0) = (float4_u){(float)y[0], (float)y[1], (float)y[2], (float)y[3]};
+            *reinterpret_cast<float4_u *>(q + i1) = (float4_u){(float)y[4], (float)y[5], (float)y[6], (float)y[7]};
+        }
+        return;
+    }
+    uint32_t top = 0;
+#pragma unroll
+    for (int e = 0; e < 8; e++) top = max(top, (uint32_t)__double2hiint(y[e]) & 0x7fffffffu);
+#pragma unroll
+    for (int off = LPR / 2; off > 0; off >>= 1) top = max(top, (uint32_t)__shfl_xor((int)top, off, WAVE));
+    if (phys < 0) return;
+    const int e1 = q8_exponent(top);
+    uint32_t n[2] = {0, 0};
+#pragma unroll
+    for (int e = 0; e < 8; e++) n[e >> 2] |= (uint32_t)(uint8_t)q8_code(y[e], e1) << (8 * (e & 3));
+    int8_t *dst = a.codes + phys * q8_block(a.Hkv, HD) + q8_k(HD, j, slot, 0);
+    *reinterpret_cast<uint32_t *>(dst + i0) = n[0];
+    *reinterpret_cast<uint32_t *>(dst + i1) = n[1];
+    if (i == 0) a.expo[((int64_t)phys * 2 * a.Hkv + j) * 16 + slot] = (int8_t)e1;
+}
+
 struct MoveArgs {
     const int32_t *table;
     int table_stride;
@@ -98,67 +203,131 @@ struct MoveArgs {
     int Hkv, max_len;
 };
 
-// Blocks of a range: logical block blockIdx.x of it, in both caches, and the slots [s0, s1) that it moves; false where there are none.
-__device__ __forceinline__ bool move_block(const MoveArgs &a, int64_t &full, int64_t &q8, int &s0, int &s1) {
-    const int32_t *r = a.ranges + 3 * blockIdx.y;
+// What a wave moves: block, KV head and keys or values of item number `item` (blocks, then keys and values, then heads: the order of memory); false where
+// the range has no such block or one side does not map it.
+struct Moved { int64_t full, q8; int j, value, s0, s1; };      // slots s0 .. s1 - 1
+__device__ __forceinline__ bool moved_block(const MoveArgs &a, uint32_t item, Moved &m) {
+    const int32_t *r = a.ranges + 3 * (int64_t)blockIdx.y;
     const int first = max(r[1], 0);
-    const int64_t end = min((int64_t)r[2], (int64_t)r[1] + a.max_len);
-    const int b = (first >> 4) + blockIdx.x;
-    s0 = max(first - b * 16, 0);
-    s1 = (int)min(end - (int64_t)b * 16, (int64_t)16);
-    if (s0 >= s1 || r[0] < 0 || b >= a.table_stride || b >= a.q8_table_stride) return false;
-    full = a.table[(int64_t)r[0] * a.table_stride + b];
-    q8 = a.q8_table[(int64_t)r[0] * a.q8_table_stride + b];
-    return full >= 0 && q8 >= 0;
+    const int64_t end = min((int64_t)r[2], (int64_t)r[1] + a.max_len), b = (int64_t)(first >> 4) + item / (uint32_t)(2 * a.Hkv);
+    m.s0 = (int)max(first - b * 16, (int64_t)0);
+    m.s1 = (int)min(end - b * 16, (int64_t)16);
+    if (m.s0 >= m.s1 || r[0] < 0 || b >= a.table_stride || b >= a.q8_table_stride) return false;
+    m.full = a.table[(int64_t)r[0] * a.table_stride + b];
+    m.q8 = a.q8_table[(int64_t)r[0] * a.q8_table_stride + b];
+    const int part = (int)(item % (uint32_t)(2 * a.Hkv));
+    m.value = part >= a.Hkv;
+    m.j = part - (m.value ? a.Hkv : 0);
+    return m.full >= 0 && m.q8 >= 0;
 }
 
-__device__ __forceinline__ float elem(const float *p) { return *p; }
-__device__ __forceinline__ float elem(const bf16_t *p) { return bf16_to_f32(*p); }
+// Eight consecutive elements as floats, and back (rounded to nearest; a code times its unit is exact).
+__device__ __forceinline__ void put8(bf16_t *p, const float (&v)[8]) {
+    *reinterpret_cast<uint4 *>(p) = make_uint4(pack2_bf16(v[0], v[1]), pack2_bf16(v[2], v[3]), pack2_bf16(v[4], v[5]), pack2_bf16(v[6], v[7]));
+}
+__device__ __forceinline__ void put8(float *p, const float (&v)[8]) {
+    reinterpret_cast<float4 *>(p)[0] = make_float4(v[0], v[1], v[2], v[3]);
+    reinterpret_cast<float4 *>(p)[1] = make_float4(v[4], v[5], v[6], v[7]);
+}
 
-// One wave a block, head, and keys or values; a position at a time.
+// A wave an item, eight elements a lane and load: of keys HD / 8 lanes a position, of values two lanes a dimension (slots 0 .. 7, 8 .. 15).  The largest
+// exponent is the exponent of the largest.  What bounds it is the traffic; whole blocks leave in 8-byte pieces in the order of memory, of others only
+// the range's slots.
 template <int HD, typename KT>
-__global__ __launch_bounds__(64) void k_to_q8(MoveArgs a, const KT *__restrict__ pool, int8_t *__restrict__ codes, int8_t *__restrict__ expo) {
-    int64_t full, q8;
-    int s0, s1;
-    if (!move_block(a, full, q8, s0, s1)) return;
-    const int j = blockIdx.z >> 1, value = blockIdx.z & 1, lane = threadIdx.x;
-    const KT *src = pool + full * kv_block_elems(a.Hkv, HD);
-    int8_t *dst = codes + q8 * q8_block(a.Hkv, HD);
-    for (int s = s0; s < s1; s++) {
-        float x[HD / 64];
-        uint32_t top = 0;
-        for (int u = 0; u < HD / 64; u++) {
-            const int d = lane + 64 * u;
-            x[u] = elem(src + (value ? kv_v_offset(a.Hkv, HD, j, s, d) : kv_k_offset(HD, j, s, d)));
-            top = max(top, (uint32_t)__double2hiint((double)x[u]) & 0x7fffffffu);
+__global__ __launch_bounds__(256) void k_to_q8(MoveArgs a, uint32_t items, const KT *__restrict__ pool, int8_t *__restrict__ codes, int8_t *__restrict__ expo) {
+    constexpr int N = HD / 32, LPR = HD / 8;      // loads; lanes a key row
+    const uint32_t item = blockIdx.x * 4u + (threadIdx.x >> 6);
+    const int lane = threadIdx.x & 63;
+    Moved m;
+    if (item >= items || !moved_block(a, item, m)) return;
+    const KT *src = pool + m.full * kv_block_elems(a.Hkv, HD) + ((int64_t)m.value * a.Hkv + m.j) * 16 * HD + 8 * lane;
+    int8_t *dst = codes + m.q8 * q8_block(a.Hkv, HD) + ((int64_t)m.value * a.Hkv + m.j) * 16 * HD + 8 * lane;
+    int8_t *ex = expo + ((m.q8 * 2 + m.value) * a.Hkv + m.j) * 16;
+    float x[N][8];
+#pragma unroll
+    for (int n = 0; n < N; n++) load8(src + 512 * n, x[n]);
+    if (!m.value) {
+#pragma unroll
+        for (int n = 0; n < N; n++) {
+            uint32_t top = 0;
+#pragma unroll
+            for (int i = 0; i < 8; i++) top = max(top, __float_as_uint(x[n][i]) & 0x7f800000u);
+#pragma unroll
+            for (int off = LPR / 2; off > 0; off >>= 1) top = max(top, (uint32_t)__shfl_xor((int)top, off, WAVE));
+            const int e1 = q8_exponent32(top), slot = (lane + 64 * n) / LPR;
+            const int e[8] = {e1, e1, e1, e1, e1, e1, e1, e1};
+            if (slot < m.s0 || slot >= m.s1) continue;
+            *reinterpret_cast<uint2 *>(dst + 512 * n) = q8_codes8(x[n], e);
+            if (lane % LPR == 0) ex[slot] = (int8_t)e1;
         }
-        for (int off = 32; off > 0; off >>= 1) top = max(top, (uint32_t)__shfl_xor((int)top, off, WAVE));
-        const int e = q8_exponent(top);
-        for (int u = 0; u < HD / 64; u++) {
-            const int d = lane + 64 * u;
-            dst[value ? q8_v(a.Hkv, HD, j, s, d) : q8_k(HD, j, s, d)] = q8_code(x[u], e);
+        return;
+    }
+    uint32_t top[8] = {};
+#pragma unroll
+    for (int i = 0; i < 8; i++) {
+#pragma unroll
+        for (int n = 0; n < N; n++) top[i] = max(top[i], __float_as_uint(x[n][i]) & 0x7f800000u);
+#pragma unroll
+        for (int off = 2; off < 64; off <<= 1) top[i] = max(top[i], (uint32_t)__shfl_xor((int)top[i], off, WAVE));
+    }
+    int e[8];
+#pragma unroll
+    for (int i = 0; i < 8; i++) e[i] = q8_exponent32(top[i]);
+    const int first = 8 * (lane & 1);
+#pragma unroll
+    for (int n = 0; n < N; n++) {
+        const uint2 c = q8_codes8(x[n], e);
+        if (m.s0 == 0 && m.s1 == 16) {
+            *reinterpret_cast<uint2 *>(dst + 512 * n) = c;
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; i++)
+                if (first + i >= m.s0 && first + i < m.s1) dst[512 * n + i] = (int8_t)((i < 4 ? c.x : c.y) >> (8 * (i & 3)));
         }
-        if (lane == 0) expo[((q8 * 2 + value) * a.Hkv + j) * 16 + s] = (int8_t)e;
+    }
+    if (lane < 2) {
+#pragma unroll
+        for (int i = 0; i < 8; i++)
+            if (first + i >= m.s0 && first + i < m.s1) ex[first + i] = (int8_t)e[i];
     }
 }
 
 template <int HD, typename KT>
-__global__ __launch_bounds__(64) void k_from_q8(MoveArgs a, const int8_t *__restrict__ codes, const int8_t *__restrict__ expo, KT *__restrict__ pool) {
-    int64_t full, q8;
-    int s0, s1;
-    if (!move_block(a, full, q8, s0, s1)) return;
-    const int j = blockIdx.z >> 1, value = blockIdx.z & 1, lane = threadIdx.x;
-    const int8_t *src = codes + q8 * q8_block(a.Hkv, HD);
-    KT *dst = pool + full * kv_block_elems(a.Hkv, HD);
-    for (int s = s0; s < s1; s++) {
-        const float unit = q8_unit(expo[((q8 * 2 + value) * a.Hkv + j) * 16 + s]);
-        for (int u = 0; u < HD / 64; u++) {
-            const int d = lane + 64 * u;
-            store_elem(dst + (value ? kv_v_offset(a.Hkv, HD, j, s, d) : kv_k_offset(HD, j, s, d)),
-                       unit * src[value ? q8_v(a.Hkv, HD, j, s, d) : q8_k(HD, j, s, d)]);
+__global__ __launch_bounds__(256) void k_from_q8(MoveArgs a, uint32_t items, const int8_t *__restrict__ codes, const int8_t *__restrict__ expo, KT *__restrict__ pool) {
+    constexpr int N = HD / 32, LPR = HD / 8;
+    const uint32_t item = blockIdx.x * 4u + (threadIdx.x >> 6);
+    const int lane = threadIdx.x & 63;
+    Moved m;
+    if (item >= items || !moved_block(a, item, m)) return;
+    const int8_t *src = codes + m.q8 * q8_block(a.Hkv, HD) + ((int64_t)m.value * a.Hkv + m.j) * 16 * HD + 8 * lane;
+    const int8_t *ex = expo + ((m.q8 * 2 + m.value) * a.Hkv + m.j) * 16;
+    KT *dst = pool + m.full * kv_block_elems(a.Hkv, HD) + ((int64_t)m.value * a.Hkv + m.j) * 16 * HD + 8 * lane;
+    const int first = 8 * (lane & 1);
+    uint2 c[N];
+#pragma unroll
+    for (int n = 0; n < N; n++) c[n] = *reinterpret_cast<const uint2 *>(src + 512 * n);
+    const uint2 ev = *reinterpret_cast<const uint2 *>(ex + first);
+#pragma unroll
+    for (int n = 0; n < N; n++) {
+        const int slot = (lane + 64 * n) / LPR;      // of keys
+        const float one = m.value ? 0.f : q8_unit(ex[slot]);
+        float v[8];
+#pragma unroll
+        for (int i = 0; i < 8; i++) {
+            const int code = (int)(int8_t)((i < 4 ? c[n].x : c[n].y) >> (8 * (i & 3))), e = (int)(int8_t)((i < 4 ? ev.x : ev.y) >> (8 * (i & 3)));
+            v[i] = (float)code * (m.value ? q8_unit(e) : one);
+        }
+        if (m.value ? m.s0 == 0 && m.s1 == 16 : slot >= m.s0 && slot < m.s1) {
+            put8(dst + 512 * n, v);
+        } else if (m.value) {
+#pragma unroll
+            for (int i = 0; i < 8; i++)
+                if (first + i >= m.s0 && first + i < m.s1) store_elem(dst + 512 * n + i, v[i]);
         }
     }
 }
+
+constexpr int MANY_ROWS = 64;
 
 bool bad_pool(const void *codes, const void *expo) { return !codes || !expo || (((uintptr_t)codes | (uintptr_t)expo) & 15); }
 
@@ -208,8 +377,16 @@ ld_status ldk_rope_kv_write_q8(const float *qkv, int32_t qkv_stride, const float
         return ld::fail(LD_E_INVAL, "ldk_rope_kv_write_q8: bad argument");
     if (H + 2 * (int64_t)Hkv > 65535) return ld::fail(LD_E_RANGE, "ldk_rope_kv_write_q8: more than 65535 heads");
     const WriteArgs a{qkv, qkv_stride, q_gain, k_gain, eps, cos_sin, rot, pos, seq_slot, table, table_stride, codes, expo, H, Hkv, q_out, q_out_stride};
-    const dim3 grid(T, H + 2 * Hkv), block(64);
     hipStream_t s = (hipStream_t)stream;
+    if (T >= MANY_ROWS && rot % 8 == 0) {
+        const dim3 grid((T + 15) / 16, H + 2 * Hkv), block(2 * hd);
+#define LD_ROWS(HD_, IL_) LD_LAUNCH((k_write_rows_q8<HD_, IL_>), grid, block, 0, s, a, T)
+        if (hd == 128) { if (interleaved) LD_ROWS(128, true); else LD_ROWS(128, false); }
+        else { if (interleaved) LD_ROWS(64, true); else LD_ROWS(64, false); }
+#undef LD_ROWS
+        return launched("k_write_rows_q8");
+    }
+    const dim3 grid(T, H + 2 * Hkv), block(64);
     if (hd == 128) { if (interleaved) LD_LAUNCH((k_write_q8<128, true>), grid, block, 0, s, a); else LD_LAUNCH((k_write_q8<128, false>), grid, block, 0, s, a); }
     else { if (interleaved) LD_LAUNCH((k_write_q8<64, true>), grid, block, 0, s, a); else LD_LAUNCH((k_write_q8<64, false>), grid, block, 0, s, a); }
     return launched("k_write_q8");
@@ -221,9 +398,11 @@ ld_status ldk_kv_to_q8(const void *pool_layer, int32_t dtype, const int32_t *tab
     if (n_ranges == 0 || max_len == 0) return LD_OK;
     const MoveArgs a{table, table_stride, q8_table, q8_table_stride, ranges, Hkv, max_len};
     if (const ld_status bad = check_move("ldk_kv_to_q8", pool_layer, dtype, a, codes, expo, n_ranges, hd)) return bad;
-    const dim3 grid((unsigned)(((int64_t)max_len + 14) / 16 + 1), n_ranges, 2 * Hkv), block(64);
+    const int64_t items = (((int64_t)max_len + 14) / 16 + 1) * 2 * Hkv;      // positions first .. first + max_len - 1 touch at most so many blocks
+    if (items > INT32_MAX) return ld::fail(LD_E_RANGE, "ldk_kv_to_q8: too many blocks a range");
+    const dim3 grid((unsigned)((items + 3) / 4), n_ranges), block(256);
     hipStream_t s = (hipStream_t)stream;
-#define LD_TO(HD_, KT_) LD_LAUNCH((k_to_q8<HD_, KT_>), grid, block, 0, s, a, (const KT_ *)pool_layer, codes, expo)
+#define LD_TO(HD_, KT_) LD_LAUNCH((k_to_q8<HD_, KT_>), grid, block, 0, s, a, (uint32_t)items, (const KT_ *)pool_layer, codes, expo)
     if (dtype == LD_BF16) { if (hd == 128) LD_TO(128, bf16_t); else LD_TO(64, bf16_t); }
     else { if (hd == 128) LD_TO(128, float); else LD_TO(64, float); }
 #undef LD_TO
@@ -236,9 +415,11 @@ ld_status ldk_kv_from_q8(const int8_t *codes, const int8_t *expo, const int32_t 
     if (n_ranges == 0 || max_len == 0) return LD_OK;
     const MoveArgs a{table, table_stride, q8_table, q8_table_stride, ranges, Hkv, max_len};
     if (const ld_status bad = check_move("ldk_kv_from_q8", pool_layer, dtype, a, codes, expo, n_ranges, hd)) return bad;
-    const dim3 grid((unsigned)(((int64_t)max_len + 14) / 16 + 1), n_ranges, 2 * Hkv), block(64);
+    const int64_t items = (((int64_t)max_len + 14) / 16 + 1) * 2 * Hkv;      // positions first .. first + max_len - 1 touch at most so many blocks
+    if (items > INT32_MAX) return ld::fail(LD_E_RANGE, "ldk_kv_from_q8: too many blocks a range");
+    const dim3 grid((unsigned)((items + 3) / 4), n_ranges), block(256);
     hipStream_t s = (hipStream_t)stream;
-#define LD_FROM(HD_, KT_) LD_LAUNCH((k_from_q8<HD_, KT_>), grid, block, 0, s, a, codes, expo, (KT_ *)pool_layer)
+#define LD_FROM(HD_, KT_) LD_LAUNCH((k_from_q8<HD_, KT_>), grid, block, 0, s, a, (uint32_t)items, codes, expo, (KT_ *)pool_layer)
     if (dtype == LD_BF16) { if (hd == 128) LD_FROM(128, bf16_t); else LD_FROM(64, bf16_t); }
     else { if (hd == 128) LD_FROM(128, float); else LD_FROM(64, float); }
 #undef LD_FROM
