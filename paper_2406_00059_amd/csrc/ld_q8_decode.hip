@@ -46,8 +46,9 @@ __global__ __launch_bounds__(64 * WAVES, 2) void k_decode_q8(Q8Attention a, cons
                                                              const int32_t *__restrict__ ctx_len, int max_ctx, int chunk, int chunks, float *__restrict__ part_o,
                                                              float2 *__restrict__ part_ml) {
     constexpr int KS = HD / 64, ND = HD / 16, TERMS = 16 / GP, PASSES = (3 + TERMS - 1) / TERMS;
-    const int t = blockIdx.x / chunks, ch = blockIdx.x % chunks;
-    const int G = a.H / a.Hkv, parts = (G + 15) / 16, j = blockIdx.y / parts, h0 = j * G + blockIdx.y % parts * 16, heads = min(G - (int)(blockIdx.y % parts) * 16, 16);
+    // heads next to each other: a block's keys and values of all heads lie together
+    const int G = a.H / a.Hkv, parts = (G + 15) / 16, groups = a.Hkv * parts, item = blockIdx.x / groups, t = item / chunks, ch = item % chunks;
+    const int hg = blockIdx.x % groups, j = hg / parts, h0 = j * G + hg % parts * 16, heads = min(G - hg % parts * 16, 16);
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = lane & 15, g = lane >> 4, head = c % GP, term = c / GP;
     const int len = ctx_len[t];
     const Seen see = seen_of(len, first ? first[t] : 0, max_ctx, a.window, a.table_stride);
@@ -278,12 +279,12 @@ __global__ __launch_bounds__(64 * WAVES, 2) void k_decode_q8(Q8Attention a, cons
             acc += ml.y == 0.f ? 0.f : f * so[w][hh][d];
         }
         const float r = L == 0.f ? 0.f : acc / L;
-        const int64_t item = (int64_t)t * a.H + h0 + hh;
+        const int64_t at = (int64_t)t * a.H + h0 + hh;
         if (chunks == 1) {
-            a.out[item * HD + d] = r;
+            a.out[at * HD + d] = r;
         } else {
-            part_o[(item * chunks + ch) * HD + d] = r;
-            if (d == 0) part_ml[item * chunks + ch] = make_float2(M, L);
+            part_o[(at * chunks + ch) * HD + d] = r;
+            if (d == 0) part_ml[at * chunks + ch] = make_float2(M, L);
         }
     }
 }
@@ -357,7 +358,7 @@ void launch_decode(const Q8Attention &a, const int32_t *seq_slot, const int32_t 
     float *part_o = (float *)(scratch + ld::align_up(p.rows * 8, 256));
     float2 *part_ml = (float2 *)scratch;
     const int parts = (a.H / a.Hkv + 15) / 16;
-    const dim3 grid(T * p.chunks, a.Hkv * parts), block(64 * WAVES);
+    const dim3 grid((unsigned)((int64_t)T * p.chunks * a.Hkv * parts)), block(64 * WAVES);
     if (a.softcap > 0.f || a.slopes)
         LD_LAUNCH((k_decode_q8<HD, GP, true>), grid, block, 0, s, a, seq_slot, first, ctx_len, max_ctx, p.chunk, p.chunks, part_o, part_ml);
     else
@@ -396,7 +397,7 @@ ld_status ldk_paged_attention_q8(const float *q, int32_t q_stride, const int8_t 
     const Q8Attention a{q, q_stride, codes, expo, table, table_stride, H, Hkv, window, softcap, slopes, out};
     if (T < 0 || max_ctx < 0 || !seq_slot || !ctx_len || bad_attention(a, hd)) return ld::fail(LD_E_INVAL, "ldk_paged_attention_q8: bad argument");
     const Plan p = plan(T, H, Hkv, max_ctx, window);
-    if (H > 65535 || (int64_t)T * p.chunks > INT32_MAX) return ld::fail(LD_E_RANGE, "ldk_paged_attention_q8: more than 65535 heads, or too many rows");
+    if (H > 65535 || (int64_t)T * p.chunks * H > INT32_MAX) return ld::fail(LD_E_RANGE, "ldk_paged_attention_q8: more than 65535 heads, or too many rows");
     if (!scratch || ((uintptr_t)scratch & 15) || scratch_bytes < ldk_attention_q8_scratch_bytes(T, H, Hkv, hd, max_ctx, window))
         return ld::fail(LD_E_INVAL, "ldk_paged_attention_q8: scratch too small, or not aligned to 16 bytes");
     hipStream_t s = (hipStream_t)stream;
