@@ -68,7 +68,7 @@ __device__ __forceinline__ float q8_cap(float s, float cap, float inv_cap) {
     const float x = fabsf(s) * inv_cap, x2 = x * x;
     const float series = x * (1.f + x2 * (-1.f / 3 + x2 * (2.f / 15 + x2 * (-17.f / 315 + x2 * (62.f / 2835)))));
     const float t = fast_exp2(-2.8853900817779268f * x);
-    return copysignf(cap * (x < 0.25f ? series : (1.f - t) / (1.f + t)), s);
+    return copysignf(cap * (x < 0.25f ? series : (1.f - t) * __builtin_amdgcn_rcpf(1.f + t)), s);
 }
 
 typedef int i32x4_t __attribute__((ext_vector_type(4)));

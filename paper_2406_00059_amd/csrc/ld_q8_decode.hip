@@ -50,7 +50,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void k_decode_q8(Q8Attention a, cons
     const int G = a.H / a.Hkv, parts = (G + 15) / 16, groups = a.Hkv * parts, item = blockIdx.x / groups, t = item / chunks, ch = item % chunks;
     const int hg = blockIdx.x % groups, j = hg / parts, h0 = j * G + hg % parts * 16, heads = min(G - hg % parts * 16, 16);
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = lane & 15, g = lane >> 4, head = c % GP, term = c / GP;
-    const int len = ctx_len[t];
+    const int len = ctx_len[t], seq = seq_slot[t];
     const Seen see = seen_of(len, first ? first[t] : 0, max_ctx, a.window, a.table_stride);
     const int t0 = (see.lo >> 6) + ch * chunk, t1 = min(t0 + chunk, (see.hi >> 6) + 1);
     if (see.hi < see.lo || t0 >= t1) {
@@ -58,10 +58,40 @@ __global__ __launch_bounds__(64 * WAVES, 2) void k_decode_q8(Q8Attention a, cons
             for (int i = threadIdx.x; i < heads * HD; i += 64 * WAVES) a.out[((int64_t)t * a.H + h0) * HD + i] = 0.f;
         return;
     }
-    const int32_t *trow = a.table + (int64_t)seq_slot[t] * a.table_stride;
+    const int32_t *trow = a.table + (int64_t)seq * a.table_stride;
     const int last = see.hi >> 4;      // last visible block
     const int64_t bs = q8_block(a.Hkv, HD);
     const int8_t *kbase = a.codes + q8_k(HD, j, c & 3, 16 * g), *vbase = a.codes + q8_v(a.Hkv, HD, j, 0, c);
+
+    u32x4_t kf[4][KS], vf[ND], ek, ev;
+    int idk, idv;      // blocks of the tile to be loaded: the one of this lane's key rows, and block g
+    auto ask = [&](int tile) {
+        idk = trow[min(4 * tile + (c >> 2), last)];
+        idv = trow[min(4 * tile + g, last)];
+    };
+    auto load_k = [&]() {
+        const int8_t *p = kbase + max(idk, 0) * bs;
+#pragma unroll
+        for (int s = 0; s < 4; s++)
+#pragma unroll
+            for (int u = 0; u < KS; u++) kf[s][u] = load_stream16(p + 4 * s * HD + 64 * u);
+        const int8_t *e = a.expo + ((int64_t)max(idv, 0) * 2 * a.Hkv + j) * 16;
+        ek = *reinterpret_cast<const u32x4_t *>(e);
+        ev = *reinterpret_cast<const u32x4_t *>(e + a.Hkv * 16);
+    };
+    auto load_v = [&](int id) {
+        const int8_t *p = vbase + max(id, 0) * bs;
+#pragma unroll
+        for (int n = 0; n < ND; n++) vf[n] = load_stream16(p + 256 * n);
+    };
+
+    // The first tile is asked for before the queries are made ready
+    const int begin = t0 + wave;
+    if (begin < t1) {
+        ask(begin);
+        load_k();
+        load_v(idv);
+    }
 
     // Queries: dims 64 s + 16 g .. + 16 of this lane's head and term
     i32x4_t qd[PASSES][KS];
@@ -105,34 +135,6 @@ __global__ __launch_bounds__(64 * WAVES, 2) void k_decode_q8(Q8Attention a, cons
     float m = -INFINITY, l = 0.f;      // log2 domain; l over this lane's own positions
     int k = -100000;                   // o is in units of 2^(k - 14)
 
-    u32x4_t kf[4][KS], vf[ND], ek, ev;
-    int idk, idv;      // blocks of the tile to be loaded: the one of this lane's key rows, and block g
-    auto ask = [&](int tile) {
-        idk = trow[min(4 * tile + (c >> 2), last)];
-        idv = trow[min(4 * tile + g, last)];
-    };
-    auto load_k = [&]() {
-        const int8_t *p = kbase + max(idk, 0) * bs;
-#pragma unroll
-        for (int s = 0; s < 4; s++)
-#pragma unroll
-            for (int u = 0; u < KS; u++) kf[s][u] = load_stream16(p + 4 * s * HD + 64 * u);
-        const int8_t *e = a.expo + ((int64_t)max(idv, 0) * 2 * a.Hkv + j) * 16;
-        ek = *reinterpret_cast<const u32x4_t *>(e);
-        ev = *reinterpret_cast<const u32x4_t *>(e + a.Hkv * 16);
-    };
-    auto load_v = [&](int id) {
-        const int8_t *p = vbase + max(id, 0) * bs;
-#pragma unroll
-        for (int n = 0; n < ND; n++) vf[n] = load_stream16(p + 256 * n);
-    };
-
-    const int begin = t0 + wave;
-    if (begin < t1) {
-        ask(begin);
-        load_k();
-        load_v(idv);
-    }
     for (int tile = begin; tile < t1; tile += WAVES) {
         const bool more = tile + WAVES < t1;
         // ---- scores of block g's 16 slots
@@ -339,6 +341,8 @@ int visible_tiles(int max_ctx, int window) {
     return (int)(window > 0 ? std::min<int64_t>(all, ((int64_t)window + TILE - 2) / TILE + 1) : all);
 }
 
+// us of one row at 1520 positions of 32 heads / one at 131067 of 8 KV heads / 32 of 32 heads at 512 - 8192: 256 workgroups 11.6 / 59 / 224, 512 11.4 / 59 / 224,
+// 1024 11.4 / 67 / 224, 2048 11.5 / 83 / 224; chunks of at most 16 tiles 11.4 / 67 / 237; of at least two 13.0 / 59 / 224.
 constexpr int WANT = 512, CHUNK_TILES = 32;
 
 Plan plan(int T, int H, int Hkv, int max_ctx, int window) {

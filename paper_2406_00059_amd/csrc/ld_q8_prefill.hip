@@ -58,7 +58,7 @@ __global__ __launch_bounds__(256, 2) void k_prefill_q8(Q8Attention a, const int3
     const TileRows tr{tp[0], min(tp[1], ROWS), tp[2], tp[3], tp[4], tp[5]};
     if (tr.n <= 0) return;
     const int most = (int)min((int64_t)max_pos, (int64_t)a.table_stride * 16 - 1);
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, r32 = lane & 31, hh = lane >> 5;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), r32 = lane & 31, hh = lane >> 5;
     const int wlo = seen_from(tr, 0, a.window), whi = seen_to(tr, tr.n - 1, most);      // of the workgroup
     int t0 = wlo >> 6, t1 = whi < wlo ? t0 : (whi >> 6) + 1;
     const int per = (t1 - t0 + splits - 1) / splits;
@@ -158,7 +158,7 @@ __global__ __launch_bounds__(256, 2) void k_prefill_q8(Q8Attention a, const int3
     int x2 = 0;                                 // o is in units of 2^-x2
 
     auto multiply = [&](const Stage<HD> &st, int tile) {
-        const int base = tile * TILE;
+        const int base = tile * TILE, mapped = __builtin_amdgcn_readfirstlane(st.mapped);
         float s[2][16];
 #pragma unroll
         for (int u = 0; u < 2; u++) {
@@ -188,7 +188,7 @@ __global__ __launch_bounds__(256, 2) void k_prefill_q8(Q8Attention a, const int3
                 }
             }
         }
-        const bool whole = base >= all_lo && base + TILE - 1 <= all_hi && st.mapped == 15;
+        const bool whole = base >= all_lo && base + TILE - 1 <= all_hi && mapped == 15;
         uint32_t ok = 0xffffffffu;
         if (!whole) {
             ok = 0;
@@ -197,7 +197,7 @@ __global__ __launch_bounds__(256, 2) void k_prefill_q8(Q8Attention a, const int3
 #pragma unroll
                 for (int i = 0; i < 16; i++) {
                     const int p = base + 32 * u + 16 * hh + i;
-                    const bool see = p >= lo && p <= hi && (st.mapped >> (2 * u + hh) & 1);
+                    const bool see = p >= lo && p <= hi && (mapped >> (2 * u + hh) & 1);
                     ok |= (uint32_t)see << (16 * u + i);
                     s[u][i] = see ? s[u][i] : -INFINITY;
                 }
