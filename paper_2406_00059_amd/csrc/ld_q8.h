@@ -89,6 +89,16 @@ __device__ __forceinline__ f16x8_t q8_halves(uint32_t w0, uint32_t w1) {
     return (f16x8_t){h[0][0], h[0][1], h[1][0], h[1][1], h[2][0], h[2][1], h[3][0], h[3][1]};
 }
 
+// a and b as sums of two fp16 numbers each (22 bits), packed in pairs: four instructions (the compiler's own way takes eight).
+__device__ __forceinline__ void split2_halves(float a, float b, uint32_t &hi, uint32_t &lo) {
+    typedef float f32x2_t __attribute__((ext_vector_type(2)));
+    hi = __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2_t){a, b}, f16x2_t));
+    float x, y;
+    asm("v_fma_mix_f32 %0, %1, -1.0, %2 op_sel_hi:[1,0,0]" : "=v"(x) : "v"(hi), "v"(a));
+    asm("v_fma_mix_f32 %0, %1, -1.0, %2 op_sel:[1,0,0] op_sel_hi:[1,0,0]" : "=v"(y) : "v"(hi), "v"(b));
+    lo = __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2_t){x, y}, f16x2_t));
+}
+
 // A query as whole numbers n = round(8355711 q / max |q|), three base-256 digits from -128 .. 127 each: q = n unit 2^exp, |n - exact| <= 1/2.
 struct Q8Query {
     double scale;      // 8355711 / max |q|, 0 for a query that is zero or not finite

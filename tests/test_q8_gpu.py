@@ -273,14 +273,14 @@ def test_moves_leave_out_unmapped_blocks_and_positions_past_max_len():
 U = 2.0 ** -24      # half a step of float32 at 1
 
 
-def _attend(q, k, v, p, lo, hi, cap, slope):
+def _attend(q, k, v, p, lo, hi, cap, slope, least=13):
     """One row and head in float64 over positions lo .. hi of k, v [positions, hd]; the result, and how far float32 may be off it.
 
     A score is at most 2^-23 of max |q| sum |k| / sqrt(hd) off by the query's 24 bits under its largest element, some eight roundings of that size by
     its sums, scales and conversions, eight of the capped score, four of the bias; a weight some sixteen roundings (the exponential's argument and its
     result, its two 11-bit halves, the value's unit) and as many as its distance from the top in the argument; the sum one each 64 positions.
-    The halves are fp16 numbers whose smallest step is 2^-24, under 2^14 for the largest p 2^e (rounded up to a power of two) of the position's share: a
-    weight times its value's unit is besides up to half a step off, 2^-25 2^-14 2 max p 2^e.  That shows where the value that draws everything has a
+    The halves are fp16 numbers whose smallest step is 2^-24, and the largest p 2^e is held at 2^least or more (the decode kernel: 2^13, the one for prompt
+    rows, which scales less often: 2^9): a weight times its value's unit is besides up to half a step off, 2^-25 2^-least max p 2^e.  That shows where the value that draws everything has a
     code of zero (a weight of 4e-10 was 0.8 % off beside one of 1)."""
     hd = len(q)
     lo, hi = max(lo, 0), min(hi, len(k) - 1)
@@ -306,7 +306,7 @@ def _attend(q, k, v, p, lo, hi, cap, slope):
     out = w @ v
     top = np.abs(v).max(1)
     unit = np.exp2(np.where(top > 0, np.floor(np.log2(np.where(top > 0, top, 1.0))) - 6, -126.0))
-    step = 2.0 ** -38 * (w * unit).max() * (np.abs(v) / unit[:, None]).sum(0)
+    step = 2.0 ** (-25 - least) * (w * unit).max() * (np.abs(v) / unit[:, None]).sum(0)
     return out, (w * off) @ np.abs(v) + np.abs(out) * (w @ off) + step + 1e-30
 
 
@@ -473,7 +473,7 @@ def test_decode_of_blocks_past_two_and_four_gigabytes():
     chunk = torch.empty((2, H, hd), device=DEV)
     scratch = torch.empty(ld.ldk_prefill_attention_q8_scratch_bytes(2, H, Hkv, hd, n), dtype=torch.uint8, device=DEV)
     ld.ldk_prefill_attention_q8(q.to(DEV), H * hd, codes, expo, _i32(places[lt]), tiles, H, Hkv, hd, chunk, n - 1, scratch=scratch)
-    _check_decode(chunk, q, lt, lc, le, range(2), [n, n], H, Hkv, hd)
+    _check_prefill(chunk, q, lt, lc, le, tiles.tolist(), [n, n], H, Hkv, hd)
     pool = torch.zeros((6, 2, Hkv, 16, hd), dtype=torch.bfloat16, device=DEV)
     ranges = _i32([[0, 0, n], [1, 0, n]])
     ld.ldk_kv_from_q8(codes, expo, _i32(places[lt]), pool, _i32(lt), ranges, n, Hkv, hd)
@@ -507,7 +507,8 @@ def _check_prefill(out, q, table, codes, expo, tiles, lengths, H, Hkv, hd, windo
             lo, hi = max(first, p - window + 1 if window else 0), max(p, prefix - 1)
             for h in heads or range(H):
                 j = h // (H // Hkv)
-                ref, bound = _attend(qd[at + r, h * hd:(h + 1) * hd], k[:, j], v[:, j], p, lo, hi, cap, float(np.float32(slopes[h])) if slopes is not None else 0.0)
+                ref, bound = _attend(qd[at + r, h * hd:(h + 1) * hd], k[:, j], v[:, j], p, lo, hi, cap, float(np.float32(slopes[h])) if slopes is not None else 0.0,
+                                     least=9)
                 g = got[at + r, h]
                 assert np.array_equal(np.isnan(g), np.isnan(ref)), (at, r, h)
                 assert (np.abs(g - ref)[~np.isnan(ref)] <= bound[~np.isnan(ref)]).all(), (at, r, h, np.nanmax(np.abs(g - ref) / np.maximum(bound, 1e-300)))
