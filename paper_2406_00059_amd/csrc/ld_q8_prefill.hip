@@ -11,9 +11,13 @@
 // Which position a row of the score tile is, is free: row 8 b + 4 h + i is slot 4 b + i of block h of a pair, so that lane (row, h) ends with the scores of
 // block h, slot by slot, which is what it has to bring as the other operand of the sums.
 //
+// What bounds it: 64 positions and 32 rows are 56 matrix instructions (1800 cycles of a SIMD) and some 590 vector ones (2700), and with two waves a SIMD, which
+// is what the registers allow, the two add up (profiles: 39 and 59 % of the time).  8191 rows of 32 heads in a band of 4096 take 810 us, 510 TFLOP/s of the
+// formula and 890 of executed products.  Measured and not kept: scores in fp16 with queries in two terms (five vector instructions an entry less, a third more
+// matrix time, registers spilled: 1055 us); one wave a SIMD with the scores of the next tile formed ahead (1794); half tiles whose instructions are
+// interleaved by hand (826).
 #include <algorithm>
 #include <cmath>
-#include <type_traits>
 #include "ld_q8.h"
 
 using namespace ldd;
@@ -26,9 +30,10 @@ typedef float f32x16_t __attribute__((ext_vector_type(16)));
 
 template <int HD>
 struct Stage {
-    uint4 k[4 * HD];        // [position][piece of 16 dims, swizzled]
-    f16x8_t v[8 * HD];      // [block][half][dim]: eight slots
-    float unit[256];        // 2^e of the keys, 2^(e - E0) of the values; NaN where a vector is not finite; the rest is room for threads without one
+    uint4 k[4 * HD];               // [position][piece of 16 dims, swizzled]
+    f16x8_t v[8 * HD];             // [block][half][dim]: eight slots
+    float ku[TILE], vu[TILE];      // units; NaN where a vector is not finite
+    int mapped;                    // bit b: block b
 };
 
 // Piece p of position r (block r / 16, slot r % 16), so that eight lanes' pieces of a score operand lie in different banks.
@@ -63,10 +68,6 @@ struct TileRows { int row, n, pos, seq, first, prefix; };
 __device__ __forceinline__ int seen_from(const TileRows &t, int r, int window) { return max(max(t.first, window > 0 ? t.pos + r - window + 1 : 0), 0); }
 __device__ __forceinline__ int seen_to(const TileRows &t, int r, int most) { return min(max(t.pos + r, t.prefix - 1), most); }
 
-// Nothing is moved over this line.  The compiler puts matrix instructions next to each other, where each waits for the one before and the vector unit for
-// all of them; the parts of a step lie in the order in which they are to be issued.
-#define LD_HERE() __builtin_amdgcn_sched_barrier(0)
-
 template <int HD, bool EXTRA>
 __global__ __launch_bounds__(256, 2) void k_prefill_q8(Q8Attention a, const int32_t *__restrict__ tiles, int n_tiles, int max_pos, int splits,
                                                        float *__restrict__ part_o, float2 *__restrict__ part_ml) {
@@ -95,7 +96,7 @@ __global__ __launch_bounds__(256, 2) void k_prefill_q8(Q8Attention a, const int3
     const int wave_lo = seen_from(tr, 32 * wave, a.window), wave_hi = seen_to(tr, nlast, most);      // any row of the wave (if busy)
     const int all_lo = seen_from(tr, nlast, a.window), all_hi = seen_to(tr, 32 * wave, most);        // every row
 
-    __shared__ __attribute__((aligned(16))) Stage<HD> stage[3];
+    __shared__ __attribute__((aligned(16))) Stage<HD> stage[2];
     const int32_t *trow = a.table + (int64_t)tr.seq * a.table_stride;
     const int last = whi >> 4;
     const int64_t bs = q8_block(a.Hkv, HD);
@@ -104,44 +105,39 @@ __global__ __launch_bounds__(256, 2) void k_prefill_q8(Q8Attention a, const int3
     int id[NP], ide;
     uint4 kr[NP], vr[NP];
     int er = 0;
-    const int8_t *kbase = a.codes + q8_k(HD, j, 0, 0) + 16 * (tid % HD);      // HD divides 256: the same place in every block
-    auto ask = [&](int tile) __attribute__((always_inline)) {
+    const uint32_t place = 16 * (tid % HD);
+    const int eb = (tid & 63) >> 4;
+    auto ask = [&](int tile) {
 #pragma unroll
-        for (int u = 0; u < NP; u++) id[u] = trow[min(4 * tile + (tid + 256 * u) / HD, last)];
-        ide = trow[min(4 * tile + (lane >> 4), last)];
+        for (int u = 0; u < NP; u++) id[u] = trow[min(4 * tile + (64 * wave + 256 * u) / HD, last)];      // a wave's pieces lie in one block
+        ide = trow[min(4 * tile + eb, last)];
     };
-    auto load_keys = [&]() __attribute__((always_inline)) {
+    auto load = [&]() {
 #pragma unroll
-        for (int u = 0; u < NP; u++) kr[u] = *reinterpret_cast<const uint4 *>(kbase + max(id[u], 0) * bs);
-    };
-    auto load_values = [&]() __attribute__((always_inline)) {
-#pragma unroll
-        for (int u = 0; u < NP; u++) vr[u] = *reinterpret_cast<const uint4 *>(kbase + (int64_t)a.Hkv * 16 * HD + max(id[u], 0) * bs);
-        er = a.expo[(((int64_t)max(ide, 0) * 2 + (wave & 1)) * a.Hkv + j) * 16 + (lane & 15)];
-    };
-    // bit b: the tile's block b is mapped
-    auto mapped_of = [&]() __attribute__((always_inline)) {
-        const uint64_t ok = __ballot(ide >= 0);
-        return (int)((ok & 1) | (ok >> 15 & 2) | (ok >> 30 & 4) | (ok >> 45 & 8));
+        for (int u = 0; u < NP; u++) {
+            const int8_t *b = a.codes + max(__builtin_amdgcn_readfirstlane(id[u]), 0) * bs + q8_k(HD, j, 0, 0);      // a scalar: the lanes differ by 32 bits
+            kr[u] = *reinterpret_cast<const uint4 *>(b + place);
+            vr[u] = *reinterpret_cast<const uint4 *>(b + a.Hkv * 16 * HD + place);
+        }
+        if (tid < 128) er = a.expo[(((int64_t)max(ide, 0) * 2 + (tid >> 6)) * a.Hkv + j) * 16 + (tid & 15)];
     };
     // E0: the largest exponent of the first tile's values (those that are all zero aside); every wave finds it for itself
     int e0 = 0;
-    auto store_keys = [&](Stage<HD> &s) __attribute__((always_inline)) {
+    auto store = [&](Stage<HD> &s, int ide_of) __attribute__((always_inline)) {
 #pragma unroll
         for (int u = 0; u < NP; u++) {
-            const int i = tid + 256 * u, in = i % HD;
-            s.k[key_piece<HD>(i / HD * 16 + in / (HD / 16), in % (HD / 16))] = kr[u];
+            const int i = tid + 256 * u, b = i / HD, in = i % HD;
+            s.k[key_piece<HD>(b * 16 + in / (HD / 16), in % (HD / 16))] = kr[u];
+            s.v[(2 * b) * HD + in] = q8_halves(vr[u].x, vr[u].y);
+            s.v[(2 * b + 1) * HD + in] = q8_halves(vr[u].z, vr[u].w);
         }
-    };
-    // part 0 .. 2 NP - 1: eight slots of a thread's values each; with the last one the unit
-    auto store_values = [&](Stage<HD> &s, int part) __attribute__((always_inline)) {
-        const int u = part >> 1, i = tid + 256 * u;
-        s.v[(2 * (i / HD) + (part & 1)) * HD + i % HD] = part & 1 ? q8_halves(vr[u].z, vr[u].w) : q8_halves(vr[u].x, vr[u].y);
-        if (part == 2 * NP - 1) s.unit[tid] = er == Q8_NAN ? __uint_as_float(0x7fc00000u) : ldexpf(1.f, er - (wave & 1 ? e0 : 0));
-    };
-    auto store_all_values = [&](Stage<HD> &s) __attribute__((always_inline)) {
-#pragma unroll
-        for (int p = 0; p < 2 * NP; p++) store_values(s, p);
+        if (tid < 64) {
+            s.ku[tid] = q8_unit(er);
+            const uint64_t ok = __ballot(ide_of >= 0);
+            if (tid == 0) s.mapped = (int)((ok & 1) | (ok >> 15 & 2) | (ok >> 30 & 4) | (ok >> 45 & 8));
+        } else if (tid < 128) {
+            s.vu[tid - 64] = er == Q8_NAN ? __uint_as_float(0x7fc00000u) : ldexpf(1.f, er - e0);
+        }
     };
 
     // ---- queries: dims 32 s + 16 hh .. + 16 of this lane's row
@@ -188,64 +184,57 @@ __global__ __launch_bounds__(256, 2) void k_prefill_q8(Q8Attention a, const int3
     float add = NONE, l = 0.f;
     float big = 0.f;      // largest weight times its value's unit
 
-    // A tile is taken in as two halves of 32 positions.  Products of a half's keys and queries: digits 2, and digits 1 and 0 ..
-    i32x16_t acc2, acc;
-    i32x4_t kf[KS];
-    auto ask_keys = [&](const Stage<HD> &st, int u) __attribute__((always_inline)) {
-        const int row = (2 * u + ((r32 >> 2) & 1)) * 16 + (r32 >> 3) * 4 + (r32 & 3);
+    auto multiply = [&](const Stage<HD> &st, int tile) {
+        const int base = tile * TILE, mapped = __builtin_amdgcn_readfirstlane(st.mapped);
+        float s[2][16];
 #pragma unroll
-        for (int q = 0; q < KS; q++) kf[q] = __builtin_bit_cast(i32x4_t, st.k[key_piece<HD>(row, 2 * q + hh)]);
-    };
-    auto product = [&](int k) __attribute__((always_inline)) {      // 0 .. 3 KS - 1
-        if (k == 0) acc = (i32x16_t){};
-        if (k == 1) acc2 = (i32x16_t){};
-        if (k < 2 * KS) {
-            if (k & 1) acc2 = __builtin_amdgcn_mfma_i32_32x32x32_i8(kf[k >> 1], qd[2][k >> 1], acc2, 0, 0, 0);
-            else acc = __builtin_amdgcn_mfma_i32_32x32x32_i8(kf[k >> 1], qd[1][k >> 1], acc, 0, 0, 0);
-        } else {
-            if (k == 2 * KS) {
+        for (int u = 0; u < 2; u++) {
+            i32x16_t acc2 = {}, acc = {};
+            const int row = (2 * u + ((r32 >> 2) & 1)) * 16 + (r32 >> 3) * 4 + (r32 & 3);
+            i32x4_t kf[KS];
 #pragma unroll
-                for (int i = 0; i < 16; i++) acc[i] <<= 8;
-            }
-            acc = __builtin_amdgcn_mfma_i32_32x32x32_i8(kf[k - 2 * KS], qd[0][k - 2 * KS], acc, 0, 0, 0);
-        }
-    };
-    // .. and the scores that they make (times rs: in the log2 domain), four at a time
-    float s[16];
-    auto score4 = [&](int i4, const float4 &k4, int at) __attribute__((always_inline)) {
-        const float kk[4] = {k4.x, k4.y, k4.z, k4.w};
+            for (int q = 0; q < KS; q++) kf[q] = __builtin_bit_cast(i32x4_t, st.k[key_piece<HD>(row, 2 * q + hh)]);
 #pragma unroll
-        for (int e = 0; e < 4; e++) {
-            const int i = 4 * i4 + e;
-            s[i] = fmaf((float)acc2[i], 65536.f, (float)acc[i]) * kk[e];
-            if constexpr (EXTRA) {
-                float y = s[i] * unit;
-                if (a.softcap > 0.f) y = q8_cap(y, a.softcap, inv_cap);
-                s[i] = fmaf(slope, (float)(at + 16 * hh + i - (tr.pos + rr)), y * 1.4426950408889634f);
+            for (int q = 0; q < KS; q++) acc = __builtin_amdgcn_mfma_i32_32x32x32_i8(kf[q], qd[1][q], acc, 0, 0, 0);
+#pragma unroll
+            for (int q = 0; q < KS; q++) acc2 = __builtin_amdgcn_mfma_i32_32x32x32_i8(kf[q], qd[2][q], acc2, 0, 0, 0);
+#pragma unroll
+            for (int i = 0; i < 16; i++) acc[i] <<= 8;
+#pragma unroll
+            for (int q = 0; q < KS; q++) acc = __builtin_amdgcn_mfma_i32_32x32x32_i8(kf[q], qd[0][q], acc, 0, 0, 0);
+            const float4 *ku = reinterpret_cast<const float4 *>(st.ku + 32 * u + 16 * hh);
+#pragma unroll
+            for (int i = 0; i < 16; i++) {
+                const float4 k4 = ku[i >> 2];
+                const float kk = (i & 3) == 0 ? k4.x : (i & 3) == 1 ? k4.y : (i & 3) == 2 ? k4.z : k4.w;
+                s[u][i] = fmaf((float)acc2[i], 65536.f, (float)acc[i]) * kk;
+                if constexpr (EXTRA) {
+                    float y = s[u][i] * unit;
+                    if (a.softcap > 0.f) y = q8_cap(y, a.softcap, inv_cap);
+                    s[u][i] = fmaf(slope, (float)(base + 32 * u + 16 * hh + i - (tr.pos + rr)), y * 1.4426950408889634f);
+                }
             }
         }
-    };
-    // Takes in half u of tile `tile`, whose scores are in s; leaves those of the half behind it (of stage nst) there.  Its weights are formed while the next
-    // half's keys are multiplied, its values multiplied while the next half's scores are formed and (to: with the second half) a later tile is stored.
-    auto step = [&](const Stage<HD> &st, const Stage<HD> &nst, int tile, int mapped, auto half, Stage<HD> &to) __attribute__((always_inline)) {
-        constexpr int u = decltype(half)::value, un = 1 - u;
-        const int base = tile * TILE + 32 * u;
-        const bool whole = base >= all_lo && base + 31 <= all_hi && (mapped >> (2 * u) & 3) == 3;
-        // Keeps the entries whose positions the row sees.  What it compares is hidden from the compiler, which would hold the positions and as many truth
-        // values over all of the step otherwise.
-        auto keep_seen = [&](float (&x)[16], float other) __attribute__((always_inline)) {
+        const bool whole = base >= all_lo && base + TILE - 1 <= all_hi && mapped == 15;
+        // Keeps the entries whose positions the row sees.  What it compares is hidden from the compiler, which would hold 32 positions and as many
+        // truth values over all of the tile otherwise.
+        auto keep_seen = [&](float (&x)[2][16], float other) __attribute__((always_inline)) {
             int at = lo - base - 16 * hh;
             asm volatile("" : "+v"(at));
             const uint32_t range = (uint32_t)(hi - lo);
-            const bool there = (mapped >> (2 * u + hh) & 1) && hi >= lo;
 #pragma unroll
-            for (int i = 0; i < 16; i++) x[i] = there && (uint32_t)(i - at) <= range ? x[i] : other;
+            for (int u = 0; u < 2; u++) {
+                const bool there = (mapped >> (2 * u + hh) & 1) && hi >= lo;
+#pragma unroll
+                for (int i = 0; i < 16; i++) x[u][i] = there && (uint32_t)(32 * u + i - at) <= range ? x[u][i] : other;
+            }
         };
-        ask_keys(nst, un);
         if (!whole) keep_seen(s, -INFINITY);
         float most_s = -INFINITY;
 #pragma unroll
-        for (int i = 0; i < 16; i++) most_s = fmaxf(most_s, s[i]);
+        for (int u = 0; u < 2; u++)
+#pragma unroll
+            for (int i = 0; i < 16; i++) most_s = fmaxf(most_s, s[u][i]);
         most_s = max_halves(most_s) * rs;
         // the first score makes the largest weight 2^12; one that would be above 2^30 does so too
         if (__any(most_s + add > 30.f)) {
@@ -259,44 +248,24 @@ __global__ __launch_bounds__(256, 2) void k_prefill_q8(Q8Attention a, const int3
 #pragma unroll
                 for (int i = 0; i < 16; i++) o[n][i] *= keep;
         }
-        // ---- weights, beside the next half's products
-        const float4 *vu = reinterpret_cast<const float4 *>(st.unit + 64 + 32 * u + 16 * hh);
         float sum = 0.f, top = 0.f;
-        float4 v4 = vu[0];
-        LD_HERE();
 #pragma unroll
-        for (int k = 0; k < 2 * KS; k++) {
-            product(k);
-            constexpr int per = 16 / (2 * KS);      // weights a product
+        for (int u = 0; u < 2; u++) {
+            const float4 *vu = reinterpret_cast<const float4 *>(st.vu + 32 * u + 16 * hh);
 #pragma unroll
-            for (int e = 0; e < per; e++) {
-                const int i = per * k + e;
+            for (int i = 0; i < 16; i++) {
+                const float4 v4 = vu[i >> 2];
                 const float vv = (i & 3) == 0 ? v4.x : (i & 3) == 1 ? v4.y : (i & 3) == 2 ? v4.z : v4.w;
-                const float p = fast_exp2(fmaf(s[i], rs, add));
+                const float p = fast_exp2(fmaf(s[u][i], rs, add));
                 sum += p;
-                s[i] = p * vv;
-                if ((i & 3) == 3 && i < 15) v4 = vu[(i >> 2) + 1];
+                s[u][i] = p * vv;
             }
-            LD_HERE();
         }
         if (!whole) keep_seen(s, 0.f);      // units of positions that are not seen may be anything
-        constexpr int PAIRS = ND / 2;
-        f16x8_t vf[2][2];      // values of a pair of 32 dimensions, and of the next
-        auto ask_values = [&](int g) __attribute__((always_inline)) {
-            const int q = g / PAIRS, n = g % PAIRS * 2;
 #pragma unroll
-            for (int e = 0; e < 2; e++) vf[g & 1][e] = st.v[(2 * (2 * u + hh) + q) * HD + 32 * (n + e) + r32];
-        };
-        ask_values(0);
-        LD_HERE();
+        for (int u = 0; u < 2; u++)
 #pragma unroll
-        for (int k = 2 * KS; k < 3 * KS; k++) {
-            product(k);
-            constexpr int per = 16 / KS;
-#pragma unroll
-            for (int e = 0; e < per; e++) top = fmaxf(top, s[per * (k - 2 * KS) + e]);
-            LD_HERE();
-        }
+            for (int i = 0; i < 16; i++) top = fmaxf(top, s[u][i]);
         top = max_halves(top);
         // the largest product leaves 2^9 .. 65504: scaled to 2^12 .. 2^13, what is there and what comes
         big = fmaxf(big, top);
@@ -313,93 +282,67 @@ __global__ __launch_bounds__(256, 2) void k_prefill_q8(Q8Attention a, const int3
 #pragma unroll
                 for (int i = 0; i < 16; i++) o[n][i] *= up;
 #pragma unroll
-            for (int i = 0; i < 16; i++) s[i] *= up;
+            for (int u = 0; u < 2; u++)
+#pragma unroll
+                for (int i = 0; i < 16; i++) s[u][i] *= up;
         }
         l += sum;
-        // ---- sums, beside the next half's scores and a later tile
-        f16x8_t wh[2], wl[2];
-        auto split_pair = [&](int i) __attribute__((always_inline)) {
-            uint32_t hi2, lo2;
-            split2_halves(s[i], s[i + 1], hi2, lo2);
-            const f16x2_t y = __builtin_bit_cast(f16x2_t, hi2), z = __builtin_bit_cast(f16x2_t, lo2);
-            wh[i >> 3][i & 7] = y[0];
-            wh[i >> 3][(i & 7) + 1] = y[1];
-            wl[i >> 3][i & 7] = z[0];
-            wl[i >> 3][(i & 7) + 1] = z[1];
-        };
+        #pragma unroll
+        for (int u = 0; u < 2; u++) {
+            f16x8_t wh[2], wl[2];
 #pragma unroll
-        for (int i = 0; i < 8; i += 2) split_pair(i);
-        const float4 *ku = reinterpret_cast<const float4 *>(nst.unit + 32 * un + 16 * hh);
-        float4 k4;
-        LD_HERE();
+            for (int i = 0; i < 16; i += 2) {
+                uint32_t hi, lo;
+                split2_halves(s[u][i], s[u][i + 1], hi, lo);
+                const f16x2_t y = __builtin_bit_cast(f16x2_t, hi), z = __builtin_bit_cast(f16x2_t, lo);
+                wh[i >> 3][i & 7] = y[0];
+                wh[i >> 3][(i & 7) + 1] = y[1];
+                wl[i >> 3][i & 7] = z[0];
+                wl[i >> 3][(i & 7) + 1] = z[1];
+            }
 #pragma unroll
-        for (int k = 0; k < 4 * ND; k++) {      // pairs of dimensions: both leading terms, then both second ones
-            const int g = k >> 2, q = g / PAIRS, n = g % PAIRS * 2 + (k & 1);
-            if ((k & 3) == 0 && g + 1 < 2 * PAIRS) ask_values(g + 1);
-            o[n] = __builtin_amdgcn_mfma_f32_32x32x16_f16(vf[g & 1][k & 1], k & 2 ? wl[q] : wh[q], o[n], 0, 0, 0);
-            if (k < 4) split_pair(8 + 2 * k);
-            constexpr int EVERY = (4 * ND - 4) / 4;      // a score of four each so many products
-            if (k >= 4 && (k - 4) % EVERY == EVERY - 1) score4((k - 4) / EVERY, k4, (tile + u) * TILE + 32 * un);
-            if (k >= 3 && (k - 3) % EVERY == 0 && (k - 3) / EVERY < 4) k4 = ku[(k - 3) / EVERY];
-            if (u == 0 && k == 2) store_keys(to);
-            if (u == 1 && k >= 3 && (k - 3) % 3 == 0 && (k - 3) / 3 < 2 * NP) store_values(to, (k - 3) / 3);
-            LD_HERE();
-        }
+            for (int q = 0; q < 2; q++) {
+                f16x8_t vf[ND];
+#pragma unroll
+                for (int n = 0; n < ND; n++) vf[n] = st.v[(2 * (2 * u + hh) + q) * HD + 32 * n + r32];
+#pragma unroll
+                for (int n = 0; n < ND; n++) o[n] = __builtin_amdgcn_mfma_f32_32x32x16_f16(vf[n], wh[q], o[n], 0, 0, 0);
+#pragma unroll
+                for (int n = 0; n < ND; n++) o[n] = __builtin_amdgcn_mfma_f32_32x32x16_f16(vf[n], wl[q], o[n], 0, 0, 0);
+            }
+                    }
     };
 
     if (t0 < t1) {
-        // the tiles that the wave takes in: of those of the workgroup, the ones that one of its rows sees
-        const int w0 = busy ? max(t0, wave_lo >> 6) : t1, w1 = busy && wave_hi >= 0 ? min(t1, (wave_hi >> 6) + 1) : w0;
+        ask(t0);
+        load();
+        int ide_of = ide;
         {
             const int at = t0 * TILE + lane, ph = trow[min(at >> 4, last)];
             const int e = a.expo[(((int64_t)max(ph, 0) * 2 + 1) * a.Hkv + j) * 16 + (lane & 15)];
             const int top = wave_max(at >= wlo && at <= whi && ph >= 0 && e > -126 ? e : -1000);
             e0 = top == -1000 ? 0 : top;
         }
-        // With tile t its keys and values and the keys of t + 1 are read, t + 2 is stored (in the place of t - 1): its keys, asked for a half earlier, in the
-        // first half, its values in the second, so that few registers hold them.  Past the end the last tile comes again, which nobody reads.
-        ask(t0);
-        load_keys();
-        load_values();
-        int map0 = mapped_of(), map1, map2;
-        ask(min(t0 + 1, t1 - 1));
-        store_keys(stage[0]);
-        store_all_values(stage[0]);
-        load_keys();
-        load_values();
-        map1 = mapped_of();
-        ask(min(t0 + 2, t1 - 1));
-        store_keys(stage[1]);
-        store_all_values(stage[1]);
-        load_keys();
+        if (t0 + 1 < t1) ask(t0 + 1);
+        store(stage[0], ide_of);
+        if (t0 + 1 < t1) {
+            load();
+            ide_of = ide;
+        }
+        if (t0 + 2 < t1) ask(t0 + 2);
         lds_barrier();
-        int cur = 0;
         for (int tile = t0; tile < t1; tile++) {
-            const int nxt = cur == 2 ? 0 : cur + 1, then = nxt == 2 ? 0 : nxt + 1;
-            const bool in = tile >= w0 && tile < w1;
-            if (in) {
-                if (tile == w0) {
-                    ask_keys(stage[cur], 0);
-#pragma unroll
-                    for (int k = 0; k < 3 * KS; k++) product(k);
-                    const float4 *ku = reinterpret_cast<const float4 *>(stage[cur].unit + 16 * hh);
-#pragma unroll
-                    for (int i = 0; i < 4; i++) score4(i, ku[i], tile * TILE);
+            const int cur = (tile - t0) & 1;
+            if (busy && tile * TILE <= wave_hi && tile * TILE + TILE - 1 >= wave_lo) multiply(stage[cur], tile);
+            if (tile + 1 < t1) {
+                store(stage[cur ^ 1], ide_of);
+                if (tile + 2 < t1) {
+                    load();
+                    ide_of = ide;
                 }
-                step(stage[cur], stage[cur], tile, map0, std::integral_constant<int, 0>{}, stage[then]);
-            } else {
-                store_keys(stage[then]);
+                if (tile + 3 < t1) ask(tile + 3);
+                lds_barrier();
             }
-            load_values();
-            map2 = mapped_of();
-            ask(min(tile + 3, t1 - 1));
-            if (in) step(stage[cur], stage[nxt], tile, map0, std::integral_constant<int, 1>{}, stage[then]);
-            else store_all_values(stage[then]);
-            load_keys();
-            map0 = map1;
-            map1 = map2;
-            lds_barrier();
-            cur = nxt;
         }
     }
 
@@ -445,11 +388,15 @@ __global__ __launch_bounds__(256) void k_join_prefill_q8(Q8Attention a, const in
     for (int u = 0; u < HD / 64; u++) a.out[((int64_t)(tp[0] + r) * a.H + h) * HD + lane + 64 * u] = L == 0.f ? 0.f : acc[u] / L;
 }
 
-constexpr int WANT = 512, LEAST = 4;      // workgroups, tiles of positions a share
+constexpr int MOST = 1024, LEAST = 4;      // workgroups with shares, 64-position tiles a share
 
+// Shares of a tile's positions, by the number of (tile, head) pairs.  Up to a pair a CU: what fills the CUs once with two workgroups each, or nearly; more: about
+// four a CU, so that the last ones do not work alone.  us, 1 / 2 / 3 / 4 / 5 / 6 / 8 shares: 96 pairs of 24 tiles - / 50 / 49 / 44 / 47 / 56 / 56, 280 pairs of up to
+// 68 tiles 318 / 184 / 177 / 157 / 165 / 160 / 188.
 int shares(int n_tiles, int H, int max_pos) {
     const int64_t pairs = (int64_t)n_tiles * H, kt = ((int64_t)max_pos + TILE) / TILE;
-    return (int)std::max<int64_t>(1, std::min<int64_t>((WANT + pairs - 1) / pairs, kt / LEAST));
+    const int64_t n = pairs <= 256 ? std::max<int64_t>(2, 400 / pairs) : (MOST + pairs - 1) / pairs;
+    return (int)std::max<int64_t>(1, std::min<int64_t>(n, kt / LEAST));
 }
 
 template <int HD>
@@ -468,8 +415,8 @@ extern "C" {
 
 size_t ldk_prefill_attention_q8_scratch_bytes(int32_t n_tiles, int32_t H, int32_t Hkv, int32_t hd, int32_t max_pos, int32_t window) {
     if (n_tiles <= 0 || H <= 0 || Hkv <= 0 || H % Hkv || (hd != 64 && hd != 128) || max_pos < 0 || window < 0) return 0;
-    // no more shares than fill the machine, whatever the number of tiles: pairs * shares < WANT + pairs
-    const size_t rows = ((size_t)n_tiles * H + WANT) * ROWS;
+    // pairs * shares < MOST + pairs, whatever the number of tiles
+    const size_t rows = ((size_t)n_tiles * H + MOST) * ROWS;
     return shares(1, 1, max_pos) == 1 ? 256 : ld::align_up(rows * 8, 256) + rows * hd * 4;
 }
 
