@@ -77,6 +77,33 @@ typedef float float4_u __attribute__((ext_vector_type(4), aligned(4)));      // 
 typedef _Float16 f16x2_t __attribute__((ext_vector_type(2)));
 typedef _Float16 f16x8_t __attribute__((ext_vector_type(8)));
 
+// The larger of a lane's number and its partner's, 32 or 16 lanes away; the largest of 16 lanes.  Vector instructions: no way through LDS.
+__device__ __forceinline__ float max_halves(float x) {
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+__device__ __forceinline__ float max_quarters(float x) {
+    const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+#define LD_ROR(X_, N_) __builtin_amdgcn_update_dpp(0, X_, 0x120 + N_, 0xf, 0xf, true)      // X_ of the lane N_ on, within 16
+__device__ __forceinline__ float max_of16(float x) {
+    x = fmaxf(x, __int_as_float(LD_ROR(__float_as_int(x), 8)));
+    x = fmaxf(x, __int_as_float(LD_ROR(__float_as_int(x), 4)));
+    x = fmaxf(x, __int_as_float(LD_ROR(__float_as_int(x), 2)));
+    return fmaxf(x, __int_as_float(LD_ROR(__float_as_int(x), 1)));
+}
+__device__ __forceinline__ int wave_max(int x) {
+    x = max(x, LD_ROR(x, 8));
+    x = max(x, LD_ROR(x, 4));
+    x = max(x, LD_ROR(x, 2));
+    x = max(x, LD_ROR(x, 1));
+    const auto r = __builtin_amdgcn_permlane16_swap(x, x, false, false);
+    x = max((int)r[0], (int)r[1]);
+    const auto q = __builtin_amdgcn_permlane32_swap(x, x, false, false);
+    return __builtin_amdgcn_readfirstlane(max((int)q[0], (int)q[1]));
+}
+
 // Eight codes (two words) as fp16, exact: a byte c + 128 under the exponent of 1024 is the fp16 number 1152 + c.
 __device__ __forceinline__ f16x8_t q8_halves(uint32_t w0, uint32_t w1) {
     const f16x2_t bias = {(_Float16)1152.f, (_Float16)1152.f};

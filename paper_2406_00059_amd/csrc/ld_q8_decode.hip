@@ -14,6 +14,7 @@
 // block g, slot by slot, which is what it has to bring as the other operand of the sums.
 #include <algorithm>
 #include <cmath>
+#include <type_traits>
 #include "ld_q8.h"
 
 using namespace ldd;
@@ -32,12 +33,10 @@ __device__ __forceinline__ Seen seen_of(int ctx_len, int first, int max_ctx, int
 // x summed over the lanes of 16 that hold the same head's terms; the same bits in all of them.
 template <int GP>
 __device__ __forceinline__ float sum_terms(float x) {
-#define LD_ROR(N_) __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), 0x120 + N_, 0xf, 0xf, true))
-    if constexpr (GP <= 8) x += LD_ROR(8);
-    if constexpr (GP <= 4) x += LD_ROR(4);
-    if constexpr (GP <= 2) x += LD_ROR(2);
-    if constexpr (GP <= 1) x += LD_ROR(1);
-#undef LD_ROR
+    if constexpr (GP <= 8) x += __int_as_float(LD_ROR(__float_as_int(x), 8));
+    if constexpr (GP <= 4) x += __int_as_float(LD_ROR(__float_as_int(x), 4));
+    if constexpr (GP <= 2) x += __int_as_float(LD_ROR(__float_as_int(x), 2));
+    if constexpr (GP <= 1) x += __int_as_float(LD_ROR(__float_as_int(x), 1));
     return x;
 }
 
@@ -49,7 +48,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void k_decode_q8(Q8Attention a, cons
     // heads next to each other: a block's keys and values of all heads lie together
     const int G = a.H / a.Hkv, parts = (G + 15) / 16, groups = a.Hkv * parts, item = blockIdx.x / groups, t = item / chunks, ch = item % chunks;
     const int hg = blockIdx.x % groups, j = hg / parts, h0 = j * G + hg % parts * 16, heads = min(G - hg % parts * 16, 16);
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = lane & 15, g = lane >> 4, head = c % GP, term = c / GP;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c = lane & 15, g = lane >> 4, head = c % GP, term = c / GP;
     const int len = ctx_len[t], seq = seq_slot[t];
     const Seen see = seen_of(len, first ? first[t] : 0, max_ctx, a.window, a.table_stride);
     const int t0 = (see.lo >> 6) + ch * chunk, t1 = min(t0 + chunk, (see.hi >> 6) + 1);
@@ -63,7 +62,8 @@ __global__ __launch_bounds__(64 * WAVES, 2) void k_decode_q8(Q8Attention a, cons
     const int64_t bs = q8_block(a.Hkv, HD);
     const int8_t *kbase = a.codes + q8_k(HD, j, c & 3, 16 * g), *vbase = a.codes + q8_v(a.Hkv, HD, j, 0, c);
 
-    u32x4_t kf[4][KS], vf[ND], ek, ev;
+    typename std::conditional<GP == 1, int, u32x4_t>::type ek, ev;      // exponents of position 64 tile + lane, or of block g's
+    u32x4_t kf[4][KS], vf[ND];
     int idk, idv;      // blocks of the tile to be loaded: the one of this lane's key rows, and block g
     auto ask = [&](int tile) {
         idk = trow[min(4 * tile + (c >> 2), last)];
@@ -75,9 +75,14 @@ __global__ __launch_bounds__(64 * WAVES, 2) void k_decode_q8(Q8Attention a, cons
         for (int s = 0; s < 4; s++)
 #pragma unroll
             for (int u = 0; u < KS; u++) kf[s][u] = load_stream16(p + 4 * s * HD + 64 * u);
-        const int8_t *e = a.expo + ((int64_t)max(idv, 0) * 2 * a.Hkv + j) * 16;
-        ek = *reinterpret_cast<const u32x4_t *>(e);
-        ev = *reinterpret_cast<const u32x4_t *>(e + a.Hkv * 16);
+        const int8_t *e = a.expo + ((int64_t)max(idv, 0) * 2 * a.Hkv + j) * 16 + (GP == 1 ? c : 0);
+        if constexpr (GP == 1) {
+            ek = e[0];
+            ev = e[a.Hkv * 16];
+        } else {
+            ek = *reinterpret_cast<const u32x4_t *>(e);
+            ev = *reinterpret_cast<const u32x4_t *>(e + a.Hkv * 16);
+        }
     };
     auto load_v = [&](int id) {
         const int8_t *p = vbase + max(id, 0) * bs;
@@ -135,13 +140,49 @@ __global__ __launch_bounds__(64 * WAVES, 2) void k_decode_q8(Q8Attention a, cons
     float m = -INFINITY, l = 0.f;      // log2 domain; l over this lane's own positions
     int k = -100000;                   // o is in units of 2^(k - 14)
 
+    // A score (in the log2 domain) from a sum of products
+    auto score = [&](float x, int kexp, int pos) __attribute__((always_inline)) {
+        x = ldexpf(x, kexp + query.exp) * query.unit;
+        if constexpr (EXTRA) {
+            if (a.softcap > 0.f) x = q8_cap(x, a.softcap, inv_cap);
+            x = fmaf(slope, (float)(pos - (len - 1)), x * 1.4426950408889634f);
+        }
+        return kexp == Q8_NAN ? __uint_as_float(0x7fc00000u) : x;
+    };
+    // Brings m to the largest score and k to (at least) the largest exponent of what a column adds up, in the new reference; mb, top: the largest
+    // score and p 2^e of a lane's own positions
+    float ref = 0.f;
+    auto rescale = [&](float mb, float top) __attribute__((always_inline)) {
+        if constexpr (GP == 1) {
+            mb = max_of16(mb);
+            top = max_of16(top);
+        }
+        mb = max_halves(max_quarters(mb));
+        top = max_halves(max_quarters(top));
+        const float mn = fmaxf(m, mb);
+        ref = mn > -INFINITY ? mn : 0.f;
+        const float keep = fast_exp2(m - ref), lift = m > -INFINITY ? ref - m : 0.f;
+        const int fall = (int)ceilf(fminf(lift, 100000.f));
+        const int kt = top > -INFINITY ? (int)ceilf(fminf(fmaxf(top - ref, -90000.f), 90000.f)) : -100000;
+        const int kn = max(max(k - fall, kt), -100000);
+        const float scale = ldexpf(keep, max(min(k - kn, 300), -300));
+        l *= keep;
+        m = mn;
+        k = kn;
+        if (__any(scale != 1.f)) {
+#pragma unroll
+            for (int n = 0; n < ND; n++)
+#pragma unroll
+                for (int i = 0; i < 4; i++) o[n][i] *= scale;
+        }
+    };
     for (int tile = begin; tile < t1; tile += WAVES) {
         const bool more = tile + WAVES < t1;
         // ---- scores of block g's 16 slots
         float s[16];
         const int at = (4 * tile + g) * 16;      // position of slot 0
         const bool mapped = idv >= 0;
-        const u32x4_t ekn = ek, evn = ev;
+        const auto ekn = ek, evn = ev;
 #pragma unroll
         for (int q = 0; q < 4; q++) {
             float sum[4] = {0.f, 0.f, 0.f, 0.f};
@@ -161,75 +202,80 @@ __global__ __launch_bounds__(64 * WAVES, 2) void k_decode_q8(Q8Attention a, cons
             load_k();
         }
         const int id_next = idv;
-        // ---- online softmax of this lane's column
-        bool all = mapped && at >= see.lo && at + 15 <= see.hi;
-        float mb = -INFINITY;
-        int e[16];      // exponents of the values
+        f16x8_t wb[2][GP == 16 ? 2 : 1];
+        if constexpr (GP == 1) {
+            // One head: every column of 16 holds its score, lane c goes on with slot c's, so that a lane has one position (64 tile + lane), and gets the others'
+            // weights back by broadcasts within the 16.
+            float x = s[0];
 #pragma unroll
-        for (int i = 0; i < 16; i++) {
-            const int kexp = (int)(int8_t)(ekn[i >> 2] >> (8 * (i & 3)));
-            e[i] = (int)(int8_t)(evn[i >> 2] >> (8 * (i & 3)));
-            float x = ldexpf(s[i], kexp + query.exp) * query.unit;
-            if constexpr (EXTRA) {
-                if (a.softcap > 0.f) x = q8_cap(x, a.softcap, inv_cap);
-                x = fmaf(slope, (float)(at + i - (len - 1)), x * 1.4426950408889634f);
-            }
-            x = kexp == Q8_NAN ? __uint_as_float(0x7fc00000u) : x;
-            s[i] = x;
-        }
-        if (!__all(all)) {
+            for (int i = 1; i < 16; i++) x = c == i ? s[i] : x;
+            const int pos = tile * TILE + lane, kexp = ekn;
+            x = score(x, kexp, pos);
+            const bool ok = mapped && pos >= see.lo && pos <= see.hi;
+            x = ok ? x : -INFINITY;
+            const int e = ok ? evn : -1000;
+            rescale(x, x + (float)e);
+            const float p = fast_exp2(x - ref);
+            l += p;
+            float w = ldexpf(p, e - k + 14);
+            w = e == Q8_NAN ? __uint_as_float(0x7fc00000u) : w;
+            const _Float16 hi = (_Float16)w, lo = (_Float16)(w - (float)hi);
+            const int both = (int)((uint32_t)__builtin_bit_cast(uint16_t, hi) | (uint32_t)__builtin_bit_cast(uint16_t, lo) << 16);
+            const uint32_t take = term == 0 ? 0x05040100u : term == 1 ? 0x07060302u : 0x0c0c0c0cu;      // leading terms, second terms, zeros
+            uint32_t words[8];
+#define LD_PAIR(I_) words[I_] = __builtin_amdgcn_perm((uint32_t)__builtin_amdgcn_update_dpp(0, both, 0x150 + 2 * I_ + 1, 0xf, 0xf, true), \
+                                                      (uint32_t)__builtin_amdgcn_update_dpp(0, both, 0x150 + 2 * I_, 0xf, 0xf, true), take)
+            LD_PAIR(0); LD_PAIR(1); LD_PAIR(2); LD_PAIR(3); LD_PAIR(4); LD_PAIR(5); LD_PAIR(6); LD_PAIR(7);
+#undef LD_PAIR
+            wb[0][0] = __builtin_bit_cast(f16x8_t, (u32x4_t){words[0], words[1], words[2], words[3]});
+            wb[1][0] = __builtin_bit_cast(f16x8_t, (u32x4_t){words[4], words[5], words[6], words[7]});
+        } else {
+            // ---- online softmax of this lane's column
+            const bool all = mapped && at >= see.lo && at + 15 <= see.hi;
+            int e[16];      // exponents of the values
 #pragma unroll
             for (int i = 0; i < 16; i++) {
-                const bool ok = mapped && at + i >= see.lo && at + i <= see.hi;
-                s[i] = ok ? s[i] : -INFINITY;
-                e[i] = ok ? e[i] : -1000;
+                e[i] = (int)(int8_t)(evn[i >> 2] >> (8 * (i & 3)));
+                s[i] = score(s[i], (int)(int8_t)(ekn[i >> 2] >> (8 * (i & 3))), at + i);
             }
-        }
-        float top = -INFINITY;      // of p 2^e
+            if (!__all(all)) {
 #pragma unroll
-        for (int i = 0; i < 16; i++) {
-            mb = fmaxf(mb, s[i]);
-            top = fmaxf(top, s[i] + (float)e[i]);
-        }
-        mb = fmaxf(mb, __shfl_xor(mb, 16, WAVE));
-        top = fmaxf(top, __shfl_xor(top, 16, WAVE));
-        mb = fmaxf(mb, __shfl_xor(mb, 32, WAVE));
-        top = fmaxf(top, __shfl_xor(top, 32, WAVE));
-        const float mn = fmaxf(m, mb), ref = mn > -INFINITY ? mn : 0.f;
-        const float keep = fast_exp2(m - ref);
-        // k: at least the largest exponent so far of what a column adds up, in units of the new reference
-        const float lift = m > -INFINITY ? ref - m : 0.f;
-        const int fall = (int)ceilf(fminf(lift, 100000.f));
-        const int kt = top > -INFINITY ? (int)ceilf(fminf(fmaxf(top - ref, -90000.f), 90000.f)) : -100000;
-        const int kn = max(max(k - fall, kt), -100000);
-        const float scale = ldexpf(keep, max(min(k - kn, 300), -300));
-        l *= keep;
-        m = mn;
-        k = kn;
-        if (__any(scale != 1.f)) {
+                for (int i = 0; i < 16; i++) {
+                    const bool ok = mapped && at + i >= see.lo && at + i <= see.hi;
+                    s[i] = ok ? s[i] : -INFINITY;
+                    e[i] = ok ? e[i] : -1000;
+                }
+            }
+            float mb = -INFINITY, top = -INFINITY;
 #pragma unroll
-            for (int n = 0; n < ND; n++)
+            for (int i = 0; i < 16; i++) {
+                mb = fmaxf(mb, s[i]);
+                top = fmaxf(top, s[i] + (float)e[i]);
+            }
+            rescale(mb, top);
 #pragma unroll
-                for (int i = 0; i < 4; i++) o[n][i] *= scale;
-        }
-        float hi[16], lo[16];
+            for (int i = 0; i < 16; i += 2) {
+                float w[2];
 #pragma unroll
-        for (int i = 0; i < 16; i++) {
-            const float p = fast_exp2(s[i] - ref);
-            l += p;
-            float w = ldexpf(p, e[i] - k + 14);
-            w = e[i] == Q8_NAN ? __uint_as_float(0x7fc00000u) : w;
-            hi[i] = (float)(_Float16)w;
-            lo[i] = w - hi[i];
-        }
-        f16x8_t wb[2][GP == 16 ? 2 : 1];
-#pragma unroll
-        for (int i = 0; i < 16; i++) {
-            if constexpr (GP == 16) {
-                wb[i >> 3][0][i & 7] = (_Float16)hi[i];
-                wb[i >> 3][1][i & 7] = (_Float16)lo[i];
-            } else {
-                wb[i >> 3][0][i & 7] = (_Float16)(term == 0 ? hi[i] : term == 1 ? lo[i] : 0.f);
+                for (int u = 0; u < 2; u++) {
+                    const float p = fast_exp2(s[i + u] - ref);
+                    l += p;
+                    w[u] = ldexpf(p, e[i + u] - k + 14);
+                    w[u] = e[i + u] == Q8_NAN ? __uint_as_float(0x7fc00000u) : w[u];
+                }
+                uint32_t hi, lo;
+                split2_halves(w[0], w[1], hi, lo);
+                if constexpr (GP == 16) {
+                    const f16x2_t y = __builtin_bit_cast(f16x2_t, hi), z = __builtin_bit_cast(f16x2_t, lo);
+                    wb[i >> 3][0][i & 7] = y[0];
+                    wb[i >> 3][0][(i & 7) + 1] = y[1];
+                    wb[i >> 3][1][i & 7] = z[0];
+                    wb[i >> 3][1][(i & 7) + 1] = z[1];
+                } else {
+                    const f16x2_t y = __builtin_bit_cast(f16x2_t, term == 0 ? hi : term == 1 ? lo : 0u);
+                    wb[i >> 3][0][i & 7] = y[0];
+                    wb[i >> 3][0][(i & 7) + 1] = y[1];
+                }
             }
         }
         // ---- sums
@@ -245,8 +291,8 @@ __global__ __launch_bounds__(64 * WAVES, 2) void k_decode_q8(Q8Attention a, cons
         if (more) load_v(id_next);
     }
 
-    l += __shfl_xor(l, 16, WAVE);
-    l += __shfl_xor(l, 32, WAVE);
+#pragma unroll
+    for (int off = GP == 1 ? 1 : 16; off < 64; off <<= 1) l += __shfl_xor(l, off, WAVE);
     __shared__ __attribute__((aligned(16))) float so[WAVES][GP][HD + 4];
     __shared__ float2 sml[WAVES][GP];
     const float inv = l == 0.f ? 0.f : 1.f / l;

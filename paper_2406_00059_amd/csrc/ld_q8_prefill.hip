@@ -43,25 +43,6 @@ __device__ __forceinline__ int key_piece(int r, int p) {
     return N == 8 ? r * 8 + (p ^ ((r & 3) | ((r >> 2) & 4))) : r * 4 + (p ^ (((r >> 1) & 1) | ((r >> 3) & 2)));
 }
 
-// The larger of a lane's and its partner's (lane ^ 32) number.
-__device__ __forceinline__ float max_halves(float x) {
-    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
-    return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
-}
-// The largest of a wave.
-__device__ __forceinline__ int wave_max(int x) {
-#define LD_ROR(N_) x = max(x, __builtin_amdgcn_update_dpp(0, x, 0x120 + N_, 0xf, 0xf, true))
-    LD_ROR(8);
-    LD_ROR(4);
-    LD_ROR(2);
-    LD_ROR(1);
-#undef LD_ROR
-    const auto r = __builtin_amdgcn_permlane16_swap(x, x, false, false);
-    x = max((int)r[0], (int)r[1]);
-    const auto q = __builtin_amdgcn_permlane32_swap(x, x, false, false);
-    return __builtin_amdgcn_readfirstlane(max((int)q[0], (int)q[1]));
-}
-
 struct TileRows { int row, n, pos, seq, first, prefix; };
 
 // Positions that rows r0 .. r1 - 1 of a tile see at least one of.
