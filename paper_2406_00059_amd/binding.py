@@ -599,7 +599,7 @@ def ldk_choose_scratch_bytes(R, V):
     return lib().ldk_choose_scratch_bytes(R, V)
 
 
-_I32, _I64, _F32 = torch.int32, torch.int64, torch.float32
+_I8, _I32, _I64, _F32 = torch.int8, torch.int32, torch.int64, torch.float32
 _BITS = {_I32: torch.uint32, _I64: torch.uint64}      # what else may hold bit patterns
 
 
@@ -653,7 +653,7 @@ def _refuse(what):
 def _q8_layer(call, codes, expo, Hkv, hd):
     """Addresses of a layer's codes int8 [blocks, 2, Hkv, 16, hd] and exponents int8 [blocks, 2, Hkv, 16]."""
     n = expo.numel()
-    if Hkv < 1 or hd < 1 or codes.dtype is not torch.int8 or expo.dtype is not torch.int8 or codes.numel() != n * hd or n % (32 * Hkv) or not codes.is_contiguous() or \
+    if Hkv < 1 or hd < 1 or codes.dtype is not _I8 or expo.dtype is not _I8 or codes.numel() != n * hd or n % (32 * Hkv) or not codes.is_contiguous() or \
             not expo.is_contiguous():
         _refuse(f"{call}: codes int8 [blocks, 2, {Hkv}, 16, {hd}] and expo int8 [blocks, 2, {Hkv}, 16], contiguous, not {codes.dtype} {tuple(codes.shape)} "
                 f"and {expo.dtype} {tuple(expo.shape)}")
@@ -687,28 +687,58 @@ def ldk_rope_kv_write_q8(qkv, cos_sin, pos, seq_slot, table, codes, expo, H, Hkv
                          eps=0.0, stream=None):
     """qkv float32 [T, at least (H + 2 Hkv) hd], q_out float32 [T, at least H hd] (or qkv itself); rot: rotated elements of a head (all of them if not
     given), cos_sin float32 [T, rot / 2, 2] (None for rot 0); gains float32 [hd] or None; codes and expo: a layer of the 8-bit pool."""
-    call = "ldk_rope_kv_write_q8"
     rot = hd if rot is None else rot
-    T = pos.numel()
-    if qkv.dim() != 2 or q_out.dim() < 2 or qkv.shape[0] != T or q_out.shape[0] != T:
+    T, ne = pos.numel(), expo.numel()
+    rows, qs = qkv.shape if qkv.dim() == 2 else (-1, 0)
+    _, stride = table.shape if table.dim() == 2 else (0, 0)
+    os_, rest = divmod(q_out.numel(), T) if T else (H * hd, 0)
+    # All at once, which takes half as long as one by one (3 us of a call whose kernel takes 3)
+    if not (rows == T and rest == 0 and stride and seq_slot.numel() == T and qkv.dtype is _F32 and q_out.dtype is _F32 and pos.dtype is _I32 and
+            seq_slot.dtype is _I32 and table.dtype is _I32 and codes.dtype is _I8 and expo.dtype is _I8 and Hkv > 0 and ne % (32 * Hkv) == 0 and
+            codes.numel() == ne * hd and qkv.is_contiguous() and q_out.is_contiguous() and pos.is_contiguous() and seq_slot.is_contiguous() and
+            table.is_contiguous() and codes.is_contiguous() and expo.is_contiguous()):
+        _append_fits(qkv, pos, seq_slot, table, codes, expo, Hkv, hd, q_out)
+    rc = (_lib or lib()).ldk_rope_kv_write_q8(
+        qkv.data_ptr(), qs, q_gain if q_gain is None else _at("q_gain", q_gain, _F32, hd), k_gain if k_gain is None else _at("k_gain", k_gain, _F32, hd), eps,
+        _at("cos_sin", cos_sin, _F32, T * rot), rot, 1 if interleaved else 0, pos.data_ptr(), seq_slot.data_ptr(), table.data_ptr(), stride, codes.data_ptr(),
+        expo.data_ptr(), T, H, Hkv, hd, q_out.data_ptr(), os_, _stream(stream))
+    if rc:
+        _check(rc)
+
+
+def _append_fits(qkv, pos, seq_slot, table, codes, expo, Hkv, hd, q_out):
+    """Raises what ldk_rope_kv_write_q8's tensors lack."""
+    call, T = "ldk_rope_kv_write_q8", pos.numel()
+    if qkv.dim() != 2 or qkv.shape[0] != T or (T and q_out.numel() % T):
         _refuse(f"{call}: qkv and q_out have a row for each of the {T} positions, not {tuple(qkv.shape)} and {tuple(q_out.shape)}")
-    qs, os_ = qkv.shape[1], q_out.numel() // T if T else H * hd
-    c, e = _q8_layer(call, codes, expo, Hkv, hd)
-    _check((_lib or lib()).ldk_rope_kv_write_q8(
-        _rows_of(call, qkv, "qkv", qs, (H + 2 * Hkv) * hd, T), qs, _at("q_gain", q_gain, _F32, hd), _at("k_gain", k_gain, _F32, hd), eps,
-        _at("cos_sin", cos_sin, _F32, T * rot), rot, int(interleaved), _at("pos", pos, _I32, T), _at("seq_slot", seq_slot, _I32, T),
-        _q8_table(call, table), table.shape[1], c, e, T, H, Hkv, hd, _rows_of(call, q_out, "q_out", os_, H * hd, T), os_, _stream(stream)))
+    _q8_layer(call, codes, expo, Hkv, hd)
+    _q8_table(call, table)
+    _at("pos", pos, _I32, T)
+    _at("seq_slot", seq_slot, _I32, T)
+    for name, t in (("qkv", qkv), ("q_out", q_out)):
+        _rows_of(call, t, name, 0, 0)
 
 
 def _move(call, pool_layer, table, codes, expo, q8_table, ranges, Hkv, hd):
     """(pool, table), (codes and expo, 8-bit table) and ranges as arguments of the two moves; their types and sizes."""
-    if Hkv < 1 or hd < 1 or pool_layer.dtype not in _W4_FLOATS or not pool_layer.is_contiguous() or pool_layer.numel() % (32 * Hkv * hd):
-        _refuse(f"{call}: a pool is bf16 or float32 [blocks, 2, {Hkv}, 16, {hd}], contiguous, not {pool_layer.dtype} {tuple(pool_layer.shape)}")
-    if ranges.dim() != 2 or ranges.shape[1] != 3:
-        _refuse(f"{call}: ranges int32 [n, 3], not {tuple(ranges.shape)}")
-    return ((pool_layer.data_ptr(), _dt(pool_layer.dtype), _q8_table(call, table), table.shape[1]),
-            (*_q8_layer(call, codes, expo, Hkv, hd), _q8_table(call, q8_table), q8_table.shape[1]),
-            (_at("ranges", ranges, _I32, ranges.numel()), ranges.shape[0]))
+    kind, ne = pool_layer.dtype, expo.numel()
+    _, stride = table.shape if table.dim() == 2 else (0, 0)
+    _, q8_stride = q8_table.shape if q8_table.dim() == 2 else (0, 0)
+    n, three = ranges.shape if ranges.dim() == 2 else (0, 0)
+    if not ((kind is torch.bfloat16 or kind is _F32) and Hkv > 0 and hd > 0 and stride and q8_stride and three == 3 and table.dtype is _I32 and
+            q8_table.dtype is _I32 and ranges.dtype is _I32 and codes.dtype is _I8 and expo.dtype is _I8 and ne % (32 * Hkv) == 0 and
+            codes.numel() == ne * hd and pool_layer.numel() % (32 * Hkv * hd) == 0 and pool_layer.is_contiguous() and table.is_contiguous() and
+            q8_table.is_contiguous() and ranges.is_contiguous() and codes.is_contiguous() and expo.is_contiguous()):
+        if Hkv < 1 or hd < 1 or pool_layer.dtype not in _W4_FLOATS or not pool_layer.is_contiguous() or pool_layer.numel() % (32 * Hkv * hd):
+            _refuse(f"{call}: a pool is bf16 or float32 [blocks, 2, {Hkv}, 16, {hd}], contiguous, not {pool_layer.dtype} {tuple(pool_layer.shape)}")
+        if ranges.dim() != 2 or ranges.shape[1] != 3:
+            _refuse(f"{call}: ranges int32 [n, 3], not {tuple(ranges.shape)}")
+        for t in (table, q8_table):
+            _q8_table(call, t)
+        _q8_layer(call, codes, expo, Hkv, hd)
+        _at("ranges", ranges, _I32, ranges.numel())
+    return ((pool_layer.data_ptr(), LD_F32 if kind is _F32 else LD_BF16, table.data_ptr(), stride),
+            (codes.data_ptr(), expo.data_ptr(), q8_table.data_ptr(), q8_stride), (ranges.data_ptr(), n))
 
 
 def ldk_kv_to_q8(pool_layer, table, codes, expo, q8_table, ranges, max_len, Hkv, hd, stream=None):
