@@ -62,13 +62,16 @@ inline bool bad_attention(const Q8Attention &a, int hd) {
            !std::isfinite(a.softcap) || !a.out;
 }
 
-// cap tanh(s / cap).  Small arguments by the odd series (next term 2e-9 of the sum at 0.25), the others by the exponential, which would
-// cancel there.
+// cap tanh(s / cap).  |s| below cap / 2: the odd series up to the 13th power (the next term is at most 9e-8 of the sum there); above, by the exponential,
+// which would cancel below.
+constexpr float Q8_SERIES = 0.5f;
+__device__ __forceinline__ float q8_cap_small(float s, float inv_cap) {
+    const float x = s * inv_cap, x2 = x * x;
+    return s * (1.f + x2 * (-1.f / 3 + x2 * (2.f / 15 + x2 * (-17.f / 315 + x2 * (62.f / 2835 + x2 * (-1382.f / 155925 + x2 * (21844.f / 6081075)))))));
+}
 __device__ __forceinline__ float q8_cap(float s, float cap, float inv_cap) {
-    const float x = fabsf(s) * inv_cap, x2 = x * x;
-    const float series = x * (1.f + x2 * (-1.f / 3 + x2 * (2.f / 15 + x2 * (-17.f / 315 + x2 * (62.f / 2835)))));
-    const float t = fast_exp2(-2.8853900817779268f * x);
-    return copysignf(cap * (x < 0.25f ? series : (1.f - t) * __builtin_amdgcn_rcpf(1.f + t)), s);
+    const float x = fabsf(s) * inv_cap, t = fast_exp2(-2.8853900817779268f * x);
+    return x < Q8_SERIES ? q8_cap_small(s, inv_cap) : copysignf(cap * ((1.f - t) * __builtin_amdgcn_rcpf(1.f + t)), s);
 }
 
 typedef int i32x4_t __attribute__((ext_vector_type(4)));

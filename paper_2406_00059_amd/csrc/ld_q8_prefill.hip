@@ -152,8 +152,8 @@ __global__ __launch_bounds__(256, 2) void k_prefill_q8(Q8Attention a, const int3
                 for (int n = 0; n < 3; n++) qd[n][s][w] = (int)d[n];
             }
     }
-    const float rs = EXTRA ? 1.f : unit;
-    const float slope = EXTRA && a.slopes ? a.slopes[h] * 1.4426950408889634f : 0.f, inv_cap = EXTRA && a.softcap > 0.f ? 1.f / a.softcap : 0.f;
+    const float rs = EXTRA ? 1.4426950408889634f : unit;
+    const float slope = EXTRA && a.slopes ? a.slopes[h] : 0.f, inv_cap = EXTRA && a.softcap > 0.f ? 1.f / a.softcap : 0.f;
 
     f32x16_t o[ND];
 #pragma unroll
@@ -189,11 +189,36 @@ __global__ __launch_bounds__(256, 2) void k_prefill_q8(Q8Attention a, const int3
                 const float4 k4 = ku[i >> 2];
                 const float kk = (i & 3) == 0 ? k4.x : (i & 3) == 1 ? k4.y : (i & 3) == 2 ? k4.z : k4.w;
                 s[u][i] = fmaf((float)acc2[i], 65536.f, (float)acc[i]) * kk;
-                if constexpr (EXTRA) {
-                    float y = s[u][i] * unit;
-                    if (a.softcap > 0.f) y = q8_cap(y, a.softcap, inv_cap);
-                    s[u][i] = fmaf(slope, (float)(base + 32 * u + 16 * hh + i - (tr.pos + rr)), y * 1.4426950408889634f);
+            }
+        }
+        if constexpr (EXTRA) {
+            float most = 0.f;
+#pragma unroll
+            for (int u = 0; u < 2; u++)
+#pragma unroll
+                for (int i = 0; i < 16; i++) {
+                    s[u][i] *= unit;
+                    most = fmaxf(most, fabsf(s[u][i]));
                 }
+            if (a.softcap > 0.f) {
+                if (__any(most * inv_cap >= Q8_SERIES)) {
+#pragma unroll
+                    for (int u = 0; u < 2; u++)
+#pragma unroll
+                        for (int i = 0; i < 16; i++) s[u][i] = q8_cap(s[u][i], a.softcap, inv_cap);
+                } else {      // scores far below the cap, as they mostly are: a third of the instructions
+#pragma unroll
+                    for (int u = 0; u < 2; u++)
+#pragma unroll
+                        for (int i = 0; i < 16; i++) s[u][i] = q8_cap_small(s[u][i], inv_cap);
+                }
+            }
+            if (a.slopes) {
+                const float from = (float)(base + 16 * hh - (tr.pos + rr));
+#pragma unroll
+                for (int u = 0; u < 2; u++)
+#pragma unroll
+                    for (int i = 0; i < 16; i++) s[u][i] = fmaf(slope, from + (float)(32 * u + i), s[u][i]);
             }
         }
         const bool whole = base >= all_lo && base + TILE - 1 <= all_hi && mapped == 15;
