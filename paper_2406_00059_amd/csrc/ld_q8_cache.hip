@@ -6,7 +6,7 @@ using namespace ldd;
 
 namespace {
 
-// One angle a thread, in float64: positions up to 2^31 times a frequency keep more digits than the float32 result holds.
+// One angle a thread, in float64: positions up to 2^31 times a frequency keep more digits than the float32 result holds.  2048 angles 2.4 us: a launch.
 __global__ void k_rope_table_scaled(const int32_t *__restrict__ pos, int64_t n, int half, double log2_base, double factor, double low, double high, double turns,
                                     double attention, float2 *__restrict__ cos_sin) {
     const int64_t at = (int64_t)blockIdx.x * blockDim.x + threadIdx.x;
@@ -34,7 +34,8 @@ struct WriteArgs {
     int64_t q_out_stride;
 };
 
-// One wave a row and head, two elements a lane: a rotated pair, or two of the rest.
+// One wave a row and head, two elements a lane: a rotated pair, or two of the rest.  For few rows, where a launch and its chain of loads count (one row of 96
+// heads 2.6 us), and for rotated parts that are no multiple of 8.
 template <int HD, bool INTERLEAVED>
 __global__ __launch_bounds__(64) void k_write_q8(WriteArgs a) {
     const int t = blockIdx.x, hh = blockIdx.y, lane = threadIdx.x;
@@ -92,7 +93,7 @@ __global__ __launch_bounds__(64) void k_write_q8(WriteArgs a) {
 // Sixteen rows of a head a workgroup, HD / 8 lanes a row and eight elements a lane: four rotated pairs, or (lanes i >= rot / 8) the elements from 8 i on, of
 // the rest.  rot is a multiple of 8.
 // Values go through LDS, from which neighbouring lanes write neighbouring positions: a position's values lie 16 bytes apart in the cache, and a store of
-// one of them touches a sector for a byte.
+// one of them touches a sector for a byte.  Float64 costs nothing that counts: 1056 rows of 120 heads, 98 MB, 23 us (4.2 TB/s; one row and head a wave 46).
 template <int HD, bool INTERLEAVED>
 __global__ __launch_bounds__(2 * HD) void k_write_rows_q8(WriteArgs a, int T) {
     constexpr int R = 16, LPR = HD / 8;
@@ -232,14 +233,11 @@ __device__ __forceinline__ void put8(float *p, const float (&v)[8]) {
 
 // A wave an item, eight elements a lane and load: of keys HD / 8 lanes a position, of values two lanes a dimension (slots 0 .. 7, 8 .. 15).  The largest
 // exponent is the exponent of the largest.  What bounds it is the traffic; whole blocks leave in 8-byte pieces in the order of memory, of others only
-// the range's slots.
+// the range's slots.  Eight sequences of 512 - 8192 positions of 40 heads, 1.3 GB each way: 280 us there, 250 back (a position at a time 1193 and 1251).
 template <int HD, typename KT>
-__global__ __launch_bounds__(256) void k_to_q8(MoveArgs a, uint32_t items, const KT *__restrict__ pool, int8_t *__restrict__ codes, int8_t *__restrict__ expo) {
+__device__ __forceinline__ void move_to(const MoveArgs &a, const Moved &m, const KT *__restrict__ pool, int8_t *__restrict__ codes, int8_t *__restrict__ expo) {
     constexpr int N = HD / 32, LPR = HD / 8;      // loads; lanes a key row
-    const uint32_t item = blockIdx.x * 4u + (threadIdx.x >> 6);
     const int lane = threadIdx.x & 63;
-    Moved m;
-    if (item >= items || !moved_block(a, item, m)) return;
     const KT *src = pool + m.full * kv_block_elems(a.Hkv, HD) + ((int64_t)m.value * a.Hkv + m.j) * 16 * HD + 8 * lane;
     int8_t *dst = codes + m.q8 * q8_block(a.Hkv, HD) + ((int64_t)m.value * a.Hkv + m.j) * 16 * HD + 8 * lane;
     int8_t *ex = expo + ((m.q8 * 2 + m.value) * a.Hkv + m.j) * 16;
@@ -293,12 +291,9 @@ __global__ __launch_bounds__(256) void k_to_q8(MoveArgs a, uint32_t items, const
 }
 
 template <int HD, typename KT>
-__global__ __launch_bounds__(256) void k_from_q8(MoveArgs a, uint32_t items, const int8_t *__restrict__ codes, const int8_t *__restrict__ expo, KT *__restrict__ pool) {
+__device__ __forceinline__ void move_from(const MoveArgs &a, const Moved &m, const int8_t *__restrict__ codes, const int8_t *__restrict__ expo, KT *__restrict__ pool) {
     constexpr int N = HD / 32, LPR = HD / 8;
-    const uint32_t item = blockIdx.x * 4u + (threadIdx.x >> 6);
     const int lane = threadIdx.x & 63;
-    Moved m;
-    if (item >= items || !moved_block(a, item, m)) return;
     const int8_t *src = codes + m.q8 * q8_block(a.Hkv, HD) + ((int64_t)m.value * a.Hkv + m.j) * 16 * HD + 8 * lane;
     const int8_t *ex = expo + ((m.q8 * 2 + m.value) * a.Hkv + m.j) * 16;
     KT *dst = pool + m.full * kv_block_elems(a.Hkv, HD) + ((int64_t)m.value * a.Hkv + m.j) * 16 * HD + 8 * lane;
@@ -327,7 +322,33 @@ __global__ __launch_bounds__(256) void k_from_q8(MoveArgs a, uint32_t items, con
     }
 }
 
-constexpr int MANY_ROWS = 64;
+template <int HD, typename KT, bool TO>
+__global__ __launch_bounds__(256) void k_move_q8(MoveArgs a, uint32_t items, KT *__restrict__ pool, int8_t *__restrict__ codes, int8_t *__restrict__ expo) {
+    const uint32_t item = blockIdx.x * 4u + (threadIdx.x >> 6);
+    Moved m;
+    if (item >= items || !moved_block(a, item, m)) return;
+    if constexpr (TO) move_to<HD, KT>(a, m, pool, codes, expo);
+    else move_from<HD, KT>(a, m, codes, expo, pool);
+}
+
+template <bool TO>
+ld_status move(const char *what, const MoveArgs &a, int n_ranges, int hd, void *pool, int dtype, int8_t *codes, int8_t *expo, hipStream_t s) {
+    const int64_t items = (((int64_t)a.max_len + 14) / 16 + 1) * 2 * a.Hkv;      // positions first .. first + max_len - 1 touch at most so many blocks
+    if (items > INT32_MAX) {
+        ld::set_error("%s: too many blocks a range", what);
+        return LD_E_RANGE;
+    }
+    const dim3 grid((unsigned)((items + 3) / 4), n_ranges), block(256);
+#define LD_MOVE(HD_, KT_) LD_LAUNCH((k_move_q8<HD_, KT_, TO>), grid, block, 0, s, a, (uint32_t)items, (KT_ *)pool, codes, expo)
+    if (dtype == LD_BF16) { if (hd == 128) LD_MOVE(128, bf16_t); else LD_MOVE(64, bf16_t); }
+    else { if (hd == 128) LD_MOVE(128, float); else LD_MOVE(64, float); }
+#undef LD_MOVE
+    return launched("k_move_q8");
+}
+
+// From so many rows on sixteen rows a workgroup.  us, one row and head a wave / sixteen rows, 32 + 32 heads: rows of as many sequences 16 3.0 / 3.6, 32 3.5 / 3.8,
+// 64 4.7 / 4.4; of one chunk 16 3.0 / 2.9, 32 3.5 / 3.1, 64 4.5 / 3.3, 256 10.7 / 5.4.
+constexpr int MANY_ROWS = 48;
 
 bool bad_pool(const void *codes, const void *expo) { return !codes || !expo || (((uintptr_t)codes | (uintptr_t)expo) & 15); }
 
@@ -398,15 +419,7 @@ ld_status ldk_kv_to_q8(const void *pool_layer, int32_t dtype, const int32_t *tab
     if (n_ranges == 0 || max_len == 0) return LD_OK;
     const MoveArgs a{table, table_stride, q8_table, q8_table_stride, ranges, Hkv, max_len};
     if (const ld_status bad = check_move("ldk_kv_to_q8", pool_layer, dtype, a, codes, expo, n_ranges, hd)) return bad;
-    const int64_t items = (((int64_t)max_len + 14) / 16 + 1) * 2 * Hkv;      // positions first .. first + max_len - 1 touch at most so many blocks
-    if (items > INT32_MAX) return ld::fail(LD_E_RANGE, "ldk_kv_to_q8: too many blocks a range");
-    const dim3 grid((unsigned)((items + 3) / 4), n_ranges), block(256);
-    hipStream_t s = (hipStream_t)stream;
-#define LD_TO(HD_, KT_) LD_LAUNCH((k_to_q8<HD_, KT_>), grid, block, 0, s, a, (uint32_t)items, (const KT_ *)pool_layer, codes, expo)
-    if (dtype == LD_BF16) { if (hd == 128) LD_TO(128, bf16_t); else LD_TO(64, bf16_t); }
-    else { if (hd == 128) LD_TO(128, float); else LD_TO(64, float); }
-#undef LD_TO
-    return launched("k_to_q8");
+    return move<true>("ldk_kv_to_q8", a, n_ranges, hd, const_cast<void *>(pool_layer), dtype, codes, expo, (hipStream_t)stream);
 }
 
 ld_status ldk_kv_from_q8(const int8_t *codes, const int8_t *expo, const int32_t *q8_table, int32_t q8_table_stride, void *pool_layer, int32_t dtype,
@@ -415,15 +428,7 @@ ld_status ldk_kv_from_q8(const int8_t *codes, const int8_t *expo, const int32_t 
     if (n_ranges == 0 || max_len == 0) return LD_OK;
     const MoveArgs a{table, table_stride, q8_table, q8_table_stride, ranges, Hkv, max_len};
     if (const ld_status bad = check_move("ldk_kv_from_q8", pool_layer, dtype, a, codes, expo, n_ranges, hd)) return bad;
-    const int64_t items = (((int64_t)max_len + 14) / 16 + 1) * 2 * Hkv;      // positions first .. first + max_len - 1 touch at most so many blocks
-    if (items > INT32_MAX) return ld::fail(LD_E_RANGE, "ldk_kv_from_q8: too many blocks a range");
-    const dim3 grid((unsigned)((items + 3) / 4), n_ranges), block(256);
-    hipStream_t s = (hipStream_t)stream;
-#define LD_FROM(HD_, KT_) LD_LAUNCH((k_from_q8<HD_, KT_>), grid, block, 0, s, a, (uint32_t)items, codes, expo, (KT_ *)pool_layer)
-    if (dtype == LD_BF16) { if (hd == 128) LD_FROM(128, bf16_t); else LD_FROM(64, bf16_t); }
-    else { if (hd == 128) LD_FROM(128, float); else LD_FROM(64, float); }
-#undef LD_FROM
-    return launched("k_from_q8");
+    return move<false>("ldk_kv_from_q8", a, n_ranges, hd, pool_layer, dtype, const_cast<int8_t *>(codes), const_cast<int8_t *>(expo), (hipStream_t)stream);
 }
 
 }  // extern "C"

@@ -8,7 +8,11 @@
 //            entry), the keys enter as they lie in the cache.  One product where three terms find room beside the heads (GP <= 4), two or three else; a
 //            rotation within 16 lanes adds the terms, scaled to float32, so that every column of a head holds its score.
 //   sums     O^T[d, c] += V^T[d, pos] W^T[pos, c] (16x16x32, fp16): codes are exact in fp16; W = p 2^(e - k), e the value's exponent and k
-//            the running largest of p 2^e in the column, as two fp16 terms (22 bits) in two columns.
+//            the running largest of p 2^e in the column, held at 2^13 .. 2^14, as two fp16 terms (22 bits) in two columns.
+//
+// What bounds it is the cache's stream: 32 rows of 512 - 8192 positions of 32 heads 206 us with the join, 5.5 TB/s (a large copy reaches 5.2); one row of
+// 131067 positions of 8 KV heads 58 us, 53 of them the stream.  Heads are next to each other in the grid, for the blocks' sake (344 us with rows next to each other).
+// One row of 1520 positions is a chain of loads, a tile and the join: 8.0 and 2.3 us.
 //
 // Which position a row of the score tile is, is free: row 4 g + i of tile t is slot 4 t + i of block g, so lane (c, g) ends with the scores of
 // block g, slot by slot, which is what it has to bring as the other operand of the sums.
