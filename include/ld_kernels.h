@@ -269,7 +269,7 @@ ld_status ldk_choose(const float *logits, int32_t R, int32_t V, const ld_token_r
  * c 2^e is exact in bf16 and float32, so positions that go through a bf16 pool and back keep their codes.  What unwritten slots hold never
  * reaches a result.  Tables, slots and positions as in ldk_rope_kv_write; hd is 64 or 128, H a multiple of Hkv.  In every call of this
  * section blocks that a table does not map (entry < 0, or positions beyond table_stride blocks) are not touched: nothing is written to them, and no
- * position of theirs is visible. */
+ * position of theirs is visible.  Nothing in scratch has to be clear; calls that may overlap (on two streams) have scratch of their own. */
 
 /* ldk_rope_table for any even rot >= 2 (the rotated part of a head; pairs i < rot / 2) and scaled frequencies: with f = rope_base^(-2i/rot),
  *   r = original f / 2 pi (turns over the original context),  g = clamp((r - low) / (high - low), 0, 1),  f' = f ((1 - g) / factor + g),

@@ -650,9 +650,16 @@ def _refuse(what):
     raise LdError(LD_E_INVAL, what)
 
 
+def _on_device(call, t):
+    """Refuses a tensor that is not on the current device, where the call is launched."""
+    if _cuda_up() and t.get_device() != _current_device():
+        _refuse(f"{call}: tensors have to be on the current device ({_current_device()}), not on {t.device}")
+
+
 def _q8_layer(call, codes, expo, Hkv, hd):
     """Addresses of a layer's codes int8 [blocks, 2, Hkv, 16, hd] and exponents int8 [blocks, 2, Hkv, 16]."""
     n = expo.numel()
+    _on_device(call, codes)
     if Hkv < 1 or hd < 1 or codes.dtype is not _I8 or expo.dtype is not _I8 or codes.numel() != n * hd or n % (32 * Hkv) or not codes.is_contiguous() or \
             not expo.is_contiguous():
         _refuse(f"{call}: codes int8 [blocks, 2, {Hkv}, 16, {hd}] and expo int8 [blocks, 2, {Hkv}, 16], contiguous, not {codes.dtype} {tuple(codes.shape)} "
@@ -698,6 +705,7 @@ def ldk_rope_kv_write_q8(qkv, cos_sin, pos, seq_slot, table, codes, expo, H, Hkv
             codes.numel() == ne * hd and qkv.is_contiguous() and q_out.is_contiguous() and pos.is_contiguous() and seq_slot.is_contiguous() and
             table.is_contiguous() and codes.is_contiguous() and expo.is_contiguous()):
         _append_fits(qkv, pos, seq_slot, table, codes, expo, Hkv, hd, q_out)
+    _on_device("ldk_rope_kv_write_q8", codes)
     rc = (_lib or lib()).ldk_rope_kv_write_q8(
         qkv.data_ptr(), qs, q_gain if q_gain is None else _at("q_gain", q_gain, _F32, hd), k_gain if k_gain is None else _at("k_gain", k_gain, _F32, hd), eps,
         _at("cos_sin", cos_sin, _F32, T * rot), rot, 1 if interleaved else 0, pos.data_ptr(), seq_slot.data_ptr(), table.data_ptr(), stride, codes.data_ptr(),
@@ -737,6 +745,7 @@ def _move(call, pool_layer, table, codes, expo, q8_table, ranges, Hkv, hd):
             _q8_table(call, t)
         _q8_layer(call, codes, expo, Hkv, hd)
         _at("ranges", ranges, _I32, ranges.numel())
+    _on_device(call, codes)
     return ((pool_layer.data_ptr(), LD_F32 if kind is _F32 else LD_BF16, table.data_ptr(), stride),
             (codes.data_ptr(), expo.data_ptr(), q8_table.data_ptr(), q8_stride), (ranges.data_ptr(), n))
 

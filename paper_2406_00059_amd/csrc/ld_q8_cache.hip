@@ -379,7 +379,7 @@ ld_status ldk_rope_table_scaled(const int32_t *pos, int32_t T, int32_t rot, floa
     if (T == 0) return LD_OK;
     if (!pos || !cos_sin) return ld::fail(LD_E_INVAL, "ldk_rope_table_scaled: bad argument");
     const int64_t n = (int64_t)T * (rot / 2);
-    if (n > (int64_t)1 << 38) return ld::fail(LD_E_RANGE, "ldk_rope_table_scaled: too many angles");
+    if (n > (int64_t)1 << 36) return ld::fail(LD_E_RANGE, "ldk_rope_table_scaled: too many angles");
     LD_LAUNCH(k_rope_table_scaled, dim3((unsigned)((n + 63) / 64)), dim3(64), 0, (hipStream_t)stream, pos, n, rot / 2, std::log2((double)rope_base),
               (double)sc.factor, (double)sc.low, (double)sc.high, sc.original / (2 * M_PI), (double)sc.attention, reinterpret_cast<float2 *>(cos_sin));
     return launched("k_rope_table_scaled");

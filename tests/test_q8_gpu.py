@@ -676,3 +676,89 @@ def test_recorded_steps_and_other_streams():
         step()
         assert all(torch.equal(x, y) for x, y in zip(got, (q, a, b, dc, de)))
         assert (a - b).norm().item() <= 4e-6 * b.norm().item()      # two kernels, the same rows
+
+
+def test_tensors_in_host_memory_are_refused():
+    H = Hkv = 2
+    hd = 64
+    z = lambda *s, dtype=torch.float32: torch.zeros(s, dtype=dtype)      # noqa: E731
+    codes, expo, table = z(1, 2, Hkv, 16, hd, dtype=torch.int8), z(1, 2, Hkv, 16, dtype=torch.int8), z(1, 1, dtype=torch.int32)
+    i1, scratch = z(1, dtype=torch.int32), z(1 << 20)
+    torch.cuda.current_stream()
+    calls = [lambda: ld.ldk_rope_kv_write_q8(z(1, 3 * H * hd), z(1, hd // 2, 2), i1, i1, table, codes, expo, H, Hkv, hd, z(1, H * hd)),
+             lambda: ld.ldk_kv_to_q8(z(1, 2, Hkv, 16, hd), table, codes, expo, table, z(1, 3, dtype=torch.int32), 1, Hkv, hd),
+             lambda: ld.ldk_kv_from_q8(codes, expo, table, z(1, 2, Hkv, 16, hd), table, z(1, 3, dtype=torch.int32), 1, Hkv, hd),
+             lambda: ld.ldk_paged_attention_q8(z(1, H * hd), H * hd, codes, expo, table, i1, i1, 1, H, Hkv, hd, z(1, H, hd), scratch),
+             lambda: ld.ldk_prefill_attention_q8(z(1, H * hd), H * hd, codes, expo, table, z(1, 6, dtype=torch.int32), H, Hkv, hd, z(1, H, hd), 0, scratch=scratch)]
+    torch.zeros(1, device=DEV)      # the GPU is up
+    for call in calls:
+        with pytest.raises(ld.LdError) as e:
+            call()
+        assert e.value.status == ld.LD_E_INVAL and "device" in str(e.value)
+
+
+@pytest.mark.parametrize("G", [1, 3, 16])
+def test_unmapped_blocks_inside_a_sequence_are_not_seen(G):
+    """Positions whose block the table does not map take no part, in both attention calls; neither do positions beyond the table."""
+    Hkv, hd, n = 2, 128, 300
+    H = G * Hkv
+    table, codes, expo = _layer([n], Hkv, hd, 15)
+    table[0, [0, 4, 5, 11]] = -1
+    kept = np.array([p for p in range(n) if table[0, p // 16] >= 0])
+    q = gen.normal(15, 13, (1, H * hd))
+    full = table.copy()
+    full[0, table[0] < 0] = 0      # for reading the values: these positions are dropped below
+    k, v = _sequence(full, codes, expo, 0, n)
+    for width, wide in ((19, n), (15, 240)):      # the second table ends at position 240
+        cut = np.ascontiguousarray(table[:, :width])
+        out = _run_decode(q, cut, codes, expo, [0], [n], H, Hkv, hd)
+        chunk = _run_prefill(q, 1, cut, codes, expo, [(0, 1, n - 1, 0, 0, 0)], H, Hkv, hd, n - 1)
+        use = kept[kept < wide]
+        for h in range(H):
+            ref, bound = _attend(q[0, h * hd:(h + 1) * hd].double().numpy(), k[use, h // G], v[use, h // G], 0, 0, len(use) - 1, 0.0, 0.0, least=9)
+            for got in (out, chunk):
+                assert (np.abs(got[0, h].double().cpu().numpy() - ref) <= bound).all()
+
+
+def test_two_streams_at_once():
+    """Calls on two streams over one cache, each with its own scratch, give what they give alone."""
+    H, Hkv, hd, n = 8, 2, 128, 5000
+    table, codes, expo = _layer([n, n - 7], Hkv, hd, 16)
+    dc, de = _device_layer(codes, expo)
+    dt = _i32(table)
+    qs = [gen.normal(16, 20 + i, (2, H * hd)).to(DEV) for i in range(2)]
+    size = ld.ldk_attention_q8_scratch_bytes(2, H, Hkv, hd, n)
+
+    def call(q, out, scratch, stream):
+        ld.ldk_paged_attention_q8(q, H * hd, dc, de, dt, _ctx[0], _ctx[1], n, H, Hkv, hd, out, scratch, stream=stream)
+
+    _ctx = _i32([0, 1]), _i32([n, n - 7])
+    alone = []
+    for q in qs:
+        alone.append(torch.empty((2, H, hd), device=DEV))
+        call(q, alone[-1], torch.empty(size, dtype=torch.uint8, device=DEV), None)
+    torch.cuda.synchronize()
+    streams, outs, scratch = [torch.cuda.Stream() for _ in qs], [torch.zeros((2, H, hd), device=DEV) for _ in qs], [torch.empty(size, dtype=torch.uint8, device=DEV) for _ in qs]
+    torch.cuda.synchronize()
+    for _ in range(20):
+        for q, o, s, st in zip(qs, outs, scratch, streams):
+            call(q, o, s, st)
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(alone, outs))
+
+
+@pytest.mark.parametrize("hd,H,Hkv", [(128, 4, 4), (64, 8, 2)])
+def test_empty_calls_and_padded_tiles(hd, H, Hkv):
+    """No rows, no tiles; tiles of no rows beside others; a batch in which no row sees anything."""
+    table, codes, expo = _layer([20, 30], Hkv, hd, 17)
+    none = torch.empty((0, H * hd), device=DEV)
+    assert _run_decode(none, table, codes, expo, [], [], H, Hkv, hd, max_ctx=0).shape[0] == 0
+    out = _run_decode(gen.normal(17, 1, (2, H * hd)), table, codes, expo, [0, 1], [0, 0], H, Hkv, hd, max_ctx=0)
+    assert (out == 0).all()
+    q = gen.normal(17, 2, (8, H * hd))
+    tiles = [(0, 0, 0, 0, 0, 0), (3, 4, 16, 0, 0, 0), (0, 0, 0, -1, 0, 0), (0, 2, 5, 1, 0, 0)]
+    out = _run_prefill(q, 8, table, codes, expo, tiles, H, Hkv, hd, 19)
+    _check_prefill(out, q, table, codes, expo, tiles, [20, 30], H, Hkv, hd)
+    assert (out[[2, 7]] == 9.0).all()
+    ld.ldk_prefill_attention_q8(q.to(DEV), H * hd, *_device_layer(codes, expo), _i32(table), torch.empty((0, 6), dtype=torch.int32, device=DEV), H, Hkv, hd, out, 0,
+                                scratch=torch.empty(16, dtype=torch.uint8, device=DEV))
