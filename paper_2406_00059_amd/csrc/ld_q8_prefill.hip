@@ -18,6 +18,7 @@
 // interleaved by hand (826).
 #include <algorithm>
 #include <cmath>
+#include <utility>
 #include "ld_q8.h"
 
 using namespace ldd;
@@ -30,7 +31,7 @@ typedef float f32x16_t __attribute__((ext_vector_type(16)));
 
 template <int HD>
 struct Stage {
-    uint4 k[4 * HD];               // [position][piece of 16 dims, swizzled]
+    i32x4_t k[4 * HD];             // [position][piece of 16 dims, swizzled]
     f16x8_t v[8 * HD];             // [block][half][dim]: eight slots
     float ku[TILE], vu[TILE];      // units; NaN where a vector is not finite
     int mapped;                    // bit b: block b
@@ -41,6 +42,12 @@ template <int HD>
 __device__ __forceinline__ int key_piece(int r, int p) {
     constexpr int N = HD / 16;
     return N == 8 ? r * 8 + (p ^ ((r & 3) | ((r >> 2) & 4))) : r * 4 + (p ^ (((r >> 1) & 1) | ((r >> 3) & 2)));
+}
+
+// x[i] *= the unit that lane i of these sixteen holds.
+template <int... I>
+__device__ __forceinline__ void times_units(float (&x)[16], float unit, std::integer_sequence<int, I...>) {
+    ((x[I] *= __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(unit), 0x150 + I, 0xf, 0xf, true))), ...);
 }
 
 struct TileRows { int row, n, pos, seq, first, prefix; };
@@ -84,7 +91,7 @@ __global__ __launch_bounds__(256, 2) void k_prefill_q8(Q8Attention a, const int3
 
     // ---- what a thread brings of a tile: NP pieces of keys and of values, and one exponent
     int id[NP], ide;
-    uint4 kr[NP], vr[NP];
+    i32x4_t kr[NP], vr[NP];
     int er = 0;
     const uint32_t place = 16 * (tid % HD);
     const int eb = (tid & 63) >> 4;
@@ -97,8 +104,8 @@ __global__ __launch_bounds__(256, 2) void k_prefill_q8(Q8Attention a, const int3
 #pragma unroll
         for (int u = 0; u < NP; u++) {
             const int8_t *b = a.codes + max(__builtin_amdgcn_readfirstlane(id[u]), 0) * bs + q8_k(HD, j, 0, 0);      // a scalar: the lanes differ by 32 bits
-            kr[u] = *reinterpret_cast<const uint4 *>(b + place);
-            vr[u] = *reinterpret_cast<const uint4 *>(b + a.Hkv * 16 * HD + place);
+            kr[u] = *reinterpret_cast<const i32x4_t *>(b + place);
+            vr[u] = *reinterpret_cast<const i32x4_t *>(b + a.Hkv * 16 * HD + place);
         }
         if (tid < 128) er = a.expo[(((int64_t)max(ide, 0) * 2 + (tid >> 6)) * a.Hkv + j) * 16 + (tid & 15)];
     };
@@ -109,8 +116,8 @@ __global__ __launch_bounds__(256, 2) void k_prefill_q8(Q8Attention a, const int3
         for (int u = 0; u < NP; u++) {
             const int i = tid + 256 * u, b = i / HD, in = i % HD;
             s.k[key_piece<HD>(b * 16 + in / (HD / 16), in % (HD / 16))] = kr[u];
-            s.v[(2 * b) * HD + in] = q8_halves(vr[u].x, vr[u].y);
-            s.v[(2 * b + 1) * HD + in] = q8_halves(vr[u].z, vr[u].w);
+            s.v[(2 * b) * HD + in] = q8_halves(vr[u][0], vr[u][1]);
+            s.v[(2 * b + 1) * HD + in] = q8_halves(vr[u][2], vr[u][3]);
         }
         if (tid < 64) {
             s.ku[tid] = q8_unit(er);
@@ -174,7 +181,7 @@ __global__ __launch_bounds__(256, 2) void k_prefill_q8(Q8Attention a, const int3
             const int row = (2 * u + ((r32 >> 2) & 1)) * 16 + (r32 >> 3) * 4 + (r32 & 3);
             i32x4_t kf[KS];
 #pragma unroll
-            for (int q = 0; q < KS; q++) kf[q] = __builtin_bit_cast(i32x4_t, st.k[key_piece<HD>(row, 2 * q + hh)]);
+            for (int q = 0; q < KS; q++) kf[q] = st.k[key_piece<HD>(row, 2 * q + hh)];
 #pragma unroll
             for (int q = 0; q < KS; q++) acc = __builtin_amdgcn_mfma_i32_32x32x32_i8(kf[q], qd[1][q], acc, 0, 0, 0);
 #pragma unroll
@@ -183,13 +190,9 @@ __global__ __launch_bounds__(256, 2) void k_prefill_q8(Q8Attention a, const int3
             for (int i = 0; i < 16; i++) acc[i] <<= 8;
 #pragma unroll
             for (int q = 0; q < KS; q++) acc = __builtin_amdgcn_mfma_i32_32x32x32_i8(kf[q], qd[0][q], acc, 0, 0, 0);
-            const float4 *ku = reinterpret_cast<const float4 *>(st.ku + 32 * u + 16 * hh);
 #pragma unroll
-            for (int i = 0; i < 16; i++) {
-                const float4 k4 = ku[i >> 2];
-                const float kk = (i & 3) == 0 ? k4.x : (i & 3) == 1 ? k4.y : (i & 3) == 2 ? k4.z : k4.w;
-                s[u][i] = fmaf((float)acc2[i], 65536.f, (float)acc[i]) * kk;
-            }
+            for (int i = 0; i < 16; i++) s[u][i] = fmaf((float)acc2[i], 65536.f, (float)acc[i]);
+            times_units(s[u], st.ku[32 * u + 16 * hh + (lane & 15)], std::make_integer_sequence<int, 16>());
         }
         if constexpr (EXTRA) {
             float most = 0.f;
@@ -257,15 +260,12 @@ __global__ __launch_bounds__(256, 2) void k_prefill_q8(Q8Attention a, const int3
         float sum = 0.f, top = 0.f;
 #pragma unroll
         for (int u = 0; u < 2; u++) {
-            const float4 *vu = reinterpret_cast<const float4 *>(st.vu + 32 * u + 16 * hh);
 #pragma unroll
             for (int i = 0; i < 16; i++) {
-                const float4 v4 = vu[i >> 2];
-                const float vv = (i & 3) == 0 ? v4.x : (i & 3) == 1 ? v4.y : (i & 3) == 2 ? v4.z : v4.w;
-                const float p = fast_exp2(fmaf(s[u][i], rs, add));
-                sum += p;
-                s[u][i] = p * vv;
+                s[u][i] = fast_exp2(fmaf(s[u][i], rs, add));
+                sum += s[u][i];
             }
+            times_units(s[u], st.vu[32 * u + 16 * hh + (lane & 15)], std::make_integer_sequence<int, 16>());
         }
         if (!whole) keep_seen(s, 0.f);      // units of positions that are not seen may be anything
 #pragma unroll
