@@ -369,29 +369,34 @@ __global__ __launch_bounds__(256, 2) void k_prefill_q8(Q8Attention a, const int3
     if (splits > 1 && hh == 0) part_ml[item] = make_float2(l == 0.f ? -INFINITY : -add, l);
 }
 
-// Joins the shares of a row and head, in their order: one wave a row.
+// Joins the shares of a row and head, in their order: HD / 4 lanes a row, four shares' loads in flight (a wave a row and one load at a time: 8.8 us for the 96
+// pairs below, 16.4 for the 280).
 template <int HD>
 __global__ __launch_bounds__(256) void k_join_prefill_q8(Q8Attention a, const int32_t *__restrict__ tiles, int splits, const float *__restrict__ part_o,
                                                          const float2 *__restrict__ part_ml) {
-    const int tile_no = blockIdx.x, h = blockIdx.y, lane = threadIdx.x & 63, r = blockIdx.z * 4 + (threadIdx.x >> 6);
+    constexpr int PER = HD / 4;
+    const int tile_no = blockIdx.x, h = blockIdx.y, d = threadIdx.x % PER, r = blockIdx.z * (256 / PER) + threadIdx.x / PER;
     const int32_t *tp = tiles + 6 * (int64_t)tile_no;
     if (r >= min(tp[1], ROWS)) return;
     const int64_t first = ((int64_t)tile_no * a.H + h) * splits * ROWS + r;
+    const float2 *ml = part_ml + first;
+    const float4 *po = reinterpret_cast<const float4 *>(part_o + first * HD) + d;
     float M = -INFINITY;
-    for (int i = 0; i < splits; i++) M = fmaxf(M, part_ml[first + (int64_t)i * ROWS].x);
+#pragma unroll 4
+    for (int i = 0; i < splits; i++) M = fmaxf(M, ml[i * ROWS].x);
     const float ref = M > -INFINITY ? M : 0.f;
-    float L = 0.f, acc[HD / 64] = {};
+    float L = 0.f;
+    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 4
     for (int i = 0; i < splits; i++) {
-        const int64_t at = first + (int64_t)i * ROWS;
-        const float2 ml = part_ml[at];
-        if (ml.y == 0.f) continue;
-        const float f = fast_exp2(ml.x - ref) * ml.y;
+        const float2 w = ml[i * ROWS];
+        const float4 o = po[(int64_t)i * ROWS * PER];
+        const float f = w.y == 0.f ? 0.f : fast_exp2(w.x - ref) * w.y;      // a share without a position that the row sees left zeros
         L += f;
-#pragma unroll
-        for (int u = 0; u < HD / 64; u++) acc[u] += f * part_o[at * HD + lane + 64 * u];
+        acc = make_float4(fmaf(f, o.x, acc.x), fmaf(f, o.y, acc.y), fmaf(f, o.z, acc.z), fmaf(f, o.w, acc.w));
     }
-#pragma unroll
-    for (int u = 0; u < HD / 64; u++) a.out[((int64_t)(tp[0] + r) * a.H + h) * HD + lane + 64 * u] = L == 0.f ? 0.f : acc[u] / L;
+    const float inv = L == 0.f ? 0.f : 1.f / L;
+    *reinterpret_cast<float4_u *>(a.out + ((int64_t)(tp[0] + r) * a.H + h) * HD + 4 * d) = (float4_u){acc.x * inv, acc.y * inv, acc.z * inv, acc.w * inv};
 }
 
 constexpr int MOST = 1024, LEAST = 4;      // workgroups with shares, 64-position tiles a share
@@ -412,7 +417,7 @@ void launch_prefill(const Q8Attention &a, const int32_t *tiles, int n_tiles, int
     const dim3 grid((unsigned)((int64_t)n_tiles * a.H * splits)), block(256);
     if (a.softcap > 0.f || a.slopes) LD_LAUNCH((k_prefill_q8<HD, true>), grid, block, 0, s, a, tiles, n_tiles, max_pos, splits, part_o, part_ml);
     else LD_LAUNCH((k_prefill_q8<HD, false>), grid, block, 0, s, a, tiles, n_tiles, max_pos, splits, part_o, part_ml);
-    if (splits > 1) LD_LAUNCH(k_join_prefill_q8<HD>, dim3(n_tiles, a.H, ROWS / 4), block, 0, s, a, tiles, splits, part_o, part_ml);
+    if (splits > 1) LD_LAUNCH(k_join_prefill_q8<HD>, dim3(n_tiles, a.H, ROWS * HD / 1024), block, 0, s, a, tiles, splits, part_o, part_ml);
 }
 
 }  // namespace
