@@ -11,11 +11,16 @@
 // Which position a row of the score tile is, is free: row 8 b + 4 h + i is slot 4 b + i of block h of a pair, so that lane (row, h) ends with the scores of
 // block h, slot by slot, which is what it has to bring as the other operand of the sums.
 //
-// What bounds it: 64 positions and 32 rows are 56 matrix instructions (1800 cycles of a SIMD) and some 590 vector ones (2700), and with two waves a SIMD, which
-// is what the registers allow, the two add up (profiles: 39 and 59 % of the time).  8191 rows of 32 heads in a band of 4096 take 810 us, 510 TFLOP/s of the
-// formula and 890 of executed products.  Measured and not kept: scores in fp16 with queries in two terms (five vector instructions an entry less, a third more
+// Units of positions are held by sixteen lanes each and enter products from there (row_newbcast); read by every lane they cost a third of the LDS reads, and
+// the registers that brought some of the staged keys into scratch memory (8191 rows below: 812 us).
+//
+// What bounds it: 64 positions and 32 rows are 56 matrix instructions (1800 cycles of a SIMD) and some 540 vector ones.  With two waves a SIMD, which is what
+// the registers allow, matrix instructions take 49 % and vector ones 69 % of the time.  8191 rows of 32 heads in a band of 4096 take 730 - 760 us, some 555 TFLOP/s
+// of the formula and 970 of executed products, at a clock that falls to 1.6 - 2.0 GHz meanwhile: vector instructions saved (sums that the matrix cores begin
+// at a number whose bits are a float's) and the two kinds of work ordered otherwise (scores of both halves first, wave priorities) no longer change it.
+// Measured and not kept, the first three with keys in scratch: scores in fp16 with queries in two terms (five vector instructions an entry less, a third more
 // matrix time, registers spilled: 1055 us); one wave a SIMD with the scores of the next tile formed ahead (1794); half tiles whose instructions are
-// interleaved by hand (826).
+// interleaved by hand (826); two groups of four waves that take turns at matrix and vector instructions, a barrier between (913).
 #include <algorithm>
 #include <cmath>
 #include <utility>
@@ -26,6 +31,9 @@ using namespace ldd;
 namespace {
 
 constexpr int TILE = 64, ROWS = 128;
+// Units of keys are 2^-23 too small and those of queries as much too large, so that a whole-number score (below 2^38) times a key's unit stays in float32 for keys
+// up to 2^120; the smallest unit, 2^-149, is still a float.
+constexpr int KEY_SHIFT = 23;
 typedef int i32x16_t __attribute__((ext_vector_type(16)));
 typedef float f32x16_t __attribute__((ext_vector_type(16)));
 
@@ -120,7 +128,7 @@ __global__ __launch_bounds__(256, 2) void k_prefill_q8(Q8Attention a, const int3
             s.v[(2 * b + 1) * HD + in] = q8_halves(vr[u][2], vr[u][3]);
         }
         if (tid < 64) {
-            s.ku[tid] = q8_unit(er);
+            s.ku[tid] = er == Q8_NAN ? __uint_as_float(0x7fc00000u) : ldexpf(1.f, er - KEY_SHIFT);
             const uint64_t ok = __ballot(ide_of >= 0);
             if (tid == 0) s.mapped = (int)((ok & 1) | (ok >> 15 & 2) | (ok >> 30 & 4) | (ok >> 45 & 8));
         } else if (tid < 128) {
@@ -144,7 +152,7 @@ __global__ __launch_bounds__(256, 2) void k_prefill_q8(Q8Attention a, const int3
             }
         top = max(top, (uint32_t)__shfl_xor((int)top, 32, WAVE));
         const Q8Query query = q8_query(top, (EXTRA ? 1.0 : 1.4426950408889634) / sqrt((double)HD));
-        unit = ldexpf(query.unit, query.exp);
+        unit = ldexpf(query.unit, query.exp + KEY_SHIFT);
         unit = unit < 0x1p-126f ? 0x1p-126f : unit;      // not zero: it multiplies -infinity
 #pragma unroll
         for (int s = 0; s < KS; s++)
@@ -369,8 +377,8 @@ __global__ __launch_bounds__(256, 2) void k_prefill_q8(Q8Attention a, const int3
     if (splits > 1 && hh == 0) part_ml[item] = make_float2(l == 0.f ? -INFINITY : -add, l);
 }
 
-// Joins the shares of a row and head, in their order: HD / 4 lanes a row, four shares' loads in flight (a wave a row and one load at a time: 8.8 us for the 96
-// pairs below, 16.4 for the 280).
+// Joins the shares of a row and head, in their order: HD / 4 lanes a row, four shares' loads in flight (5.7 us for the 96 pairs
+// below and 11.3 for the 280; a wave a row and one load at a time 8.8 and 16.4).
 template <int HD>
 __global__ __launch_bounds__(256) void k_join_prefill_q8(Q8Attention a, const int32_t *__restrict__ tiles, int splits, const float *__restrict__ part_o,
                                                          const float2 *__restrict__ part_ml) {
@@ -402,8 +410,8 @@ __global__ __launch_bounds__(256) void k_join_prefill_q8(Q8Attention a, const in
 constexpr int MOST = 1024, LEAST = 4;      // workgroups with shares, 64-position tiles a share
 
 // Shares of a tile's positions, by the number of (tile, head) pairs.  Up to a pair a CU: what fills the CUs once with two workgroups each, or nearly; more: about
-// four a CU, so that the last ones do not work alone.  us, 1 / 2 / 3 / 4 / 5 / 6 / 8 shares: 96 pairs of 24 tiles - / 50 / 49 / 44 / 47 / 56 / 56, 280 pairs of up to
-// 68 tiles 318 / 184 / 177 / 157 / 165 / 160 / 188.
+// four a CU, so that the last ones do not work alone.  us, 1 / 2 / 3 / 4 / 5 / 6 / 8 shares: 96 pairs of 24 tiles 64 / 45 / 46 / 42 / 44 / 50 / 50, 280 pairs of up to
+// 68 tiles 192 / 131 / 134 / 124 / 127 / 132 / 149 (with a join one load at a time).
 int shares(int n_tiles, int H, int max_pos) {
     const int64_t pairs = (int64_t)n_tiles * H, kt = ((int64_t)max_pos + TILE) / TILE;
     const int64_t n = pairs <= 256 ? std::max<int64_t>(2, 400 / pairs) : (MOST + pairs - 1) / pairs;

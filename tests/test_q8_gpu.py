@@ -762,3 +762,23 @@ def test_empty_calls_and_padded_tiles(hd, H, Hkv):
     assert (out[[2, 7]] == 9.0).all()
     ld.ldk_prefill_attention_q8(q.to(DEV), H * hd, *_device_layer(codes, expo), _i32(table), torch.empty((0, 6), dtype=torch.int32, device=DEV), H, Hkv, hd, out, 0,
                                 scratch=torch.empty(16, dtype=torch.uint8, device=DEV))
+
+
+@pytest.mark.parametrize("hd,H,Hkv", [(128, 2, 2), (64, 4, 1)])
+def test_keys_and_values_near_the_ends_of_their_range(hd, H, Hkv):
+    """Keys up to 2^120 under queries of 2^-115, and keys of 2^-120 and 2^-104 under queries of 2^108; values over 2^84, zeros first."""
+    n = 150
+    for keys, small in (((113, 100, 90), -115), ((-126, -124, -110), 108)):
+        table, codes, expo = _layer([n], Hkv, hd, 18)
+        pick = gen.randint(18, 1, 0, len(keys) - 1, 10 * Hkv * 16).numpy().reshape(10, Hkv, 16)
+        expo[table[0, :10], 0] = np.array(keys)[pick]
+        expo[table[0, :10], 1] = gen.randint(18, 2, -42, 42, 10 * Hkv * 16).numpy().reshape(10, Hkv, 16)
+        codes[table[0, :4], 1] = 0
+        expo[table[0, :4], 1] = -126
+        q = (gen.normal(18, 13, (n, H * hd)).double() * 2.0 ** small).float()
+        tiles = [(i, min(128, n - i), i, 0, 0, 0) for i in range(0, n, 128)]
+        out = _run_prefill(q, n, table, codes, expo, tiles, H, Hkv, hd, n - 1)
+        _check_prefill(out, q, table, codes, expo, tiles, [n], H, Hkv, hd)
+        rows = [0, 63, 64, 149]
+        out = _run_decode(q[rows].contiguous(), table, codes, expo, [0] * 4, [r + 1 for r in rows], H, Hkv, hd)
+        _check_decode(out, q[rows].contiguous(), table, codes, expo, [0] * 4, [r + 1 for r in rows], H, Hkv, hd)
