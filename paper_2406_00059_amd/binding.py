@@ -650,16 +650,18 @@ def _refuse(what):
     raise LdError(LD_E_INVAL, what)
 
 
-def _on_device(call, t):
-    """Refuses a tensor that is not on the current device, where the call is launched."""
-    if _cuda_up() and t.get_device() != _current_device():
-        _refuse(f"{call}: tensors have to be on the current device ({_current_device()}), not on {t.device}")
+def _on_device(call, *tensors):
+    """Refuses tensors (or None) that are not on the current device, where the call is launched."""
+    if _cuda_up():
+        here = _current_device()
+        for t in tensors:
+            if t is not None and t.get_device() != here:
+                _refuse(f"{call}: tensors have to be on the current device ({here}), not on {t.device}")
 
 
 def _q8_layer(call, codes, expo, Hkv, hd):
     """Addresses of a layer's codes int8 [blocks, 2, Hkv, 16, hd] and exponents int8 [blocks, 2, Hkv, 16]."""
     n = expo.numel()
-    _on_device(call, codes)
     if Hkv < 1 or hd < 1 or codes.dtype is not _I8 or expo.dtype is not _I8 or codes.numel() != n * hd or n % (32 * Hkv) or not codes.is_contiguous() or \
             not expo.is_contiguous():
         _refuse(f"{call}: codes int8 [blocks, 2, {Hkv}, 16, {hd}] and expo int8 [blocks, 2, {Hkv}, 16], contiguous, not {codes.dtype} {tuple(codes.shape)} "
@@ -685,6 +687,7 @@ def _rows_of(call, t, what, stride, width, n=None):
 def ldk_rope_table_scaled(pos, rot, rope_base, cos_sin, factor=1.0, low=0.0, high=0.0, original=0, attention=1.0, stream=None):
     """pos int32 [T], cos_sin float32 [T, rot / 2, 2]; the other numbers as in ld_rope_scaling."""
     T = pos.numel()
+    _on_device("ldk_rope_table_scaled", pos, cos_sin)
     scaling = ld_rope_scaling(factor, low, high, original, attention)
     _check(lib().ldk_rope_table_scaled(_at("pos", pos, _I32, T), T, rot, rope_base, C.addressof(scaling), _at("cos_sin", cos_sin, _F32, T * max(rot, 0)),
                                        _stream(stream)))
@@ -703,9 +706,11 @@ def ldk_rope_kv_write_q8(qkv, cos_sin, pos, seq_slot, table, codes, expo, H, Hkv
     if not (rows == T and rest == 0 and stride and seq_slot.numel() == T and qkv.dtype is _F32 and q_out.dtype is _F32 and pos.dtype is _I32 and
             seq_slot.dtype is _I32 and table.dtype is _I32 and codes.dtype is _I8 and expo.dtype is _I8 and Hkv > 0 and ne % (32 * Hkv) == 0 and
             codes.numel() == ne * hd and qkv.is_contiguous() and q_out.is_contiguous() and pos.is_contiguous() and seq_slot.is_contiguous() and
-            table.is_contiguous() and codes.is_contiguous() and expo.is_contiguous()):
+            table.is_contiguous() and codes.is_contiguous() and expo.is_contiguous() and
+            (_current_device() if _cuda_up() else -1) == qkv.get_device() == pos.get_device() == seq_slot.get_device() == table.get_device() ==
+            codes.get_device() == expo.get_device() == q_out.get_device()):
         _append_fits(qkv, pos, seq_slot, table, codes, expo, Hkv, hd, q_out)
-    _on_device("ldk_rope_kv_write_q8", codes)
+    _on_device("ldk_rope_kv_write_q8", cos_sin, q_gain, k_gain)
     rc = (_lib or lib()).ldk_rope_kv_write_q8(
         qkv.data_ptr(), qs, q_gain if q_gain is None else _at("q_gain", q_gain, _F32, hd), k_gain if k_gain is None else _at("k_gain", k_gain, _F32, hd), eps,
         _at("cos_sin", cos_sin, _F32, T * rot), rot, 1 if interleaved else 0, pos.data_ptr(), seq_slot.data_ptr(), table.data_ptr(), stride, codes.data_ptr(),
@@ -717,6 +722,7 @@ def ldk_rope_kv_write_q8(qkv, cos_sin, pos, seq_slot, table, codes, expo, H, Hkv
 def _append_fits(qkv, pos, seq_slot, table, codes, expo, Hkv, hd, q_out):
     """Raises what ldk_rope_kv_write_q8's tensors lack."""
     call, T = "ldk_rope_kv_write_q8", pos.numel()
+    _on_device(call, qkv, pos, seq_slot, table, codes, expo, q_out)
     if qkv.dim() != 2 or qkv.shape[0] != T or (T and q_out.numel() % T):
         _refuse(f"{call}: qkv and q_out have a row for each of the {T} positions, not {tuple(qkv.shape)} and {tuple(q_out.shape)}")
     _q8_layer(call, codes, expo, Hkv, hd)
@@ -736,7 +742,10 @@ def _move(call, pool_layer, table, codes, expo, q8_table, ranges, Hkv, hd):
     if not ((kind is torch.bfloat16 or kind is _F32) and Hkv > 0 and hd > 0 and stride and q8_stride and three == 3 and table.dtype is _I32 and
             q8_table.dtype is _I32 and ranges.dtype is _I32 and codes.dtype is _I8 and expo.dtype is _I8 and ne % (32 * Hkv) == 0 and
             codes.numel() == ne * hd and pool_layer.numel() % (32 * Hkv * hd) == 0 and pool_layer.is_contiguous() and table.is_contiguous() and
-            q8_table.is_contiguous() and ranges.is_contiguous() and codes.is_contiguous() and expo.is_contiguous()):
+            q8_table.is_contiguous() and ranges.is_contiguous() and codes.is_contiguous() and expo.is_contiguous() and
+            (_current_device() if _cuda_up() else -1) == pool_layer.get_device() == table.get_device() == codes.get_device() == expo.get_device() ==
+            q8_table.get_device() == ranges.get_device()):
+        _on_device(call, pool_layer, table, codes, expo, q8_table, ranges)
         if Hkv < 1 or hd < 1 or pool_layer.dtype not in _W4_FLOATS or not pool_layer.is_contiguous() or pool_layer.numel() % (32 * Hkv * hd):
             _refuse(f"{call}: a pool is bf16 or float32 [blocks, 2, {Hkv}, 16, {hd}], contiguous, not {pool_layer.dtype} {tuple(pool_layer.shape)}")
         if ranges.dim() != 2 or ranges.shape[1] != 3:
@@ -745,7 +754,6 @@ def _move(call, pool_layer, table, codes, expo, q8_table, ranges, Hkv, hd):
             _q8_table(call, t)
         _q8_layer(call, codes, expo, Hkv, hd)
         _at("ranges", ranges, _I32, ranges.numel())
-    _on_device(call, codes)
     return ((pool_layer.data_ptr(), LD_F32 if kind is _F32 else LD_BF16, table.data_ptr(), stride),
             (codes.data_ptr(), expo.data_ptr(), q8_table.data_ptr(), q8_stride), (ranges.data_ptr(), n))
 
@@ -770,6 +778,7 @@ def ldk_paged_attention_q8(q, q_stride, codes, expo, table, seq_slot, ctx_len, m
     """q float32, rows q_stride elements apart; seq_slot, ctx_len, first int32 [T]; slopes float32 [H]; out float32 [T, H, hd]."""
     call = "ldk_paged_attention_q8"
     T = ctx_len.numel()
+    _on_device(call, q, codes, expo, table, seq_slot, ctx_len, out, first, slopes, scratch if isinstance(scratch, torch.Tensor) else None)
     c, e = _q8_layer(call, codes, expo, Hkv, hd)
     _check((_lib or lib()).ldk_paged_attention_q8(
         _rows_of(call, q, "q", q_stride, H * hd, T), q_stride, c, e, _q8_table(call, table), table.shape[1], _at("seq_slot", seq_slot, _I32, T),
@@ -788,6 +797,7 @@ def ldk_prefill_attention_q8(q, q_stride, codes, expo, table, tiles, H, Hkv, hd,
     call = "ldk_prefill_attention_q8"
     if tiles.dim() != 2 or tiles.shape[1] != 6:
         _refuse(f"{call}: tiles int32 [n, 6], not {tuple(tiles.shape)}")
+    _on_device(call, q, codes, expo, table, tiles, out, slopes, scratch if isinstance(scratch, torch.Tensor) else None)
     c, e = _q8_layer(call, codes, expo, Hkv, hd)
     if H < 1:
         _refuse(f"{call}: {H} heads")

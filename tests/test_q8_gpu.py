@@ -678,6 +678,32 @@ def test_recorded_steps_and_other_streams():
         assert (a - b).norm().item() <= 4e-6 * b.norm().item()      # two kernels, the same rows
 
 
+def test_one_tensor_in_host_memory_is_refused():
+    """Each tensor of each call in turn; a refused call launches nothing."""
+    H = Hkv = 2
+    hd = 64
+    z = lambda *s, dtype=torch.float32: torch.zeros(s, dtype=dtype, device=DEV)      # noqa: E731
+    codes, expo, table = z(1, 2, Hkv, 16, hd, dtype=torch.int8), z(1, 2, Hkv, 16, dtype=torch.int8), z(1, 1, dtype=torch.int32)
+    i1, gain, scratch = z(1, dtype=torch.int32), z(hd), z(1 << 20)
+    pool, ranges, tiles, q, out, slopes = z(1, 2, Hkv, 16, hd), z(1, 3, dtype=torch.int32), z(1, 6, dtype=torch.int32), z(1, H * hd), z(1, H, hd), z(H)
+    calls = [(ld.ldk_rope_table_scaled, (i1, hd, 1e4, z(1, hd // 2, 2)), {}),
+             (ld.ldk_rope_kv_write_q8, (z(1, 3 * H * hd), z(1, hd // 2, 2), i1, i1, table, codes, expo, H, Hkv, hd, q), dict(q_gain=gain, k_gain=gain)),
+             (ld.ldk_kv_to_q8, (pool, table, codes, expo, table, ranges, 1, Hkv, hd), {}),
+             (ld.ldk_kv_from_q8, (codes, expo, table, pool, table, ranges, 1, Hkv, hd), {}),
+             (ld.ldk_paged_attention_q8, (q, H * hd, codes, expo, table, i1, i1, 1, H, Hkv, hd, out, scratch), dict(first=i1, slopes=slopes)),
+             (ld.ldk_prefill_attention_q8, (q, H * hd, codes, expo, table, tiles, H, Hkv, hd, out, 0), dict(scratch=scratch, slopes=slopes))]
+    for call, args, more in calls:
+        call(*args, **more)
+        for i, t in enumerate(args):
+            if isinstance(t, torch.Tensor):
+                with pytest.raises(ld.LdError, match="device"):
+                    call(*args[:i], t.cpu(), *args[i + 1:], **more)
+        for name, t in more.items():
+            with pytest.raises(ld.LdError, match="device"):
+                call(*args, **{**more, name: t.cpu()})
+    torch.cuda.synchronize()
+
+
 def test_tensors_in_host_memory_are_refused():
     H = Hkv = 2
     hd = 64
