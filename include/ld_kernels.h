@@ -308,7 +308,7 @@ ld_status ldk_kv_from_q8(const int8_t *codes, const int8_t *expo, const int32_t 
 
 /* ldk_paged_attention over an 8-bit pool.  Row t, at position p = ctx_len[t] - 1, sees positions max(first[t], ctx_len[t] - window) .. p of its
  * sequence (first NULL: 0; window 0: no band); ctx_len[t] may be 0, and a row that sees nothing gives 0.
- *   s_j = q.k_j / sqrt(hd);  softcap > 0: s_j = softcap tanh(s_j / softcap);  slopes (DEVICE [H], may be NULL): s_j += slopes[h] (j - p);
+ *   s_j = q.k_j / sqrt(hd);  softcap > 0 (1e-30 at least): s_j = softcap tanh(s_j / softcap);  slopes (DEVICE [H], may be NULL): s_j += slopes[h] (j - p);
  *   out = sum_j softmax(s)_j v_j.
  * A query enters as a multiple of 1 / 8355711 of its largest entry, a weight times its value's 2^e with 22 bits, of which at most 2^-34 of the row's largest such product
  * gets lost besides; codes are exact, sums float32.  A query head with a NaN or an infinity gives NaN, as does a head that sees a key or value that stands for NaN.  max_ctx (HOST) >= every ctx_len.

@@ -59,7 +59,7 @@ struct Q8Attention {
 inline bool bad_attention(const Q8Attention &a, int hd) {
     return !a.q || !a.codes || !a.expo || (((uintptr_t)a.codes | (uintptr_t)a.expo) & 15) || !a.table || a.table_stride < 0 || a.H <= 0 || a.Hkv <= 0 ||
            a.H % a.Hkv || (hd != 64 && hd != 128) || (int64_t)a.q_stride < (int64_t)a.H * hd || a.window < 0 || !(a.softcap >= 0.f) ||
-           !std::isfinite(a.softcap) || !a.out;
+           !std::isfinite(a.softcap) || (a.softcap > 0.f && a.softcap < 1e-30f) || !a.out;      // 1 / cap, times a score of zero
 }
 
 // cap tanh(s / cap).  |s| below cap / 2: an odd polynomial of the ninth degree, its coefficients fitted so that the largest error there relative to tanh is as small

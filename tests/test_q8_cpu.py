@@ -88,6 +88,11 @@ def test_prefill_refuses(bad):
     assert _call("ldk_prefill_attention_q8", PREFILL, **bad) == ld.LD_E_INVAL and "ldk_prefill_attention_q8" in ld.ld_last_error()
 
 
+@pytest.mark.parametrize("name,args", [("ldk_paged_attention_q8", DECODE), ("ldk_prefill_attention_q8", PREFILL)])
+def test_attention_refuses_caps_next_to_zero(name, args):
+    assert _call(name, args, softcap=1e-39) == ld.LD_E_INVAL and _call(name, args, softcap=9e-31) == ld.LD_E_INVAL
+
+
 def test_attention_refuses_scratch_that_is_too_small():
     L = ld.lib()
     n = L.ldk_attention_q8_scratch_bytes(1, 8, 2, 64, 100000, 0)
