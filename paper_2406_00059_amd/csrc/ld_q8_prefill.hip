@@ -15,7 +15,7 @@
 // the registers that brought some of the staged keys into scratch memory (8191 rows below: 812 us).
 //
 // What bounds it: 64 positions and 32 rows are 56 matrix instructions (1800 cycles of a SIMD) and some 540 vector ones.  With two waves a SIMD, which is what
-// the registers allow, matrix instructions take 49 % and vector ones 69 % of the time.  8191 rows of 32 heads in a band of 4096 take 730 - 760 us, some 555 TFLOP/s
+// the registers allow, matrix instructions take 49 % and vector ones 69 % of the time.  8191 rows of 32 heads in a band of 4096 take 720 - 760 us, some 555 TFLOP/s
 // of the formula and 970 of executed products, at a clock that falls to 1.6 - 2.0 GHz meanwhile: vector instructions saved (sums that the matrix cores begin
 // at a number whose bits are a float's) and the two kinds of work ordered otherwise (scores of both halves first, wave priorities) no longer change it.
 // Measured and not kept, the first three with keys in scratch: scores in fp16 with queries in two terms (five vector instructions an entry less, a third more
