@@ -808,3 +808,33 @@ def test_keys_and_values_near_the_ends_of_their_range(hd, H, Hkv):
         rows = [0, 63, 64, 149]
         out = _run_decode(q[rows].contiguous(), table, codes, expo, [0] * 4, [r + 1 for r in rows], H, Hkv, hd)
         _check_decode(out, q[rows].contiguous(), table, codes, expo, [0] * 4, [r + 1 for r in rows], H, Hkv, hd)
+
+
+def test_appends_and_moves_to_blocks_past_two_and_four_gigabytes():
+    """Few and many rows, and a range moved: what lands in blocks whose bytes begin past 2^31 and 2^32 is what lands in a pool of four blocks."""
+    H = Hkv = 32
+    hd, n = 128, 60
+    each = 2 * Hkv * 16 * hd
+    total = (1 << 32) // each + 5
+    places = np.array([total - 1, (1 << 31) // each + 1, total - 3, 1], np.int32)
+    far = torch.empty((total, 2, Hkv, 16, hd), dtype=torch.int8, device=DEV), torch.empty((total, 2, Hkv, 16), dtype=torch.int8, device=DEV)
+    near = torch.zeros((4, 2, Hkv, 16, hd), dtype=torch.int8, device=DEV), torch.zeros((4, 2, Hkv, 16), dtype=torch.int8, device=DEV)
+    at = torch.as_tensor(places, device=DEV).long()
+    far_table, near_table = _i32(places[None]), _i32([[0, 1, 2, 3]])
+    cos_sin = torch.empty((n, hd // 2, 2), device=DEV)
+    ld.ldk_rope_table_scaled(_i32(np.arange(n)), hd, 1e4, cos_sin)
+    pool = gen.normal(19, 3, (4, 2, Hkv, 16, hd)).to(torch.bfloat16).to(DEV)
+    for pos in ([5, 59], list(range(n)), None):
+        for (codes, expo), table in ((far, far_table), (near, near_table)):
+            if pos is None:
+                ld.ldk_kv_to_q8(pool, near_table, codes, expo, table, _i32([[0, 1, n - 1]]), n, Hkv, hd)
+                continue
+            qkv = gen.normal(19, len(pos), (len(pos), 3 * H * hd)).to(DEV)
+            ld.ldk_rope_kv_write_q8(qkv, cos_sin[pos].contiguous(), _i32(pos), _i32([0] * len(pos)), table, codes, expo, H, Hkv, hd, torch.empty((len(pos), H * hd), device=DEV))
+        slots = [5, 59] if pos == [5, 59] else list(range(n))
+        for p in slots:
+            b, i = p // 16, p % 16
+            assert torch.equal(far[1][at[b], :, :, i], near[1][b, :, :, i])
+            assert torch.equal(far[0][at[b], 0, :, i], near[0][b, 0, :, i])
+            a, c = (x.view(Hkv, hd, 16)[:, :, i] for x in (far[0][at[b], 1], near[0][b, 1]))
+            assert torch.equal(a, c)
