@@ -18,9 +18,10 @@
 // the registers allow, matrix instructions take 49 % and vector ones 69 % of the time.  8191 rows of 32 heads in a band of 4096 take 720 - 760 us, some 555 TFLOP/s
 // of the formula and 970 of executed products, at a clock that falls to 1.6 - 2.0 GHz meanwhile: vector instructions saved (sums that the matrix cores begin
 // at a number whose bits are a float's) and the two kinds of work ordered otherwise (scores of both halves first, wave priorities) no longer change it.
-// Measured and not kept, the first three with keys in scratch: scores in fp16 with queries in two terms (five vector instructions an entry less, a third more
+// Measured and not kept, the first two with keys in scratch: scores in fp16 with queries in two terms (five vector instructions an entry less, a third more
 // matrix time, registers spilled: 1055 us); one wave a SIMD with the scores of the next tile formed ahead (1794); half tiles whose instructions are
-// interleaved by hand (826); two groups of four waves that take turns at matrix and vector instructions, a barrier between (913).
+// interleaved by hand (760; four capped observations 170 us against 115); two groups of four waves that take turns at matrix and vector instructions, a
+// barrier between (913).
 #include <algorithm>
 #include <cmath>
 #include <utility>
