@@ -181,6 +181,8 @@ __global__ __launch_bounds__(256, 2) void k_prefill_q8(Q8Attention a, const int3
     float add = NONE, l = 0.f;
     float big = 0.f;      // largest weight times its value's unit
 
+    auto exponent = [](float x) { return (int)(__float_as_uint(x) >> 23) - 127; };      // of x > 0
+
     auto multiply = [&](const Stage<HD> &st, int tile) {
         const int base = tile * TILE, mapped = __builtin_amdgcn_readfirstlane(st.mapped);
         float s[2][16];
@@ -285,8 +287,9 @@ __global__ __launch_bounds__(256, 2) void k_prefill_q8(Q8Attention a, const int3
         // the largest product leaves 2^9 .. 65504: scaled to 2^12 .. 2^13, what is there and what comes
         big = fmaxf(big, top);
         if (__any(big > 65504.f || (big > 0.f && big < 512.f))) {
-            // the exponent of the exponential's argument stays below 100
-            const int x = big > 0.f ? min(12 - ((int)(__float_as_uint(big) >> 23) - 127), (int)fminf(100.f - add - fmaxf(most_s, -1e4f), 126.f)) : 0;
+            // the sum of the row's weights, of this tile and of earlier ones, stays below 2^97: where the values that draw most are zero, nothing else holds
+            // the weights down
+            const int x = big > 0.f ? min(min(12 - exponent(big), 96 - exponent(max_halves(l + sum))), 126) : 0;
             const float up = ldexpf(1.f, x);
             add += (float)x;
             l *= up;

@@ -1,0 +1,90 @@
+"""Prompt attention over the 8-bit cache where a tile's positions are split into shares: chunks behind long sequences, at odd starts, under every mask,
+against the plain implementation in 64 bits of test_q8_gpu.py."""
+import numpy as np
+import pytest
+
+from workloads import gen
+from test_q8_gpu import _attend, _layer, _run_prefill, _sequence
+
+pytestmark = pytest.mark.gpu
+
+
+def _check_rows(out, q, table, codes, expo, tile, length, H, Hkv, hd, rows, window=0):
+    """These rows of one sequence's tile against float64; positions of blocks that the table does not map take no part."""
+    at, n, pos, s, first, prefix = tile
+    mapped = np.array([table[s, p // 16] >= 0 for p in range(length)])
+    whole = table.copy()
+    whole[s, whole[s] < 0] = 0      # for reading the values: these positions are dropped below
+    k, v = _sequence(whole, codes, expo, s, length)
+    got = out.double().cpu().numpy()
+    for r in rows:
+        p = pos + r
+        lo, hi = max(first, p - window + 1 if window else 0, 0), min(max(p, prefix - 1), length - 1)
+        use = np.arange(lo, hi + 1)[mapped[lo:hi + 1]] if lo <= hi else np.arange(0)
+        for h in range(H):
+            j = h // (H // Hkv)
+            ref, bound = _attend(q[at + r, h * hd:(h + 1) * hd].double().numpy(), k[use, j], v[use, j], 0, 0, len(use) - 1, 0.0, 0.0, least=9)
+            g = got[at + r, h]
+            assert np.array_equal(np.isnan(g), np.isnan(ref)), (r, h)
+            assert (np.abs(g - ref) <= bound)[~np.isnan(ref)].all(), (r, h, np.nanmax(np.abs(g - ref) / np.maximum(bound, 1e-300)))
+
+
+def _tiles(n, before):
+    return [(i, min(128, n - i), before + i, 0, 0, 0) for i in range(0, n, 128)]
+
+
+@pytest.mark.parametrize("hd,H,Hkv", [(128, 2, 2), (64, 4, 2)])
+@pytest.mark.parametrize("zeros", ["all", "ends of shares", "starts of shares", "all but one"])
+@pytest.mark.parametrize("n,before", [(257, 1263), (65, 1999), (128, 500)])
+def test_prefill_of_zero_values_over_shares(hd, H, Hkv, zeros, n, before):
+    """Values that are zero, as an append stores them (e = -126), over whole 64-position steps: rows whose wave goes on to steps that they do not see."""
+    length = before + n
+    table, codes, expo = _layer([length], Hkv, hd, n + hd)
+    where = np.arange(length)
+    none = {"all": where >= 0, "ends of shares": where >= before - 70, "starts of shares": where // 64 % 4 == 0, "all but one": where != 1150 % length}[zeros]
+    for p in where[none]:
+        codes[table[0, p // 16], 1, :, p % 16], expo[table[0, p // 16], 1, :, p % 16] = 0, -126
+    q = gen.normal(n, 13, (n, H * hd))
+    tiles = _tiles(n, before)
+    out = _run_prefill(q, n, table, codes, expo, tiles, H, Hkv, hd, length - 1)
+    assert out.isfinite().all()
+    if zeros == "all":
+        assert (out == 0).all()
+    for t in tiles:
+        _check_rows(out, q, table, codes, expo, t, length, H, Hkv, hd, range(0, t[1], 5))
+
+
+@pytest.mark.parametrize("hd,H,Hkv", [(128, 2, 2), (64, 4, 2)])
+@pytest.mark.parametrize("n,before", [(40, 201), (60, 1900)])
+def test_prefill_of_zero_values_before_unmapped_blocks(hd, H, Hkv, n, before):
+    """64 zeros, 64 positions that the table does not map, then other values."""
+    length = before + n
+    table, codes, expo = _layer([length], Hkv, hd, 3 * n)
+    for a in (range(0, length, 256) if before > 1000 else (0,)):
+        blocks = table[0, a // 16:a // 16 + 4]
+        codes[blocks, 1], expo[blocks, 1] = 0, -126
+        table[0, a // 16 + 4:a // 16 + 8] = -1
+    q = gen.normal(n, 13, (n, H * hd))
+    tile = _tiles(n, before)[0]
+    out = _run_prefill(q, n, table, codes, expo, [tile], H, Hkv, hd, length - 1)
+    _check_rows(out, q, table, codes, expo, tile, length, H, Hkv, hd, range(0, n, 3))
+
+
+@pytest.mark.parametrize("down", [8.0, 40.0, 60.0])
+@pytest.mark.parametrize("n,before", [(40, 201), (60, 1900)])
+def test_prefill_of_small_weights_beside_a_zero_value(down, n, before):
+    """The position that draws nearly everything has a zero value, the first 64 do: what is left are weights of 2^-down and less."""
+    H = Hkv = 2
+    hd, length = 128, before + n
+    table, codes, expo = _layer([length], Hkv, hd, 5 * n)
+    codes[table[0, :4], 1], expo[table[0, :4], 1] = 0, -126
+    q = gen.normal(n, 13, (n, H * hd), std=0.02)
+    q[:, ::hd] = 8.0
+    codes[:, 0, :, :, 0] = 0
+    b = table[0, 1]
+    codes[b, 0, :, 3], expo[b, 0, :, 3] = 0, 0
+    codes[b, 0, :, 3, 0] = round(down * np.log(2.0) * hd ** 0.5 / 8.0)
+    tile = _tiles(n, before)[0]
+    out = _run_prefill(q, n, table, codes, expo, [tile], H, Hkv, hd, length - 1)
+    assert (out != 0).any()
+    _check_rows(out, q, table, codes, expo, tile, length, H, Hkv, hd, range(0, n, 3))
