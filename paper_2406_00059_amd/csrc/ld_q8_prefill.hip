@@ -65,8 +65,9 @@ struct TileRows { int row, n, pos, seq, first, prefix; };
 __device__ __forceinline__ int seen_from(const TileRows &t, int r, int window) { return max(max(t.first, window > 0 ? t.pos + r - window + 1 : 0), 0); }
 __device__ __forceinline__ int seen_to(const TileRows &t, int r, int most) { return min(max(t.pos + r, t.prefix - 1), most); }
 
+// Heads of 64 without caps and slopes fit three waves a SIMD (4096 rows of 32 heads over 8: 183 us, 192 with two).
 template <int HD, bool EXTRA>
-__global__ __launch_bounds__(256, 2) void k_prefill_q8(Q8Attention a, const int32_t *__restrict__ tiles, int n_tiles, int max_pos, int splits,
+__global__ __launch_bounds__(256, HD == 64 && !EXTRA ? 3 : 2) void k_prefill_q8(Q8Attention a, const int32_t *__restrict__ tiles, int n_tiles, int max_pos, int splits,
                                                        float *__restrict__ part_o, float2 *__restrict__ part_ml) {
     constexpr int KS = HD / 32, ND = HD / 32, NP = HD / 64;
     // the last tiles first (they see the most); KV heads next to each other, so that one cache's L2 serves one of them where there are eight
@@ -94,6 +95,7 @@ __global__ __launch_bounds__(256, 2) void k_prefill_q8(Q8Attention a, const int3
     const int all_lo = seen_from(tr, nlast, a.window), all_hi = seen_to(tr, 32 * wave, most);        // every row
 
     __shared__ __attribute__((aligned(16))) Stage<HD> stage[2];
+    __shared__ float froms[256];
     const int32_t *trow = a.table + (int64_t)tr.seq * a.table_stride;
     const int last = whi >> 4;
     const int64_t bs = q8_block(a.Hkv, HD);
@@ -176,9 +178,13 @@ __global__ __launch_bounds__(256, 2) void k_prefill_q8(Q8Attention a, const int3
     for (int n = 0; n < ND; n++)
 #pragma unroll
         for (int i = 0; i < 16; i++) o[n][i] = 0.f;
-    // weights are 2^(score + add), score in the log2 domain; l: their sum over this lane's positions
-    constexpr float NONE = 1e30f;      // of a row that has seen no score yet
+    // weights are 2^((s - from) rs + add), s rs a score in the log2 domain; l: their sum over this lane's positions.  from is 0, or a score that is so large that
+    // add could not hold it: a product s rs is off by up to 2^-25 of itself from what a multiple of it in add was rounded to, which must not reach an exponent.
+    // It seldom is, and has no register: large has a bit for the lanes whose from is in froms.
+    constexpr float NONE = 3e38f;         // add of a row that has seen no score yet
+    constexpr float LARGE = 32768.f;      // of a score
     float add = NONE, l = 0.f;
+    uint64_t large = 0;
     float big = 0.f;      // largest weight times its value's unit
 
     auto exponent = [](float x) { return (int)(__float_as_uint(x) >> 23) - 127; };      // of x > 0
@@ -228,11 +234,11 @@ __global__ __launch_bounds__(256, 2) void k_prefill_q8(Q8Attention a, const int3
                 }
             }
             if (a.slopes) {
-                const float from = (float)(base + 16 * hh - (tr.pos + rr));
+                const float at = (float)(base + 16 * hh - (tr.pos + rr));
 #pragma unroll
                 for (int u = 0; u < 2; u++)
 #pragma unroll
-                    for (int i = 0; i < 16; i++) s[u][i] = fmaf(slope, from + (float)(32 * u + i), s[u][i]);
+                    for (int i = 0; i < 16; i++) s[u][i] = fmaf(slope, at + (float)(32 * u + i), s[u][i]);
             }
         }
         const bool whole = base >= all_lo && base + TILE - 1 <= all_hi && mapped == 15;
@@ -255,11 +261,14 @@ __global__ __launch_bounds__(256, 2) void k_prefill_q8(Q8Attention a, const int3
         for (int u = 0; u < 2; u++)
 #pragma unroll
             for (int i = 0; i < 16; i++) most_s = fmaxf(most_s, s[u][i]);
-        most_s = max_halves(most_s) * rs;
+        most_s = max_halves(most_s);
+        float from = 0.f;
+        if (large) from = large >> lane & 1 ? froms[tid] : 0.f;
         // the first score makes the largest weight 2^12; one that would be above 2^30 does so too
-        if (__any(most_s + add > 30.f)) {
-            const float an = most_s + add > 30.f ? 12.f - most_s : add;
-            const float keep = add == NONE ? 0.f : fast_exp2(an - add);
+        const bool lower = fmaf(most_s - from, rs, add) > 30.f;
+        if (__any(lower)) {
+            const float fn = !lower ? from : fabsf(most_s * rs) >= LARGE ? most_s : 0.f, an = lower ? 12.f - (most_s - fn) * rs : add;
+            const float keep = add == NONE ? 0.f : fast_exp2(fmaf(from - fn, rs, an - add));
             add = an;
             l *= keep;
             big *= keep;
@@ -267,6 +276,15 @@ __global__ __launch_bounds__(256, 2) void k_prefill_q8(Q8Attention a, const int3
             for (int n = 0; n < ND; n++)
 #pragma unroll
                 for (int i = 0; i < 16; i++) o[n][i] *= keep;
+            large = __ballot(fn != 0.f);
+            if (large) froms[tid] = fn;
+            from = fn;
+        }
+        if (large) {
+#pragma unroll
+            for (int u = 0; u < 2; u++)
+#pragma unroll
+                for (int i = 0; i < 16; i++) s[u][i] -= from;
         }
         float sum = 0.f, top = 0.f;
 #pragma unroll
@@ -378,7 +396,7 @@ __global__ __launch_bounds__(256, 2) void k_prefill_q8(Q8Attention a, const int3
             for (int i = 0; i < 4; i++) y[i] = ldexpf(o[n][4 * b + i] * inv, e0);
             *reinterpret_cast<float4_u *>(dst + 32 * n + 8 * b + 4 * hh) = y;
         }
-    if (splits > 1 && hh == 0) part_ml[item] = make_float2(l == 0.f ? -INFINITY : -add, l);
+    if (splits > 1 && hh == 0) part_ml[item] = make_float2(l == 0.f ? -INFINITY : large >> lane & 1 ? fmaf(froms[tid], rs, -add) : -add, l);
 }
 
 // Joins the shares of a row and head, in their order: HD / 4 lanes a row, four shares' loads in flight (5.7 us for the 96 pairs
