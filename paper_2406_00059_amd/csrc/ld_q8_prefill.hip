@@ -142,6 +142,7 @@ __global__ __launch_bounds__(256, HD == 64 && !EXTRA ? 3 : 2) void k_prefill_q8(
     // ---- queries: dims 32 s + 16 hh .. + 16 of this lane's row
     i32x4_t qd[3][KS];
     float unit;
+    uint64_t broken;      // lanes whose query is not finite: theirs is taken as zero until the end, where a row that has seen anything becomes NaN
     {
         const float *qp = a.q + (int64_t)(tr.row + rr) * a.q_stride + h * HD + 16 * hh;
         float v[KS][16];
@@ -155,7 +156,8 @@ __global__ __launch_bounds__(256, HD == 64 && !EXTRA ? 3 : 2) void k_prefill_q8(
             }
         top = max(top, (uint32_t)__shfl_xor((int)top, 32, WAVE));
         const Q8Query query = q8_query(top, (EXTRA ? 1.0 : 1.4426950408889634) / sqrt((double)HD));
-        unit = ldexpf(query.unit, query.exp + KEY_SHIFT);
+        broken = __ballot(top >= 0x7f800000u);
+        unit = top >= 0x7f800000u ? 1.f : ldexpf(query.unit, query.exp + KEY_SHIFT);
         unit = unit < 0x1p-126f ? 0x1p-126f : unit;      // not zero: it multiplies -infinity
 #pragma unroll
         for (int s = 0; s < KS; s++)
@@ -323,7 +325,7 @@ __global__ __launch_bounds__(256, HD == 64 && !EXTRA ? 3 : 2) void k_prefill_q8(
                 for (int i = 0; i < 16; i++) s[u][i] *= up;
         }
         l += sum;
-        #pragma unroll
+#pragma unroll
         for (int u = 0; u < 2; u++) {
             f16x8_t wh[2], wl[2];
 #pragma unroll
@@ -346,7 +348,7 @@ __global__ __launch_bounds__(256, HD == 64 && !EXTRA ? 3 : 2) void k_prefill_q8(
 #pragma unroll
                 for (int n = 0; n < ND; n++) o[n] = __builtin_amdgcn_mfma_f32_32x32x16_f16(vf[n], wl[q], o[n], 0, 0, 0);
             }
-                    }
+        }
     };
 
     if (t0 < t1) {
@@ -384,6 +386,7 @@ __global__ __launch_bounds__(256, HD == 64 && !EXTRA ? 3 : 2) void k_prefill_q8(
 
     l += __shfl_xor(l, 32, WAVE);
     if (!real) return;
+    if (l > 0.f && (broken >> lane & 1)) l = __uint_as_float(0x7fc00000u);
     const float inv = l == 0.f ? 0.f : 1.f / l;
     const int64_t item = splits == 1 ? (int64_t)(tr.row + r) * a.H + h : (((int64_t)tile_no * a.H + h) * splits + sp) * ROWS + r;
     float *dst = (splits == 1 ? a.out : part_o) + item * HD;

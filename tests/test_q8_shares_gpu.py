@@ -4,7 +4,7 @@ import numpy as np
 import pytest
 
 from workloads import gen
-from test_q8_gpu import _attend, _layer, _run_prefill, _sequence
+from test_q8_gpu import _attend, _layer, _run_prefill, _sequence, _slopes
 
 pytestmark = pytest.mark.gpu
 
@@ -88,3 +88,24 @@ def test_prefill_of_small_weights_beside_a_zero_value(down, n, before):
     out = _run_prefill(q, n, table, codes, expo, [tile], H, Hkv, hd, length - 1)
     assert (out != 0).any()
     _check_rows(out, q, table, codes, expo, tile, length, H, Hkv, hd, range(0, n, 3))
+
+
+@pytest.mark.parametrize("hd,H,Hkv", [(128, 2, 2), (64, 4, 2)])
+@pytest.mark.parametrize("n,before", [(100, 30), (100, 1500)])
+@pytest.mark.parametrize("cap,bias", [(0.0, False), (20.0, False), (0.0, True)])
+def test_prefill_of_queries_that_are_not_finite(hd, H, Hkv, n, before, cap, bias):
+    """A head that is not finite gives NaN where its row sees anything, and 0 where it does not: before its document, or in unmapped blocks alone."""
+    length = before + n
+    table, codes, expo = _layer([length, length], Hkv, hd, n + before)
+    table[1, :(before + 60) // 16 + 1] = -1
+    q = gen.normal(n, 13, (2 * n, H * hd))
+    for r in (0, 5, 31, 40, 90):
+        q[r, 3], q[n + r, hd + 1] = float("nan"), float("inf")
+    tiles = [(0, n, before, 0, before + 35, 0), (n, n, before, 1, 0, 0)]
+    out = _run_prefill(q, 2 * n, table, codes, expo, tiles, H, Hkv, hd, length - 1, cap=cap, slopes=_slopes(H) if bias else None).cpu()
+    for r in range(n):
+        for head in range(H):
+            for s, sees in ((0, r >= 35), (1, before + r > (before + 60) // 16 * 16 + 15)):
+                got, nan = out[s * n + r, head], r in (0, 5, 31, 40, 90) and head == s
+                assert got.isnan().all() if nan and sees else got.isfinite().all(), (r, head, s)
+                assert sees or (got == 0).all(), (r, head, s)
