@@ -153,25 +153,26 @@ __global__ __launch_bounds__(64 * WAVES, 2) void k_decode_q8(Q8Attention a, cons
         }
         return kexp == Q8_NAN ? __uint_as_float(0x7fc00000u) : x;
     };
-    // Brings m to the largest score and k to (at least) the largest exponent of what a column adds up, in the new reference; mb, top: the largest
-    // score and p 2^e of a lane's own positions
-    float ref = 0.f;
-    auto rescale = [&](float mb, float top) __attribute__((always_inline)) {
-        if constexpr (GP == 1) {
-            mb = max_of16(mb);
-            top = max_of16(top);
-        }
+    // Brings m to the largest score, mb being that of a lane's own positions, then k to (at least) the largest exponent of what a column adds up, top that of
+    // p 2^e over a lane's own positions.  The latter is formed from differences to m: beside a score of 2^25 an exponent is lost to rounding.
+    float ref = 0.f, keep = 1.f;
+    int fall = 0;
+    auto raise = [&](float mb) __attribute__((always_inline)) {
+        if constexpr (GP == 1) mb = max_of16(mb);
         mb = max_halves(max_quarters(mb));
-        top = max_halves(max_quarters(top));
         const float mn = fmaxf(m, mb);
         ref = mn > -INFINITY ? mn : 0.f;
-        const float keep = fast_exp2(m - ref), lift = m > -INFINITY ? ref - m : 0.f;
-        const int fall = (int)ceilf(fminf(lift, 100000.f));
-        const int kt = top > -INFINITY ? (int)ceilf(fminf(fmaxf(top - ref, -90000.f), 90000.f)) : -100000;
+        keep = fast_exp2(m - ref);
+        fall = (int)ceilf(fminf(m > -INFINITY ? ref - m : 0.f, 100000.f));
+        m = mn;
+    };
+    auto rescale = [&](float top) __attribute__((always_inline)) {
+        if constexpr (GP == 1) top = max_of16(top);
+        top = max_halves(max_quarters(top));
+        const int kt = top > -INFINITY ? (int)ceilf(fminf(fmaxf(top, -90000.f), 90000.f)) : -100000;
         const int kn = max(max(k - fall, kt), -100000);
         const float scale = ldexpf(keep, max(min(k - kn, 300), -300));
         l *= keep;
-        m = mn;
         k = kn;
         if (__any(scale != 1.f)) {
 #pragma unroll
@@ -218,8 +219,10 @@ __global__ __launch_bounds__(64 * WAVES, 2) void k_decode_q8(Q8Attention a, cons
             const bool ok = mapped && pos >= see.lo && pos <= see.hi;
             x = ok ? x : -INFINITY;
             const int e = ok ? evn : -1000;
-            rescale(x, x + (float)e);
-            const float p = fast_exp2(x - ref);
+            raise(x);
+            x -= ref;
+            rescale(x + (float)e);
+            const float p = fast_exp2(x);
             l += p;
             float w = ldexpf(p, e - k + 14);
             w = e == Q8_NAN ? __uint_as_float(0x7fc00000u) : w;
@@ -252,17 +255,20 @@ __global__ __launch_bounds__(64 * WAVES, 2) void k_decode_q8(Q8Attention a, cons
             }
             float mb = -INFINITY, top = -INFINITY;
 #pragma unroll
+            for (int i = 0; i < 16; i++) mb = fmaxf(mb, s[i]);
+            raise(mb);
+#pragma unroll
             for (int i = 0; i < 16; i++) {
-                mb = fmaxf(mb, s[i]);
+                s[i] -= ref;
                 top = fmaxf(top, s[i] + (float)e[i]);
             }
-            rescale(mb, top);
+            rescale(top);
 #pragma unroll
             for (int i = 0; i < 16; i += 2) {
                 float w[2];
 #pragma unroll
                 for (int u = 0; u < 2; u++) {
-                    const float p = fast_exp2(s[i + u] - ref);
+                    const float p = fast_exp2(s[i + u]);
                     l += p;
                     w[u] = ldexpf(p, e[i + u] - k + 14);
                     w[u] = e[i + u] == Q8_NAN ? __uint_as_float(0x7fc00000u) : w[u];

@@ -3,7 +3,7 @@ import numpy as np
 import pytest
 
 from workloads import gen
-from test_q8_gpu import _check_prefill, _layer, _run_prefill, _sequence, _slopes
+from test_q8_gpu import _check_decode, _check_prefill, _layer, _run_decode, _run_prefill, _sequence, _slopes
 
 pytestmark = pytest.mark.gpu
 
@@ -75,3 +75,53 @@ def test_prefill_of_scores_of_any_size(hd, H, Hkv, n, before, bias):
     kw = dict(slopes=_slopes(H) if bias else None)
     out = _run_prefill(q, n, table, codes, expo, tiles, H, Hkv, hd, length - 1, **kw)
     _check_prefill(out, q, table, codes, expo, tiles, [length], H, Hkv, hd, some=2, **kw)
+
+
+@pytest.mark.parametrize("hd,H,Hkv", [(128, 2, 2), (128, 2, 1), (64, 4, 1), (128, 8, 1), (64, 16, 1)])
+@pytest.mark.parametrize("order,sign", [("up", 1), ("down", 1), ("mixed", 1), ("mixed", -1)])
+@pytest.mark.parametrize("size", [12, 20, 25, 27, 33, 60, 75])
+@pytest.mark.parametrize("bias", [False, True])
+def test_decode_of_large_scores(hd, H, Hkv, order, sign, size, bias):
+    n = 1900
+    ctx = [n, n - 1, 700, 64, 63, 17, 2, 1]
+    table, codes, expo = _one_winner(n, order, sign, Hkv, hd, size + H)
+    q = np.zeros((len(ctx), H, hd), np.float32)
+    q[:, :, 0] = 2.0 ** (size - 6) * hd ** 0.5
+    slopes = np.minimum(_slopes(H), 2.0 ** (size - 14)) if bias else None
+    out = _run_decode(gen.normal(1, 1, (1,)).new_tensor(q.reshape(len(ctx), -1)), table, codes, expo, [0] * len(ctx), ctx, H, Hkv, hd, slopes=slopes)
+    got = out.double().cpu().numpy()
+    k, v = _sequence(table, codes, expo, 0, n)
+    for r, end in enumerate(ctx):
+        for h in range(H):
+            j = h // (H // Hkv)
+            ref, bound = _sharp(k[:end, j, 0], v[:end, j], float(q[r, h, 0]), end - 1, float(np.float32(slopes[h])) if bias else 0.0)
+            assert (np.abs(got[r, h] - ref) <= bound).all(), (r, h, np.nanmax(np.abs(got[r, h] - ref) / np.maximum(bound, 1e-300)))
+
+
+@pytest.mark.parametrize("H,Hkv", [(2, 2), (4, 1)])
+@pytest.mark.parametrize("value", [-126, -40, -12, -6, -5, 0, 50])
+def test_decode_of_values_of_one_unit_under_large_scores(H, Hkv, value):
+    """A score of 7e7 beside smaller ones, under values of each of these units."""
+    hd, n = 64, 300
+    table, codes, expo = _layer([n], Hkv, hd, 4)
+    expo[table[0, :19], 1] = value
+    codes[table[0, :19], 0], expo[table[0, :19], 0] = 0, 0
+    codes[table[0, 11], 0, :, 3, 0] = 70
+    codes[table[0, 4], 0, :, 9, 0] = 69
+    q = np.zeros((1, H, hd), np.float32)
+    q[:, :, 0] = 8e6
+    out = _run_decode(gen.normal(1, 1, (1,)).new_tensor(q.reshape(1, -1)), table, codes, expo, [0], [n], H, Hkv, hd).double().cpu().numpy()
+    v = _sequence(table, codes, expo, 0, n)[1][11 * 16 + 3]
+    assert (np.abs(out[0] - np.repeat(v, H // Hkv, 0)) <= 2.0 ** -20 * np.abs(np.repeat(v, H // Hkv, 0))).all()
+
+
+@pytest.mark.parametrize("hd,H,Hkv", [(128, 2, 2), (64, 4, 1), (128, 16, 1)])
+@pytest.mark.parametrize("bias", [False, True])
+def test_decode_of_scores_of_any_size(hd, H, Hkv, bias):
+    """Rows whose scores span 2^-4 .. 2^17, side by side."""
+    ctx = [1300] * 10 + [200] * 9
+    table, codes, expo = _layer([1300], Hkv, hd, hd)
+    q = gen.normal(hd, 13, (len(ctx), H * hd)) * (2.0 ** (gen.randint(hd, 14, -5, 13, len(ctx)).double()))[:, None].float()
+    kw = dict(slopes=_slopes(H) if bias else None)
+    out = _run_decode(q, table, codes, expo, [0] * len(ctx), ctx, H, Hkv, hd, **kw)
+    _check_decode(out, q, table, codes, expo, [0] * len(ctx), ctx, H, Hkv, hd, **kw)
