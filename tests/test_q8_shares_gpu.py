@@ -4,7 +4,7 @@ import numpy as np
 import pytest
 
 from workloads import gen
-from test_q8_gpu import _attend, _layer, _run_prefill, _sequence, _slopes
+from test_q8_gpu import _attend, _check_prefill, _layer, _run_prefill, _sequence, _slopes
 
 pytestmark = pytest.mark.gpu
 
@@ -109,3 +109,76 @@ def test_prefill_of_queries_that_are_not_finite(hd, H, Hkv, n, before, cap, bias
                 got, nan = out[s * n + r, head], r in (0, 5, 31, 40, 90) and head == s
                 assert got.isnan().all() if nan and sees else got.isfinite().all(), (r, head, s)
                 assert sees or (got == 0).all(), (r, head, s)
+
+
+@pytest.mark.parametrize("hd,H,Hkv", [(128, 2, 2), (64, 4, 1)])
+@pytest.mark.parametrize("window,cap,bias", [(0, 0.0, False), (1, 0.0, False), (40, 10.0, False), (0, 30.0, True), (1500, 0.0, True), (900, 5.0, False)])
+def test_prefill_segments_over_shares(hd, H, Hkv, window, cap, bias):
+    """Chunks behind some 2000 positions that begin and end anywhere, documents that begin in every share, prefixes that reach past the chunk."""
+    # (rows, positions before, first visible, prefix) of each sequence
+    segs = [(1, 2000, 0, 0), (130, 1987, 0, 0), (33, 2101, 1100, 0), (64, 2037, 2050, 0), (17, 2300, 2310, 0), (100, 1963, 0, 2120), (5, 2015, 2017, 2019),
+            (31, 129, 0, 1700), (90, 1791, 700, 1850), (40, 0, 0, 0)]
+    lengths = [max(b + n, x) for n, b, _, x in segs]
+    table, codes, expo = _layer(lengths, Hkv, hd, hd + H + window)
+    tiles, at = [], 1
+    for s, (n, before, first, prefix) in enumerate(segs):
+        for i in range(0, n, 128):
+            tiles.append((at + i, min(128, n - i), before + i, s, first, prefix))
+        at += n + s % 3
+    q = gen.normal(window + H, 13, (at + 2, H * hd))
+    kw = dict(window=window, cap=cap, slopes=_slopes(H) if bias else None)
+    out = _run_prefill(q, at + 2, table, codes, expo, tiles, H, Hkv, hd, max(lengths) - 1, **kw)
+    _check_prefill(out, q, table, codes, expo, tiles, lengths, H, Hkv, hd, some=5, **kw)
+    named = np.zeros(at + 2, bool)
+    for t in tiles:
+        named[t[0]:t[0] + t[1]] = True
+    assert (out.cpu().numpy()[~named] == 9.0).all()
+
+
+@pytest.mark.parametrize("window", [0, 700])
+def test_prefill_keeps_what_is_not_finite_where_it_is_over_shares(window):
+    H, Hkv, hd, n, before = 4, 2, 128, 70, 1801
+    length = before + n
+    table, codes, expo = _layer([length, length], Hkv, hd, 9)
+    expo[table[0, 113], 0, 1, 7] = -128      # the key of KV head 1 at position 1815
+    expo[table[1, 70], 1, 0, 2] = -128       # the value of KV head 0 at position 1122: in the band of some rows
+    q = gen.normal(9, 13, (2 * n, H * hd))
+    q[10, 3] = float("nan")
+    q[20, 2 * hd + 5] = float("inf")
+    tiles = [(s * n, n, before, s, 0, 0) for s in range(2)]
+    out = _run_prefill(q, 2 * n, table, codes, expo, tiles, H, Hkv, hd, length - 1, window=window)
+    _check_prefill(out, q, table, codes, expo, tiles, [length, length], H, Hkv, hd, window=window, some=2)
+
+
+@pytest.mark.parametrize("hd,H,Hkv", [(128, 2, 2), (64, 4, 2)])
+def test_prefill_of_unmapped_blocks_over_shares(hd, H, Hkv):
+    """Blocks that the table does not map: a whole share's, a step's, single ones, and those at the chunk's own positions."""
+    n, before = 100, 1501
+    table, codes, expo = _layer([before + n], Hkv, hd, 21)
+    table[0, [*range(16, 33), *range(40, 44), 50, 61, 62, 95]] = -1
+    q = gen.normal(21, 13, (n, H * hd))
+    tile = (0, n, before, 0, 0, 0)
+    out = _run_prefill(q, n, table, codes, expo, [tile], H, Hkv, hd, before + n - 1)
+    _check_rows(out, q, table, codes, expo, tile, before + n, H, Hkv, hd, range(0, n, 4))
+
+
+@pytest.mark.parametrize("hd,H,Hkv", [(128, 2, 2), (64, 4, 1)])
+@pytest.mark.parametrize("zeros", [False, True])
+def test_keys_and_values_near_the_ends_of_their_range_over_shares(hd, H, Hkv, zeros):
+    """Keys up to 2^120 under queries of 2^-115, and keys of 2^-120 and 2^-104 under queries of 2^108; values over 2^84, zeros first in every share."""
+    n, before = 70, 1777
+    length = before + n
+    nb = -(-length // 16)
+    for keys, small in (((113, 100, 90), -115), ((-126, -124, -110), 108)):
+        table, codes, expo = _layer([length], Hkv, hd, 18)
+        pick = gen.randint(18, 1, 0, len(keys) - 1, nb * Hkv * 16).numpy().reshape(nb, Hkv, 16)
+        expo[table[0, :nb], 0] = np.array(keys)[pick]
+        expo[table[0, :nb], 1] = gen.randint(18, 2, -42, 42, nb * Hkv * 16).numpy().reshape(nb, Hkv, 16)
+        if zeros:
+            for a in range(0, nb, 16):
+                codes[table[0, a:a + 4], 1] = 0
+                expo[table[0, a:a + 4], 1] = -126
+        q = (gen.normal(18, 13, (n, H * hd)).double() * 2.0 ** small).float()
+        tiles = [(0, n, before, 0, 0, 0)]
+        out = _run_prefill(q, n, table, codes, expo, tiles, H, Hkv, hd, length - 1)
+        _check_prefill(out, q, table, codes, expo, tiles, [length], H, Hkv, hd, some=3)
