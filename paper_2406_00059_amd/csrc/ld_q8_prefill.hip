@@ -399,7 +399,11 @@ __global__ __launch_bounds__(256, HD == 64 && !EXTRA ? 3 : 2) void k_prefill_q8(
             for (int i = 0; i < 4; i++) y[i] = ldexpf(o[n][4 * b + i] * inv, e0);
             *reinterpret_cast<float4_u *>(dst + 32 * n + 8 * b + 4 * hh) = y;
         }
-    if (splits > 1 && hh == 0) part_ml[item] = make_float2(l == 0.f ? -INFINITY : large >> lane & 1 ? fmaf(froms[tid], rs, -add) : -add, l);
+    if (splits > 1 && hh == 0) {
+        // beside a large score add would be lost: it is a whole number there, and goes into the sum
+        const bool far = large >> lane & 1;
+        part_ml[item] = l == 0.f ? make_float2(-INFINITY, 0.f) : far ? make_float2(froms[tid] * rs, ldexpf(l, -(int)add)) : make_float2(-add, l);
+    }
 }
 
 // Joins the shares of a row and head, in their order: HD / 4 lanes a row, four shares' loads in flight (5.7 us for the 96 pairs

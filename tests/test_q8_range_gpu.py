@@ -125,3 +125,31 @@ def test_decode_of_scores_of_any_size(hd, H, Hkv, bias):
     kw = dict(slopes=_slopes(H) if bias else None)
     out = _run_decode(q, table, codes, expo, [0] * len(ctx), ctx, H, Hkv, hd, **kw)
     _check_decode(out, q, table, codes, expo, [0] * len(ctx), ctx, H, Hkv, hd, **kw)
+
+
+@pytest.mark.parametrize("hd,H,Hkv", [(128, 2, 2), (64, 4, 1)])
+@pytest.mark.parametrize("size", [3, 20, 26, 33, 60, 100])
+@pytest.mark.parametrize("zeros", ["none", "first half", "every other step", "all but a few"])
+def test_prefill_of_large_scores_that_are_all_alike(hd, H, Hkv, size, zeros):
+    """Equal scores in every share, and values that are zero in some: the mean of the values."""
+    n, before = 37, 1830
+    length = before + n
+    table, codes, expo = _layer([length], Hkv, hd, 31)
+    blocks = table[0, :-(-length // 16)]
+    codes[blocks, 0], expo[blocks, 0] = 0, 0
+    codes[blocks, 0, :, :, 0] = 64
+    at = np.arange(length)
+    none = {"none": at < 0, "first half": at < 1000, "every other step": at // 64 % 2 == 0, "all but a few": at % 500 != 450}[zeros]
+    for p in at[none]:
+        codes[table[0, p // 16], 1, :, p % 16], expo[table[0, p // 16], 1, :, p % 16] = 0, -126
+    q = np.zeros((n, H, hd), np.float32)
+    q[:, :, 0] = 2.0 ** (size - 6) * hd ** 0.5
+    out = _run_prefill(gen.normal(1, 1, (1,)).new_tensor(q.reshape(n, -1)), n, table, codes, expo, [(0, n, before, 0, 0, 0)], H, Hkv, hd, length - 1)
+    got = out.double().cpu().numpy()
+    v = _sequence(table, codes, expo, 0, length)[1]
+    for r in range(0, n, 6):
+        seen = v[:before + r + 1].repeat(H // Hkv, 1)
+        # weights that are the same bits but between shares, whose two largest scores are rounded (2^-24 each where they are not large): sums of 2^11 numbers
+        # one after another, 2^-13 at most of the mean magnitude, and as much as one share's weight may be off
+        off = 2.0 ** -13 * np.abs(seen).mean(0)
+        assert (np.abs(got[r] - seen.mean(0)) <= off).all(), (r, np.abs(got[r] - seen.mean(0)).max())
