@@ -325,18 +325,20 @@ __global__ __launch_bounds__(64 * WAVES, 2) void k_decode_q8(Q8Attention a, cons
     __syncthreads();
     for (int idx = threadIdx.x; idx < heads * HD; idx += 64 * WAVES) {
         const int hh = idx / HD, d = idx % HD;
-        float M = -INFINITY, L = 0.f, acc = 0.f;
+        float M = -INFINITY, L = 0.f, r = 0.f, f[WAVES];
 #pragma unroll
         for (int w = 0; w < WAVES; w++) M = fmaxf(M, sml[w][hh].x);
         const float ref = M > -INFINITY ? M : 0.f;
 #pragma unroll
         for (int w = 0; w < WAVES; w++) {
             const float2 ml = sml[w][hh];
-            const float f = fast_exp2(ml.x - ref) * ml.y;
-            L += ml.y == 0.f ? 0.f : f;
-            acc += ml.y == 0.f ? 0.f : f * so[w][hh][d];
+            f[w] = ml.y == 0.f ? 0.f : fast_exp2(ml.x - ref) * ml.y;
+            L += f[w];
         }
-        const float r = L == 0.f ? 0.f : acc / L;
+        // shares of one: the sum stays within the values, up to the ends of float32
+        const float inv = L == 0.f ? 0.f : 1.f / L;
+#pragma unroll
+        for (int w = 0; w < WAVES; w++) r = fmaf(f[w] * inv, so[w][hh][d], r);
         const int64_t at = (int64_t)t * a.H + h0 + hh;
         if (chunks == 1) {
             a.out[at * HD + d] = r;
@@ -366,13 +368,15 @@ __global__ __launch_bounds__(256) void k_join_q8(Q8Attention a, const int32_t *_
 #pragma unroll
     for (int off = 32; off > 0; off >>= 1) M = fmaxf(M, __shfl_xor(M, off, WAVE));
     const float ref = M > -INFINITY ? M : 0.f;
+    // a position weighs at most one, and there are at most max_ctx: all weights together at most 1, so that the sum stays within the values up to the ends of float32
+    const float scale = ldexpf(1.f, -(32 - __clz(max_ctx)));
     float L = 0.f;
     float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll 4
     for (int i = gr; i < n; i += GROUPS) {
         const float2 w = ml[i];
         const float4 o = po[(int64_t)i * PER];
-        const float f = w.y == 0.f ? 0.f : fast_exp2(w.x - ref) * w.y;      // a chunk without a visible position left zeros
+        const float f = w.y == 0.f ? 0.f : fast_exp2(w.x - ref) * (w.y * scale);      // a chunk without a visible position left zeros
         L += f;
         acc = make_float4(fmaf(f, o.x, acc.x), fmaf(f, o.y, acc.y), fmaf(f, o.z, acc.z), fmaf(f, o.w, acc.w));
     }

@@ -418,17 +418,23 @@ __global__ __launch_bounds__(256) void k_join_prefill_q8(Q8Attention a, const in
     const int64_t first = ((int64_t)tile_no * a.H + h) * splits * ROWS + r;
     const float2 *ml = part_ml + first;
     const float4 *po = reinterpret_cast<const float4 *>(part_o + first * HD) + d;
-    float M = -INFINITY;
+    // The weights of all shares, together at most 1, so that the sum stays within the values up to the ends of float32: a row's own sums go up to 2^97
+    float M = -INFINITY, most = -INFINITY;
 #pragma unroll 4
-    for (int i = 0; i < splits; i++) M = fmaxf(M, ml[i * ROWS].x);
+    for (int i = 0; i < splits; i++) {
+        const float2 w = ml[i * ROWS];
+        M = fmaxf(M, w.x);
+        most = fmaxf(most, w.x + __builtin_amdgcn_logf(w.y));
+    }
     const float ref = M > -INFINITY ? M : 0.f;
+    const float scale = most > -INFINITY ? ldexpf(1.f, -(int)ceilf(most - ref) - (33 - __clz(splits))) : 0.f;
     float L = 0.f;
     float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll 4
     for (int i = 0; i < splits; i++) {
         const float2 w = ml[i * ROWS];
         const float4 o = po[(int64_t)i * ROWS * PER];
-        const float f = w.y == 0.f ? 0.f : fast_exp2(w.x - ref) * w.y;      // a share without a position that the row sees left zeros
+        const float f = w.y == 0.f ? 0.f : fast_exp2(w.x - ref) * w.y * scale;      // a share without a position that the row sees left zeros
         L += f;
         acc = make_float4(fmaf(f, o.x, acc.x), fmaf(f, o.y, acc.y), fmaf(f, o.z, acc.z), fmaf(f, o.w, acc.w));
     }

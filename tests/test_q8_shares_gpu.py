@@ -4,7 +4,7 @@ import numpy as np
 import pytest
 
 from workloads import gen
-from test_q8_gpu import _attend, _check_prefill, _layer, _run_prefill, _sequence, _slopes
+from test_q8_gpu import _attend, _check_decode, _check_prefill, _layer, _run_decode, _run_prefill, _sequence, _slopes
 
 pytestmark = pytest.mark.gpu
 
@@ -182,3 +182,22 @@ def test_keys_and_values_near_the_ends_of_their_range_over_shares(hd, H, Hkv, ze
         tiles = [(0, n, before, 0, 0, 0)]
         out = _run_prefill(q, n, table, codes, expo, tiles, H, Hkv, hd, length - 1)
         _check_prefill(out, q, table, codes, expo, tiles, [length], H, Hkv, hd, some=3)
+
+
+@pytest.mark.parametrize("H,Hkv", [(2, 2), (4, 1), (16, 1)])
+@pytest.mark.parametrize("unit", [121, 100, -110, -126])
+@pytest.mark.parametrize("size", [1.0, 1e-3])
+def test_values_at_the_ends_of_float32(H, Hkv, unit, size):
+    """Values of one unit, up to the largest that float32 holds, whose weights are many and alike: every sum stays within the values."""
+    hd, n, before = 64, 40, 1777
+    length = before + n
+    table, codes, expo = _layer([length], Hkv, hd, 22)
+    expo[table[0, :-(-length // 16)], 1] = unit
+    q = gen.normal(22, 13, (n, H * hd), std=size)
+    tiles = [(0, n, before, 0, 0, 0)]
+    out = _run_prefill(q, n, table, codes, expo, tiles, H, Hkv, hd, length - 1)
+    _check_prefill(out, q, table, codes, expo, tiles, [length], H, Hkv, hd, some=5)
+    rows = [0, 3, 39]
+    ctx = [before + r + 1 for r in rows]
+    out = _run_decode(q[rows].contiguous(), table, codes, expo, [0] * 3, ctx, H, Hkv, hd)
+    _check_decode(out, q[rows].contiguous(), table, codes, expo, [0] * 3, ctx, H, Hkv, hd)
