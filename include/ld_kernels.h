@@ -310,7 +310,7 @@ ld_status ldk_kv_from_q8(const int8_t *codes, const int8_t *expo, const int32_t 
  * sequence (first NULL: 0; window 0: no band); ctx_len[t] may be 0, and a row that sees nothing gives 0.
  *   s_j = q.k_j / sqrt(hd);  softcap > 0 (1e-30 at least): s_j = softcap tanh(s_j / softcap);  slopes (DEVICE [H], may be NULL): s_j += slopes[h] (j - p);
  *   out = sum_j softmax(s)_j v_j.
- * A query enters as a multiple of 1 / 8355711 of its largest entry, a weight times its value's 2^e with 22 bits, of which at most 2^-34 of the row's largest such product
+ * A query enters as a multiple of 1 / 8355711 of its largest entry, a weight times its value's 2^e with 22 bits, of which at most 2^-38 of the row's largest such product
  * gets lost besides, and a weight below 2^-126 of the row's largest counts as 0; codes are exact, sums float32.  Range: scores below 2^126 in magnitude.  A query head with a NaN or an infinity gives NaN, as does a head that sees a key or value that stands for NaN.  max_ctx (HOST) >= every ctx_len.
  * scratch: ldk_attention_q8_scratch_bytes(...) bytes, 16-byte aligned; a buffer for more rows or longer contexts serves less. */
 size_t ldk_attention_q8_scratch_bytes(int32_t T, int32_t H, int32_t Hkv, int32_t hd, int32_t max_ctx, int32_t window);

@@ -6,7 +6,7 @@
 //   scores   S^T[pos, row] = K[pos, :] . Q[row, :] in whole numbers (32x32x32, 8 bits): a query is three base-256 digits (24 bits under its largest
 //            entry), kept in registers.
 //   sums     O^T[d, row] += V^T[d, pos] W^T[pos, row] (32x32x16, fp16): codes are exact in fp16; W = p 2^e 2^x, e the value's exponent and 2^x the power
-//            of two that brings the largest p 2^e of the row so far to 2^9 .. 65504, as two fp16 terms (22 bits).
+//            of two that brings the largest p 2^e of the row so far to 2^13 .. 65504, as two fp16 terms (22 bits).
 //
 // Which position a row of the score tile is, is free: row 8 b + 4 h + i is slot 4 b + i of block h of a pair, so that lane (row, h) ends with the scores of
 // block h, slot by slot, which is what it has to bring as the other operand of the sums.
@@ -304,12 +304,12 @@ __global__ __launch_bounds__(256, HD == 64 && !EXTRA ? 3 : 2) void k_prefill_q8(
 #pragma unroll
             for (int i = 0; i < 16; i++) top = fmaxf(top, s[u][i]);
         top = max_halves(top);
-        // the largest product leaves 2^9 .. 65504: scaled to 2^12 .. 2^13, what is there and what comes
+        // the largest product leaves 2^13 .. 65504: scaled to 2^13 .. 2^14, what is there and what comes (from 2^9 on 0.4 % less time, and four bits less of small weights)
         big = fmaxf(big, top);
-        if (__any(big > 65504.f || (big > 0.f && big < 512.f))) {
+        if (__any(big > 65504.f || (big > 0.f && big < 8192.f))) {
             // the sum of the row's weights, of this tile and of earlier ones, stays below 2^97: where the values that draw most are zero, nothing else holds
             // the weights down
-            const int x = big > 0.f ? min(min(12 - exponent(big), 96 - exponent(max_halves(l + sum))), 126) : 0;
+            const int x = big > 0.f ? min(min(13 - exponent(big), 96 - exponent(max_halves(l + sum))), 126) : 0;
             const float up = ldexpf(1.f, x);
             add += (float)x;
             l *= up;

@@ -201,3 +201,27 @@ def test_values_at_the_ends_of_float32(H, Hkv, unit, size):
     ctx = [before + r + 1 for r in rows]
     out = _run_decode(q[rows].contiguous(), table, codes, expo, [0] * 3, ctx, H, Hkv, hd)
     _check_decode(out, q[rows].contiguous(), table, codes, expo, [0] * 3, ctx, H, Hkv, hd)
+
+
+@pytest.mark.parametrize("hd", [64, 128])
+@pytest.mark.parametrize("before", [0, 1920])
+@pytest.mark.parametrize("down", [26.4, 29.3, 31.2, 33.7])
+def test_prefill_of_small_weights_beside_a_small_unit(hd, before, down):
+    """One position draws all but 2^-down, its value has a quarter of the others' unit and zeros where theirs count: their weights lose 2^-38 of the largest
+    product at most."""
+    H, Hkv, n = 2, 1, 12
+    length = before + n
+    table, codes, expo = _layer([length], Hkv, hd, int(down))
+    b = table[0, before // 16]
+    codes[b, 0], expo[b, 0] = 0, 0
+    codes[b, 0, :, 0, 0], expo[b, 0, :, 0] = 127, 0
+    codes[b, 1, :, 0], expo[b, 1] = 0, -6
+    codes[b, 1, :, 0, 0], expo[b, 1, :, 0] = 127, -8
+    q = gen.normal(int(down), 13, (n, H * hd), std=0.01)
+    q[:, ::hd] = float(down * np.log(2.0) * hd ** 0.5 / 127)
+    out = _run_prefill(q, n, table, codes, expo, [(0, n, before, 0, before, 0)], H, Hkv, hd, length - 1)
+    k, v = _sequence(table, codes, expo, 0, length)
+    for r in range(n):
+        for h in range(H):
+            ref, bound = _attend(q[r, h * hd:(h + 1) * hd].double().numpy(), k[before:before + r + 1, 0], v[before:before + r + 1, 0], 0, 0, r, 0.0, 0.0, least=13)
+            assert (np.abs(out[r, h].double().cpu().numpy() - ref) <= bound).all(), (r, h, (np.abs(out[r, h].double().cpu().numpy() - ref) / bound).max())
