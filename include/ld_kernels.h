@@ -288,7 +288,8 @@ ld_status ldk_rope_table_scaled(const int32_t *pos, int32_t T, int32_t rot, floa
  * heads, Hkv v heads of hd floats).  With q_gain [hd]: every q head x becomes x / sqrt(mean x^2 + eps) * q_gain; k_gain likewise (NULL: none).
  * Then the first rot (even, 0 .. hd) elements of q and k heads are rotated by cos_sin [T, rot / 2]: pair i = elements (i, i + rot / 2), or with
  * interleaved != 0 (2i, 2i + 1).  q goes to q_out + t * q_out_stride [H hd]; q_out may be qkv itself with the same stride, otherwise they do not
- * overlap.  k and v go into the pool.  Norms, rotation and codes are computed in float64: whichever order a sum takes, no code differs.  A row with
+ * overlap.  k and v go into the pool.  Norms, rotation and codes are computed in float64, in an order that does not depend on T: a row gets the same codes in
+ * any call.  A row with
  * pos[t] < 0 is padding: nothing of it is written.  Rows of one call address distinct (sequence, position) pairs. */
 ld_status ldk_rope_kv_write_q8(const float *qkv, int32_t qkv_stride, const float *q_gain, const float *k_gain, float eps, const float *cos_sin,
                                int32_t rot, int32_t interleaved, const int32_t *pos, const int32_t *seq_slot, const int32_t *table,

@@ -34,6 +34,14 @@ struct WriteArgs {
     int64_t q_out_stride;
 };
 
+// A rotated pair.  Written out, so that both kernels below round alike: with the sum of squares added in one order they give a row the same codes, however many
+// rows a call has.  The order: pairs (of a rotation, or neighbours), then pairs of these, and so on.
+__device__ __forceinline__ void turn_pair(double &x, double &y, double c, double s) {
+    const double first = fma(x, c, -(y * s));
+    y = fma(x, s, y * c);
+    x = first;
+}
+
 // One wave a row and head, two elements a lane: a rotated pair, or two of the rest.  For few rows, where a launch and its chain of loads count (one row of 96
 // heads 2.6 us), and for rotated parts that are no multiple of 8.
 template <int HD, bool INTERLEAVED>
@@ -55,7 +63,7 @@ __global__ __launch_bounds__(64) void k_write_q8(WriteArgs a) {
     const float *gain = value ? nullptr : j < 0 ? a.q_gain : a.k_gain;
     if (gain) {
         double ss = x * x + y * y;
-        for (int off = 32; off > 0; off >>= 1) ss += __shfl_xor(ss, off, WAVE);
+        for (int off = 1; off < 64; off <<= 1) ss += __shfl_xor(ss, off, WAVE);
         const double r = 1.0 / sqrt(ss / HD + a.eps);
         if (live) {
             x *= r * gain[i0];
@@ -64,9 +72,7 @@ __global__ __launch_bounds__(64) void k_write_q8(WriteArgs a) {
     }
     if (turn) {
         const float2 c = reinterpret_cast<const float2 *>(a.cos_sin)[(int64_t)t * (a.rot / 2) + lane];
-        const double u = x * c.x - y * c.y;
-        y = x * c.y + y * c.x;
-        x = u;
+        turn_pair(x, y, c.x, c.y);
     }
     if (j < 0) {
         if (live) {
@@ -152,11 +158,15 @@ __global__ __launch_bounds__(2 * HD) void k_write_rows_q8(WriteArgs a, int T) {
     double y[8] = {x0[0], x0[1], x0[2], x0[3], x1[0], x1[1], x1[2], x1[3]};
     const float *gain = keep ? a.k_gain : a.q_gain;
     if (gain) {
-        double ss = 0;
+        double p[4];      // squares of floats are exact
 #pragma unroll
-        for (int e = 0; e < 8; e++) ss += y[e] * y[e];
+        for (int e = 0; e < 4; e++) {
+            const int u = INTERLEAVED || !turn ? 2 * e : e, w = INTERLEAVED || !turn ? 2 * e + 1 : e + 4;
+            p[e] = y[u] * y[u] + y[w] * y[w];
+        }
+        double ss = (p[0] + p[1]) + (p[2] + p[3]);
 #pragma unroll
-        for (int off = LPR / 2; off > 0; off >>= 1) ss += __shfl_xor(ss, off, WAVE);
+        for (int off = 1; off < LPR; off <<= 1) ss += __shfl_xor(ss, off, WAVE);
         const double n = 1.0 / sqrt(ss / HD + a.eps);
 #pragma unroll
         for (int e = 0; e < 8; e++) y[e] *= n * gain[(e < 4 ? i0 : i1) + (e & 3)];
@@ -166,9 +176,7 @@ __global__ __launch_bounds__(2 * HD) void k_write_rows_q8(WriteArgs a, int T) {
 #pragma unroll
         for (int e = 0; e < 4; e++) {
             const int u = INTERLEAVED ? 2 * e : e, w = INTERLEAVED ? 2 * e + 1 : e + 4;
-            const double c = cs[2 * e], s = cs[2 * e + 1], first = y[u] * c - y[w] * s;
-            y[w] = y[u] * s + y[w] * c;
-            y[u] = first;
+            turn_pair(y[u], y[w], cs[2 * e], cs[2 * e + 1]);
         }
     }
     if (!keep) {
