@@ -56,6 +56,9 @@ struct Q8Attention {
     float *out;
 };
 
+// A launch has fewer than 2^32 threads in a dimension.
+inline bool too_large(int64_t workgroups, int threads) { return workgroups > UINT32_MAX / threads; }
+
 inline bool bad_attention(const Q8Attention &a, int hd) {
     return !a.q || !a.codes || !a.expo || (((uintptr_t)a.codes | (uintptr_t)a.expo) & 15) || !a.table || a.table_stride < 0 || a.H <= 0 || a.Hkv <= 0 ||
            a.H % a.Hkv || (hd != 64 && hd != 128) || (int64_t)a.q_stride < (int64_t)a.H * hd || a.window < 0 || !(a.softcap >= 0.f) ||

@@ -342,7 +342,7 @@ __global__ __launch_bounds__(256) void k_move_q8(MoveArgs a, uint32_t items, KT 
 template <bool TO>
 ld_status move(const char *what, const MoveArgs &a, int n_ranges, int hd, void *pool, int dtype, int8_t *codes, int8_t *expo, hipStream_t s) {
     const int64_t items = (((int64_t)a.max_len + 14) / 16 + 1) * 2 * a.Hkv;      // positions first .. first + max_len - 1 touch at most so many blocks
-    if (items > INT32_MAX) {
+    if (too_large((items + 3) / 4, 256)) {
         ld::set_error("%s: too many blocks a range", what);
         return LD_E_RANGE;
     }
@@ -387,7 +387,7 @@ ld_status ldk_rope_table_scaled(const int32_t *pos, int32_t T, int32_t rot, floa
     if (T == 0) return LD_OK;
     if (!pos || !cos_sin) return ld::fail(LD_E_INVAL, "ldk_rope_table_scaled: bad argument");
     const int64_t n = (int64_t)T * (rot / 2);
-    if (n > (int64_t)1 << 36) return ld::fail(LD_E_RANGE, "ldk_rope_table_scaled: too many angles");
+    if (too_large((n + 63) / 64, 64)) return ld::fail(LD_E_RANGE, "ldk_rope_table_scaled: too many angles");
     LD_LAUNCH(k_rope_table_scaled, dim3((unsigned)((n + 63) / 64)), dim3(64), 0, (hipStream_t)stream, pos, n, rot / 2, std::log2((double)rope_base),
               (double)sc.factor, (double)sc.low, (double)sc.high, sc.original / (2 * M_PI), (double)sc.attention, reinterpret_cast<float2 *>(cos_sin));
     return launched("k_rope_table_scaled");
@@ -404,11 +404,13 @@ ld_status ldk_rope_kv_write_q8(const float *qkv, int32_t qkv_stride, const float
     if (T == 0) return LD_OK;
     if (!qkv || !pos || !seq_slot || !table || !q_out || (rot && !cos_sin) || bad_pool(codes, expo) || (q_out == qkv && q_out_stride != qkv_stride))
         return ld::fail(LD_E_INVAL, "ldk_rope_kv_write_q8: bad argument");
-    if (H + 2 * (int64_t)Hkv > 65535) return ld::fail(LD_E_RANGE, "ldk_rope_kv_write_q8: more than 65535 heads");
+    const bool many = T >= MANY_ROWS && rot % 8 == 0;
+    if (H + 2 * (int64_t)Hkv > 65535 || (many ? too_large(((int64_t)T + 15) / 16, 2 * hd) : too_large(T, 64)))
+        return ld::fail(LD_E_RANGE, "ldk_rope_kv_write_q8: more than 65535 heads, or too many rows");
     const WriteArgs a{qkv, qkv_stride, q_gain, k_gain, eps, cos_sin, rot, pos, seq_slot, table, table_stride, codes, expo, H, Hkv, q_out, q_out_stride};
     hipStream_t s = (hipStream_t)stream;
-    if (T >= MANY_ROWS && rot % 8 == 0) {
-        const dim3 grid((T + 15) / 16, H + 2 * Hkv), block(2 * hd);
+    if (many) {
+        const dim3 grid((unsigned)(((int64_t)T + 15) / 16), H + 2 * Hkv), block(2 * hd);
 #define LD_ROWS(HD_, IL_) LD_LAUNCH((k_write_rows_q8<HD_, IL_>), grid, block, 0, s, a, T)
         if (hd == 128) { if (interleaved) LD_ROWS(128, true); else LD_ROWS(128, false); }
         else { if (interleaved) LD_ROWS(64, true); else LD_ROWS(64, false); }

@@ -461,7 +461,8 @@ ld_status ldk_paged_attention_q8(const float *q, int32_t q_stride, const int8_t 
     const Q8Attention a{q, q_stride, codes, expo, table, table_stride, H, Hkv, window, softcap, slopes, out};
     if (T < 0 || max_ctx < 0 || !seq_slot || !ctx_len || bad_attention(a, hd)) return ld::fail(LD_E_INVAL, "ldk_paged_attention_q8: bad argument");
     const Plan p = plan(T, H, Hkv, max_ctx, window);
-    if (H > 65535 || (int64_t)T * p.chunks * H > INT32_MAX) return ld::fail(LD_E_RANGE, "ldk_paged_attention_q8: more than 65535 heads, or too many rows");
+    if (H > 65535 || (int64_t)T * p.chunks > INT32_MAX / H || too_large((int64_t)T * p.chunks * Hkv * ((H / Hkv + 15) / 16), 64 * WAVES))
+        return ld::fail(LD_E_RANGE, "ldk_paged_attention_q8: more than 65535 heads, or too many rows");
     if (!scratch || ((uintptr_t)scratch & 15) || scratch_bytes < ldk_attention_q8_scratch_bytes(T, H, Hkv, hd, max_ctx, window))
         return ld::fail(LD_E_INVAL, "ldk_paged_attention_q8: scratch too small, or not aligned to 16 bytes");
     hipStream_t s = (hipStream_t)stream;

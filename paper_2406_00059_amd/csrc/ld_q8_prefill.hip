@@ -482,7 +482,7 @@ ld_status ldk_prefill_attention_q8(const float *q, int32_t q_stride, const int8_
     const Q8Attention a{q, q_stride, codes, expo, table, table_stride, H, Hkv, window, softcap, slopes, out};
     if (n_tiles < 0 || max_pos < 0 || !tiles || bad_attention(a, hd)) return ld::fail(LD_E_INVAL, "ldk_prefill_attention_q8: bad argument");
     const int splits = shares(n_tiles, H, max_pos);
-    if (H > 65535 || (int64_t)n_tiles * H * splits > INT32_MAX)
+    if (H > 65535 || too_large((int64_t)n_tiles * H * splits, 256))
         return ld::fail(LD_E_RANGE, "ldk_prefill_attention_q8: more than 65535 heads, or too many tiles");
     if (!scratch || ((uintptr_t)scratch & 15) || scratch_bytes < ldk_prefill_attention_q8_scratch_bytes(n_tiles, H, Hkv, hd, max_pos, window))
         return ld::fail(LD_E_INVAL, "ldk_prefill_attention_q8: scratch too small, or not aligned to 16 bytes");

@@ -168,3 +168,16 @@ def test_binding_refuses_attention_tensors_that_do_not_fit():
     for bad in (dict(q=_z(2, H * HD)), dict(q_stride=0), dict(tiles=_z(1, 4, dtype=I32)), dict(tiles=_z(1, 6)), dict(expo=EXPO[:1]), dict(out=_z(3, H, HD - 1)), dict(H=0),
                 dict(slopes=_z(H + 1)), dict(max_pos=-1)):
         _refused(ld.ldk_prefill_attention_q8, **{**good, **bad})
+
+
+# ---------------------------------------------------------------- calls of more threads than a launch has
+
+@pytest.mark.parametrize("name,args", [("ldk_rope_table_scaled", dict(TABLE, T=1 << 26, rot=128)), ("ldk_rope_table_scaled", dict(TABLE, T=(1 << 31) - 1, rot=64)),
+                                       ("ldk_rope_kv_write_q8", dict(WRITE, T=1 << 26, rot=22)), ("ldk_rope_kv_write_q8", dict(WRITE, T=(1 << 29) + 1)),
+                                       ("ldk_rope_kv_write_q8", dict(WRITE, T=1 << 28, hd=128, qkv_stride=12 * 128, q_out_stride=8 * 128)),
+                                       ("ldk_kv_to_q8", dict(TO, max_len=1 << 28)), ("ldk_kv_from_q8", dict(FROM, max_len=1 << 24, Hkv=32)),
+                                       ("ldk_paged_attention_q8", dict(DECODE, T=1 << 23, scratch_bytes=1 << 60)),
+                                       ("ldk_paged_attention_q8", dict(DECODE, T=8192, max_ctx=131072, H=32, Hkv=32, q_stride=2048, scratch_bytes=1 << 60)),
+                                       ("ldk_prefill_attention_q8", dict(PREFILL, n_tiles=1 << 21, scratch_bytes=1 << 60))])
+def test_calls_of_more_threads_than_a_launch_has_are_refused(name, args):
+    assert _call(name, args) == ld.LD_E_RANGE and name in ld.ld_last_error()
