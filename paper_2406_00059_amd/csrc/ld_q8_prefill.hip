@@ -265,11 +265,12 @@ __global__ __launch_bounds__(256, HD == 64 && !EXTRA ? 3 : 2) void k_prefill_q8(
             for (int i = 0; i < 16; i++) most_s = fmaxf(most_s, s[u][i]);
         most_s = max_halves(most_s);
         float from = 0.f;
-        if (large) from = large >> lane & 1 ? froms[tid] : 0.f;
-        // the first score makes the largest weight 2^12; one that would be above 2^30 does so too
+        if (__builtin_expect(large != 0, 0)) from = large >> lane & 1 ? froms[tid] : 0.f;
+        // the first score makes the largest weight 2^14 (mostly within what the products are held in below); one that would be above 2^30 does so too.  What is
+        // seldom taken is told to the compiler, here and below: four capped observations 117.1 -> 114.8 us, 8191 rows 733 -> 728
         const bool lower = fmaf(most_s - from, rs, add) > 30.f;
-        if (__any(lower)) {
-            const float fn = !lower ? from : fabsf(most_s * rs) >= LARGE ? most_s : 0.f, an = lower ? 12.f - (most_s - fn) * rs : add;
+        if (__builtin_expect(__any(lower), 0)) {
+            const float fn = !lower ? from : fabsf(most_s * rs) >= LARGE ? most_s : 0.f, an = lower ? 14.f - (most_s - fn) * rs : add;
             const float keep = add == NONE ? 0.f : fast_exp2(fmaf(from - fn, rs, an - add));
             add = an;
             l *= keep;
@@ -282,7 +283,7 @@ __global__ __launch_bounds__(256, HD == 64 && !EXTRA ? 3 : 2) void k_prefill_q8(
             if (large) froms[tid] = fn;
             from = fn;
         }
-        if (large) {
+        if (__builtin_expect(large != 0, 0)) {
 #pragma unroll
             for (int u = 0; u < 2; u++)
 #pragma unroll
@@ -304,9 +305,9 @@ __global__ __launch_bounds__(256, HD == 64 && !EXTRA ? 3 : 2) void k_prefill_q8(
 #pragma unroll
             for (int i = 0; i < 16; i++) top = fmaxf(top, s[u][i]);
         top = max_halves(top);
-        // the largest product leaves 2^13 .. 65504: scaled to 2^13 .. 2^14, what is there and what comes (from 2^9 on 0.4 % less time, and four bits less of small weights)
+        // the largest product leaves 2^13 .. 65504: scaled to 2^13 .. 2^14, what is there and what comes
         big = fmaxf(big, top);
-        if (__any(big > 65504.f || (big > 0.f && big < 8192.f))) {
+        if (__builtin_expect(__any(big > 65504.f || (big > 0.f && big < 8192.f)), 0)) {
             // the sum of the row's weights, of this tile and of earlier ones, stays below 2^97: where the values that draw most are zero, nothing else holds
             // the weights down
             const int x = big > 0.f ? min(min(13 - exponent(big), 96 - exponent(max_halves(l + sum))), 126) : 0;
