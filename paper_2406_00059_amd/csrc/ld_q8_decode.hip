@@ -401,8 +401,9 @@ int visible_tiles(int max_ctx, int window) {
     return (int)(window > 0 ? std::min<int64_t>(all, ((int64_t)window + TILE - 2) / TILE + 1) : all);
 }
 
-// us of one row at 1520 positions of 32 heads / one at 131067 of 8 KV heads / 32 of 32 heads at 512 - 8192: 256 workgroups 11.6 / 59 / 224, 512 11.4 / 59 / 224,
-// 1024 11.4 / 67 / 224, 2048 11.5 / 83 / 224; chunks of at most 16 tiles 11.4 / 67 / 237; of at least two 13.0 / 59 / 224.
+// us of one row at 1520 positions of 32 heads / one at 131067 of 8 KV heads / 32 of 32 heads at 512 - 8192 / 8 capped ones of 40 heads at 1 - 2048: 256 workgroups
+// 11.6 / 59 / 206 / 22.8, 512 11.2 / 59 / 206 / 21.9, 1024 11.6 / 67 / 206 / 25.0, 2048 11.3 / 81 / 206 / 25.9; chunks of at most 16 tiles 11.0 / 66 / 214 / 21.8;
+// of at least two a wave 12.5 / 59 / 206 / 21.8.
 constexpr int WANT = 512, CHUNK_TILES = 32;
 
 Plan plan(int T, int H, int Hkv, int max_ctx, int window) {

@@ -14,8 +14,8 @@
 // Units of positions are held by sixteen lanes each and enter products from there (row_newbcast); read by every lane they cost a third of the LDS reads, and
 // the registers that brought some of the staged keys into scratch memory (8191 rows below: 812 us).
 //
-// What bounds it: 64 positions and 32 rows are 56 matrix instructions (1800 cycles of a SIMD) and some 540 vector ones.  With two waves a SIMD, which is what
-// the registers allow, matrix instructions take 49 % and vector ones 69 % of the time.  8191 rows of 32 heads in a band of 4096 take 720 - 760 us, some 555 TFLOP/s
+// What bounds it: 64 positions and 32 rows are 56 matrix instructions (1800 cycles of a SIMD) and some 545 vector ones.  With two waves a SIMD, which is what
+// the registers allow, matrix instructions take 48 % and vector ones 69 % of the time.  8191 rows of 32 heads in a band of 4096 take 720 - 760 us, some 555 TFLOP/s
 // of the formula and 970 of executed products, at a clock that falls to 1.6 - 2.0 GHz meanwhile: vector instructions saved (sums that the matrix cores begin
 // at a number whose bits are a float's) and the two kinds of work ordered otherwise (scores of both halves first, wave priorities) no longer change it.
 // Measured and not kept, the first two with keys in scratch: scores in fp16 with queries in two terms (five vector instructions an entry less, a third more
@@ -408,7 +408,7 @@ __global__ __launch_bounds__(256, HD == 64 && !EXTRA ? 3 : 2) void k_prefill_q8(
 }
 
 // Joins the shares of a row and head, in their order: HD / 4 lanes a row, four shares' loads in flight (5.7 us for the 96 pairs
-// below and 11.3 for the 280; a wave a row and one load at a time 8.8 and 16.4).
+// below and 11.7 for the 280; a wave a row and one load at a time 8.8 and 16.4).
 template <int HD>
 __global__ __launch_bounds__(256) void k_join_prefill_q8(Q8Attention a, const int32_t *__restrict__ tiles, int splits, const float *__restrict__ part_o,
                                                          const float2 *__restrict__ part_ml) {
@@ -446,8 +446,8 @@ __global__ __launch_bounds__(256) void k_join_prefill_q8(Q8Attention a, const in
 constexpr int MOST = 1024, LEAST = 4;      // workgroups with shares, 64-position tiles a share
 
 // Shares of a tile's positions, by the number of (tile, head) pairs.  Up to a pair a CU: what fills the CUs once with two workgroups each, or nearly; more: about
-// four a CU, so that the last ones do not work alone.  us, 1 / 2 / 3 / 4 / 5 / 6 / 8 shares: 96 pairs of 24 tiles 64 / 45 / 46 / 42 / 44 / 50 / 50, 280 pairs of up to
-// 68 tiles 192 / 131 / 134 / 124 / 127 / 132 / 149 (with a join one load at a time).
+// four a CU, so that the last ones do not work alone.  us, 1 / 2 / 3 / 4 / 5 / 6 / 8 shares: 96 pairs of 24 tiles 66 / 45 / 45 / 40 / 41 / 48 / 48, 280 pairs of up to
+// 68 tiles 189 / 127 / 130 / 118 / 121 / 123 / 138.
 int shares(int n_tiles, int H, int max_pos) {
     const int64_t pairs = (int64_t)n_tiles * H, kt = ((int64_t)max_pos + TILE) / TILE;
     const int64_t n = pairs <= 256 ? std::max<int64_t>(2, 400 / pairs) : (MOST + pairs - 1) / pairs;
