@@ -158,7 +158,7 @@ __global__ __launch_bounds__(256, HD == 64 && !EXTRA ? 3 : 2) void k_prefill_q8(
         const Q8Query query = q8_query(top, (EXTRA ? 1.0 : 1.4426950408889634) / sqrt((double)HD));
         broken = __ballot(top >= 0x7f800000u);
         unit = top >= 0x7f800000u ? 1.f : ldexpf(query.unit, query.exp + KEY_SHIFT);
-        unit = unit < 0x1p-126f ? 0x1p-126f : unit;      // not zero: it multiplies -infinity
+        unit = unit < 0x1p-149f ? 0x1p-149f : unit;      // not zero: it multiplies -infinity (and sums below 2^128: what a subnormal number lacks in bits shows in no weight)
 #pragma unroll
         for (int s = 0; s < KS; s++)
 #pragma unroll

@@ -153,3 +153,24 @@ def test_prefill_of_large_scores_that_are_all_alike(hd, H, Hkv, size, zeros):
         # one after another, 2^-13 at most of the mean magnitude, and as much as one share's weight may be off
         off = 2.0 ** -13 * np.abs(seen).mean(0)
         assert (np.abs(got[r] - seen.mean(0)) <= off).all(), (r, np.abs(got[r] - seen.mean(0)).max())
+
+
+@pytest.mark.parametrize("hd,H,Hkv", [(128, 2, 2), (64, 4, 1)])
+@pytest.mark.parametrize("small", [-120, -126, -130, -137, -149])
+@pytest.mark.parametrize("cap", [0.0, 1e-3])
+def test_queries_below_the_normal_numbers(hd, H, Hkv, small, cap):
+    """Queries of 2^small, subnormal ones among them, over keys up to 2^120."""
+    n, before = 40, 533
+    length = before + n
+    nb = -(-length // 16)
+    table, codes, expo = _layer([length], Hkv, hd, 41)
+    expo[table[0, :nb], 0] = np.array([113, 112, 90])[gen.randint(41, 1, 0, 2, nb * Hkv * 16).numpy().reshape(nb, Hkv, 16)]
+    q = (gen.normal(41, 13, (n, H * hd)).double() * 2.0 ** small).float()
+    assert (q != 0).any()
+    tiles = [(0, n, before, 0, 0, 0)]
+    out = _run_prefill(q, n, table, codes, expo, tiles, H, Hkv, hd, length - 1, cap=cap)
+    _check_prefill(out, q, table, codes, expo, tiles, [length], H, Hkv, hd, some=3, cap=cap)
+    rows = [0, 17, 39]
+    ctx = [before + r + 1 for r in rows]
+    out = _run_decode(q[rows].contiguous(), table, codes, expo, [0] * 3, ctx, H, Hkv, hd, cap=cap)
+    _check_decode(out, q[rows].contiguous(), table, codes, expo, [0] * 3, ctx, H, Hkv, hd, cap=cap)
