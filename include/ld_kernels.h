@@ -324,8 +324,9 @@ ld_status ldk_paged_attention_q8(const float *q, int32_t q_stride, const int8_t 
  * block-table row, first visible position, prefix length).  The row at position p sees positions max(first visible, p - window + 1) ..
  * max(p, prefix - 1): a band (window 0: none), a document's start and a prefix that sees all of itself; a row that sees nothing gives 0.
  * Scores as in ldk_paged_attention_q8.  Rows that no tile names are left as they are.  max_pos (HOST) >= every max(p, prefix - 1).
- * Range: keys below 2^120, scores below 2^126 in magnitude; values that a tile sees within a factor of 2^85 of each other, or of 1 where 64 of them in a row are zero.
- * Where a row's weight lies all but 2^-80 on zero values, or on values so much smaller than others, what gets lost is at most 2^-120 of the largest 2^e instead.
+ * Range: keys below 2^120, scores below 2^126 in magnitude; values that a tile sees within a factor of 2^85 of each other, or of 1 where 64 of them in a row are zero; values
+ * below 2^-119 count as zero.  Where a row's weight lies all but 2^-20 on zero values, or on values so much smaller than others, weights have 18 bits, and what gets lost besides
+ * is at most 2^-120 of the largest 2^e.
  * scratch: ldk_prefill_attention_q8_scratch_bytes(...) bytes, 16-byte aligned; a buffer for more tiles or longer contexts serves less. */
 size_t ldk_prefill_attention_q8_scratch_bytes(int32_t n_tiles, int32_t H, int32_t Hkv, int32_t hd, int32_t max_pos, int32_t window);
 ld_status ldk_prefill_attention_q8(const float *q, int32_t q_stride, const int8_t *codes, const int8_t *expo, const int32_t *table,

@@ -135,7 +135,8 @@ __global__ __launch_bounds__(256, HD == 64 && !EXTRA ? 3 : 2) void k_prefill_q8(
             const uint64_t ok = __ballot(ide_of >= 0);
             if (tid == 0) s.mapped = (int)((ok & 1) | (ok >> 15 & 2) | (ok >> 30 & 4) | (ok >> 45 & 8));
         } else if (tid < 128) {
-            s.vu[tid - 64] = er == Q8_NAN ? __uint_as_float(0x7fc00000u) : ldexpf(1.f, er - e0);
+            // a zero value (the lowest exponent, and out of range beside these if it is not one) asks for no scaling of a row
+            s.vu[tid - 64] = er == Q8_NAN ? __uint_as_float(0x7fc00000u) : er == -126 && e0 > -41 ? 0.f : ldexpf(1.f, er - e0);
         }
     };
 

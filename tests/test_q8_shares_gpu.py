@@ -225,3 +225,18 @@ def test_prefill_of_small_weights_beside_a_small_unit(hd, before, down):
         for h in range(H):
             ref, bound = _attend(q[r, h * hd:(h + 1) * hd].double().numpy(), k[before:before + r + 1, 0], v[before:before + r + 1, 0], 0, 0, r, 0.0, 0.0, least=13)
             assert (np.abs(out[r, h].double().cpu().numpy() - ref) <= bound).all(), (r, h, (np.abs(out[r, h].double().cpu().numpy() - ref) / bound).max())
+
+
+@pytest.mark.parametrize("hd,H,Hkv", [(128, 4, 2), (64, 8, 2)])
+@pytest.mark.parametrize("n,before", [(60, 64), (100, 65), (90, 1600)])
+def test_prefill_behind_zero_values_is_as_exact(hd, H, Hkv, n, before):
+    """Zero values in the first 64 positions of a share; queries so small that the bound is that of the weights' own roundings."""
+    length = before + n
+    table, codes, expo = _layer([length], Hkv, hd, n)
+    for p in range(length):
+        if p // 64 % 4 == 0 or before > 1000 and p < before:
+            codes[table[0, p // 16], 1, :, p % 16], expo[table[0, p // 16], 1, :, p % 16] = 0, -126
+    q = gen.normal(n, 13, (n, H * hd), std=0.02)
+    tile = _tiles(n, before)[0]
+    out = _run_prefill(q, n, table, codes, expo, [tile], H, Hkv, hd, length - 1)
+    _check_rows(out, q, table, codes, expo, tile, length, H, Hkv, hd, range(n))
